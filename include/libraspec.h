@@ -436,6 +436,154 @@ int libraspec_kv_append_paged(const uint16_t* kv_new, uint16_t* const* Kp, uint1
                               size_t ws_bytes, void* stream);
 
 /*
+ * The prompt's way into the cache, and decoding from it. A verify round needs
+ * a cache that holds the prompt: these calls rotate a ragged chunk of new
+ * tokens to their positions, append its keys and values, and let its queries
+ * attend to the whole cache. New tokens are packed: row cu_new[b] + j of every
+ * packed tensor is the j-th new token of sequence b, cu_new [B+1] i32
+ * non-decreasing within [0, T] (sequences may be empty; rows of no sequence are
+ * left alone). kv_len [B] i32 counts the sequence's keys before the chunk, so
+ * the token's position is kv_len[b] + j. Offsets that decrease or leave [0, T]
+ * set LIBRASPEC_ST_BAD_LENGTH (the sequence is skipped), a chunk that does not
+ * fit the cache LIBRASPEC_ST_KV_OVERFLOW.
+ *
+ * Rotary positions: frequencies. Pair i < rot_dim / 2 of a head turns by f_i
+ * radians per position, f_i = theta^(-2 i / rot_dim), scaled for contexts longer than the model was
+ * trained on:
+ *   LIBRASPEC_ROPE_LINEAR    f_i / factor (positions interpolated);
+ *   LIBRASPEC_ROPE_NTK       theta factor^(rot_dim / (rot_dim - 2)) in place of theta (rot_dim > 2);
+ *   LIBRASPEC_ROPE_BY_PARTS  (1 - k_i) f_i / factor + k_i f_i, where k_i is
+ *                            (r_i - low) / (high - low) clamped to [0, 1] and r_i = original_len f_i / (2 pi), the
+ *                            turns of the pair over the original context.
+ * Writes turns [rot_dim / 2, 2] f32, a HOST array: f_i / (2 pi) as hi + lo, so
+ * that kernels know a position's angle to 2^-24 of a turn however long the
+ * context. Copy it to the device once per model. rot_dim even, theta > 0 and
+ * finite, factor > 0 and finite (with a scaling), low < high and original_len > 0 (by parts).
+ */
+#define LIBRASPEC_ROPE_PLAIN 0
+#define LIBRASPEC_ROPE_LINEAR 1
+#define LIBRASPEC_ROPE_NTK 2
+#define LIBRASPEC_ROPE_BY_PARTS 3
+#define LIBRASPEC_ROPE_MAX_DIM 512
+int libraspec_rope_frequencies(int rot_dim, double theta, int scaling, double factor, double low, double high,
+                               double original_len, float* turns);
+
+/*
+ * Rotary positions of T tokens' heads: with a = pos[t] f_i,
+ *   (Y0, Y1) = magnitude (X0 cos a - X1 sin a, X0 sin a + X1 cos a)
+ * for the pairs (X0, X1) = elements (i, i + rot_dim / 2) of a head, or
+ * (2 i, 2 i + 1) if `interleaved`; elements rot_dim .. head_dim - 1 are copied.
+ * `inverse` turns by -a: the gradient of X from that of Y.
+ * X, Y [T, H, head_dim] f32 (or bf16, computed in binary32 and rounded once),
+ * each token's heads contiguous, x_stride and y_stride elements from token to
+ * token (at least H * head_dim; X may be the queries' or keys' part of a wider
+ * projection). Y may be X with the same stride; else they must not overlap.
+ * pos [T] i32 (any sign), turns [rot_dim / 2, 2] f32 from
+ * libraspec_rope_frequencies, on the device. head_dim even, rot_dim even,
+ * 2 <= rot_dim <= head_dim, rot_dim <= LIBRASPEC_ROPE_MAX_DIM. Rows that start
+ * on 16 bytes (and halves of whole 16 bytes) move in 128-bit accesses, others
+ * pair by pair. One launch, no workspace.
+ */
+int libraspec_rope(const float* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude, int T,
+                   int H, int head_dim, int rot_dim, int interleaved, int inverse, float* Y, int64_t y_stride,
+                   void* stream);
+int libraspec_rope_bf16(const uint16_t* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude,
+                        int T, int H, int head_dim, int rot_dim, int interleaved, int inverse, uint16_t* Y,
+                        int64_t y_stride, void* stream);
+
+/*
+ * Appending a chunk's keys and values to one layer's cache, the keys rotated
+ * on the way, and its queries rotated beside them (libraspec_rope's rotation
+ * at position kv_len[b] + j, or at pos[row] if pos is not NULL).
+ *   Q [T, Hq, head_dim], K, V [T, Hkv, head_dim] f32 (or bf16), strides in
+ *   elements from token to token as above; Qo [T, Hq, head_dim] bf16 out,
+ *   packed. Q and Qo NULL: only keys and values. Qo may not overlap the inputs.
+ *   Kc, Vc [B, Hkv, S_cap, head_dim] bf16, or page pools [n_pages, Hkv,
+ *   page_size, head_dim] with block_table [B, max_pages] as for
+ *   libraspec_kv_append_paged: cache row kv_len[b] + j. A row past the capacity
+ *   sets LIBRASPEC_ST_KV_OVERFLOW, a block-table entry outside [0, n_pages)
+ *   LIBRASPEC_ST_BAD_PAGE; the key and value of that row are skipped.
+ * Every value is rounded to bf16 once. head_dim in {64, 128}. The workspace
+ * holds the status word only (>= 256 bytes). One launch.
+ */
+int libraspec_rope_append(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                          int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                          const float* turns, float magnitude, int T, int B, int Hq, int Hkv, int head_dim, int rot_dim,
+                          int interleaved, uint16_t* Qo, uint16_t* Kc, uint16_t* Vc, int S_cap, void* workspace,
+                          size_t ws_bytes, void* stream);
+int libraspec_rope_append_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                               const uint16_t* V, int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len,
+                               const int32_t* pos, const float* turns, float magnitude, int T, int B, int Hq, int Hkv,
+                               int head_dim, int rot_dim, int interleaved, uint16_t* Qo, uint16_t* Kc, uint16_t* Vc,
+                               int S_cap, void* workspace, size_t ws_bytes, void* stream);
+int libraspec_rope_append_paged(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                                int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                                const float* turns, float magnitude, int T, int B, int Hq, int Hkv, int head_dim,
+                                int rot_dim, int interleaved, uint16_t* Qo, uint16_t* Kp, uint16_t* Vp,
+                                const int32_t* block_table, int max_pages, int page_size, int n_pages,
+                                void* workspace, size_t ws_bytes, void* stream);
+int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                                     const uint16_t* V, int64_t v_stride, const int32_t* cu_new,
+                                     const int32_t* kv_len, const int32_t* pos, const float* turns, float magnitude,
+                                     int T, int B, int Hq, int Hkv, int head_dim, int rot_dim, int interleaved,
+                                     uint16_t* Qo, uint16_t* Kp, uint16_t* Vp, const int32_t* block_table,
+                                     int max_pages, int page_size, int n_pages, void* workspace, size_t ws_bytes,
+                                     void* stream);
+
+/*
+ * Attention of a chunk of new tokens over the cache, one layer: a prompt, a
+ * part of one, the single token of a decode step, or all of them in one call.
+ * The chunk's keys and values are in the cache already. Query row (b, j) at
+ * position p = kv_len[b] + j, with N = kv_len[b] + (new tokens of b) keys, sees
+ * key k iff
+ *   k < N,  and  k <= p or k < prefix_len[b],
+ *   and  k > p - window  (window > 0),  and  k >= first_key[row],
+ * and for query head h
+ *   s_k = softmax_scale Q . Kc[b, h / g, k],
+ *   s_k = softcap tanh(s_k / softcap)          if softcap > 0,
+ *   s_k = s_k - slopes[h] |p - k|              if slopes is given,
+ *   O = sum_k softmax(s)_k Vc[b, h / g, k],    lse = log sum_k exp(s_k).
+ * A row that sees no key has O = 0 and lse = -infinity.
+ *   Q, O [T, Hq, head_dim] bf16 packed rows (16-byte aligned, may not
+ *   overlap), lse [T, Hq] f32 out or NULL.
+ * The options (NULL: none) are a HOST struct with device pointers:
+ *   slopes     [Hq] f32, finite: a bias by distance;
+ *   first_key  [T] i32: the first key that a row may see (the start of its
+ *              document; any order);
+ *   prefix_len [B] i32: keys that every new row sees, later ones included.
+ * Keys that no row of a sequence sees need not be initialised; pages that hold
+ * none of the others are not read, nor their block-table entries. (A NaN or
+ * infinity in a key or value that some row of a block of rows sees may reach
+ * the block's other rows.)
+ * head_dim in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 128; page_size a multiple
+ * of 16 (else LIBRASPEC_EUNSUPPORTED). Scores, sums and O accumulate in
+ * binary32; probabilities enter the second product as bf16. Results do not
+ * change from run to run. Two launches (a plan from the device's lengths, the
+ * attention); workspace: libraspec_chunk_workspace_size(T, B, Hq, Hkv,
+ * head_dim) bytes, 256-byte aligned, zero-filled once, of at least the call's
+ * T, B and heads; calls sharing it must not overlap. If a wait inside the
+ * kernel gives up (LIBRASPEC_ST_TIMEOUT), re-initialise it before its next use.
+ */
+typedef struct libraspec_score_opts {
+  float softcap;              /* 0: none */
+  int window;                 /* 0: none */
+  const float* slopes;        /* NULL: none */
+  const int32_t* first_key;   /* NULL: none */
+  const int32_t* prefix_len;  /* NULL: none */
+} libraspec_score_opts;
+
+size_t libraspec_chunk_workspace_size(int T, int B, int Hq, int Hkv, int head_dim);
+int libraspec_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* cu_new,
+                         const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap,
+                         float softmax_scale, const libraspec_score_opts* opts, uint16_t* O, float* lse,
+                         void* workspace, size_t ws_bytes, void* stream);
+int libraspec_chunk_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint16_t* Vp, const int32_t* block_table,
+                               int max_pages, int page_size, int n_pages, const int32_t* cu_new,
+                               const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, float softmax_scale,
+                               const libraspec_score_opts* opts, uint16_t* O, float* lse, void* workspace,
+                               size_t ws_bytes, void* stream);
+
+/*
  * Failure-detection self-test (no counterpart in the paper: it checks the
  * library's own bounded waits). One CTA waits, with the bounded wait that
  * acceptance's draws use for their sequence's decision, until the device

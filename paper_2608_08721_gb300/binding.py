@@ -25,6 +25,7 @@ MAX_TREE_NODES = 512
 # Every entry point declared in include/libraspec.h, with its ctypes signature.
 _P, _I, _U32, _U64, _F, _SZ = (ctypes.c_void_p, ctypes.c_int, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
                                ctypes.c_size_t)
+_I64, _D = ctypes.c_int64, ctypes.c_double
 SIGNATURES = {
     "libraspec_version": (ctypes.c_char_p, []),
     "libraspec_status_string": (ctypes.c_char_p, [_I]),
@@ -60,6 +61,18 @@ SIGNATURES = {
     "libraspec_lm_head_stats": (_I, [_P, _P, _P, _I, _P, _I, _I, _I, _P, _P, _P, _P, _SZ, _P]),
     "libraspec_kv_append": (_I, [_P, _P, _P, _I, _P, _I, _I, _I, _I, _I, _P, _SZ, _P]),
     "libraspec_kv_append_paged": (_I, [_P, _P, _P, _I, _P, _I, _I, _I, _P, _I, _I, _I, _I, _P, _SZ, _P]),
+    "libraspec_rope_frequencies": (_I, [_I, _D, _I, _D, _D, _D, _D, _P]),
+    "libraspec_rope": (_I, [_P, _I64, _P, _P, _F] + [_I] * 6 + [_P, _I64, _P]),
+    "libraspec_rope_bf16": (_I, [_P, _I64, _P, _P, _F] + [_I] * 6 + [_P, _I64, _P]),
+    "libraspec_rope_append": (_I, [_P, _I64] * 3 + [_P] * 4 + [_F] + [_I] * 7 + [_P] * 3 + [_I, _P, _SZ, _P]),
+    "libraspec_rope_append_bf16": (_I, [_P, _I64] * 3 + [_P] * 4 + [_F] + [_I] * 7 + [_P] * 3 + [_I, _P, _SZ, _P]),
+    "libraspec_rope_append_paged": (_I, [_P, _I64] * 3 + [_P] * 4 + [_F] + [_I] * 7 + [_P] * 4 + [_I] * 3 +
+                                    [_P, _SZ, _P]),
+    "libraspec_rope_append_paged_bf16": (_I, [_P, _I64] * 3 + [_P] * 4 + [_F] + [_I] * 7 + [_P] * 4 + [_I] * 3 +
+                                         [_P, _SZ, _P]),
+    "libraspec_chunk_workspace_size": (_SZ, [_I] * 5),
+    "libraspec_chunk_attn": (_I, [_P] * 5 + [_I] * 6 + [_F] + [_P] * 4 + [_SZ, _P]),
+    "libraspec_chunk_attn_paged": (_I, [_P] * 4 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_F] + [_P] * 4 + [_SZ, _P]),
     "libraspec_accept": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _U64, _U64, _U32, _P, _P, _P, _SZ, _P]),
     "libraspec_accept_bf16": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _U64, _U64, _U32, _P, _P, _P, _SZ, _P]),
     "libraspec_verify_round": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _I, _I, _I, _I, _I, _I, _I,
@@ -548,6 +561,211 @@ def libraspec_lm_head_stats(H, W, ws: "LmHeadWorkspace", temperature=None, rows_
                                         _stream(stream))
     _check(rc, "libraspec_lm_head_stats")
     return row_stat, row_argmax, token_prob
+
+
+class RopeFreqs:
+    """Frequencies of a rotation, made once per model: ``turns`` [rot_dim / 2, 2] f32 on the device (turns per
+    position of each pair, as two floats) and ``magnitude``, the factor of the rotated pairs.
+
+    scaling: "none", "linear" (f / factor), "ntk" (theta grows with factor) or "parts" (pairs of less than ``low``
+    turns over ``original_len`` positions as "linear", of more than ``high`` unchanged, a ramp between)."""
+
+    SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+
+    def __init__(self, rot_dim: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                 original_len: float = 0.0, low: float = 1.0, high: float = 32.0, magnitude: float = 1.0, device=None):
+        if scaling not in self.SCALINGS:
+            raise ValueError("scaling must be one of %s" % ", ".join(self.SCALINGS))
+        host = torch.empty((max(0, rot_dim // 2), 2), dtype=torch.float32)
+        rc = load().libraspec_rope_frequencies(int(rot_dim), float(theta), self.SCALINGS[scaling], float(factor),
+                                               float(low), float(high), float(original_len), _ptr(host))
+        _check(rc, "libraspec_rope_frequencies")
+        self.rot_dim, self.magnitude = int(rot_dim), float(magnitude)
+        self.turns = host.to(torch.device("cuda") if device is None else torch.device(device))
+
+
+def _req_heads(t: torch.Tensor, dtype, name: str, shape=None) -> torch.Tensor:
+    """[T, H, d] whose tokens' heads are contiguous (any stride from token to token, as in a slice of a wider
+    projection)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be on a CUDA device" % name)
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, shape or "[T, H, d]", tuple(t.shape)))
+    T, H, d = t.shape
+    if T and ((d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d) or (T > 1 and t.stride(0) < H * d)):
+        raise ValueError("%s: each token's heads must be contiguous" % name)
+    return t
+
+
+def _token_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y=None, stream=None) -> torch.Tensor:
+    """X [T, H, d] (f32 or bf16) rotated to the positions pos [T] int32; ``inverse`` rotates back (the gradient of X
+    from that of Y). Y may be X (in place)."""
+    bf16 = isinstance(X, torch.Tensor) and X.dtype == torch.bfloat16
+    dt = torch.bfloat16 if bf16 else torch.float32
+    _req_heads(X, dt, "X")
+    T, H, d = X.shape
+    _req(pos, torch.int32, "pos", (T,))
+    Y = torch.empty((T, H, d), dtype=dt, device=X.device) if Y is None else _req_heads(Y, dt, "Y", X.shape)
+    name = "libraspec_rope_bf16" if bf16 else "libraspec_rope"
+    rc = getattr(load(), name)(_ptr(X), _token_stride(X), _ptr(pos), _ptr(freqs.turns), freqs.magnitude, T, H, d,
+                               freqs.rot_dim, int(bool(interleaved)), int(bool(inverse)), _ptr(Y), _token_stride(Y),
+                               _stream(stream))
+    _check(rc, name)
+    return Y
+
+
+def libraspec_rope_append(Q, K, V, Kc, Vc, cu_new, kv_len, freqs: RopeFreqs, ws, pos=None, interleaved=False, Qo=None,
+                          stream=None):
+    """Rotates a ragged chunk's keys into the dense caches Kc, Vc [B, Hkv, S_cap, d] beside its values, and its queries
+    into Qo [T, Hq, d] bf16 (Q None: keys and values alone). Returns Qo."""
+    return _rope_append(Q, K, V, Kc, Vc, None, cu_new, kv_len, freqs, ws, pos, interleaved, Qo, stream)
+
+
+def libraspec_rope_append_paged(Q, K, V, Kp, Vp, block_table, cu_new, kv_len, freqs: RopeFreqs, ws, pos=None,
+                                interleaved=False, Qo=None, stream=None):
+    """libraspec_rope_append into page pools Kp, Vp [n_pages, Hkv, page_size, d] by block_table [B, max_pages]."""
+    return _rope_append(Q, K, V, Kp, Vp, block_table, cu_new, kv_len, freqs, ws, pos, interleaved, Qo, stream)
+
+
+def _check_new(cu_new, kv_len):
+    """Offsets of the new tokens [B + 1] and cache lengths [B]; returns B."""
+    _req(kv_len, torch.int32, "kv_len")
+    if kv_len.dim() != 1:
+        raise ValueError("kv_len must be [B]")
+    B = kv_len.shape[0]
+    _req(cu_new, torch.int32, "cu_new", (B + 1,))
+    return B
+
+
+def _check_caches(Kc, Vc, block_table, B, Hkv, d):
+    """Dense caches, or pools and their table; returns (capacity, max_pages, page_size, n_pages)."""
+    k, v = ("Kc", "Vc") if block_table is None else ("Kp", "Vp")
+    _req(Kc, torch.bfloat16, k)
+    if Kc.dim() != 4 or Kc.shape[1] != Hkv or Kc.shape[3] != d or (block_table is None and Kc.shape[0] != B):
+        raise ValueError("%s must be %s, got %s" % (k, "[%s, %d, %s, %d]" % (
+            (B, Hkv, "S_cap", d) if block_table is None else ("n_pages", Hkv, "page_size", d)), tuple(Kc.shape)))
+    _req(Vc, torch.bfloat16, v, Kc.shape)
+    if block_table is None:
+        return Kc.shape[2], 0, 0, 0
+    _req(block_table, torch.int32, "block_table")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    return 0, block_table.shape[1], Kc.shape[2], Kc.shape[0]
+
+
+def _rope_append(Q, K, V, Kc, Vc, block_table, cu_new, kv_len, freqs, ws, pos, interleaved, Qo, stream):
+    bf16 = isinstance(K, torch.Tensor) and K.dtype == torch.bfloat16
+    dt = torch.bfloat16 if bf16 else torch.float32
+    _req_heads(K, dt, "K")
+    T, Hkv, d = K.shape
+    _req_heads(V, dt, "V", K.shape)
+    B = _check_new(cu_new, kv_len)
+    S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
+    if pos is not None:
+        _req(pos, torch.int32, "pos", (T,))
+    Hq = 0
+    if Q is not None:
+        _req_heads(Q, dt, "Q")
+        Hq = Q.shape[1]
+        if Q.shape[0] != T or Q.shape[2] != d:
+            raise ValueError("Q must have shape [%d, Hq, %d], got %s" % (T, d, tuple(Q.shape)))
+        Qo = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=K.device) if Qo is None else _req(
+            Qo, torch.bfloat16, "Qo", (T, Hq, d))
+    elif Qo is not None:
+        raise ValueError("Qo without Q")
+    args = [_ptr(Q), _token_stride(Q) if Q is not None else 0, _ptr(K), _token_stride(K), _ptr(V), _token_stride(V),
+            _ptr(cu_new), _ptr(kv_len), _ptr(pos), _ptr(freqs.turns), freqs.magnitude, T, B, Hq, Hkv, d, freqs.rot_dim,
+            int(bool(interleaved)), _ptr(Qo), _ptr(Kc), _ptr(Vc)]
+    name = "libraspec_rope_append" + ("" if block_table is None else "_paged") + ("_bf16" if bf16 else "")
+    args += [S_cap] if block_table is None else [_ptr(block_table), max_pages, page_size, n_pages]
+    rc = getattr(load(), name)(*args, ws.ptr, ws.nbytes, _stream(stream))
+    _check(rc, name)
+    return Qo
+
+
+class ChunkWorkspace:
+    """Device scratch of the chunk calls, for up to T new tokens of B sequences."""
+
+    def __init__(self, T, B, Hq, Hkv, head_dim, device=None):
+        self.nbytes = int(load().libraspec_chunk_workspace_size(T, B, Hq, Hkv, head_dim))
+        if self.nbytes == 0:
+            raise ValueError("invalid chunk workspace shapes")
+        dev = torch.device("cuda") if device is None else torch.device(device)
+        self.buf = torch.zeros(self.nbytes, dtype=torch.uint8, device=dev)
+
+    @property
+    def ptr(self) -> int:
+        return self.buf.data_ptr()
+
+
+class _ScoreOpts(ctypes.Structure):
+    _fields_ = [("softcap", _F), ("window", _I), ("slopes", _P), ("first_key", _P), ("prefix_len", _P)]
+
+
+def libraspec_chunk_attn(Q, Kc, Vc, cu_new, kv_len, ws: ChunkWorkspace, softmax_scale=None, softcap: float = 0.0,
+                         slopes=None, window: int = 0, first_key=None, prefix_len=None, O=None, lse=None,
+                         want_lse=False, stream=None):
+    """Attention of packed new tokens Q [T, Hq, d] over the dense caches Kc, Vc [B, Hkv, S_cap, d] that hold them
+    already. Options: softcap (tanh cap of the scores), slopes [Hq] f32 (bias by distance), window (keys a row looks
+    back, itself included), first_key [T] int32 (start of the row's document), prefix_len [B] int32 (keys that all
+    rows see). Returns (O, lse or None)."""
+    return _chunk_attn(Q, Kc, Vc, None, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key,
+                       prefix_len, O, lse, want_lse, stream)
+
+
+def libraspec_chunk_attn_paged(Q, Kp, Vp, block_table, cu_new, kv_len, ws: ChunkWorkspace, softmax_scale=None,
+                               softcap: float = 0.0, slopes=None, window: int = 0, first_key=None, prefix_len=None,
+                               O=None, lse=None, want_lse=False, stream=None):
+    """libraspec_chunk_attn over page pools Kp, Vp [n_pages, Hkv, page_size, d] (page_size a multiple of 16) by
+    block_table [B, max_pages] int32."""
+    return _chunk_attn(Q, Kp, Vp, block_table, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key,
+                       prefix_len, O, lse, want_lse, stream)
+
+
+def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key,
+                prefix_len, O, lse, want_lse, stream):
+    _req(Q, torch.bfloat16, "Q")
+    if Q.dim() != 3:
+        raise ValueError("Q must be [T, Hq, d]")
+    T, Hq, d = Q.shape
+    B = _check_new(cu_new, kv_len)
+    Hkv = Kc.shape[1] if isinstance(Kc, torch.Tensor) and Kc.dim() == 4 else 0
+    S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
+    if softmax_scale is None:
+        softmax_scale = d ** -0.5
+    opts = None
+    if softcap or slopes is not None or window or first_key is not None or prefix_len is not None:
+        if slopes is not None:
+            _req(slopes, torch.float32, "slopes", (Hq,))
+        if first_key is not None:
+            _req(first_key, torch.int32, "first_key", (T,))
+        if prefix_len is not None:
+            _req(prefix_len, torch.int32, "prefix_len", (B,))
+        opts = ctypes.byref(_ScoreOpts(float(softcap), int(window), _ptr(slopes), _ptr(first_key), _ptr(prefix_len)))
+    O = torch.empty_like(Q) if O is None else _req(O, torch.bfloat16, "O", Q.shape)
+    if lse is not None:
+        _req(lse, torch.float32, "lse", (T, Hq))
+    elif want_lse:
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=Q.device)
+    tail = (float(softmax_scale), opts, _ptr(O), _ptr(lse), ws.ptr, ws.nbytes, _stream(stream))
+    if block_table is None:
+        name = "libraspec_chunk_attn"
+        rc = load().libraspec_chunk_attn(_ptr(Q), _ptr(Kc), _ptr(Vc), _ptr(cu_new), _ptr(kv_len), T, B, Hq, Hkv, d,
+                                         S_cap, *tail)
+    else:
+        name = "libraspec_chunk_attn_paged"
+        rc = load().libraspec_chunk_attn_paged(_ptr(Q), _ptr(Kc), _ptr(Vc), _ptr(block_table), max_pages, page_size,
+                                               n_pages, _ptr(cu_new), _ptr(kv_len), T, B, Hq, Hkv, d, *tail)
+    _check(rc, name)
+    return O, lse
 
 
 def _ptr_array(tensors: Sequence[Optional[torch.Tensor]]):

@@ -29,6 +29,18 @@ cudaError_t launch_lm_head_stats(const uint16_t*, const uint16_t*, const float*,
                                  float*, int32_t*, float*, char*, cudaStream_t);
 cudaError_t launch_kv_append(const uint16_t*, uint16_t* const*, uint16_t* const*, int, const int32_t*,
                              const int32_t*, int, int, int, int, int, int, int, int, int*, cudaStream_t);
+void rope_frequencies(int, double, int, double, double, double, double, float*);
+template <typename T>
+cudaError_t launch_rope(const T*, long long, const int32_t*, const float*, float, int, int, int, int, int, int, T*,
+                        long long, cudaStream_t);
+template <typename T>
+cudaError_t launch_rope_append(const T*, long long, const T*, long long, const T*, long long, const int32_t*,
+                               const int32_t*, const int32_t*, const float*, float, const int32_t*, int, int, int, int,
+                               int, int, int, int, int, int, uint16_t*, uint16_t*, uint16_t*, int, int*, cudaStream_t);
+size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);
+cudaError_t launch_chunk_attn(const uint16_t*, const uint16_t*, const uint16_t*, const int32_t*, int, int, int,
+                              const int32_t*, const int32_t*, int, int, int, int, int, int, float, float, const float*,
+                              int, const int32_t*, const int32_t*, uint16_t*, float*, char*, cudaStream_t);
 template <typename T>
 cudaError_t launch_accept_tree(const T*, const int32_t*, const int32_t*, const int32_t*, const float*, int, int, int,
                                uint64_t, uint64_t, uint32_t, int32_t*, int32_t*, int32_t*, char*, const WsLayout&,
@@ -413,6 +425,201 @@ int libraspec_kv_append_paged(const uint16_t* kv_new, uint16_t* const* Kp, uint1
   if (B > 0 && (!block_table || !aligned(block_table, 4))) return LIBRASPEC_EINVAL;
   return kv_append_checked(kv_new, Kp, Vp, n_layers, kv_len, block_table, max_pages, page_size, n_pages, B, T, Hkv,
                            head_dim, max_pages * page_size, workspace, ws_bytes, stream);
+}
+
+namespace {
+
+bool pos_finite(double x) { return x > 0.0 && x <= 1e300; }
+
+// Strides of a [T, H, d] tensor whose tokens' heads are contiguous.
+bool token_stride_ok(int64_t stride, int H, int d) { return stride >= (int64_t)H * d && stride <= (int64_t(1) << 40); }
+
+bool rope_shape_ok(int T, int H, int head_dim, int rot_dim) {
+  return T >= 0 && H >= 1 && H <= (1 << 20) && head_dim >= 2 && head_dim % 2 == 0 && head_dim <= 65536 &&
+         (long)H * head_dim <= 0x7fffffffL && rot_dim >= 2 && rot_dim % 2 == 0 && rot_dim <= head_dim &&
+         rot_dim <= LIBRASPEC_ROPE_MAX_DIM;
+}
+
+}  // namespace
+
+int libraspec_rope_frequencies(int rot_dim, double theta, int scaling, double factor, double low, double high,
+                               double original_len, float* turns) {
+  if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > LIBRASPEC_ROPE_MAX_DIM || !pos_finite(theta) || !turns)
+    return LIBRASPEC_EINVAL;
+  if (scaling < LIBRASPEC_ROPE_PLAIN || scaling > LIBRASPEC_ROPE_BY_PARTS) return LIBRASPEC_EUNSUPPORTED;
+  if (scaling != LIBRASPEC_ROPE_PLAIN && !pos_finite(factor)) return LIBRASPEC_EINVAL;
+  if (scaling == LIBRASPEC_ROPE_NTK && rot_dim == 2) return LIBRASPEC_EINVAL;
+  if (scaling == LIBRASPEC_ROPE_BY_PARTS && (!(low < high) || !pos_finite(original_len) || !(low > -1e300) || !(high < 1e300)))
+    return LIBRASPEC_EINVAL;
+  rope_frequencies(rot_dim, theta, scaling, factor, low, high, original_len, turns);
+  return LIBRASPEC_OK;
+}
+
+extern "C++" {
+template <typename T>
+static int rope_t(const T* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude, int n_tokens,
+                  int H, int head_dim, int rot_dim, int interleaved, int inverse, T* Y, int64_t y_stride,
+                  void* stream) {
+  if (!rope_shape_ok(n_tokens, H, head_dim, rot_dim)) return LIBRASPEC_EINVAL;
+  if (!token_stride_ok(x_stride, H, head_dim) || !token_stride_ok(y_stride, H, head_dim)) return LIBRASPEC_EINVAL;
+  if (n_tokens == 0) return LIBRASPEC_OK;
+  if (!X || !Y || !pos || !turns || !aligned(X, sizeof(T)) || !aligned(Y, sizeof(T)) || !aligned(pos, 4) ||
+      !aligned(turns, 8) || (X == Y && x_stride != y_stride))
+    return LIBRASPEC_EINVAL;
+  return from_cuda(launch_rope<T>(X, x_stride, pos, turns, magnitude, n_tokens, H, head_dim, rot_dim, interleaved,
+                                  inverse, Y, y_stride, static_cast<cudaStream_t>(stream)));
+}
+
+template <typename T>
+static int rope_append_t(const T* Q, int64_t q_stride, const T* K, int64_t k_stride, const T* V, int64_t v_stride,
+                         const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos, const float* turns,
+                         float magnitude, int n_tokens, int B, int Hq, int Hkv, int head_dim, int rot_dim,
+                         int interleaved, uint16_t* Qo, uint16_t* Kc, uint16_t* Vc, bool paged,
+                         const int32_t* block_table, int max_pages, int page_size, int n_pages, int S_cap,
+                         void* workspace, size_t ws_bytes, void* stream) {
+  if (head_dim != 64 && head_dim != 128) return LIBRASPEC_EUNSUPPORTED;
+  if (!rope_shape_ok(n_tokens, Hkv, head_dim, rot_dim) || B < 0 || B > LIBRASPEC_MAX_B) return LIBRASPEC_EINVAL;
+  if ((Q != nullptr) != (Qo != nullptr)) return LIBRASPEC_EINVAL;
+  if (Q && (!rope_shape_ok(n_tokens, Hq, head_dim, rot_dim) || !token_stride_ok(q_stride, Hq, head_dim)))
+    return LIBRASPEC_EINVAL;
+  if (!token_stride_ok(k_stride, Hkv, head_dim) || !token_stride_ok(v_stride, Hkv, head_dim)) return LIBRASPEC_EINVAL;
+  if (paged) {
+    if (page_size < 1 || max_pages < 1 || n_pages < 1 || (long)max_pages * page_size > 0x7fffffffL)
+      return LIBRASPEC_EINVAL;
+    S_cap = max_pages * page_size;
+  }
+  if (S_cap < 1) return LIBRASPEC_EINVAL;
+  if (n_tokens == 0 || B == 0) return LIBRASPEC_OK;
+  if (!K || !V || !Kc || !Vc || !cu_new || !kv_len || !turns || (paged && !block_table)) return LIBRASPEC_EINVAL;
+  if ((Q && (!aligned(Q, sizeof(T)) || !aligned(Qo, 16))) || !aligned(K, sizeof(T)) || !aligned(V, sizeof(T)) ||
+      !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(cu_new, 4) || !aligned(kv_len, 4) || !aligned(pos, 4) ||
+      !aligned(turns, 8) || !aligned(block_table, 4))
+    return LIBRASPEC_EINVAL;
+  if (!workspace || !aligned(workspace, 256) || ws_bytes < 256) return LIBRASPEC_EINVAL;
+  return from_cuda(launch_rope_append<T>(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude,
+                                         paged ? block_table : nullptr, max_pages, page_size, n_pages, n_tokens, B, Hq,
+                                         Hkv, head_dim, rot_dim, interleaved, Qo, Kc, Vc, S_cap,
+                                         static_cast<int*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+}  // extern "C++"
+
+int libraspec_rope(const float* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude, int T,
+                   int H, int head_dim, int rot_dim, int interleaved, int inverse, float* Y, int64_t y_stride,
+                   void* stream) {
+  return rope_t(X, x_stride, pos, turns, magnitude, T, H, head_dim, rot_dim, interleaved, inverse, Y, y_stride, stream);
+}
+
+int libraspec_rope_bf16(const uint16_t* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude,
+                        int T, int H, int head_dim, int rot_dim, int interleaved, int inverse, uint16_t* Y,
+                        int64_t y_stride, void* stream) {
+  return rope_t(X, x_stride, pos, turns, magnitude, T, H, head_dim, rot_dim, interleaved, inverse, Y, y_stride, stream);
+}
+
+int libraspec_rope_append(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                          int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                          const float* turns, float magnitude, int T, int B, int Hq, int Hkv, int head_dim, int rot_dim,
+                          int interleaved, uint16_t* Qo, uint16_t* Kc, uint16_t* Vc, int S_cap, void* workspace,
+                          size_t ws_bytes, void* stream) {
+  return rope_append_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, T, B, Hq, Hkv,
+                       head_dim, rot_dim, interleaved, Qo, Kc, Vc, false, nullptr, 0, 0, 0, S_cap, workspace, ws_bytes,
+                       stream);
+}
+
+int libraspec_rope_append_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                               const uint16_t* V, int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len,
+                               const int32_t* pos, const float* turns, float magnitude, int T, int B, int Hq, int Hkv,
+                               int head_dim, int rot_dim, int interleaved, uint16_t* Qo, uint16_t* Kc, uint16_t* Vc,
+                               int S_cap, void* workspace, size_t ws_bytes, void* stream) {
+  return rope_append_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, T, B, Hq, Hkv,
+                       head_dim, rot_dim, interleaved, Qo, Kc, Vc, false, nullptr, 0, 0, 0, S_cap, workspace, ws_bytes,
+                       stream);
+}
+
+int libraspec_rope_append_paged(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                                int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                                const float* turns, float magnitude, int T, int B, int Hq, int Hkv, int head_dim,
+                                int rot_dim, int interleaved, uint16_t* Qo, uint16_t* Kp, uint16_t* Vp,
+                                const int32_t* block_table, int max_pages, int page_size, int n_pages,
+                                void* workspace, size_t ws_bytes, void* stream) {
+  return rope_append_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, T, B, Hq, Hkv,
+                       head_dim, rot_dim, interleaved, Qo, Kp, Vp, true, block_table, max_pages, page_size, n_pages, 0,
+                       workspace, ws_bytes, stream);
+}
+
+int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                                     const uint16_t* V, int64_t v_stride, const int32_t* cu_new,
+                                     const int32_t* kv_len, const int32_t* pos, const float* turns, float magnitude,
+                                     int T, int B, int Hq, int Hkv, int head_dim, int rot_dim, int interleaved,
+                                     uint16_t* Qo, uint16_t* Kp, uint16_t* Vp, const int32_t* block_table,
+                                     int max_pages, int page_size, int n_pages, void* workspace, size_t ws_bytes,
+                                     void* stream) {
+  return rope_append_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, T, B, Hq, Hkv,
+                       head_dim, rot_dim, interleaved, Qo, Kp, Vp, true, block_table, max_pages, page_size, n_pages, 0,
+                       workspace, ws_bytes, stream);
+}
+
+namespace {
+
+bool chunk_shape_ok(int T, int B, int Hq, int Hkv) {
+  return T >= 0 && T <= (1 << 24) && B >= 0 && B <= LIBRASPEC_MAX_B && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 &&
+         Hq / Hkv <= kAttnRows && Hq <= (1 << 16);
+}
+
+int chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, bool paged, const int32_t* block_table,
+               int max_pages, int page_size, int n_pages, const int32_t* cu_new, const int32_t* kv_len, int T, int B,
+               int Hq, int Hkv, int head_dim, int S_cap, float softmax_scale, const libraspec_score_opts* opts,
+               uint16_t* O, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  if (head_dim != 64 && head_dim != 128) return LIBRASPEC_EUNSUPPORTED;
+  if (!chunk_shape_ok(T, B, Hq, Hkv)) return LIBRASPEC_EINVAL;
+  if (paged) {
+    if (page_size < 1 || max_pages < 1 || n_pages < 1 || (long)max_pages * page_size > 0x7fffffffL ||
+        (long)n_pages * Hkv > 0x7fffffffL)
+      return LIBRASPEC_EINVAL;
+    if (page_size % 16 != 0) return LIBRASPEC_EUNSUPPORTED;
+    S_cap = max_pages * page_size;
+  }
+  if (S_cap < 1 || (long)B * Hkv > (1L << 30)) return LIBRASPEC_EINVAL;
+  libraspec_score_opts o{};
+  if (opts) o = *opts;
+  if (!(softmax_scale > 0.f) || !isfinite(softmax_scale) || !(o.softcap >= 0.f) || !isfinite(o.softcap) ||
+      o.window < 0)
+    return LIBRASPEC_EINVAL;
+  if (T == 0 || B == 0) return LIBRASPEC_OK;
+  if (!Q || !Kc || !Vc || !O || !cu_new || !kv_len || (paged && !block_table)) return LIBRASPEC_EINVAL;
+  if (!aligned(Q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(O, 16) || !aligned(lse, 4) ||
+      !aligned(cu_new, 4) || !aligned(kv_len, 4) || !aligned(block_table, 4) || !aligned(o.slopes, 4) ||
+      !aligned(o.first_key, 4) || !aligned(o.prefix_len, 4))
+    return LIBRASPEC_EINVAL;
+  if (!workspace || !aligned(workspace, 256) || ws_bytes < chunk_workspace_bytes(T, B, Hq, Hkv, head_dim))
+    return LIBRASPEC_EINVAL;
+  return from_cuda(launch_chunk_attn(Q, Kc, Vc, paged ? block_table : nullptr, max_pages, page_size, n_pages, cu_new,
+                                     kv_len, T, B, Hq, Hkv, head_dim, S_cap, softmax_scale, o.softcap, o.slopes,
+                                     o.window, o.first_key, o.prefix_len, O, lse, static_cast<char*>(workspace),
+                                     static_cast<cudaStream_t>(stream)));
+}
+
+}  // namespace
+
+size_t libraspec_chunk_workspace_size(int T, int B, int Hq, int Hkv, int head_dim) {
+  if (!chunk_shape_ok(T, B, Hq, Hkv) || (head_dim != 64 && head_dim != 128)) return 0;
+  return chunk_workspace_bytes(T, B, Hq, Hkv, head_dim);
+}
+
+int libraspec_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* cu_new,
+                         const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap,
+                         float softmax_scale, const libraspec_score_opts* opts, uint16_t* O, float* lse,
+                         void* workspace, size_t ws_bytes, void* stream) {
+  return chunk_attn(Q, Kc, Vc, false, nullptr, 0, 0, 0, cu_new, kv_len, T, B, Hq, Hkv, head_dim, S_cap, softmax_scale,
+                    opts, O, lse, workspace, ws_bytes, stream);
+}
+
+int libraspec_chunk_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint16_t* Vp, const int32_t* block_table,
+                               int max_pages, int page_size, int n_pages, const int32_t* cu_new,
+                               const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, float softmax_scale,
+                               const libraspec_score_opts* opts, uint16_t* O, float* lse, void* workspace,
+                               size_t ws_bytes, void* stream) {
+  return chunk_attn(Q, Kp, Vp, true, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
+                    head_dim, 0, softmax_scale, opts, O, lse, workspace, ws_bytes, stream);
 }
 
 extern "C++" {

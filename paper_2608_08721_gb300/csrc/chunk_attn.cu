@@ -1,0 +1,1032 @@
+// Attention of a ragged chunk of new tokens over the KV cache, dense or paged
+// (a prompt, a part of one, or the one token of a decode step), one layer.
+//
+// Row (b, j, h): query head h of the j-th new token of sequence b, at position
+// p = kv_len_b + j; the keys of the new tokens are in the cache already, so
+// the sequence has N_b = kv_len_b + n_b keys. The row sees keys [lo, hi):
+//   lo = max(0, p - window + 1 if a window is given, first_key of the token)
+//   hi = min(N_b, max(p + 1, prefix_len_b))
+// and with s = scale q.k (then cap tanh(s / cap), then - slope_h |p - k|):
+//   O = sum exp(s - m) V / sum exp(s - m),  lse = m + log sum exp(s - m);
+// a row that sees nothing has O = 0 and lse = -inf.
+//
+// Work. The rows of a (sequence, kv head), g = Hq / Hkv per token, are cut into
+// blocks of two row tiles of R = g floor(128 / g) rows (whole tokens, one
+// tcgen05 M = 128 tile each), the keys that a block sees into 128-key tiles.
+// All (block, kv head, key tile) triples form one sequence, cut over the
+// persistent grid (one CTA per SM) by cost: each block weighs its tiles plus C
+// tile-equivalents (its queries' load and its epilogue), and CTA c takes the
+// tiles of the c-th share of the weight, so that CTAs finish together whatever
+// the lengths. A plan kernel lists the blocks and their key tiles from the
+// device-resident lengths; a launch dependent on it does the work.
+//
+// Two streams per CTA, each a softmax warpgroup with its own scores and O
+// accumulator in tensor memory, so that one stream's MMAs run beside the
+// other's softmax. A block of two row tiles gives each stream one of them, both
+// reading the same K and V tiles in shared memory (loaded once for 256 rows:
+// at 128 rows per load, L2 would bound a prompt's attention). A block of one
+// row tile (decode, short chunks) gives the streams alternate key tiles of the
+// same rows; the epilogue combines them.
+//
+// Roles in a CTA (320 threads): two softmax warpgroups; a producer warp whose
+// lanes each load their own piece of a K or V tile by TMA (a piece lies within
+// one page) into a ring of chunks; an MMA warp with one issuing thread. Thread
+// i of a warpgroup owns row i of its tile: it reads the tile's 128 scores,
+// masks them only where the tile reaches beyond what its warp's rows all see,
+// and writes P over them as bf16 (16 bits are what the tensor cores take; sums
+// are of the unrounded values, in 32 bits). The reference maximum of a row is
+// raised only when a score exceeds it by more than 8 (a factor of 2^8), so O
+// is rarely rescaled; p <= 2^8 keeps P and O in range.
+//
+// Keys that no row of a block sees take no part: K and V pieces that hold none
+// of them are not read (their pages need not exist), and V rows beyond the
+// block's range are cleared in shared memory before the MMA, so that what an
+// unwritten cache row holds (NaN, say) does not meet the zeros of P.
+//
+// A block cut over CTAs c0..c1 leaves one fp32 partial (O, m, l) per CTA; the
+// CTA that delivers the last of them merges all, in CTA order (results do not
+// depend on timing). No CTA waits for another.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include "common.cuh"
+#include "tc.cuh"
+
+namespace libraspec {
+
+int num_sms_current();
+
+constexpr int kCStreams = 2;
+constexpr int kCSoftmaxWarps = 4 * kCStreams;
+constexpr int kCProducerWarp = kCSoftmaxWarps;
+constexpr int kCMmaWarp = kCSoftmaxWarps + 1;
+constexpr int kCThreads = (kCSoftmaxWarps + 2) * 32;
+constexpr int kCRows = 128;                 // rows of a tile (tensor-memory lanes)
+constexpr int kCKeys = 128;                 // keys of a tile
+constexpr int kCMaxCtas = 192;
+constexpr int kCTmemCols = 512;
+constexpr float kCRescaleLog2 = 8.f;
+constexpr int kPlanThreads = 1024;
+constexpr int kCMaxKeys = 0x7fffffff - 2 * kCKeys;  // of a sequence: its last tile's end is an int
+
+// ---------------------------------------------------------------------------
+// Workspace: status, plan header, merge counters, block table of the plan,
+// partials.
+// ---------------------------------------------------------------------------
+struct PlanBlock {       // the rows of one block and the key tiles that they see
+  long long tiles_before;  // key tiles of the blocks before it (per kv head)
+  int b, tok0, n_tok;      // sequence; first packed row and tokens
+  int pos0;                // position of the first token
+  int klo, khi;            // keys that some row sees lie in [klo, khi)
+  int tile0, n_tiles;      // 128-key tiles
+};
+static_assert(sizeof(PlanBlock) == 40, "");
+
+struct PlanHead {
+  long long tiles;  // of all blocks (per kv head)
+  int blocks;
+  int pad;
+};
+
+struct ChunkWs {
+  size_t status, head, count, blocks, part_o, part_ml, total;
+};
+
+// Tokens of a block and the most blocks that T tokens of B sequences have.
+inline int block_tokens(int g) { return 2 * (kCRows / g); }
+inline long long max_blocks(long long T, int B, int g) {
+  const long long a = T / block_tokens(g) + B;
+  return a < T ? a : T;
+}
+
+static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
+  ChunkWs w{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align256(off + bytes); return o; };
+  w.status = take(256);
+  w.head = take(sizeof(PlanHead));
+  w.count = take(kCMaxCtas * sizeof(uint32_t));
+  w.blocks = take((size_t)max_blocks(T, B, Hq / Hkv) * sizeof(PlanBlock));
+  // two slots per CTA: its first item, and its last where that goes on in the next CTA
+  w.part_o = take(size_t(2 * kCMaxCtas) * 2 * kCRows * d * sizeof(float));
+  w.part_ml = take(size_t(2 * kCMaxCtas) * 2 * kCRows * 2 * sizeof(float));
+  w.total = off;
+  return w;
+}
+
+size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d) { return chunk_ws(T, B, Hq, Hkv, d).total; }
+
+// What a row sees.
+struct MaskArgs {
+  const int32_t* first_key;   // [T] or NULL
+  const int32_t* prefix_len;  // [B] or NULL
+  int window;                 // 0: none
+};
+
+__device__ __forceinline__ void row_range(int pos, int n_keys, int prefix, int first, int window, int& lo, int& hi) {
+  lo = max(0, first);
+  if (window > 0 && pos >= window) lo = max(lo, pos - window + 1);
+  hi = min(n_keys, max(pos + 1, prefix));
+  if (hi < lo) hi = lo;
+}
+
+// ---------------------------------------------------------------------------
+// The plan: blocks in sequence order.
+// ---------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ T block_scan(T v, T* warp_sums, T& total) {  // inclusive, kPlanThreads threads
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const T a = __shfl_up_sync(0xffffffffu, v, off);
+    if (lane >= off) v += a;
+  }
+  __syncthreads();  // (the sums of the scan before have been read)
+  if (lane == 31) warp_sums[warp] = v;
+  __syncthreads();
+  T w = warp_sums[lane];
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const T a = __shfl_up_sync(0xffffffffu, w, off);
+    if (lane >= off) w += a;
+  }
+  total = __shfl_sync(0xffffffffu, w, 31);
+  const T before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
+  return warp > 0 ? v + before : v;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t* __restrict__ cu_new,
+                                                                  const int32_t* __restrict__ kv_len,
+                                                                  const MaskArgs mask, int T, int B, int TB, int S_cap,
+                                                                  PlanBlock* __restrict__ blocks,
+                                                                  PlanHead* __restrict__ head, int* status) {
+  __shared__ int first_block[LIBRASPEC_MAX_B + 1];  // of each sequence
+  __shared__ int warp_i[32];
+  __shared__ long long warp_l[32];
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int tid = threadIdx.x;
+  int carry = 0;
+  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int nb = 0;
+    if (b < B) {
+      const int lo = cu_new[b], hi = cu_new[b + 1], kv = kv_len[b];
+      if (lo < 0 || hi < lo || hi > T) raise_status(status, LIBRASPEC_ST_BAD_LENGTH);
+      else if (kv < 0 || (long long)kv + (hi - lo) > S_cap) raise_status(status, LIBRASPEC_ST_KV_OVERFLOW);
+      else nb = (hi - lo + TB - 1) / TB;
+    }
+    int total;
+    const int inc = block_scan(nb, warp_i, total);
+    if (b < B) first_block[b] = carry + inc - nb;
+    carry += total;
+  }
+  if (tid == 0) first_block[B] = carry;
+  __syncthreads();
+  // (offsets that run backwards could ask for more blocks than the table holds)
+  const long long room = min((long long)T, (long long)T / TB + B);
+  const int n_blocks = (int)min((long long)carry, room);
+  if (carry > room && tid == 0) raise_status(status, LIBRASPEC_ST_BAD_LENGTH);
+  long long tiles = 0;
+  for (int e0 = 0; e0 < n_blocks; e0 += kPlanThreads) {
+    const int e = e0 + tid;
+    PlanBlock p{};
+    if (e < n_blocks) {
+      int lo = 0, hi = B;  // the sequence: the last b with first_block[b] <= e (which has blocks: e < first_block[b + 1])
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first_block[mid] <= e) lo = mid;
+        else hi = mid;
+      }
+      const int b = lo, c0 = cu_new[b], n = cu_new[b + 1] - c0, kv = kv_len[b], N = kv + n;
+      const int j0 = (e - first_block[b]) * TB, j1 = min(n, j0 + TB);
+      const int prefix = mask.prefix_len ? mask.prefix_len[b] : 0;
+      int klo = 0x7fffffff, khi = 0;
+      if (!mask.first_key) {  // ranges move forward with the position
+        int l, h;
+        row_range(kv + j0, N, prefix, 0, mask.window, klo, h);
+        row_range(kv + j1 - 1, N, prefix, 0, mask.window, l, khi);
+      } else {
+        for (int j = j0; j < j1; ++j) {
+          int l, h;
+          row_range(kv + j, N, prefix, mask.first_key[c0 + j], mask.window, l, h);
+          if (l < h) {
+            klo = min(klo, l);
+            khi = max(khi, h);
+          }
+        }
+        if (klo >= khi) klo = khi = N - 1;  // no row sees anything: one tile, of which nothing is read
+      }
+      p.b = b;
+      p.tok0 = c0 + j0;
+      p.n_tok = j1 - j0;
+      p.pos0 = kv + j0;
+      p.klo = klo;
+      p.khi = khi;
+      p.tile0 = klo / kCKeys;
+      p.n_tiles = max(1, (khi + kCKeys - 1) / kCKeys - p.tile0);
+    }
+    long long total;
+    const long long inc = block_scan((long long)p.n_tiles, warp_l, total);
+    if (e < n_blocks) {
+      p.tiles_before = tiles + inc - p.n_tiles;
+      blocks[e] = p;
+    }
+    tiles += total;
+  }
+  if (tid == 0) {
+    head->tiles = tiles;
+    head->blocks = n_blocks;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The attention kernel.
+// ---------------------------------------------------------------------------
+struct ChunkArgs {
+  CUtensorMap K, V, Q;
+  __nv_bfloat16* O;
+  float* lse;
+  const int32_t* cu_new;
+  const int32_t* kv_len;
+  const int32_t* block_table;
+  const float* slopes;  // [Hq] or NULL
+  MaskArgs mask;
+  const PlanBlock* blocks;
+  const PlanHead* head;
+  float* part_o;
+  float* part_ml;
+  uint32_t* count;
+  int* status;
+  float scale, softcap;
+  int B, Hq, Hkv, max_pages, page_size, n_pages, piece;  // piece: keys of one TMA box
+  int item_tiles;
+};
+
+// One item: a run of key tiles of one block for one kv head.
+struct ChunkItem {
+  int b, kvh, tok0, pos0;
+  int rows;            // of the block
+  int pair;            // two row tiles (a stream each), else one (alternate key tiles)
+  int tile0, n_tiles;
+  int klo, khi;
+  int partial, slot;   // write a partial to this slot, else O
+  int c0, np;          // first CTA of the block and how many share it
+  int last;            // the CTA's last item; 2: it has none
+  int pad;
+};
+static_assert(sizeof(ChunkItem) == 64, "items lie in 64-byte slots");
+
+template <int D>
+struct ChunkSmem {
+  static constexpr int kBoxes = D / 64;
+  static constexpr int kTile = kBoxes * 16384;           // 128 rows of Q, K or V: per 64 columns 128 rows of 128 bytes
+  static constexpr int kChunks = D == 128 ? 5 : 10;
+  static constexpr int kQ = 0;                           // two row tiles
+  static constexpr int kRing = 2 * kTile;
+  static constexpr int kBar = kRing + kChunks * kTile;
+  // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], pfull[2][2], pvdone[2], ofree[2], qfull, qempty, drain
+  static constexpr int kNumBars = 2 * kChunks + 14 + 3;
+  static constexpr int kInfo = kBar + (8 * kNumBars + 63) / 64 * 64;
+  static constexpr int kMisc = kInfo + 2 * 64;           // [0] abort, [1] this CTA merges, [2] tensor-memory address
+  static constexpr int kStat = kMisc + 16;               // (m, l) of each stream's rows (streams to be combined)
+  static constexpr int kBytes = kStat + kCStreams * kCRows * 8;
+  static constexpr int kColS = 0, kColO = 256;           // per stream 128 columns each
+  static_assert(kBytes <= 227 * 1024, "shared memory per CTA");
+};
+
+__device__ __forceinline__ void bar_sync_n(int bar, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory");
+}
+constexpr int kCAllBar = 1;
+
+__device__ __forceinline__ void c_fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d0), "=f"(d1)
+      : "f"(a0), "f"(a1), "f"(b), "f"(c));
+}
+__device__ __forceinline__ void c_add2(float& d0, float& d1, float a0, float a1) {
+  asm("{\n\t.reg .b64 a, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 d, {%0, %1};\n\t"
+      "add.rn.f32x2 d, d, a;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "+f"(d0), "+f"(d1)
+      : "f"(a0), "f"(a1));
+}
+__device__ __forceinline__ uint32_t c_pack(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// The CTA whose share of the weight W holds position y: the largest c with floor(c W / G) <= y.
+__device__ __forceinline__ int share_of(long long y, long long W, int G) {
+  return (int)(((y + 1) * (long long)G - 1) / W);
+}
+
+// Where weighted position x lies.
+struct Place {
+  int e, kvh, tile;     // block, kv head, tile within the block
+  long long before;     // tiles before it in the tile sequence
+};
+
+// Warp-wide. Block e's Hkv copies start at Hkv (tiles_before + C e); x < the total weight.
+__device__ Place find_place(long long x, const PlanBlock* __restrict__ blocks, int n_blocks, int Hkv, int C) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = n_blocks;  // the last block of [lo, lo + n) that starts at or before x
+  while (n > 1) {
+    const int step = (n + 31) / 32, i = lo + lane * step;
+    const bool at = lane * step < n && (long long)Hkv * (blocks[i].tiles_before + (long long)C * i) <= x;
+    const int k = 31 - __clz(__ballot_sync(0xffffffffu, at));  // (lane 0 always holds)
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  Place p;
+  p.e = lo;
+  const long long o = x - (long long)Hkv * (blocks[lo].tiles_before + (long long)C * lo);
+  const int nt = blocks[lo].n_tiles, w = nt + C;
+  p.kvh = (int)(o / w);
+  const int r = (int)(o - (long long)p.kvh * w);
+  p.tile = r > C ? r - C : 0;
+  p.before = (long long)Hkv * blocks[lo].tiles_before + (long long)p.kvh * nt + p.tile;
+  return p;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_constant__ ChunkArgs A) {
+  using SM = ChunkSmem<D>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sQ = smem_u32(smem + SM::kQ);
+  const uint32_t sRing = smem_u32(smem + SM::kRing);
+  const uint32_t bFull = smem_u32(smem + SM::kBar);
+  const uint32_t bEmpty = bFull + 8 * SM::kChunks;
+  const uint32_t bIFull = bEmpty + 8 * SM::kChunks;
+  const uint32_t bIEmpty = bIFull + 16;
+  const uint32_t bSFull = bIEmpty + 16;   // [stream]
+  const uint32_t bPFull = bSFull + 16;    // [stream][half]
+  const uint32_t bPVDone = bPFull + 32;   // [stream]
+  const uint32_t bOFree = bPVDone + 16;   // [stream]
+  const uint32_t bQFull = bOFree + 16;
+  const uint32_t bQEmpty = bQFull + 8;
+  const uint32_t bDrain = bQEmpty + 8;
+  ChunkItem* info = reinterpret_cast<ChunkItem*>(smem + SM::kInfo);
+  volatile int* misc = reinterpret_cast<int*>(smem + SM::kMisc);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = A.Hq / A.Hkv;
+  const int Rt = kCRows / g, R = g * Rt;  // tokens and rows of a row tile
+
+  if (warp == kCProducerWarp && lane < 3)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane == 0   ? &A.Q
+                                                                             : lane == 1 ? &A.K
+                                                                                         : &A.V))
+                 : "memory");
+  if (tid == 0) {
+    for (int s = 0; s < SM::kChunks; ++s) {
+      mbar_init(bFull + 8 * s, 1);
+      mbar_init(bEmpty + 8 * s, 1);  // the MMA warp's commit after the chunk's last use
+    }
+    for (int q = 0; q < 2; ++q) {
+      mbar_init(bIFull + 8 * q, 1);
+      mbar_init(bIEmpty + 8 * q, 1 + kCSoftmaxWarps);
+      mbar_init(bSFull + 8 * q, 1);
+      mbar_init(bPFull + 16 * q, 4);
+      mbar_init(bPFull + 16 * q + 8, 4);
+      mbar_init(bPVDone + 8 * q, 1);
+      mbar_init(bOFree + 8 * q, 4);
+    }
+    mbar_init(bQFull, 1);
+    mbar_init(bQEmpty, 1);
+    mbar_init(bDrain, 1);
+    misc[0] = (sQ & 1023) != 0;  // (the swizzled tiles need the alignment that the declaration asks for)
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kCMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(const_cast<int*>(misc + 2))),
+                 "n"(kCTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)misc[2];
+  const bool misaligned = misc[0] != 0;
+
+  if (misaligned) {
+    if (tid == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+  } else if (warp == kCProducerWarp) {
+    // ======================= producer =======================
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n_blocks = A.head->blocks;
+    const long long tiles = (long long)A.Hkv * A.head->tiles;
+    int G = (int)gridDim.x;
+    if (tiles < G) G = (int)tiles;
+    const int C = tiles > 0 ? (int)min((long long)A.item_tiles, tiles / (4 * (long long)G)) : 0;
+    const long long W = tiles + (long long)C * A.Hkv * n_blocks;
+    const int c = blockIdx.x;
+    Place at{};
+    long long left = 0;  // the CTA's tiles
+    if (c < G) {
+      const long long x0 = c * W / G, x1 = (c + 1) * W / G;
+      at = find_place(x0, A.blocks, n_blocks, A.Hkv, C);
+      const long long end = x1 < W ? find_place(x1, A.blocks, n_blocks, A.Hkv, C).before : tiles;
+      left = end - at.before;
+    }
+    if (left <= 0 && lane == 0) {
+      info[0].last = 2;
+      mbar_arrive(bIFull);
+    }
+    // a lane's piece of a K or V tile: keys [row, row + piece) of the tile, columns [64 hb, 64 hb + 64)
+    const int per_tile = kCKeys / A.piece;
+    const int my_row = (lane % per_tile) * A.piece, my_hb = lane / per_tile;
+    const bool mine = my_hb < SM::kBoxes;
+    uint32_t item_ctr = 0, chunk_ctr = 0;
+    const uint64_t once = evict_first_policy(), again = evict_normal_policy();
+    bool ok = true;
+    while (left > 0 && ok) {
+      const PlanBlock p = A.blocks[at.e];
+      ChunkItem it{};
+      it.b = p.b;
+      it.kvh = at.kvh;
+      it.tok0 = p.tok0;
+      it.pos0 = p.pos0;
+      it.rows = p.n_tok * g;
+      it.pair = p.n_tok > Rt;
+      it.tile0 = p.tile0 + at.tile;
+      it.n_tiles = (int)min((long long)(p.n_tiles - at.tile), left);
+      it.klo = p.klo;
+      it.khi = p.khi;
+      it.partial = it.n_tiles != p.n_tiles;
+      it.slot = at.tile == 0 ? 2 * c + 1 : 2 * c;
+      it.c0 = c;
+      it.np = 1;
+      if (it.partial) {
+        const long long y = (long long)A.Hkv * (p.tiles_before + (long long)C * at.e) +
+                            (long long)at.kvh * (p.n_tiles + C) + C;  // of the block's first tile
+        it.c0 = share_of(y, W, G);
+        it.np = share_of(y + p.n_tiles - 1, W, G) - it.c0 + 1;
+      }
+      left -= it.n_tiles;
+      it.last = left <= 0;
+      const int n = it.n_tiles, lag = it.pair ? 1 : 2;
+      // keys of a sequence that has one block are read once per kv head
+      const int n_new = A.cu_new[p.b + 1] - A.cu_new[p.b];
+      const uint64_t policy = n_new <= 2 * Rt ? once : again;
+      // pages of the item's tiles, four tiles at a time: lane 8 k + i holds that of piece i of the k-th
+      auto load_pages = [&](int group) {
+        if (!A.block_table) return p.b;
+        const int tile = 4 * group + lane / 8, i = lane % 8;
+        const int key = (it.tile0 + tile) * kCKeys + i * A.piece;
+        if (tile >= n || i >= per_tile || key >= p.khi || key + A.piece <= p.klo) return 0;
+        return __ldg(A.block_table + (size_t)p.b * A.max_pages + key / A.page_size);
+      };
+      int pages_before = 0, pages = load_pages(0), pages_next = load_pages(1);
+      // the item's queries, once the item before has issued its last S
+      ok = warp_wait(bIEmpty + 8 * (item_ctr & 1), ((item_ctr >> 1) & 1) ^ 1) &&
+           warp_wait(bQEmpty, (item_ctr & 1) ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        info[item_ctr & 1] = it;
+        mbar_arrive(bIFull + 8 * (item_ctr & 1));
+        mbar_expect_tx(bQFull, (it.pair ? 2 : 1) * R * D * 2);
+        for (int s = 0; s <= it.pair; ++s)
+          for (int hb = 0; hb < SM::kBoxes; ++hb)
+            tma_load_3d(sQ + s * SM::kTile + hb * 16384, &A.Q, bQFull, hb * 64, it.kvh * g, it.tok0 + s * Rt);
+      }
+      __syncwarp();
+      // chunks in the order in which the MMA warp uses them: K of tile t, then V of tile t - lag + 1
+      for (int kt = 0, vt = 0; vt < n && ok;) {
+        const bool is_k = kt < n && kt < vt + lag;
+        const int t = is_k ? kt++ : vt++;
+        const uint32_t ch = chunk_ctr % SM::kChunks;
+        ok = warp_wait(bEmpty + 8 * ch, ((chunk_ctr / SM::kChunks) & 1) ^ 1);
+        if (!ok) break;
+        if (is_k && t > 0 && (t & 3) == 0) {
+          pages_before = pages;
+          pages = pages_next;
+          pages_next = load_pages((t >> 2) + 1);
+        }
+        const int from = t >> 2 == (kt - 1) >> 2 ? pages : pages_before;  // kt - 1: the last K tile
+        int page = __shfl_sync(0xffffffffu, from, (t & 3) * 8 + lane % per_tile);
+        const int key = (it.tile0 + t) * kCKeys + my_row;
+        const bool load = mine && key < p.khi && key + A.piece > p.klo;
+        if (A.block_table && load && (page < 0 || page >= A.n_pages)) {
+          raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
+          page = 0;  // a valid page; the sequence's output is then meaningless
+        }
+        const uint32_t bar = bFull + 8 * ch;
+        const int pieces = __popc(__ballot_sync(0xffffffffu, load));
+        if (lane == 0) mbar_expect_tx(bar, pieces * A.piece * 128);
+        __syncwarp();
+        if (load) {
+          const int z = page * A.Hkv + it.kvh, y = A.block_table ? key % A.page_size : key;
+          tma_load_3d_hint(sRing + ch * SM::kTile + my_hb * 16384 + my_row * 128, is_k ? &A.K : &A.V, bar, my_hb * 64,
+                           y, z, policy);
+        }
+        ++chunk_ctr;
+      }
+      ++item_ctr;
+      // the next item: the next kv head, or the next block
+      at.tile = 0;
+      if (++at.kvh == A.Hkv) {
+        at.kvh = 0;
+        ++at.e;
+      }
+    }
+    if (!ok) {
+      if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+      misc[0] = 1;
+    }
+    // before leaving, wait (bounded) for the copies still in flight
+    if (lane == 0) {
+      for (uint32_t k = 0; k < (uint32_t)SM::kChunks && k < chunk_ctr; ++k) {
+        const uint32_t i = chunk_ctr - 1 - k;
+        mbar_wait(bFull + 8 * (i % SM::kChunks), (i / SM::kChunks) & 1);
+      }
+      if (item_ctr > 0) mbar_wait(bQFull, (item_ctr - 1) & 1);
+    }
+    __syncwarp();
+  } else if (warp == kCMmaWarp) {
+    // ======================= MMA issue =======================
+    if (lane == 0) {
+      uint32_t item_ctr = 0, chunk_ctr = 0;
+      uint32_t p_ctr[2] = {0, 0};  // P steps of each stream
+      uint32_t o_ctr[2] = {0, 0};  // items of each stream
+      bool ok = true;
+      auto take = [&]() {  // the next chunk, once it is filled
+        const uint32_t ch = chunk_ctr % SM::kChunks;
+        ok = ok && mbar_wait(bFull + 8 * ch, (chunk_ctr / SM::kChunks) & 1);
+        ++chunk_ctr;
+        return ch;
+      };
+      for (int last = 0; !last && ok; ++item_ctr) {
+        ok = mbar_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
+        if (!ok) break;
+        const int n_tiles = info[item_ctr & 1].n_tiles, pair = info[item_ctr & 1].pair;
+        last = info[item_ctr & 1].last;
+        if (last == 2) break;
+        mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
+        // Step n belongs to stream n & 1: tile n / 2 of the stream's own rows (a pair), or tile n of the same rows.
+        // S of a step goes where P of the stream's step before lies, so that one's PV is issued first.
+        const int steps = pair ? 2 * n_tiles : n_tiles;
+        uint32_t kch = 0, vch = 0;
+        for (int n = 0; n < steps + 2 && ok; ++n) {
+          const int s = n & 1;
+          const uint32_t ts = tmem + SM::kColS + s * 128;
+          if (n >= 2) {  // O += P V of step n - 2
+            if (!pair || s == 0) vch = take();
+            if (n < 4) {
+              ok = ok && mbar_wait(bOFree + 8 * s, (o_ctr[s] & 1) ^ 1);
+              ++o_ctr[s];
+            }
+            constexpr uint32_t idesc = mma_idesc(128, D, 1);
+            const uint32_t va = desc_lo(sRing + vch * SM::kTile, 16384);
+            const uint32_t d = tmem + SM::kColO + s * 128;
+            const uint32_t par = p_ctr[s]++ & 1;
+            ok = ok && mbar_wait(bPFull + 16 * s, par);
+            if (!ok) break;
+            tc_fence_after();
+            mma_ts4<2048>(d, ts, va, idesc, n < 4 ? 0u : 1u);
+            ok = mbar_wait(bPFull + 16 * s + 8, par);
+            if (!ok) break;
+            tc_fence_after();
+            mma_ts4<2048>(d, ts + 32, va + 512, idesc, 1u);
+            mma_commit(bPVDone + 8 * s);
+            if (!pair || s == 1) mma_commit(bEmpty + 8 * vch);
+          }
+          if (n < steps) {  // S = Q K^T of step n
+            if (!pair || s == 0) kch = take();
+            if (n == 0) ok = ok && mbar_wait(bQFull, item_ctr & 1);
+            if (!ok) break;
+            tc_fence_after();
+            constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
+            const uint32_t qa = desc_lo(sQ + (pair ? s : 0) * SM::kTile, 16);
+            const uint32_t ka = desc_lo(sRing + kch * SM::kTile, 16);
+#pragma unroll
+            for (int hb = 0; hb < SM::kBoxes; ++hb)
+              mma_ss4<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
+            mma_commit(bSFull + 8 * s);
+            if (!pair || s == 1) mma_commit(bEmpty + 8 * kch);
+            if (n == steps - 1) mma_commit(bQEmpty);
+          }
+        }
+      }
+      if (!ok) {
+        raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+        misc[0] = 1;
+      }
+      // every MMA issued has completed before the tensor memory is released
+      mma_commit(bDrain);
+      mbar_wait(bDrain, 0);
+    }
+    __syncwarp();
+  } else {
+    // ======================= softmax warpgroups =======================
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int st = warp >> 2, wq = warp & 3;
+    const int row = wq * 32 + lane;  // tensor-memory lane
+    const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+    const uint32_t ts = tmem + lane_off + SM::kColS + st * 128;
+    const uint32_t to = tmem + lane_off + SM::kColO;
+    float2* stat = reinterpret_cast<float2*>(smem + SM::kStat);  // [stream][128]
+    const float scale_log2 = A.scale * kLog2e;
+    uint32_t item_ctr = 0, chunk_base = 0;
+    uint32_t done0 = 0, done1 = 0;  // steps of streams 0 and 1 in the items before this one
+    bool ok = true;
+    // A wait that fails leaves `ok` false; the item is then finished without further waits, so that every thread
+    // still reaches every named barrier.
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && warp_wait(bar, parity); };
+    for (int last = 0; !last;) {
+      wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
+      if (bar_any<kCAllBar, kCSoftmaxWarps * 32>(!ok)) {
+        ok = false;
+        break;
+      }
+      const ChunkItem& it = info[item_ctr & 1];
+      last = it.last;
+      if (last == 2) break;
+      const bool pair = it.pair;
+      const int n_tiles = it.n_tiles;
+      const int steps0 = pair ? n_tiles : (n_tiles + 1) >> 1, steps1 = pair ? n_tiles : n_tiles >> 1;
+      const int my_steps = st ? steps1 : steps0;
+      const int rr = (pair ? st * R : 0) + row;  // row of the block
+      const bool valid = row < R && rr < it.rows;
+      const bool warp_live = wq * 32 < R && (pair ? st * R : 0) + wq * 32 < it.rows;
+      const int tok = it.tok0 + rr / g, hq = it.kvh * g + rr % g, pos = it.pos0 + rr / g;
+      int lo = 0, hi = 0;
+      float slope = 0.f;
+      if (valid) {
+        const int n_keys = A.kv_len[it.b] + A.cu_new[it.b + 1] - A.cu_new[it.b];
+        row_range(pos, n_keys, A.mask.prefix_len ? A.mask.prefix_len[it.b] : 0,
+                  A.mask.first_key ? A.mask.first_key[tok] : 0, A.mask.window, lo, hi);
+        if (A.slopes) slope = A.slopes[hq] * kLog2e;
+      }
+      const bool shaped = A.softcap > 0.f || A.slopes;  // scores are more than a scaled product
+      const float sc = shaped ? 1.f : scale_log2;
+      float m_run = -INFINITY, l_run = 0.f;
+      for (int i = 0; i < my_steps; ++i) {
+        const int j = pair ? i : 2 * i + st;  // the item's tile
+        const int kt0 = (it.tile0 + j) * kCKeys;
+        const uint32_t n = (st ? done1 : done0) + i;
+        if (kt0 < it.klo || kt0 + kCKeys > it.khi) {
+          // V rows that no row of the block sees: cleared once they have landed
+          const uint32_t ci = chunk_base + (pair ? 2 * j + 1 : j + min(j + 2, n_tiles));
+          const uint32_t ch = ci % SM::kChunks;
+          wait(bFull + 8 * ch, (ci / SM::kChunks) & 1);
+          const int key = kt0 + row;
+          if (ok && (key < it.klo || key >= it.khi)) {
+#pragma unroll
+            for (int hb = 0; hb < SM::kBoxes; ++hb) {
+              uint4* v = reinterpret_cast<uint4*>(smem + SM::kRing + ch * SM::kTile + hb * 16384 + row * 128);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] = make_uint4(0, 0, 0, 0);
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        wait(bSFull + 8 * st, n & 1);
+        if (!warp_live) {
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bPFull + 16 * st);
+            mbar_arrive(bPFull + 16 * st + 8);
+          }
+          continue;
+        }
+        tc_fence_after();
+        uint32_t x[4][32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(ts + 32 * q, x[q]);
+        tmem_wait_ld();
+        if (shaped) {  // the scores in units of log 2
+          const float cap2 = A.softcap * kLog2e, u2 = A.softcap > 0.f ? 2.f * scale_log2 / A.softcap : 0.f;
+          const float d0 = (float)(kt0 - pos);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              float y = __uint_as_float(x[q][c]);
+              // cap tanh(s / cap) = cap (1 - 2 / (e^(2 s / cap) + 1))
+              if (A.softcap > 0.f) y = cap2 - __fdividef(2.f * cap2, ex2_approx(y * u2) + 1.f);
+              else y *= scale_log2;
+              x[q][c] = __float_as_uint(fmaf(-slope, fabsf(d0 + (float)(32 * q + c)), y));
+            }
+        }
+        if (__any_sync(0xffffffffu, valid && (kt0 < lo || kt0 + kCKeys > hi))) {
+          const int a = lo - kt0, span = hi - lo;
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              if ((uint32_t)(32 * q + c - a) >= (uint32_t)span) x[q][c] = __float_as_uint(-INFINITY);
+        }
+        float mx[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          mx[q] = __uint_as_float(x[q][0]);
+#pragma unroll
+          for (int c = 1; c < 31; c += 2)
+            mx[q] = fmaxf(fmaxf(mx[q], __uint_as_float(x[q][c])), __uint_as_float(x[q][c + 1]));
+          mx[q] = fmaxf(mx[q], __uint_as_float(x[q][31]));
+        }
+        // (a lane past the block's rows holds scores of whatever its Q row is: it asks for no raise)
+        float cmax = valid ? fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sc : 0.f;
+        if (cmax != cmax) cmax = 0.f;  // nothing but NaN: the row's sum is NaN whatever the reference
+        if (i == 0) {
+          m_run = cmax;
+        } else if (__any_sync(0xffffffffu, cmax > m_run + kCRescaleLog2)) {
+          // O and l against the new reference
+          const bool raise = cmax > m_run + kCRescaleLog2;
+          const float f = !raise ? 1.f : m_run == -INFINITY ? 0.f : ex2_approx(m_run - cmax);
+          m_run = raise ? cmax : m_run;
+          l_run *= f;
+          wait(bPVDone + 8 * st, (n - 1) & 1);
+          tc_fence_after();
+#pragma unroll 1
+          for (int c0 = 0; c0 < D; c0 += 16) {
+            uint32_t o[16];
+            tmem_ld16(to + st * 128 + c0, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+            tmem_st16(to + st * 128 + c0, o);
+          }
+          tmem_wait_st();
+        }
+        const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+        float la[2] = {0.f, 0.f}, lb[2] = {0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int c = 0; c < 32; c += 4) {
+            float y0, y1, y2, y3;
+            c_fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), sc, neg_m);
+            c_fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), sc, neg_m);
+            y0 = ex2_approx(y0);
+            y1 = ex2_approx(y1);
+            y2 = ex2_approx(y2);
+            y3 = ex2_approx(y3);
+            c_add2(la[0], la[1], y0, y1);
+            c_add2(lb[0], lb[1], y2, y3);
+            pk[c >> 1] = c_pack(y0, y1);
+            pk[(c >> 1) + 1] = c_pack(y2, y3);
+          }
+          tmem_st16(ts + 16 * q, pk);
+          if (q & 1) {  // 64 keys of P: the first half's MMAs may start
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bPFull + 16 * st + 8 * (q >> 1));
+          }
+        }
+        l_run += (la[0] + la[1]) + (lb[0] + lb[1]);
+      }
+      // ---- epilogue ----
+      float f0 = 1.f, f1 = 0.f;  // factors of the streams' O
+      const bool both = !pair && steps1 > 0;  // the streams hold keys of the same rows
+      if (both) {
+        if (warp_live) stat[st * kCRows + row] = make_float2(m_run, l_run);
+        bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+        if (warp_live) {
+          const float2 a = stat[row], b = stat[kCRows + row];
+          const float M = fmaxf(a.x, b.x);
+          f0 = M == -INFINITY ? 0.f : ex2_approx(a.x - M);
+          f1 = M == -INFINITY ? 0.f : ex2_approx(b.x - M);
+          m_run = M;
+          l_run = f0 * a.y + f1 * b.y;
+        }
+      }
+      if (pair) {
+        wait(bPVDone + 8 * st, ((st ? done1 : done0) + my_steps - 1) & 1);
+      } else {
+        wait(bPVDone, (done0 + steps0 - 1) & 1);
+        if (both) wait(bPVDone + 8, (done1 + steps1 - 1) & 1);
+      }
+      tc_fence_after();
+      // of rows in two streams each warpgroup writes half of the columns; a single step leaves all to the first
+      if (warp_live && (pair || both || st == 0)) {
+        const bool partial = it.partial;
+        const size_t prow = (size_t)it.slot * 2 * kCRows + rr;
+        if (!partial) {
+          const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // (NaN stays)
+          f0 *= inv;
+          f1 *= inv;
+        }
+        const uint32_t oa = to + (pair ? st * 128 : 0);
+        const int cb = both ? st * (D / 2) : 0, ce = both ? cb + D / 2 : D;
+        __nv_bfloat16* orow = A.O + ((size_t)tok * A.Hq + hq) * D;
+#pragma unroll 1
+        for (int c0 = cb; c0 < ce; c0 += 32) {
+          uint32_t o[32];
+          tmem_ld32(oa + c0, o);
+          if (both) {
+            uint32_t o1[32];
+            tmem_ld32(oa + 128 + c0, o1);
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c)
+              o[c] = __float_as_uint(fmaf(__uint_as_float(o1[c]), f1, __uint_as_float(o[c]) * f0));
+          } else {
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f0);
+          }
+          if (!valid) continue;
+          if (!partial) {
+            uint4* dst = reinterpret_cast<uint4*>(orow + c0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              dst[k] = make_uint4(c_pack(__uint_as_float(o[8 * k]), __uint_as_float(o[8 * k + 1])),
+                                  c_pack(__uint_as_float(o[8 * k + 2]), __uint_as_float(o[8 * k + 3])),
+                                  c_pack(__uint_as_float(o[8 * k + 4]), __uint_as_float(o[8 * k + 5])),
+                                  c_pack(__uint_as_float(o[8 * k + 6]), __uint_as_float(o[8 * k + 7])));
+          } else {
+            uint4* dst = reinterpret_cast<uint4*>(A.part_o + prow * D + c0);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dst[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+          }
+        }
+        if (valid && (pair || st == 0)) {
+          if (partial) *reinterpret_cast<float2*>(A.part_ml + prow * 2) = make_float2(m_run, l_run);
+          else if (A.lse) A.lse[(size_t)tok * A.Hq + hq] = (m_run + __log2f(l_run)) * kLn2;
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      // a stream's accumulator is free once all that read it have: its own rows' warps, or (combined) both streams'
+      if (both) bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+      if (lane == 0 && my_steps > 0) mbar_arrive(bOFree + 8 * st);
+      if (it.partial) {
+        // counted in once every thread's part is written; the CTA that counts the last merges
+        __threadfence();
+        bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+        if (tid == 0) {
+          const uint32_t old = atomicAdd(A.count + it.c0, 1u);
+          misc[1] = old == (uint32_t)it.np - 1;
+          if (misc[1]) A.count[it.c0] = 0u;
+          __threadfence();
+        }
+        bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+        if (misc[1]) {
+          constexpr int C4 = D / 4;
+          const int np = it.np, c0 = it.c0, items = it.rows * C4;
+          for (int k = tid; k < items; k += kCSoftmaxWarps * 32) {
+            const int r = k / C4, c = k - r * C4;
+            float M = -INFINITY, L = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p0 = 0; p0 < np; p0 += 4) {
+              float2 ml[4];
+              float4 v[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const int p = p0 + q;
+                if (p < np) {
+                  const size_t prow = (size_t)(p == 0 ? 2 * c0 + 1 : 2 * (c0 + p)) * 2 * kCRows + r;
+                  ml[q] = __ldcg(reinterpret_cast<const float2*>(A.part_ml + prow * 2));
+                  v[q] = __ldcg(reinterpret_cast<const float4*>(A.part_o + prow * D) + c);
+                } else {
+                  ml[q] = make_float2(-INFINITY, 0.f);
+                  v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+              }
+              const float Mn = fmaxf(M, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+              if (Mn == -INFINITY) continue;
+              const float f = ex2_approx(M - Mn);  // 0 while M is -inf
+              acc.x *= f;
+              acc.y *= f;
+              acc.z *= f;
+              acc.w *= f;
+              L *= f;
+              M = Mn;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                const float w = ex2_approx(ml[q].x - Mn);
+                acc.x += w * v[q].x;
+                acc.y += w * v[q].y;
+                acc.z += w * v[q].z;
+                acc.w += w * v[q].w;
+                L += w * ml[q].y;
+              }
+            }
+            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+            const size_t orow = (size_t)(it.tok0 + r / g) * A.Hq + it.kvh * g + r % g;
+            uint2 o;
+            o.x = c_pack(acc.x * inv, acc.y * inv);
+            o.y = c_pack(acc.z * inv, acc.w * inv);
+            *reinterpret_cast<uint2*>(A.O + orow * D + c * 4) = o;
+            if (A.lse && c == 0) A.lse[orow] = (M + __log2f(L)) * kLn2;
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));  // `it` has been read
+      done0 += steps0;
+      done1 += steps1;
+      chunk_base += 2 * n_tiles;
+      ++item_ctr;
+    }
+    if (!ok) {
+      if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+      misc[0] = 1;
+    }
+  }
+  // every role is done with the tensor memory
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kCMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kCTmemCols) : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+// A [planes, rows, D] tensor of bf16 in boxes of 64 columns x `box_rows` rows x `box_planes` planes (of dimension 1
+// for the queries [T, Hq, D]: box_rows heads of box_planes tokens), 128-byte swizzle.
+static bool make_map(CUtensorMap* map, const void* base, int D, long long rows, long long planes, int box_rows,
+                     int box_planes, CUtensorMapL2promotion promote) {
+  auto enc = get_encode();
+  if (!enc) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)rows, (cuuint64_t)planes};
+  cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)rows * D * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_planes};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promote,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stream) {
+  using SM = ChunkSmem<D>;
+  static bool configured = false;
+  if (!configured) {
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes);
+    if (e != cudaSuccess) return e;
+    configured = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kCThreads);
+  cfg.dynamicSmemBytes = SM::kBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D>, a);
+}
+
+// block_table == nullptr: dense caches [B, Hkv, S_cap, D]. page_size: a multiple of 16.
+cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* block_table,
+                              int max_pages, int page_size, int n_pages, const int32_t* cu_new, const int32_t* kv_len,
+                              int T, int B, int Hq, int Hkv, int D, int S_cap, float scale, float softcap,
+                              const float* slopes, int window, const int32_t* first_key, const int32_t* prefix_len,
+                              uint16_t* O, float* lse, char* ws, cudaStream_t stream) {
+  if (T == 0 || B == 0) return cudaSuccess;
+  const ChunkWs lay = chunk_ws(T, B, Hq, Hkv, D);
+  const int g = Hq / Hkv;
+  ChunkArgs a;
+  a.O = reinterpret_cast<__nv_bfloat16*>(O);
+  a.lse = lse;
+  a.cu_new = cu_new;
+  a.kv_len = kv_len;
+  a.block_table = block_table;
+  a.slopes = slopes;
+  a.mask = MaskArgs{first_key, prefix_len, window};
+  a.blocks = reinterpret_cast<const PlanBlock*>(ws + lay.blocks);
+  a.head = reinterpret_cast<const PlanHead*>(ws + lay.head);
+  a.part_o = reinterpret_cast<float*>(ws + lay.part_o);
+  a.part_ml = reinterpret_cast<float*>(ws + lay.part_ml);
+  a.count = reinterpret_cast<uint32_t*>(ws + lay.count);
+  a.status = reinterpret_cast<int*>(ws + lay.status);
+  a.scale = scale;
+  a.softcap = softcap;
+  a.B = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  a.n_pages = n_pages;
+  // a box lies within one page: the largest power of two up to 64 that divides the page size
+  a.piece = 64;
+  if (block_table)
+    while (page_size % a.piece) a.piece /= 2;
+  a.item_tiles = 2;
+  const long long rows = block_table ? page_size : S_cap, planes = (long long)(block_table ? n_pages : B) * Hkv;
+  if (!make_map(&a.K, Kc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
+      !make_map(&a.V, Vc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
+      !make_map(&a.Q, Q, D, Hq, T, g, kCRows / g, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
+    return cudaErrorInvalidValue;
+  chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(cu_new, kv_len, a.mask, T, B, block_tokens(g),
+                                                    std::min(S_cap, kCMaxKeys),
+                                                    reinterpret_cast<PlanBlock*>(ws + lay.blocks),
+                                                    reinterpret_cast<PlanHead*>(ws + lay.head), a.status);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const int grid = std::min(num_sms_current(), kCMaxCtas);
+  return D == 128 ? launch_attn_t<128>(a, grid, stream) : launch_attn_t<64>(a, grid, stream);
+}
+
+}  // namespace libraspec

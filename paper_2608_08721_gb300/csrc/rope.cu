@@ -1,0 +1,323 @@
+// Rotary positions, and the append of a ragged chunk of new tokens to the KV
+// cache with the rotation on the way.
+//
+// Pair i of a head turns by the angle pos * f_i: (x0, x1) -> m (x0 cos - x1
+// sin, x0 sin + x1 cos). The frequencies come as turns per position, f / 2pi
+// = hi + lo in two floats, so that the part of the angle that counts, its
+// fraction of a turn, is exact to 2^-24 turns at any position: p = pos hi has
+// the exact error e = fma(pos, hi, -p), p - rint(p) is exact, and sincospi
+// needs no further reduction. (A binary32 angle of 131072 radians is off by
+// 0.004.)
+//
+// Bound by HBM: every element is read once and written once. One CTA works on
+// one token: its first threads form the token's cosines and sines in shared
+// memory (once for all heads) while every thread's first loads are on their
+// way, then the threads share out the token's heads in units of 16 bytes.
+#include <cmath>
+#include <type_traits>
+
+#include "common.cuh"
+
+namespace libraspec {
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopeMaxPairs = 256;
+
+// cos and sin of pair i at position pos, times the magnitude.
+__device__ __forceinline__ float2 rope_turn(int pos, float2 f, float magnitude) {
+  // positions from 2^24 on are not binary32 numbers: their remainder turns by itself
+  const float pf = (float)pos;
+  const float rest = (float)((long long)pos - (long long)pf);
+  const float p = __fmul_rn(pf, f.x);
+  const float e = __fmaf_rn(pf, f.x, -p);
+  const float r = (p - rintf(p)) + (e + __fmaf_rn(pf, f.y, rest * f.x));
+  float s, c;
+  sincospif(2.f * r, &s, &c);
+  return make_float2(c * magnitude, s * magnitude);
+}
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ void from_f32(float& d, float x) { d = x; }
+__device__ __forceinline__ void from_f32(uint16_t& d, float x) { d = __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
+
+// N consecutive elements as one access of N * sizeof(T) bytes
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Pack {
+  T v[N];
+};
+
+template <typename Tin, typename Tout, int N>
+__device__ __forceinline__ Pack<Tout, N> convert(const Pack<Tin, N>& a) {
+  if constexpr (std::is_same<Tin, Tout>::value) {
+    return a;
+  } else {
+    Pack<Tout, N> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) from_f32(r.v[i], to_f32(a.v[i]));
+    return r;
+  }
+}
+
+// One row (a head of a token) of the call: where it is read and written, and whether it turns.
+template <typename Tin, typename Tout>
+struct RopeRow {
+  const Tin* src;
+  Tout* dst;
+  bool turns;
+};
+
+// A head as units: N elements of the first half of the rotated part with the N they pair with (half layout), or 2N
+// consecutive ones (interleaved), then 2N at a time of the part that is only copied.
+template <typename Tin, typename Tout, int N, bool INTER>
+struct RopeUnit {
+  Pack<Tin, N> a, b;
+  __device__ __forceinline__ void load(const RopeRow<Tin, Tout>& r, int u, int half) {
+    const int i = at(u, half), j = partner(u, half);
+    a = *reinterpret_cast<const Pack<Tin, N>*>(r.src + i);
+    b = *reinterpret_cast<const Pack<Tin, N>*>(r.src + j);
+  }
+  __device__ __forceinline__ void store(const RopeRow<Tin, Tout>& r, int u, int half, const float2* cs) const {
+    Pack<Tout, N> x, y;
+    if (u * N >= half || !r.turns) {
+      x = convert<Tin, Tout, N>(a);
+      y = convert<Tin, Tout, N>(b);
+    } else if (INTER) {
+      if constexpr (N == 1) {
+        const float2 t = cs[u];
+        turn(to_f32(a.v[0]), to_f32(b.v[0]), t, x.v[0], y.v[0]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < N / 2; ++k) {
+          turn(to_f32(a.v[2 * k]), to_f32(a.v[2 * k + 1]), cs[u * N + k], x.v[2 * k], x.v[2 * k + 1]);
+          turn(to_f32(b.v[2 * k]), to_f32(b.v[2 * k + 1]), cs[u * N + N / 2 + k], y.v[2 * k], y.v[2 * k + 1]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) turn(to_f32(a.v[k]), to_f32(b.v[k]), cs[u * N + k], x.v[k], y.v[k]);
+    }
+    *reinterpret_cast<Pack<Tout, N>*>(r.dst + at(u, half)) = x;
+    *reinterpret_cast<Pack<Tout, N>*>(r.dst + partner(u, half)) = y;
+  }
+  // (past the rotated part both layouts take 2N consecutive elements)
+  __device__ static __forceinline__ int at(int u, int half) { return INTER || u * N >= half ? 2 * u * N : u * N; }
+  __device__ static __forceinline__ int partner(int u, int half) {
+    return INTER || u * N >= half ? (2 * u + 1) * N : half + u * N;
+  }
+  __device__ static __forceinline__ void turn(float x0, float x1, float2 t, Tout& y0, Tout& y1) {
+    from_f32(y0, fmaf(x0, t.x, -x1 * t.y));
+    from_f32(y1, fmaf(x0, t.y, x1 * t.x));
+  }
+};
+
+// Rows h of a token: h < Hq queries, then (append) Hkv keys and Hkv values.
+struct RopeArgs {
+  const void *Q, *K, *V;
+  long long q_stride, k_stride, v_stride, o_stride;  // elements between tokens
+  const int32_t* pos;     // [T], or NULL (append): kv_len of the token's sequence + its index there
+  const float2* turns;    // [rot / 2]
+  float magnitude;
+  int inverse;
+  int T, Hq, Hkv, d, half;
+  void* Qo;
+  // append
+  const int32_t *cu_new, *kv_len, *block_table;
+  int B, max_pages, page_size, n_pages, S_cap;
+  uint16_t *Kc, *Vc;
+  int* status;
+};
+
+template <typename Tin, typename Tout, int N, bool INTER, bool APPEND>
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
+  __shared__ float2 cs[kRopeMaxPairs];
+  __shared__ int s_seq, s_pos;
+  __shared__ long long s_row;  // the token's row of the cache (of kv head 0), negative: none
+  const int t = blockIdx.x, tid = threadIdx.x;
+  const int per_head = A.d / (2 * N);
+  const int heads = APPEND ? A.Hq + 2 * A.Hkv : A.Hq;
+  const int units = heads * per_head;
+  long long head_step = 0;  // between the rows of neighbouring kv heads in the cache
+
+  auto row = [&](int h, long long cache_row) {
+    RopeRow<Tin, Tout> r;
+    if (!APPEND || h < A.Hq) {
+      r.src = static_cast<const Tin*>(A.Q) + t * A.q_stride + (long long)h * A.d;
+      r.dst = static_cast<Tout*>(A.Qo) + t * A.o_stride + (long long)h * A.d;
+      r.turns = true;
+    } else {
+      const bool key = h < A.Hq + A.Hkv;
+      const int kvh = h - A.Hq - (key ? 0 : A.Hkv);
+      r.src = static_cast<const Tin*>(key ? A.K : A.V) + t * (key ? A.k_stride : A.v_stride) + (long long)kvh * A.d;
+      r.dst = reinterpret_cast<Tout*>(key ? A.Kc : A.Vc) + cache_row + kvh * head_step;
+      r.turns = key;
+    }
+    return r;
+  };
+
+  // the first unit's loads go out before anything else is known
+  RopeUnit<Tin, Tout, N, INTER> first;
+  if (tid < units) first.load(row(tid / per_head, 0), tid % per_head, A.half);
+
+  if constexpr (APPEND) {
+    if (tid == 0) s_seq = -1;
+    __syncthreads();
+    // the token's sequence: every thread looks at its share of the offsets
+    for (int b = tid; b < A.B; b += kRopeThreads) {
+      const int lo = A.cu_new[b], hi = A.cu_new[b + 1], kv = A.kv_len[b];
+      if (t == 0 && (lo < 0 || hi < lo || hi > A.T)) raise_status(A.status, LIBRASPEC_ST_BAD_LENGTH);
+      if (t < lo || t >= hi) continue;
+      s_seq = b;
+      const long long s = (long long)kv + (t - lo);
+      long long at = -1;
+      if (kv < 0 || s >= A.S_cap) {
+        raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
+      } else if (A.block_table) {
+        const int page = A.block_table[(size_t)b * A.max_pages + s / A.page_size];
+        if (page < 0 || page >= A.n_pages) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
+        else at = ((long long)page * A.Hkv * A.page_size + s % A.page_size) * A.d;
+      } else {
+        at = ((long long)b * A.Hkv * A.S_cap + s) * A.d;
+      }
+      s_row = at;
+      s_pos = A.pos ? A.pos[t] : (int)s;
+    }
+    __syncthreads();
+    if (s_seq < 0) return;  // a row of no sequence
+    head_step = (long long)(A.block_table ? A.page_size : A.S_cap) * A.d;
+  }
+  const int pos = APPEND ? s_pos : A.pos[t];
+  for (int i = tid; i < A.half; i += kRopeThreads) {
+    float2 c = rope_turn(pos, A.turns[i], A.magnitude);
+    if (A.inverse) c.y = -c.y;
+    cs[i] = c;
+  }
+  __syncthreads();
+  const long long cache_row = APPEND ? s_row : 0;
+  const int live = APPEND && cache_row < 0 ? A.Hq * per_head : units;  // no place in the cache: the queries alone
+  for (int i = tid; i < live; i += kRopeThreads) {
+    const RopeRow<Tin, Tout> r = row(i / per_head, cache_row);
+    const int u = i % per_head;
+    if (i != tid) first.load(r, u, A.half);
+    first.store(r, u, A.half, cs);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+// Turns per position of each pair as (hi, lo) floats; scaling as in the header.
+void rope_frequencies(int rot, double theta, int scaling, double factor, double low, double high, double original_len,
+                      float* turns) {
+  const double two_pi = 6.283185307179586476925;
+  if (scaling == LIBRASPEC_ROPE_NTK) theta *= std::pow(factor, rot / (rot - 2.0));
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / rot);
+    if (scaling == LIBRASPEC_ROPE_LINEAR) f /= factor;
+    if (scaling == LIBRASPEC_ROPE_BY_PARTS) {
+      const double r = original_len * f / two_pi;  // turns over the original context
+      const double keep = std::min(1.0, std::max(0.0, (r - low) / (high - low)));
+      f = (1.0 - keep) * f / factor + keep * f;
+    }
+    const double t = f / two_pi;
+    turns[2 * i] = (float)t;
+    turns[2 * i + 1] = (float)(t - (double)turns[2 * i]);
+  }
+}
+
+template <typename Tin, typename Tout, int N, bool APPEND>
+static cudaError_t launch_n(const RopeArgs& a, int interleaved, cudaStream_t stream) {
+  if (interleaved) rope_kernel<Tin, Tout, N, true, APPEND><<<a.T, kRopeThreads, 0, stream>>>(a);
+  else rope_kernel<Tin, Tout, N, false, APPEND><<<a.T, kRopeThreads, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
+// Units of N elements where every access they make is aligned to its size: the rotated half and the head in whole
+// units, and all rows starting on a multiple of N elements. Else pair by pair.
+template <typename Tin, typename Tout, bool APPEND>
+static cudaError_t launch_rope_t(const RopeArgs& a, int interleaved, cudaStream_t stream) {
+  constexpr int N = 16 / (int)sizeof(Tin);
+  auto fits = [&](const void* p, long long stride, size_t size) {
+    return reinterpret_cast<uintptr_t>(p) % (N * size) == 0 && stride % N == 0;
+  };
+  bool vec = a.half % N == 0 && a.d % (2 * N) == 0;
+  if (a.Hq > 0) vec = vec && fits(a.Q, a.q_stride, sizeof(Tin)) && fits(a.Qo, a.o_stride, sizeof(Tout));
+  if (APPEND) vec = vec && fits(a.K, a.k_stride, sizeof(Tin)) && fits(a.V, a.v_stride, sizeof(Tin));
+  return vec ? launch_n<Tin, Tout, N, APPEND>(a, interleaved, stream)
+             : launch_n<Tin, Tout, 1, APPEND>(a, interleaved, stream);
+}
+
+template <typename T>
+cudaError_t launch_rope(const T* X, long long x_stride, const int32_t* pos, const float* turns, float magnitude,
+                        int n_tokens, int H, int d, int rot, int interleaved, int inverse, T* Y, long long y_stride,
+                        cudaStream_t stream) {
+  if (n_tokens == 0) return cudaSuccess;
+  RopeArgs a{};
+  a.Q = X;
+  a.q_stride = x_stride;
+  a.o_stride = y_stride;
+  a.pos = pos;
+  a.turns = reinterpret_cast<const float2*>(turns);
+  a.magnitude = magnitude;
+  a.inverse = inverse;
+  a.T = n_tokens;
+  a.Hq = H;
+  a.d = d;
+  a.half = rot / 2;
+  a.Qo = Y;
+  return launch_rope_t<T, T, false>(a, interleaved, stream);
+}
+template cudaError_t launch_rope<float>(const float*, long long, const int32_t*, const float*, float, int, int, int,
+                                        int, int, int, float*, long long, cudaStream_t);
+template cudaError_t launch_rope<uint16_t>(const uint16_t*, long long, const int32_t*, const float*, float, int, int,
+                                           int, int, int, int, uint16_t*, long long, cudaStream_t);
+
+template <typename T>
+cudaError_t launch_rope_append(const T* Q, long long q_stride, const T* K, long long k_stride, const T* V,
+                               long long v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                               const float* turns, float magnitude, const int32_t* block_table, int max_pages,
+                               int page_size, int n_pages, int n_tokens, int B, int Hq, int Hkv, int d, int rot,
+                               int interleaved, uint16_t* Qo, uint16_t* Kc, uint16_t* Vc, int S_cap, int* status,
+                               cudaStream_t stream) {
+  if (n_tokens == 0 || B == 0) return cudaSuccess;
+  RopeArgs a{};
+  a.Q = Q;
+  a.K = K;
+  a.V = V;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.o_stride = (long long)Hq * d;
+  a.pos = pos;
+  a.turns = reinterpret_cast<const float2*>(turns);
+  a.magnitude = magnitude;
+  a.T = n_tokens;
+  a.Hq = Q ? Hq : 0;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.half = rot / 2;
+  a.Qo = Qo;
+  a.cu_new = cu_new;
+  a.kv_len = kv_len;
+  a.block_table = block_table;
+  a.B = B;
+  a.max_pages = max_pages;
+  a.page_size = page_size;
+  a.n_pages = n_pages;
+  a.S_cap = S_cap;
+  a.Kc = Kc;
+  a.Vc = Vc;
+  a.status = status;
+  return launch_rope_t<T, uint16_t, true>(a, interleaved, stream);
+}
+template cudaError_t launch_rope_append<float>(const float*, long long, const float*, long long, const float*,
+                                               long long, const int32_t*, const int32_t*, const int32_t*, const float*,
+                                               float, const int32_t*, int, int, int, int, int, int, int, int, int, int,
+                                               uint16_t*, uint16_t*, uint16_t*, int, int*, cudaStream_t);
+template cudaError_t launch_rope_append<uint16_t>(const uint16_t*, long long, const uint16_t*, long long,
+                                                  const uint16_t*, long long, const int32_t*, const int32_t*,
+                                                  const int32_t*, const float*, float, const int32_t*, int, int, int,
+                                                  int, int, int, int, int, int, int, uint16_t*, uint16_t*, uint16_t*,
+                                                  int, int*, cudaStream_t);
+
+}  // namespace libraspec
