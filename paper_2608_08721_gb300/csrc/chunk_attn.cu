@@ -666,8 +666,11 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         const int j = pair ? i : 2 * i + st;  // the item's tile
         const int kt0 = (it.tile0 + j) * kCKeys;
         const uint32_t n = (st ? done1 : done0) + i;
+        wait(bSFull + 8 * st, n & 1);
         if (kt0 < it.klo || kt0 + kCKeys > it.khi) {
-          // V rows that no row of the block sees: cleared once they have landed
+          // V rows that no row of the block sees: cleared once they have landed. (Asked after S: a wait on a parity
+          // may be one phase ahead of the barrier, not two, and the MMA warp has by now taken every chunk that lay
+          // in this place of the ring before.)
           const uint32_t ci = chunk_base + (pair ? 2 * j + 1 : j + min(j + 2, n_tiles));
           const uint32_t ch = ci % SM::kChunks;
           wait(bFull + 8 * ch, (ci / SM::kChunks) & 1);
@@ -682,7 +685,6 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        wait(bSFull + 8 * st, n & 1);
         if (!warp_live) {
           __syncwarp();
           if (lane == 0) {

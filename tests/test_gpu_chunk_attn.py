@@ -289,6 +289,14 @@ def test_violations_set_status_and_spare_the_other_sequences():
     assert_close(O[:5], lse[:5], want[:5], A[:5], want_lse[:5])
 
 
+@pytest.mark.parametrize("d,page", [(128, 128), (64, 16)])
+def test_decode_batch_of_uneven_lengths(d, page):
+    """Every CTA works through pieces of several sequences, each with a last tile of its own length."""
+    r = np.random.default_rng(7)
+    kv = np.exp(r.uniform(math.log(100), math.log(4000), 48)).astype(int).tolist()
+    check([1] * 48, kv, 8, 4, d, page, seed=43, fill=float("nan"))
+
+
 def test_many_sequences():
     """More sequences than the plan's threads; some without new tokens."""
     r = np.random.default_rng(3)
