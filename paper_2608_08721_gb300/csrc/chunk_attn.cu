@@ -28,7 +28,7 @@
 // row tile (decode, short chunks) gives the streams alternate key tiles of the
 // same rows; the epilogue combines them.
 //
-// Roles in a CTA (320 threads): two softmax warpgroups; a producer warp whose
+// Roles in a CTA (384 threads): two softmax warpgroups; a producer warp whose
 // lanes each load their own piece of a K or V tile by TMA (a piece lies within
 // one page) into a ring of chunks; an MMA warp with one issuing thread. Thread
 // i of a warpgroup owns row i of its tile: it reads the tile's 128 scores,
@@ -60,7 +60,7 @@ constexpr int kCStreams = 2;
 constexpr int kCSoftmaxWarps = 4 * kCStreams;
 constexpr int kCProducerWarp = kCSoftmaxWarps;
 constexpr int kCMmaWarp = kCSoftmaxWarps + 1;
-constexpr int kCThreads = (kCSoftmaxWarps + 2) * 32;
+constexpr int kCThreads = (kCSoftmaxWarps + 4) * 32;  // (the last two warps only make up a warpgroup)
 constexpr int kCRows = 128;                 // rows of a tile (tensor-memory lanes)
 constexpr int kCKeys = 128;                 // keys of a tile
 constexpr int kCMaxCtas = 192;
@@ -294,6 +294,15 @@ struct ChunkSmem {
   static_assert(kBytes <= 227 * 1024, "shared memory per CTA");
 };
 
+// Registers by role: 384 threads start with 168 each (64512 in all); the softmax warpgroups take 208, the third
+// warpgroup keeps 88 (256 x 208 + 128 x 88 = 64512).
+constexpr int kCSoftmaxRegs = 208, kCOtherRegs = 88;
+static_assert(kCSoftmaxWarps * 32 * kCSoftmaxRegs + 128 * kCOtherRegs <= kCThreads * 168, "");
+template <int N>
+__device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_leave() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 __device__ __forceinline__ void bar_sync_n(int bar, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory");
 }
@@ -412,7 +421,9 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 
   if (misaligned) {
     if (tid == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-  } else if (warp == kCProducerWarp) {
+  } else if (warp >= kCSoftmaxWarps) {
+   regs_leave<kCOtherRegs>();
+   if (warp == kCProducerWarp) {
     // ======================= producer =======================
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int n_blocks = A.head->blocks;
@@ -546,79 +557,82 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     __syncwarp();
   } else if (warp == kCMmaWarp) {
     // ======================= MMA issue =======================
-    if (lane == 0) {
-      uint32_t item_ctr = 0, chunk_ctr = 0;
-      uint32_t p_ctr[2] = {0, 0};  // P steps of each stream
-      uint32_t o_ctr[2] = {0, 0};  // items of each stream
-      bool ok = true;
-      auto take = [&]() {  // the next chunk, once it is filled
-        const uint32_t ch = chunk_ctr % SM::kChunks;
-        ok = ok && mbar_wait(bFull + 8 * ch, (chunk_ctr / SM::kChunks) & 1);
-        ++chunk_ctr;
-        return ch;
-      };
-      for (int last = 0; !last && ok; ++item_ctr) {
-        ok = mbar_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
-        if (!ok) break;
-        const int n_tiles = info[item_ctr & 1].n_tiles, pair = info[item_ctr & 1].pair;
-        last = info[item_ctr & 1].last;
-        if (last == 2) break;
-        mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
-        // Step n belongs to stream n & 1: tile n / 2 of the stream's own rows (a pair), or tile n of the same rows.
-        // S of a step goes where P of the stream's step before lies, so that one's PV is issued first.
-        const int steps = pair ? 2 * n_tiles : n_tiles;
-        uint32_t kch = 0, vch = 0;
-        for (int n = 0; n < steps + 2 && ok; ++n) {
-          const int s = n & 1;
-          const uint32_t ts = tmem + SM::kColS + s * 128;
-          if (n >= 2) {  // O += P V of step n - 2
-            if (!pair || s == 0) vch = take();
-            if (n < 4) {
-              ok = ok && mbar_wait(bOFree + 8 * s, (o_ctr[s] & 1) ^ 1);
-              ++o_ctr[s];
-            }
-            constexpr uint32_t idesc = mma_idesc(128, D, 1);
-            const uint32_t va = desc_lo(sRing + vch * SM::kTile, 16384);
-            const uint32_t d = tmem + SM::kColO + s * 128;
-            const uint32_t par = p_ctr[s]++ & 1;
-            ok = ok && mbar_wait(bPFull + 16 * s, par);
-            if (!ok) break;
-            tc_fence_after();
-            mma_ts4<2048>(d, ts, va, idesc, n < 4 ? 0u : 1u);
-            ok = mbar_wait(bPFull + 16 * s + 8, par);
-            if (!ok) break;
-            tc_fence_after();
-            mma_ts4<2048>(d, ts + 32, va + 512, idesc, 1u);
-            mma_commit(bPVDone + 8 * s);
-            if (!pair || s == 1) mma_commit(bEmpty + 8 * vch);
+    // The whole warp walks the steps, one elected lane issues.
+    uint32_t item_ctr = 0, chunk_ctr = 0;
+    uint32_t p_ctr = 0;  // bit s: parity of the next P of stream s
+    uint32_t o_ctr = 3;  // bit s: parity of stream s's accumulator being free
+    bool ok = true;
+    auto take = [&]() {  // the next chunk, once it is filled
+      const uint32_t ch = chunk_ctr % SM::kChunks;
+      ok = ok && warp_wait(bFull + 8 * ch, (chunk_ctr / SM::kChunks) & 1);
+      ++chunk_ctr;
+      return ch;
+    };
+    for (int last = 0; !last && ok; ++item_ctr) {
+      ok = warp_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
+      if (!ok) break;
+      const int n_tiles = __shfl_sync(0xffffffffu, info[item_ctr & 1].n_tiles, 0);
+      const bool pair = __shfl_sync(0xffffffffu, info[item_ctr & 1].pair, 0);
+      last = __shfl_sync(0xffffffffu, info[item_ctr & 1].last, 0);
+      if (last == 2) break;
+      if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
+      __syncwarp();
+      // Step n belongs to stream n & 1: tile n / 2 of the stream's own rows (a pair), or tile n of the same rows.
+      // S of a step goes where P of the stream's step before lies, so that one's PV is issued first.
+      const int steps = pair ? 2 * n_tiles : n_tiles;
+      uint32_t kch = 0, vch = 0;
+      for (int n = 0; n < steps + 2 && ok; ++n) {
+        const int s = n & 1;
+        const uint32_t ts = tmem + SM::kColS + s * 128;
+        if (n >= 2) {  // O += P V of step n - 2
+          if (!pair || s == 0) vch = take();
+          if (n < 4) {
+            ok = ok && warp_wait(bOFree + 8 * s, (o_ctr >> s) & 1);
+            o_ctr ^= 1u << s;
           }
-          if (n < steps) {  // S = Q K^T of step n
-            if (!pair || s == 0) kch = take();
-            if (n == 0) ok = ok && mbar_wait(bQFull, item_ctr & 1);
-            if (!ok) break;
-            tc_fence_after();
-            constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
-            const uint32_t qa = desc_lo(sQ + (pair ? s : 0) * SM::kTile, 16);
-            const uint32_t ka = desc_lo(sRing + kch * SM::kTile, 16);
+          constexpr uint32_t idesc = mma_idesc(128, D, 1);
+          const uint32_t va = desc_lo(sRing + vch * SM::kTile, 16384);
+          const uint32_t d = tmem + SM::kColO + s * 128;
+          const uint32_t par = (p_ctr >> s) & 1;
+          p_ctr ^= 1u << s;
+          ok = ok && warp_wait(bPFull + 16 * s, par);
+          if (!ok) break;
+          tc_fence_after();
+          mma_ts4_warp<2048>(d, ts, va, idesc, n < 4 ? 0u : 1u);
+          ok = warp_wait(bPFull + 16 * s + 8, par);
+          if (!ok) break;
+          tc_fence_after();
+          mma_ts4_warp<2048>(d, ts + 32, va + 512, idesc, 1u);
+          mma_commit_warp(bPVDone + 8 * s);
+          if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * vch);
+        }
+        if (n < steps) {  // S = Q K^T of step n
+          if (!pair || s == 0) kch = take();
+          if (n == 0) ok = ok && warp_wait(bQFull, item_ctr & 1);
+          if (!ok) break;
+          tc_fence_after();
+          constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
+          const uint32_t qa = desc_lo(sQ + (pair ? s : 0) * SM::kTile, 16);
+          const uint32_t ka = desc_lo(sRing + kch * SM::kTile, 16);
 #pragma unroll
-            for (int hb = 0; hb < SM::kBoxes; ++hb)
-              mma_ss4<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
-            mma_commit(bSFull + 8 * s);
-            if (!pair || s == 1) mma_commit(bEmpty + 8 * kch);
-            if (n == steps - 1) mma_commit(bQEmpty);
-          }
+          for (int hb = 0; hb < SM::kBoxes; ++hb)
+            mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
+          mma_commit_warp(bSFull + 8 * s);
+          if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * kch);
+          if (n == steps - 1) mma_commit_warp(bQEmpty);
         }
       }
-      if (!ok) {
-        raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-        misc[0] = 1;
-      }
-      // every MMA issued has completed before the tensor memory is released
-      mma_commit(bDrain);
-      mbar_wait(bDrain, 0);
     }
-    __syncwarp();
+    if (!ok) {
+      if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+      misc[0] = 1;
+    }
+    // every MMA issued has completed before the tensor memory is released
+    mma_commit_warp(bDrain);
+    warp_wait(bDrain, 0);
+   }
   } else {
+    regs_take<kCSoftmaxRegs>();
     // ======================= softmax warpgroups =======================
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int st = warp >> 2, wq = warp & 3;
