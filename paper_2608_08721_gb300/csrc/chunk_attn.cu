@@ -62,11 +62,13 @@ constexpr int kCProducerWarp = kCSoftmaxWarps;
 constexpr int kCMmaWarp = kCSoftmaxWarps + 1;
 constexpr int kCThreads = (kCSoftmaxWarps + 4) * 32;  // (the last two warps only make up a warpgroup)
 constexpr int kCRows = 128;                 // rows of a tile (tensor-memory lanes)
+constexpr int kCBlockRows = 2 * kCRows;     // rows of a block, at most
 constexpr int kCKeys = 128;                 // keys of a tile
 constexpr int kCMaxCtas = 192;
 constexpr int kCTmemCols = 512;
 constexpr float kCRescaleLog2 = 8.f;
 constexpr int kPlanThreads = 1024;
+constexpr int kCSharedBytes = 64 << 20;     // K and V beyond half of L2: see the plan's waves
 constexpr int kCMaxKeys = 0x7fffffff - 2 * kCKeys;  // of a sequence: its last tile's end is an int
 
 // ---------------------------------------------------------------------------
@@ -75,16 +77,19 @@ constexpr int kCMaxKeys = 0x7fffffff - 2 * kCKeys;  // of a sequence: its last t
 // ---------------------------------------------------------------------------
 struct PlanBlock {       // the rows of one block and the key tiles that they see
   long long tiles_before;  // key tiles of the blocks before it (per kv head)
+  int pairs_before;        // blocks of two row tiles before it
   int b, tok0, n_tok;      // sequence; first packed row and tokens
   int pos0;                // position of the first token
   int klo, khi;            // keys that some row sees lie in [klo, khi)
   int tile0, n_tiles;      // 128-key tiles
+  int pad;
 };
-static_assert(sizeof(PlanBlock) == 40, "");
+static_assert(sizeof(PlanBlock) == 48, "");
 
 struct PlanHead {
   long long tiles;  // of all blocks (per kv head)
-  int blocks;
+  int blocks, pairs;
+  int waves;        // whole items (a block for a kv head) that each CTA takes before the rest is cut by cost
   int pad;
 };
 
@@ -108,8 +113,8 @@ static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
   w.count = take(kCMaxCtas * sizeof(uint32_t));
   w.blocks = take((size_t)max_blocks(T, B, Hq / Hkv) * sizeof(PlanBlock));
   // two slots per CTA: its first item, and its last where that goes on in the next CTA
-  w.part_o = take(size_t(2 * kCMaxCtas) * 2 * kCRows * d * sizeof(float));
-  w.part_ml = take(size_t(2 * kCMaxCtas) * 2 * kCRows * 2 * sizeof(float));
+  w.part_o = take(size_t(2 * kCMaxCtas) * kCBlockRows * d * sizeof(float));
+  w.part_ml = take(size_t(2 * kCMaxCtas) * kCBlockRows * 2 * sizeof(float));
   w.total = off;
   return w;
 }
@@ -158,6 +163,7 @@ __device__ __forceinline__ T block_scan(T v, T* warp_sums, T& total) {  // inclu
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t* __restrict__ cu_new,
                                                                   const int32_t* __restrict__ kv_len,
                                                                   const MaskArgs mask, int T, int B, int TB, int S_cap,
+                                                                  int Hkv, int grid, int shared_tiles,
                                                                   PlanBlock* __restrict__ blocks,
                                                                   PlanHead* __restrict__ head, int* status) {
   __shared__ int first_block[LIBRASPEC_MAX_B + 1];  // of each sequence
@@ -166,15 +172,23 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t*
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x;
   int carry = 0;
+  long long kv_tiles = 0;  // of the sequences that have new tokens
+  int n_seqs = 0;
   for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int nb = 0;
+    long long nt = 0;
     if (b < B) {
       const int lo = cu_new[b], hi = cu_new[b + 1], kv = kv_len[b];
       if (lo < 0 || hi < lo || hi > T) raise_status(status, LIBRASPEC_ST_BAD_LENGTH);
       else if (kv < 0 || (long long)kv + (hi - lo) > S_cap) raise_status(status, LIBRASPEC_ST_KV_OVERFLOW);
       else nb = (hi - lo + TB - 1) / TB;
+      if (nb) nt = ((long long)kv + hi - lo + kCKeys - 1) / kCKeys;
     }
+    long long all;
+    block_scan(nt, warp_l, all);
+    kv_tiles += all;
+    n_seqs += __syncthreads_count(nb > 0);
     int total;
     const int inc = block_scan(nb, warp_i, total);
     if (b < B) first_block[b] = carry + inc - nb;
@@ -187,6 +201,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t*
   const int n_blocks = (int)min((long long)carry, room);
   if (carry > room && tid == 0) raise_status(status, LIBRASPEC_ST_BAD_LENGTH);
   long long tiles = 0;
+  int pairs = 0, t_min = 0x7fffffff, t_max = 0;
   for (int e0 = 0; e0 < n_blocks; e0 += kPlanThreads) {
     const int e = e0 + tid;
     PlanBlock p{};
@@ -227,21 +242,48 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t*
     }
     long long total;
     const long long inc = block_scan((long long)p.n_tiles, warp_l, total);
+    const int pair = p.n_tok > TB / 2;
+    int n_pairs;
+    const int inc_p = block_scan(pair, warp_i, n_pairs);
     if (e < n_blocks) {
       p.tiles_before = tiles + inc - p.n_tiles;
+      p.pairs_before = pairs + inc_p - pair;
       blocks[e] = p;
+      t_min = min(t_min, p.n_tiles);
+      t_max = max(t_max, p.n_tiles);
     }
     tiles += total;
+    pairs += n_pairs;
   }
+  t_min = __reduce_min_sync(0xffffffffu, t_min);
+  t_max = __reduce_max_sync(0xffffffffu, t_max);
+  __syncthreads();
+  if ((tid & 31) == 0) warp_l[tid >> 5] = ((long long)t_max << 32) | t_min;
+  __syncthreads();
   if (tid == 0) {
+    for (int w = 0; w < kPlanThreads / 32; ++w) {
+      t_min = min(t_min, (int)(warp_l[w] & 0x7fffffff));
+      t_max = max(t_max, (int)(warp_l[w] >> 32));
+    }
+    // Blocks of a sequence that start together and walk its keys in step read each K and V tile from HBM once and from
+    // L2 after that; cut by cost their CTAs are all at different keys, which matters where the keys do not fit L2.
+    const long long items = (long long)n_blocks * Hkv;
+    const bool together = n_blocks >= 2 * n_seqs && kv_tiles * Hkv > shared_tiles && t_max - t_min <= t_max / 8;
     head->tiles = tiles;
     head->blocks = n_blocks;
+    head->pairs = pairs;
+    head->waves = together ? (int)min(items / grid, (long long)1 << 20) : 0;
   }
 }
 
 // ---------------------------------------------------------------------------
 // The attention kernel.
 // ---------------------------------------------------------------------------
+// What a block weighs beside its tiles, in tiles: `one` for every block, `pair` more for two row tiles.
+struct FixedCost {
+  int one, pair;
+};
+
 struct ChunkArgs {
   CUtensorMap K, V, Q;
   __nv_bfloat16* O;
@@ -259,7 +301,7 @@ struct ChunkArgs {
   int* status;
   float scale, softcap;
   int B, Hq, Hkv, max_pages, page_size, n_pages, piece;  // piece: keys of one TMA box
-  int item_tiles;
+  FixedCost fixed;
 };
 
 // One item: a run of key tiles of one block for one kv head.
@@ -330,32 +372,117 @@ __device__ __forceinline__ int share_of(long long y, long long W, int G) {
   return (int)(((y + 1) * (long long)G - 1) / W);
 }
 
+// Weight of the blocks before block e (per kv head), and of block e.
+__device__ __forceinline__ long long weight_before(const PlanBlock& p, int e, FixedCost f) {
+  return p.tiles_before + (long long)f.one * e + (long long)f.pair * p.pairs_before;
+}
+__device__ __forceinline__ int fixed_of(const PlanBlock& p, int g, FixedCost f) {
+  return f.one + (p.n_tok > kCRows / g ? f.pair : 0);
+}
+
 // Where weighted position x lies.
 struct Place {
   int e, kvh, tile;     // block, kv head, tile within the block
   long long before;     // tiles before it in the tile sequence
 };
 
-// Warp-wide. Block e's Hkv copies start at Hkv (tiles_before + C e); x < the total weight.
-__device__ Place find_place(long long x, const PlanBlock* __restrict__ blocks, int n_blocks, int Hkv, int C) {
+// Warp-wide. Block e's Hkv copies start at Hkv times the weight before it, each with its fixed cost first; x < the total.
+__device__ Place find_place(long long x, const PlanBlock* __restrict__ blocks, int n_blocks, int Hkv, int g,
+                            FixedCost f) {
   const int lane = threadIdx.x & 31;
   int lo = 0, n = n_blocks;  // the last block of [lo, lo + n) that starts at or before x
   while (n > 1) {
     const int step = (n + 31) / 32, i = lo + lane * step;
-    const bool at = lane * step < n && (long long)Hkv * (blocks[i].tiles_before + (long long)C * i) <= x;
+    const bool at = lane * step < n && (long long)Hkv * weight_before(blocks[i], i, f) <= x;
     const int k = 31 - __clz(__ballot_sync(0xffffffffu, at));  // (lane 0 always holds)
     n = min(step, n - k * step);
     lo += k * step;
   }
   Place p;
   p.e = lo;
-  const long long o = x - (long long)Hkv * (blocks[lo].tiles_before + (long long)C * lo);
-  const int nt = blocks[lo].n_tiles, w = nt + C;
+  const long long o = x - (long long)Hkv * weight_before(blocks[lo], lo, f);
+  const int nt = blocks[lo].n_tiles, c = fixed_of(blocks[lo], g, f), w = nt + c;
   p.kvh = (int)(o / w);
   const int r = (int)(o - (long long)p.kvh * w);
-  p.tile = r > C ? r - C : 0;
+  p.tile = r > c ? r - c : 0;
   p.before = (long long)Hkv * blocks[lo].tiles_before + (long long)p.kvh * nt + p.tile;
   return p;
+}
+
+// Merges the np partials of an item's rows: O = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - M), M = max m_p. A
+// thread of the softmax warpgroups takes a row and eight columns at a time, two of them with four parts' loads in
+// flight (one at a time a merge of two parts of 256 rows took 20 us, a round trip for each of 32 steps); neighbouring
+// threads take neighbouring rows, which lie side by side in the partials.
+template <int D>
+__device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem& it, int g) {
+  constexpr int U = 2, P = 4;
+  const int np = it.np, c0 = it.c0, rows = it.rows, units = rows * (D / 8);
+  const int step = kCSoftmaxWarps * 32;
+  for (int k0 = threadIdx.x; k0 < units; k0 += U * step) {
+    float M[U], L[U];
+    float acc[U][8];
+    int r[U], c[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = min(k0 + u * step, units - 1);  // (a unit past the end repeats the last)
+      c[u] = k / rows;
+      r[u] = k - c[u] * rows;
+      M[u] = -INFINITY;
+      L[u] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[u][e] = 0.f;
+    }
+    for (int p0 = 0; p0 < np; p0 += P) {
+      float2 ml[U][P];
+      float4 v[U][P][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+          const int p = p0 + q;
+          ml[u][q] = make_float2(-INFINITY, 0.f);
+          v[u][q][0] = v[u][q][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (p < np) {
+            const size_t slot = p == 0 ? 2 * c0 + 1 : 2 * (c0 + p);
+            ml[u][q] = __ldcg(reinterpret_cast<const float2*>(A.part_ml) + slot * kCBlockRows + r[u]);
+            const float4* o = reinterpret_cast<const float4*>(A.part_o) + (slot * (D / 4) + 2 * c[u]) * kCBlockRows + r[u];
+            v[u][q][0] = __ldcg(o);
+            v[u][q][1] = __ldcg(o + kCBlockRows);
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float Mn = M[u];
+#pragma unroll
+        for (int q = 0; q < P; ++q) Mn = fmaxf(Mn, ml[u][q].x);
+        if (Mn == -INFINITY) continue;  // nothing seen so far
+        const float f = ex2_approx(M[u] - Mn);  // 0 while M is -inf
+        M[u] = Mn;
+        L[u] *= f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[u][e] *= f;
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+          const float w = ex2_approx(ml[u][q].x - Mn);
+          L[u] += w * ml[u][q].y;
+          const float x[8] = {v[u][q][0].x, v[u][q][0].y, v[u][q][0].z, v[u][q][0].w,
+                              v[u][q][1].x, v[u][q][1].y, v[u][q][1].z, v[u][q][1].w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[u][e] += w * x[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k0 + u * step >= units) continue;
+      const float inv = L[u] > 0.f ? 1.f / L[u] : L[u] == 0.f ? 0.f : L[u];  // (NaN stays)
+      const size_t row = (size_t)(it.tok0 + r[u] / g) * A.Hq + it.kvh * g + r[u] % g;
+      reinterpret_cast<uint4*>(A.O + row * D)[c[u]] =
+          make_uint4(c_pack(acc[u][0] * inv, acc[u][1] * inv), c_pack(acc[u][2] * inv, acc[u][3] * inv),
+                     c_pack(acc[u][4] * inv, acc[u][5] * inv), c_pack(acc[u][6] * inv, acc[u][7] * inv));
+      if (A.lse && c[u] == 0) A.lse[row] = (M[u] + __log2f(L[u])) * kLn2;
+    }
+  }
 }
 
 template <int D>
@@ -426,22 +553,49 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
    if (warp == kCProducerWarp) {
     // ======================= producer =======================
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int n_blocks = A.head->blocks;
-    const long long tiles = (long long)A.Hkv * A.head->tiles;
+    const PlanHead head = *A.head;
+    const int c = blockIdx.x;
+    // the whole items first, in step; the rest is cut by cost from tile `done` on, weighted position x_done
+    const long long all = (long long)A.Hkv * head.tiles;
+    const int n_whole = head.waves * (int)gridDim.x;
+    FixedCost fixed = A.fixed;
+    auto place_of_item = [&](int id) {
+      Place p;
+      p.e = id / A.Hkv;
+      p.kvh = id - p.e * A.Hkv;
+      p.tile = 0;
+      p.before = p.e < head.blocks ? (long long)A.Hkv * A.blocks[p.e].tiles_before + (long long)p.kvh * A.blocks[p.e].n_tiles
+                                   : all;
+      return p;
+    };
+    const Place first_cut = place_of_item(n_whole);
+    const long long tiles = all - first_cut.before;  // to be cut
     int G = (int)gridDim.x;
     if (tiles < G) G = (int)tiles;
-    const int C = tiles > 0 ? (int)min((long long)A.item_tiles, tiles / (4 * (long long)G)) : 0;
-    const long long W = tiles + (long long)C * A.Hkv * n_blocks;
-    const int c = blockIdx.x;
+    if (tiles > 0) {  // (a CTA with few tiles would get none if a block's fixed cost were several)
+      const int most = (int)min(1ll << 20, tiles / (4 * (long long)G));
+      fixed.one = min(fixed.one, most);
+      fixed.pair = min(fixed.pair, most - fixed.one);
+    }
+    const long long x_all = (long long)A.Hkv * (head.tiles + (long long)fixed.one * head.blocks +
+                                                (long long)fixed.pair * head.pairs);
+    long long x_cut = x_all;
+    if (first_cut.e < head.blocks) {
+      const PlanBlock& p = A.blocks[first_cut.e];
+      x_cut = (long long)A.Hkv * weight_before(p, first_cut.e, fixed) +
+              (long long)first_cut.kvh * (p.n_tiles + fixed_of(p, g, fixed));
+    }
+    const long long W = x_all - x_cut;
     Place at{};
-    long long left = 0;  // the CTA's tiles
+    long long left = 0;  // the CTA's tiles of the cut part
     if (c < G) {
-      const long long x0 = c * W / G, x1 = (c + 1) * W / G;
-      at = find_place(x0, A.blocks, n_blocks, A.Hkv, C);
-      const long long end = x1 < W ? find_place(x1, A.blocks, n_blocks, A.Hkv, C).before : tiles;
+      const long long x0 = x_cut + c * W / G, x1 = x_cut + (c + 1) * W / G;
+      at = find_place(x0, A.blocks, head.blocks, A.Hkv, g, fixed);
+      const long long end = x1 < x_all ? find_place(x1, A.blocks, head.blocks, A.Hkv, g, fixed).before : all;
       left = end - at.before;
     }
-    if (left <= 0 && lane == 0) {
+    int whole = head.waves;  // whole items still to do
+    if (whole == 0 && left <= 0 && lane == 0) {
       info[0].last = 2;
       mbar_arrive(bIFull);
     }
@@ -452,31 +606,35 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     uint32_t item_ctr = 0, chunk_ctr = 0;
     const uint64_t once = evict_first_policy(), again = evict_normal_policy();
     bool ok = true;
-    while (left > 0 && ok) {
-      const PlanBlock p = A.blocks[at.e];
+    while ((whole > 0 || left > 0) && ok) {
+      const bool cut = whole == 0;
+      const Place pl = cut ? at : place_of_item((head.waves - whole) * (int)gridDim.x + c);
+      const PlanBlock p = A.blocks[pl.e];
       ChunkItem it{};
       it.b = p.b;
-      it.kvh = at.kvh;
+      it.kvh = pl.kvh;
       it.tok0 = p.tok0;
       it.pos0 = p.pos0;
       it.rows = p.n_tok * g;
       it.pair = p.n_tok > Rt;
-      it.tile0 = p.tile0 + at.tile;
-      it.n_tiles = (int)min((long long)(p.n_tiles - at.tile), left);
+      it.tile0 = p.tile0 + pl.tile;
+      it.n_tiles = cut ? (int)min((long long)(p.n_tiles - pl.tile), left) : p.n_tiles;
       it.klo = p.klo;
       it.khi = p.khi;
       it.partial = it.n_tiles != p.n_tiles;
-      it.slot = at.tile == 0 ? 2 * c + 1 : 2 * c;
+      it.slot = pl.tile == 0 ? 2 * c + 1 : 2 * c;
       it.c0 = c;
       it.np = 1;
       if (it.partial) {
-        const long long y = (long long)A.Hkv * (p.tiles_before + (long long)C * at.e) +
-                            (long long)at.kvh * (p.n_tiles + C) + C;  // of the block's first tile
+        const int fc = fixed_of(p, g, fixed);
+        const long long y = (long long)A.Hkv * weight_before(p, pl.e, fixed) + (long long)pl.kvh * (p.n_tiles + fc) + fc -
+                            x_cut;  // of the block's first tile, from the cut part's start
         it.c0 = share_of(y, W, G);
         it.np = share_of(y + p.n_tiles - 1, W, G) - it.c0 + 1;
       }
-      left -= it.n_tiles;
-      it.last = left <= 0;
+      if (cut) left -= it.n_tiles;
+      else --whole;
+      it.last = whole == 0 && left <= 0;
       const int n = it.n_tiles, lag = it.pair ? 1 : 2;
       // keys of a sequence that has one block are read once per kv head
       const int n_new = A.cu_new[p.b + 1] - A.cu_new[p.b];
@@ -535,11 +693,12 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         ++chunk_ctr;
       }
       ++item_ctr;
-      // the next item: the next kv head, or the next block
-      at.tile = 0;
-      if (++at.kvh == A.Hkv) {
-        at.kvh = 0;
-        ++at.e;
+      if (cut) {  // the next item: the next kv head, or the next block
+        at.tile = 0;
+        if (++at.kvh == A.Hkv) {
+          at.kvh = 0;
+          ++at.e;
+        }
       }
     }
     if (!ok) {
@@ -821,7 +980,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       // of rows in two streams each warpgroup writes half of the columns; a single step leaves all to the first
       if (warp_live && (pair || both || st == 0)) {
         const bool partial = it.partial;
-        const size_t prow = (size_t)it.slot * 2 * kCRows + rr;
+        const size_t prow = (size_t)it.slot * kCBlockRows + rr;
         if (!partial) {
           const float inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;  // (NaN stays)
           f0 *= inv;
@@ -856,9 +1015,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
                                   c_pack(__uint_as_float(o[8 * k + 4]), __uint_as_float(o[8 * k + 5])),
                                   c_pack(__uint_as_float(o[8 * k + 6]), __uint_as_float(o[8 * k + 7])));
           } else {
-            uint4* dst = reinterpret_cast<uint4*>(A.part_o + prow * D + c0);
+            uint4* dst = reinterpret_cast<uint4*>(A.part_o) + ((size_t)it.slot * (D / 4) + c0 / 4) * kCBlockRows + rr;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) dst[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+            for (int k = 0; k < 8; ++k)
+              dst[k * kCBlockRows] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
           }
         }
         if (valid && (pair || st == 0)) {
@@ -882,56 +1042,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           __threadfence();
         }
         bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
-        if (misc[1]) {
-          constexpr int C4 = D / 4;
-          const int np = it.np, c0 = it.c0, items = it.rows * C4;
-          for (int k = tid; k < items; k += kCSoftmaxWarps * 32) {
-            const int r = k / C4, c = k - r * C4;
-            float M = -INFINITY, L = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int p0 = 0; p0 < np; p0 += 4) {
-              float2 ml[4];
-              float4 v[4];
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const int p = p0 + q;
-                if (p < np) {
-                  const size_t prow = (size_t)(p == 0 ? 2 * c0 + 1 : 2 * (c0 + p)) * 2 * kCRows + r;
-                  ml[q] = __ldcg(reinterpret_cast<const float2*>(A.part_ml + prow * 2));
-                  v[q] = __ldcg(reinterpret_cast<const float4*>(A.part_o + prow * D) + c);
-                } else {
-                  ml[q] = make_float2(-INFINITY, 0.f);
-                  v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-              }
-              const float Mn = fmaxf(M, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
-              if (Mn == -INFINITY) continue;
-              const float f = ex2_approx(M - Mn);  // 0 while M is -inf
-              acc.x *= f;
-              acc.y *= f;
-              acc.z *= f;
-              acc.w *= f;
-              L *= f;
-              M = Mn;
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const float w = ex2_approx(ml[q].x - Mn);
-                acc.x += w * v[q].x;
-                acc.y += w * v[q].y;
-                acc.z += w * v[q].z;
-                acc.w += w * v[q].w;
-                L += w * ml[q].y;
-              }
-            }
-            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-            const size_t orow = (size_t)(it.tok0 + r / g) * A.Hq + it.kvh * g + r % g;
-            uint2 o;
-            o.x = c_pack(acc.x * inv, acc.y * inv);
-            o.y = c_pack(acc.z * inv, acc.w * inv);
-            *reinterpret_cast<uint2*>(A.O + orow * D + c * 4) = o;
-            if (A.lse && c == 0) A.lse[orow] = (M + __log2f(L)) * kLn2;
-          }
-        }
+        if (misc[1]) merge_parts<D>(A, it, g);
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));  // `it` has been read
@@ -1029,19 +1140,20 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   a.piece = 64;
   if (block_table)
     while (page_size % a.piece) a.piece /= 2;
-  a.item_tiles = 2;
+  a.fixed = FixedCost{2, 2};
   const long long rows = block_table ? page_size : S_cap, planes = (long long)(block_table ? n_pages : B) * Hkv;
   if (!make_map(&a.K, Kc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
       !make_map(&a.V, Vc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
       !make_map(&a.Q, Q, D, Hq, T, g, kCRows / g, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
     return cudaErrorInvalidValue;
+  const int grid = std::min(num_sms_current(), kCMaxCtas);
   chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(cu_new, kv_len, a.mask, T, B, block_tokens(g),
-                                                    std::min(S_cap, kCMaxKeys),
+                                                    std::min(S_cap, kCMaxKeys), Hkv, grid,
+                                                    kCSharedBytes / (2 * kCKeys * D * 2),
                                                     reinterpret_cast<PlanBlock*>(ws + lay.blocks),
                                                     reinterpret_cast<PlanHead*>(ws + lay.head), a.status);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int grid = std::min(num_sms_current(), kCMaxCtas);
   return D == 128 ? launch_attn_t<128>(a, grid, stream) : launch_attn_t<64>(a, grid, stream);
 }
 
