@@ -410,12 +410,11 @@ __device__ Place find_place(long long x, const PlanBlock* __restrict__ blocks, i
 }
 
 // Merges the np partials of an item's rows: O = sum_p w_p O_p / sum_p w_p l_p with w_p = 2^(m_p - M), M = max m_p. A
-// thread of the softmax warpgroups takes a row and eight columns at a time, two of them with four parts' loads in
-// flight (one at a time a merge of two parts of 256 rows took 20 us, a round trip for each of 32 steps); neighbouring
+// thread of the softmax warpgroups takes a row and eight columns at a time, U of them with P parts' loads in flight
+// (one by four columns a merge of two parts of 256 rows took 20 us, a round trip for each of 32 steps); neighbouring
 // threads take neighbouring rows, which lie side by side in the partials.
-template <int D>
+template <int D, int U, int P>
 __device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem& it, int g) {
-  constexpr int U = 2, P = 4;
   const int np = it.np, c0 = it.c0, rows = it.rows, units = rows * (D / 8);
   const int step = kCSoftmaxWarps * 32;
   for (int k0 = threadIdx.x; k0 < units; k0 += U * step) {
@@ -485,7 +484,11 @@ __device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem&
   }
 }
 
-template <int D>
+// What scores are beside a scaled product: bit 0 capped, bit 1 biased by distance. (Instantiations: the code of either
+// in the plain kernel's loop costs it instruction fetches.)
+constexpr int kCap = 1, kBias = 2;
+
+template <int D, int SHAPE>
 __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_constant__ ChunkArgs A) {
   using SM = ChunkSmem<D>;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -830,10 +833,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         const int n_keys = A.kv_len[it.b] + A.cu_new[it.b + 1] - A.cu_new[it.b];
         row_range(pos, n_keys, A.mask.prefix_len ? A.mask.prefix_len[it.b] : 0,
                   A.mask.first_key ? A.mask.first_key[tok] : 0, A.mask.window, lo, hi);
-        if (A.slopes) slope = A.slopes[hq] * kLog2e;
+        if (SHAPE & kBias) slope = A.slopes[hq] * kLog2e;
       }
-      const bool shaped = A.softcap > 0.f || A.slopes;  // scores are more than a scaled product
-      const float sc = shaped ? 1.f : scale_log2;
+      const float sc = SHAPE ? 1.f : scale_log2;
+      const float cap2 = A.softcap * kLog2e, u2 = 2.f * scale_log2 / A.softcap;
       float m_run = -INFINITY, l_run = 0.f;
       for (int i = 0; i < my_steps; ++i) {
         const int j = pair ? i : 2 * i + st;  // the item's tile
@@ -871,8 +874,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(ts + 32 * q, x[q]);
         tmem_wait_ld();
-        if (shaped) {  // the scores in units of log 2
-          const float cap2 = A.softcap * kLog2e, u2 = A.softcap > 0.f ? 2.f * scale_log2 / A.softcap : 0.f;
+        if constexpr (SHAPE != 0) {  // the scores in units of log 2
           const float d0 = (float)(kt0 - pos);
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -880,9 +882,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
             for (int c = 0; c < 32; ++c) {
               float y = __uint_as_float(x[q][c]);
               // cap tanh(s / cap) = cap (1 - 2 / (e^(2 s / cap) + 1))
-              if (A.softcap > 0.f) y = cap2 - __fdividef(2.f * cap2, ex2_approx(y * u2) + 1.f);
+              if (SHAPE & kCap) y = cap2 - __fdividef(2.f * cap2, ex2_approx(y * u2) + 1.f);
               else y *= scale_log2;
-              x[q][c] = __float_as_uint(fmaf(-slope, fabsf(d0 + (float)(32 * q + c)), y));
+              if (SHAPE & kBias) y = fmaf(-slope, fabsf(d0 + (float)(32 * q + c)), y);
+              x[q][c] = __float_as_uint(y);
             }
         }
         if (__any_sync(0xffffffffu, valid && (kt0 < lo || kt0 + kCKeys > hi))) {
@@ -1042,7 +1045,10 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           __threadfence();
         }
         bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
-        if (misc[1]) merge_parts<D>(A, it, g);
+        if (misc[1]) {
+          if (it.np <= 2) merge_parts<D, 4, 2>(A, it, g);
+          else merge_parts<D, 1, 8>(A, it, g);
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));  // `it` has been read
@@ -1083,12 +1089,12 @@ static bool make_map(CUtensorMap* map, const void* base, int D, long long rows, 
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, int SHAPE>
 static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stream) {
   using SM = ChunkSmem<D>;
   static bool configured = false;
   if (!configured) {
-    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes);
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D, SHAPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes);
     if (e != cudaSuccess) return e;
     configured = true;
   }
@@ -1102,7 +1108,7 @@ static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stre
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D>, a);
+  return cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D, SHAPE>, a);
 }
 
 // block_table == nullptr: dense caches [B, Hkv, S_cap, D]. page_size: a multiple of 16.
@@ -1154,7 +1160,11 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
                                                     reinterpret_cast<PlanHead*>(ws + lay.head), a.status);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  return D == 128 ? launch_attn_t<128>(a, grid, stream) : launch_attn_t<64>(a, grid, stream);
+  using Launch = cudaError_t (*)(const ChunkArgs&, int, cudaStream_t);
+  static const Launch launch[2][4] = {
+      {launch_attn_t<64, 0>, launch_attn_t<64, kCap>, launch_attn_t<64, kBias>, launch_attn_t<64, kCap | kBias>},
+      {launch_attn_t<128, 0>, launch_attn_t<128, kCap>, launch_attn_t<128, kBias>, launch_attn_t<128, kCap | kBias>}};
+  return launch[D == 128][(softcap > 0.f ? kCap : 0) | (slopes ? kBias : 0)](a, grid, stream);
 }
 
 }  // namespace libraspec
