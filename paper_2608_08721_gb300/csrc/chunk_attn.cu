@@ -302,6 +302,7 @@ struct ChunkArgs {
   float scale, softcap;
   int B, Hq, Hkv, max_pages, page_size, n_pages, piece;  // piece: keys of one TMA box
   FixedCost fixed;
+  int o_wide;  // O is aligned to 32 bytes
 };
 
 // One item: a run of key tiles of one block for one kv head.
@@ -361,6 +362,26 @@ __device__ __forceinline__ void c_add2(float& d0, float& d1, float a0, float a1)
       "add.rn.f32x2 d, d, a;\n\tmov.b64 {%0, %1}, d;\n\t}"
       : "+f"(d0), "+f"(d1)
       : "f"(a0), "f"(a1));
+}
+// (d0, d1) = (a0, a1) * b + (c0, c1)
+__device__ __forceinline__ void c_fma2v(float& d0, float& d1, float a0, float a1, float b, float c0, float c1) {
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %6};\n\t"
+      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d0), "=f"(d1)
+      : "f"(a0), "f"(a1), "f"(b), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// bits [0, n) set, n clamped to [0, 32]
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+// 32 bytes at once
+__device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ uint32_t c_pack(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -874,27 +895,55 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(ts + 32 * q, x[q]);
         tmem_wait_ld();
-        if constexpr (SHAPE != 0) {  // the scores in units of log 2
-          const float d0 = (float)(kt0 - pos);
+        if constexpr (SHAPE & kCap) {  // the scores in units of log 2
+          // cap tanh(s / cap) = cap (1 - 2 / (e + 1)), e = exp(2 s / cap)
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              float y = __uint_as_float(x[q][c]);
-              // cap tanh(s / cap) = cap (1 - 2 / (e^(2 s / cap) + 1))
-              if (SHAPE & kCap) y = cap2 - __fdividef(2.f * cap2, ex2_approx(y * u2) + 1.f);
-              else y *= scale_log2;
-              if (SHAPE & kBias) y = fmaf(-slope, fabsf(d0 + (float)(32 * q + c)), y);
-              x[q][c] = __float_as_uint(y);
+            for (int c = 0; c < 32; c += 2) {
+              float a, b;
+              c_fma2(a, b, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), u2, 0.f);
+              a = ex2_approx(a);
+              b = ex2_approx(b);
+              c_add2(a, b, 1.f, 1.f);
+              a = rcp_approx(a);
+              b = rcp_approx(b);
+              c_fma2(a, b, a, b, -2.f * cap2, cap2);
+              x[q][c] = __float_as_uint(a);
+              x[q][c + 1] = __float_as_uint(b);
             }
         }
-        if (__any_sync(0xffffffffu, valid && (kt0 < lo || kt0 + kCKeys > hi))) {
-          const int a = lo - kt0, span = hi - lo;
+        if constexpr (SHAPE & kBias) {
+          const float to_log2 = SHAPE & kCap ? 1.f : scale_log2, d0 = (float)(kt0 - pos);
+          if (__any_sync(0xffffffffu, valid && kt0 + kCKeys - 1 > pos)) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                x[q][c] = __float_as_uint(
+                    fmaf(__uint_as_float(x[q][c]), to_log2, -slope * fabsf(d0 + (float)(32 * q + c))));
+          } else {  // no key lies ahead: |p - k| = p - k
+            const float b0 = slope * d0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int c = 0; c < 32; c += 2) {
+                float y0, y1;
+                c_fma2v(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), to_log2,
+                        fmaf(slope, (float)(32 * q + c), b0), fmaf(slope, (float)(32 * q + c + 1), b0));
+                x[q][c] = __float_as_uint(y0);
+                x[q][c + 1] = __float_as_uint(y1);
+              }
+          }
+        }
+        if (__any_sync(0xffffffffu, valid && (kt0 < lo || kt0 + kCKeys > hi))) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t seen = bits_below(hi - kt0 - 32 * q) & ~bits_below(lo - kt0 - 32 * q);
 #pragma unroll
             for (int c = 0; c < 32; ++c)
-              if ((uint32_t)(32 * q + c - a) >= (uint32_t)span) x[q][c] = __float_as_uint(-INFINITY);
+              if (!((seen >> c) & 1u)) x[q][c] = __float_as_uint(-INFINITY);
+          }
         }
         float mx[4];
 #pragma unroll
@@ -1010,13 +1059,19 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           }
           if (!valid) continue;
           if (!partial) {
-            uint4* dst = reinterpret_cast<uint4*>(orow + c0);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              dst[k] = make_uint4(c_pack(__uint_as_float(o[8 * k]), __uint_as_float(o[8 * k + 1])),
-                                  c_pack(__uint_as_float(o[8 * k + 2]), __uint_as_float(o[8 * k + 3])),
-                                  c_pack(__uint_as_float(o[8 * k + 4]), __uint_as_float(o[8 * k + 5])),
-                                  c_pack(__uint_as_float(o[8 * k + 6]), __uint_as_float(o[8 * k + 7])));
+            for (int k = 0; k < 2; ++k) {
+              uint32_t r[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                r[e] = c_pack(__uint_as_float(o[16 * k + 2 * e]), __uint_as_float(o[16 * k + 2 * e + 1]));
+              if (A.o_wide) {
+                store32(orow + c0 + 16 * k, r);
+              } else {
+                reinterpret_cast<uint4*>(orow + c0)[2 * k] = make_uint4(r[0], r[1], r[2], r[3]);
+                reinterpret_cast<uint4*>(orow + c0)[2 * k + 1] = make_uint4(r[4], r[5], r[6], r[7]);
+              }
+            }
           } else {
             uint4* dst = reinterpret_cast<uint4*>(A.part_o) + ((size_t)it.slot * (D / 4) + c0 / 4) * kCBlockRows + rr;
 #pragma unroll
@@ -1147,6 +1202,7 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   if (block_table)
     while (page_size % a.piece) a.piece /= 2;
   a.fixed = FixedCost{2, 2};
+  a.o_wide = reinterpret_cast<uintptr_t>(O) % 32 == 0;
   const long long rows = block_table ? page_size : S_cap, planes = (long long)(block_table ? n_pages : B) * Hkv;
   if (!make_map(&a.K, Kc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
       !make_map(&a.V, Vc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
