@@ -479,8 +479,8 @@ int libraspec_rope_frequencies(int rot_dim, double theta, int scaling, double fa
  * token (at least H * head_dim; X may be the queries' or keys' part of a wider
  * projection). Y may be X with the same stride; else they must not overlap.
  * pos [T] i32 (any sign), turns [rot_dim / 2, 2] f32 from
- * libraspec_rope_frequencies, on the device. head_dim even, rot_dim even,
- * 2 <= rot_dim <= head_dim, rot_dim <= LIBRASPEC_ROPE_MAX_DIM. Rows that start
+ * libraspec_rope_frequencies, on the device. head_dim and rot_dim even,
+ * 2 <= rot_dim <= head_dim <= LIBRASPEC_ROPE_MAX_DIM. Rows that start
  * on 16 bytes (and halves of whole 16 bytes) move in 128-bit accesses, others
  * pair by pair. One launch, no workspace.
  */

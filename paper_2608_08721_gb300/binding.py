@@ -582,11 +582,18 @@ class RopeFreqs:
         _check(rc, "libraspec_rope_frequencies")
         self.rot_dim, self.magnitude = int(rot_dim), float(magnitude)
         self.turns = host.to(torch.device("cuda") if device is None else torch.device(device))
+        self.turns_ptr = self.turns.data_ptr()
 
 
-def _req_heads(t: torch.Tensor, dtype, name: str, shape=None) -> torch.Tensor:
-    """[T, H, d] whose tokens' heads are contiguous (any stride from token to token, as in a slice of a wider
-    projection)."""
+def _heads_stride(t: torch.Tensor, dtype, name: str, shape=None) -> int:
+    """Checks [T, H, d] whose tokens' heads are contiguous (any stride from token to token, as in a slice of a wider
+    projection); returns that stride."""
+    # every condition at once; what fails is named below
+    if isinstance(t, torch.Tensor) and t.dtype == dtype and t.is_cuda and t.dim() == 3:
+        s0, s1, s2 = t.stride()
+        T, H, d = t.shape
+        if s2 == 1 and s1 == d and s0 >= H * d and (shape is None or t.shape == shape):
+            return s0
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch tensor" % name)
     if t.dtype != dtype:
@@ -594,15 +601,11 @@ def _req_heads(t: torch.Tensor, dtype, name: str, shape=None) -> torch.Tensor:
     if not t.is_cuda:
         raise ValueError("%s must be on a CUDA device" % name)
     if t.dim() != 3 or (shape is not None and t.shape != shape):
-        raise ValueError("%s must have shape %s, got %s" % (name, shape or "[T, H, d]", tuple(t.shape)))
-    T, H, d = t.shape
-    if T and ((d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d) or (T > 1 and t.stride(0) < H * d)):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape) if shape else "[T, H, d]", tuple(t.shape)))
+    T, H, d = t.shape  # (strides of dimensions of size 0 or 1 say nothing)
+    if t.numel() and ((d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d) or (T > 1 and t.stride(0) < H * d)):
         raise ValueError("%s: each token's heads must be contiguous" % name)
-    return t
-
-
-def _token_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return t.stride(0) if T > 1 and t.numel() else H * d
 
 
 def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y=None, stream=None) -> torch.Tensor:
@@ -610,15 +613,21 @@ def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y
     from that of Y). Y may be X (in place)."""
     bf16 = isinstance(X, torch.Tensor) and X.dtype == torch.bfloat16
     dt = torch.bfloat16 if bf16 else torch.float32
-    _req_heads(X, dt, "X")
-    T, H, d = X.shape
+    xs = _heads_stride(X, dt, "X")
+    shape = X.shape
+    T, H, d = shape
     _req(pos, torch.int32, "pos", (T,))
-    Y = torch.empty((T, H, d), dtype=dt, device=X.device) if Y is None else _req_heads(Y, dt, "Y", X.shape)
-    name = "libraspec_rope_bf16" if bf16 else "libraspec_rope"
-    rc = getattr(load(), name)(_ptr(X), _token_stride(X), _ptr(pos), _ptr(freqs.turns), freqs.magnitude, T, H, d,
-                               freqs.rot_dim, int(bool(interleaved)), int(bool(inverse)), _ptr(Y), _token_stride(Y),
-                               _stream(stream))
-    _check(rc, name)
+    if Y is None:
+        Y = torch.empty(shape, dtype=dt, device=X.device)
+        ys = H * d
+    else:
+        ys = _heads_stride(Y, dt, "Y", shape)
+    lib = load()
+    rc = (lib.libraspec_rope_bf16 if bf16 else lib.libraspec_rope)(
+        X.data_ptr(), xs, pos.data_ptr(), freqs.turns_ptr, freqs.magnitude, T, H, d, freqs.rot_dim,
+        1 if interleaved else 0, 1 if inverse else 0, Y.data_ptr(), ys, _stream(stream))
+    if rc != OK:
+        _check(rc, "libraspec_rope_bf16" if bf16 else "libraspec_rope")
     return Y
 
 
@@ -647,47 +656,58 @@ def _check_new(cu_new, kv_len):
 
 def _check_caches(Kc, Vc, block_table, B, Hkv, d):
     """Dense caches, or pools and their table; returns (capacity, max_pages, page_size, n_pages)."""
-    k, v = ("Kc", "Vc") if block_table is None else ("Kp", "Vp")
-    _req(Kc, torch.bfloat16, k)
-    if Kc.dim() != 4 or Kc.shape[1] != Hkv or Kc.shape[3] != d or (block_table is None and Kc.shape[0] != B):
-        raise ValueError("%s must be %s, got %s" % (k, "[%s, %d, %s, %d]" % (
-            (B, Hkv, "S_cap", d) if block_table is None else ("n_pages", Hkv, "page_size", d)), tuple(Kc.shape)))
-    _req(Vc, torch.bfloat16, v, Kc.shape)
-    if block_table is None:
-        return Kc.shape[2], 0, 0, 0
+    paged = block_table is not None
+    _req(Kc, torch.bfloat16, "Kp" if paged else "Kc")
+    shape = Kc.shape
+    if len(shape) != 4 or shape[1] != Hkv or shape[3] != d or not (paged or shape[0] == B):
+        raise ValueError("%s must be %s, got %s" % (("Kp", "[n_pages, %d, page_size, %d]" % (Hkv, d), tuple(shape)) if paged
+                                                    else ("Kc", "[%d, %d, S_cap, %d]" % (B, Hkv, d), tuple(shape))))
+    _req(Vc, torch.bfloat16, "Vp" if paged else "Vc", shape)
+    if not paged:
+        return shape[2], 0, 0, 0
     _req(block_table, torch.int32, "block_table")
-    if block_table.dim() != 2 or block_table.shape[0] != B:
+    t = block_table.shape
+    if len(t) != 2 or t[0] != B:
         raise ValueError("block_table must be [B, max_pages]")
-    return 0, block_table.shape[1], Kc.shape[2], Kc.shape[0]
+    return 0, t[1], shape[2], shape[0]
 
 
 def _rope_append(Q, K, V, Kc, Vc, block_table, cu_new, kv_len, freqs, ws, pos, interleaved, Qo, stream):
     bf16 = isinstance(K, torch.Tensor) and K.dtype == torch.bfloat16
     dt = torch.bfloat16 if bf16 else torch.float32
-    _req_heads(K, dt, "K")
-    T, Hkv, d = K.shape
-    _req_heads(V, dt, "V", K.shape)
+    ks = _heads_stride(K, dt, "K")
+    shape = K.shape
+    T, Hkv, d = shape
+    vs = _heads_stride(V, dt, "V", shape)
     B = _check_new(cu_new, kv_len)
     S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
     if pos is not None:
         _req(pos, torch.int32, "pos", (T,))
-    Hq = 0
+    Hq = qs = 0
     if Q is not None:
-        _req_heads(Q, dt, "Q")
-        Hq = Q.shape[1]
-        if Q.shape[0] != T or Q.shape[2] != d:
-            raise ValueError("Q must have shape [%d, Hq, %d], got %s" % (T, d, tuple(Q.shape)))
-        Qo = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=K.device) if Qo is None else _req(
-            Qo, torch.bfloat16, "Qo", (T, Hq, d))
+        qs = _heads_stride(Q, dt, "Q")
+        shape = Q.shape
+        Hq = shape[1]
+        if shape[0] != T or shape[2] != d:
+            raise ValueError("Q must have shape [%d, Hq, %d], got %s" % (T, d, tuple(shape)))
+        if Qo is None:
+            Qo = torch.empty(shape, dtype=torch.bfloat16, device=K.device)
+        else:
+            _req(Qo, torch.bfloat16, "Qo", shape)
     elif Qo is not None:
         raise ValueError("Qo without Q")
-    args = [_ptr(Q), _token_stride(Q) if Q is not None else 0, _ptr(K), _token_stride(K), _ptr(V), _token_stride(V),
-            _ptr(cu_new), _ptr(kv_len), _ptr(pos), _ptr(freqs.turns), freqs.magnitude, T, B, Hq, Hkv, d, freqs.rot_dim,
-            int(bool(interleaved)), _ptr(Qo), _ptr(Kc), _ptr(Vc)]
+    lib = load()
     name = "libraspec_rope_append" + ("" if block_table is None else "_paged") + ("_bf16" if bf16 else "")
-    args += [S_cap] if block_table is None else [_ptr(block_table), max_pages, page_size, n_pages]
-    rc = getattr(load(), name)(*args, ws.ptr, ws.nbytes, _stream(stream))
-    _check(rc, name)
+    head = (_ptr(Q), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_new.data_ptr(), kv_len.data_ptr(), _ptr(pos),
+            freqs.turns_ptr, freqs.magnitude, T, B, Hq, Hkv, d, freqs.rot_dim, 1 if interleaved else 0, _ptr(Qo),
+            Kc.data_ptr(), Vc.data_ptr())
+    if block_table is None:
+        rc = getattr(lib, name)(*head, S_cap, ws.ptr, ws.nbytes, _stream(stream))
+    else:
+        rc = getattr(lib, name)(*head, block_table.data_ptr(), max_pages, page_size, n_pages, ws.ptr, ws.nbytes,
+                                _stream(stream))
+    if rc != OK:
+        _check(rc, name)
     return Qo
 
 
@@ -700,10 +720,7 @@ class ChunkWorkspace:
             raise ValueError("invalid chunk workspace shapes")
         dev = torch.device("cuda") if device is None else torch.device(device)
         self.buf = torch.zeros(self.nbytes, dtype=torch.uint8, device=dev)
-
-    @property
-    def ptr(self) -> int:
-        return self.buf.data_ptr()
+        self.ptr = self.buf.data_ptr()
 
 
 class _ScoreOpts(ctypes.Structure):
@@ -733,14 +750,13 @@ def libraspec_chunk_attn_paged(Q, Kp, Vp, block_table, cu_new, kv_len, ws: Chunk
 def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key,
                 prefix_len, O, lse, want_lse, stream):
     _req(Q, torch.bfloat16, "Q")
-    if Q.dim() != 3:
+    shape = Q.shape
+    if len(shape) != 3:
         raise ValueError("Q must be [T, Hq, d]")
-    T, Hq, d = Q.shape
+    T, Hq, d = shape
     B = _check_new(cu_new, kv_len)
     Hkv = Kc.shape[1] if isinstance(Kc, torch.Tensor) and Kc.dim() == 4 else 0
     S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
-    if softmax_scale is None:
-        softmax_scale = d ** -0.5
     opts = None
     if softcap or slopes is not None or window or first_key is not None or prefix_len is not None:
         if slopes is not None:
@@ -750,21 +766,25 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
         if prefix_len is not None:
             _req(prefix_len, torch.int32, "prefix_len", (B,))
         opts = ctypes.byref(_ScoreOpts(float(softcap), int(window), _ptr(slopes), _ptr(first_key), _ptr(prefix_len)))
-    O = torch.empty_like(Q) if O is None else _req(O, torch.bfloat16, "O", Q.shape)
+    if O is None:
+        O = torch.empty_like(Q)
+    else:
+        _req(O, torch.bfloat16, "O", shape)
     if lse is not None:
         _req(lse, torch.float32, "lse", (T, Hq))
     elif want_lse:
         lse = torch.empty((T, Hq), dtype=torch.float32, device=Q.device)
-    tail = (float(softmax_scale), opts, _ptr(O), _ptr(lse), ws.ptr, ws.nbytes, _stream(stream))
+    tail = (d ** -0.5 if softmax_scale is None else float(softmax_scale), opts, O.data_ptr(), _ptr(lse), ws.ptr,
+            ws.nbytes, _stream(stream))
     if block_table is None:
-        name = "libraspec_chunk_attn"
-        rc = load().libraspec_chunk_attn(_ptr(Q), _ptr(Kc), _ptr(Vc), _ptr(cu_new), _ptr(kv_len), T, B, Hq, Hkv, d,
-                                         S_cap, *tail)
+        rc = load().libraspec_chunk_attn(Q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(), cu_new.data_ptr(),
+                                         kv_len.data_ptr(), T, B, Hq, Hkv, d, S_cap, *tail)
     else:
-        name = "libraspec_chunk_attn_paged"
-        rc = load().libraspec_chunk_attn_paged(_ptr(Q), _ptr(Kc), _ptr(Vc), _ptr(block_table), max_pages, page_size,
-                                               n_pages, _ptr(cu_new), _ptr(kv_len), T, B, Hq, Hkv, d, *tail)
-    _check(rc, name)
+        rc = load().libraspec_chunk_attn_paged(Q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(), block_table.data_ptr(),
+                                               max_pages, page_size, n_pages, cu_new.data_ptr(), kv_len.data_ptr(), T, B,
+                                               Hq, Hkv, d, *tail)
+    if rc != OK:
+        _check(rc, "libraspec_chunk_attn" if block_table is None else "libraspec_chunk_attn_paged")
     return O, lse
 
 

@@ -435,9 +435,8 @@ bool pos_finite(double x) { return x > 0.0 && x <= 1e300; }
 bool token_stride_ok(int64_t stride, int H, int d) { return stride >= (int64_t)H * d && stride <= (int64_t(1) << 40); }
 
 bool rope_shape_ok(int T, int H, int head_dim, int rot_dim) {
-  return T >= 0 && H >= 1 && H <= (1 << 20) && head_dim >= 2 && head_dim % 2 == 0 && head_dim <= 65536 &&
-         (long)H * head_dim <= 0x7fffffffL && rot_dim >= 2 && rot_dim % 2 == 0 && rot_dim <= head_dim &&
-         rot_dim <= LIBRASPEC_ROPE_MAX_DIM;
+  return T >= 0 && H >= 1 && H <= (1 << 20) && head_dim >= 2 && head_dim % 2 == 0 && head_dim <= LIBRASPEC_ROPE_MAX_DIM &&
+         (long)H * head_dim <= 0x7fffffffL && rot_dim >= 2 && rot_dim % 2 == 0 && rot_dim <= head_dim;
 }
 
 }  // namespace

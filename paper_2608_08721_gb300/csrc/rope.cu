@@ -10,15 +10,17 @@
 // 0.004.)
 //
 // Bound by HBM: every element is read once and written once. One CTA works on
-// one token: its first threads form the token's cosines and sines in shared
-// memory (once for all heads) while every thread's first loads are on their
-// way, then the threads share out the token's heads in units of 16 bytes.
+// one token or four: its threads form the tokens' cosines and sines in shared
+// memory (once for all heads) while their first loads are on their way, then
+// they share out the tokens' heads in units of 16 bytes.
 #include <cmath>
 #include <type_traits>
 
 #include "common.cuh"
 
 namespace libraspec {
+
+int num_sms_current();
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxPairs = 256;
@@ -59,27 +61,19 @@ __device__ __forceinline__ Pack<Tout, N> convert(const Pack<Tin, N>& a) {
   }
 }
 
-// One row (a head of a token) of the call: where it is read and written, and whether it turns.
-template <typename Tin, typename Tout>
-struct RopeRow {
-  const Tin* src;
-  Tout* dst;
-  bool turns;
-};
-
 // A head as units: N elements of the first half of the rotated part with the N they pair with (half layout), or 2N
 // consecutive ones (interleaved), then 2N at a time of the part that is only copied.
 template <typename Tin, typename Tout, int N, bool INTER>
 struct RopeUnit {
   Pack<Tin, N> a, b;
-  __device__ __forceinline__ void load(const RopeRow<Tin, Tout>& r, int u, int half) {
-    const int i = at(u, half), j = partner(u, half);
-    a = *reinterpret_cast<const Pack<Tin, N>*>(r.src + i);
-    b = *reinterpret_cast<const Pack<Tin, N>*>(r.src + j);
+  __device__ __forceinline__ void load(const Tin* src, int u, int half) {
+    a = *reinterpret_cast<const Pack<Tin, N>*>(src + at(u, half));
+    b = *reinterpret_cast<const Pack<Tin, N>*>(src + partner(u, half));
   }
-  __device__ __forceinline__ void store(const RopeRow<Tin, Tout>& r, int u, int half, const float2* cs) const {
+  // cs: cosine and sine of the token's pairs; turns: the head is a query's or a key's
+  __device__ __forceinline__ void store(Tout* dst, bool turns, int u, int half, const float2* cs) const {
     Pack<Tout, N> x, y;
-    if (u * N >= half || !r.turns) {
+    if (u * N >= half || !turns) {
       x = convert<Tin, Tout, N>(a);
       y = convert<Tin, Tout, N>(b);
     } else if (INTER) {
@@ -97,8 +91,8 @@ struct RopeUnit {
 #pragma unroll
       for (int k = 0; k < N; ++k) turn(to_f32(a.v[k]), to_f32(b.v[k]), cs[u * N + k], x.v[k], y.v[k]);
     }
-    *reinterpret_cast<Pack<Tout, N>*>(r.dst + at(u, half)) = x;
-    *reinterpret_cast<Pack<Tout, N>*>(r.dst + partner(u, half)) = y;
+    *reinterpret_cast<Pack<Tout, N>*>(dst + at(u, half)) = x;
+    *reinterpret_cast<Pack<Tout, N>*>(dst + partner(u, half)) = y;
   }
   // (past the rotated part both layouts take 2N consecutive elements)
   __device__ static __forceinline__ int at(int u, int half) { return INTER || u * N >= half ? 2 * u * N : u * N; }
@@ -128,78 +122,109 @@ struct RopeArgs {
   int* status;
 };
 
-template <typename Tin, typename Tout, int N, bool INTER, bool APPEND>
+template <typename Tin, typename Tout, int N, bool INTER, bool APPEND, int TOKENS>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
-  __shared__ float2 cs[kRopeMaxPairs];
-  __shared__ int s_seq, s_pos;
-  __shared__ long long s_row;  // the token's row of the cache (of kv head 0), negative: none
-  const int t = blockIdx.x, tid = threadIdx.x;
-  const int per_head = A.d / (2 * N);
-  const int heads = APPEND ? A.Hq + 2 * A.Hkv : A.Hq;
-  const int units = heads * per_head;
+  __shared__ float2 cs[TOKENS][kRopeMaxPairs];
+  __shared__ int s_pos[TOKENS];
+  __shared__ long long s_row[TOKENS];  // the token's row of the cache (of kv head 0); -1: no room; -2: of no sequence
+  const int t0 = blockIdx.x * TOKENS, tid = threadIdx.x;
+  const int n_tok = min(TOKENS, A.T - t0);
+  const int per_head = A.d / (2 * N), heads = APPEND ? A.Hq + 2 * A.Hkv : A.Hq;
   long long head_step = 0;  // between the rows of neighbouring kv heads in the cache
+  if constexpr (APPEND) head_step = (long long)(A.block_table ? A.page_size : A.S_cap) * A.d;
+  // A thread has one unit of a head, and every n_heads_at_once-th head of the CTA's tokens, token after token: its
+  // cosines change with the token alone, and a step to the next head is an addition (with a division for each unit the
+  // kernel was bound by its instructions: 43 us instead of 26 for 8587 tokens of 28 + 2 x 4 heads).
+  const int n_heads_at_once = kRopeThreads / per_head;
+  const int u = tid % per_head;
+  const bool worker = tid < n_heads_at_once * per_head;
 
-  auto row = [&](int h, long long cache_row) {
-    RopeRow<Tin, Tout> r;
-    if (!APPEND || h < A.Hq) {
-      r.src = static_cast<const Tin*>(A.Q) + t * A.q_stride + (long long)h * A.d;
-      r.dst = static_cast<Tout*>(A.Qo) + t * A.o_stride + (long long)h * A.d;
-      r.turns = true;
-    } else {
-      const bool key = h < A.Hq + A.Hkv;
-      const int kvh = h - A.Hq - (key ? 0 : A.Hkv);
-      r.src = static_cast<const Tin*>(key ? A.K : A.V) + t * (key ? A.k_stride : A.v_stride) + (long long)kvh * A.d;
-      r.dst = reinterpret_cast<Tout*>(key ? A.Kc : A.Vc) + cache_row + kvh * head_step;
-      r.turns = key;
+  struct Row {
+    int j, h;  // token, head of the token
+  };
+  auto advance = [&](Row& r) {
+    r.h += n_heads_at_once;
+    while (r.h >= heads) {
+      r.h -= heads;
+      ++r.j;
     }
-    return r;
+  };
+  Row at{0, tid / per_head};
+  while (at.h >= heads) {
+    at.h -= heads;
+    ++at.j;
+  }
+  auto source = [&](const Row& r) {
+    const long long t = t0 + r.j;
+    if (!APPEND || r.h < A.Hq) return static_cast<const Tin*>(A.Q) + t * A.q_stride + (long long)r.h * A.d;
+    const bool key = r.h < A.Hq + A.Hkv;
+    return static_cast<const Tin*>(key ? A.K : A.V) + t * (key ? A.k_stride : A.v_stride) +
+           (long long)(r.h - A.Hq - (key ? 0 : A.Hkv)) * A.d;
   };
 
-  // the first unit's loads go out before anything else is known
-  RopeUnit<Tin, Tout, N, INTER> first;
-  if (tid < units) first.load(row(tid / per_head, 0), tid % per_head, A.half);
+  // the first units' loads go out before anything else is known
+  RopeUnit<Tin, Tout, N, INTER> unit;
+  if (worker && at.j < n_tok) unit.load(source(at), u, A.half);
 
   if constexpr (APPEND) {
-    if (tid == 0) s_seq = -1;
+    if (tid < TOKENS) s_row[tid] = -2;
     __syncthreads();
-    // the token's sequence: every thread looks at its share of the offsets
+    // the tokens' sequences: every thread looks at its share of the offsets
     for (int b = tid; b < A.B; b += kRopeThreads) {
       const int lo = A.cu_new[b], hi = A.cu_new[b + 1], kv = A.kv_len[b];
-      if (t == 0 && (lo < 0 || hi < lo || hi > A.T)) raise_status(A.status, LIBRASPEC_ST_BAD_LENGTH);
-      if (t < lo || t >= hi) continue;
-      s_seq = b;
-      const long long s = (long long)kv + (t - lo);
-      long long at = -1;
-      if (kv < 0 || s >= A.S_cap) {
-        raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
-      } else if (A.block_table) {
-        const int page = A.block_table[(size_t)b * A.max_pages + s / A.page_size];
-        if (page < 0 || page >= A.n_pages) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
-        else at = ((long long)page * A.Hkv * A.page_size + s % A.page_size) * A.d;
-      } else {
-        at = ((long long)b * A.Hkv * A.S_cap + s) * A.d;
+      if (blockIdx.x == 0 && (lo < 0 || hi < lo || hi > A.T)) raise_status(A.status, LIBRASPEC_ST_BAD_LENGTH);
+#pragma unroll
+      for (int j = 0; j < TOKENS; ++j) {
+        const int t = t0 + j;
+        if (j >= n_tok || t < lo || t >= hi) continue;
+        const long long s = (long long)kv + (t - lo);
+        long long at = -1;
+        if (kv < 0 || s >= A.S_cap) {
+          raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
+        } else if (A.block_table) {
+          const int page = A.block_table[(size_t)b * A.max_pages + s / A.page_size];
+          if (page < 0 || page >= A.n_pages) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
+          else at = ((long long)page * A.Hkv * A.page_size + s % A.page_size) * A.d;
+        } else {
+          at = ((long long)b * A.Hkv * A.S_cap + s) * A.d;
+        }
+        s_row[j] = at;
+        s_pos[j] = A.pos ? A.pos[t] : (int)s;
       }
-      s_row = at;
-      s_pos = A.pos ? A.pos[t] : (int)s;
     }
     __syncthreads();
-    if (s_seq < 0) return;  // a row of no sequence
-    head_step = (long long)(A.block_table ? A.page_size : A.S_cap) * A.d;
+  } else if (TOKENS > 1) {
+    if (tid < n_tok) s_pos[tid] = A.pos[t0 + tid];
+    __syncthreads();
   }
-  const int pos = APPEND ? s_pos : A.pos[t];
-  for (int i = tid; i < A.half; i += kRopeThreads) {
-    float2 c = rope_turn(pos, A.turns[i], A.magnitude);
+  for (int i = tid; i < n_tok * A.half; i += kRopeThreads) {
+    const int j = TOKENS == 1 ? 0 : i / A.half, k = i - j * A.half;
+    if (APPEND && s_row[j] == -2) continue;
+    float2 c = rope_turn(APPEND || TOKENS > 1 ? s_pos[j] : A.pos[t0], A.turns[k], A.magnitude);
     if (A.inverse) c.y = -c.y;
-    cs[i] = c;
+    cs[j][k] = c;
   }
   __syncthreads();
-  const long long cache_row = APPEND ? s_row : 0;
-  const int live = APPEND && cache_row < 0 ? A.Hq * per_head : units;  // no place in the cache: the queries alone
-  for (int i = tid; i < live; i += kRopeThreads) {
-    const RopeRow<Tin, Tout> r = row(i / per_head, cache_row);
-    const int u = i % per_head;
-    if (i != tid) first.load(r, u, A.half);
-    first.store(r, u, A.half, cs);
+  if (!worker) return;
+  // each unit's loads go out before the stores of the one before
+  while (at.j < n_tok) {
+    Row next = at;
+    advance(next);
+    RopeUnit<Tin, Tout, N, INTER> ahead;
+    if (next.j < n_tok) ahead.load(source(next), u, A.half);
+    Tout* dst = nullptr;
+    bool turns = true;
+    if (!APPEND || at.h < A.Hq) {  // (the query of a token without room is rotated all the same)
+      if (!APPEND || s_row[at.j] >= -1)
+        dst = static_cast<Tout*>(A.Qo) + (t0 + at.j) * A.o_stride + (long long)at.h * A.d;
+    } else if (s_row[at.j] >= 0) {
+      turns = at.h < A.Hq + A.Hkv;
+      dst = reinterpret_cast<Tout*>(turns ? A.Kc : A.Vc) + s_row[at.j] +
+            (at.h - A.Hq - (turns ? 0 : A.Hkv)) * head_step;
+    }
+    if (dst) unit.store(dst, turns, u, A.half, cs[at.j]);
+    unit = ahead;
+    at = next;
   }
 }
 
@@ -225,11 +250,21 @@ void rope_frequencies(int rot, double theta, int scaling, double factor, double 
   }
 }
 
+template <typename Tin, typename Tout, int N, bool APPEND, int TOKENS>
+static cudaError_t launch_tokens(const RopeArgs& a, int interleaved, cudaStream_t stream) {
+  const int grid = (a.T + TOKENS - 1) / TOKENS;
+  if (interleaved) rope_kernel<Tin, Tout, N, true, APPEND, TOKENS><<<grid, kRopeThreads, 0, stream>>>(a);
+  else rope_kernel<Tin, Tout, N, false, APPEND, TOKENS><<<grid, kRopeThreads, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
+// Four tokens a CTA where there are enough of them for every SM and one token's units do not fill a CTA several times.
 template <typename Tin, typename Tout, int N, bool APPEND>
 static cudaError_t launch_n(const RopeArgs& a, int interleaved, cudaStream_t stream) {
-  if (interleaved) rope_kernel<Tin, Tout, N, true, APPEND><<<a.T, kRopeThreads, 0, stream>>>(a);
-  else rope_kernel<Tin, Tout, N, false, APPEND><<<a.T, kRopeThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+  const int units = (APPEND ? a.Hq + 2 * a.Hkv : a.Hq) * (a.d / (2 * N));
+  return a.T >= 4 * 4 * num_sms_current() && units < 3 * kRopeThreads
+             ? launch_tokens<Tin, Tout, N, APPEND, 4>(a, interleaved, stream)
+             : launch_tokens<Tin, Tout, N, APPEND, 1>(a, interleaved, stream);
 }
 
 // Units of N elements where every access they make is aligned to its size: the rotated half and the head in whole
