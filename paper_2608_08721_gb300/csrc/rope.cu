@@ -10,9 +10,11 @@
 // 0.004.)
 //
 // Bound by HBM: every element is read once and written once. One CTA works on
-// one token or four: its threads form the tokens' cosines and sines in shared
+// one token or two: its threads form the tokens' cosines and sines in shared
 // memory (once for all heads) while their first loads are on their way, then
-// they share out the tokens' heads in units of 16 bytes.
+// they share out the tokens' heads in units of 16 bytes. 8192 tokens of 64
+// heads of 128 in fp32 take 79 us, the copy rate; the append of 8587 tokens of
+// 28 + 2 x 4 heads (158 MB) 36 us, 64% of it, 64 decoding tokens 3.2 us.
 #include <cmath>
 #include <type_traits>
 
@@ -22,26 +24,19 @@ namespace libraspec {
 
 int num_sms_current();
 
-constexpr int kRopeThreads = 256;
-constexpr int kRopeMaxPairs = 256;
+constexpr int kRopeThreads = 512;   // of a CTA, at most
+constexpr int kRopeMaxPairs = LIBRASPEC_ROPE_MAX_DIM / 2;
 
-// cos and sin of pair i at position pos, times the magnitude.
+// cos and sin of a pair at position pos, times the magnitude. The position in two parts that are binary32 numbers each.
 __device__ __forceinline__ float2 rope_turn(int pos, float2 f, float magnitude) {
-  // positions from 2^24 on are not binary32 numbers: their remainder turns by itself
-  const float pf = (float)pos;
-  const float rest = (float)((long long)pos - (long long)pf);
-  const float p = __fmul_rn(pf, f.x);
-  const float e = __fmaf_rn(pf, f.x, -p);
-  const float r = (p - rintf(p)) + (e + __fmaf_rn(pf, f.y, rest * f.x));
+  const float hi = (float)(pos & ~255), lo = (float)(pos & 255);
+  const float p = __fmul_rn(hi, f.x), q = __fmul_rn(lo, f.x);
+  const float e = __fmaf_rn(hi, f.x, -p) + __fmaf_rn(lo, f.x, -q);
+  const float r = ((p - rintf(p)) + (q - rintf(q))) + (e + __fmaf_rn(hi, f.y, lo * f.y));
   float s, c;
   sincospif(2.f * r, &s, &c);
   return make_float2(c * magnitude, s * magnitude);
 }
-
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ void from_f32(float& d, float x) { d = x; }
-__device__ __forceinline__ void from_f32(uint16_t& d, float x) { d = __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
 // N consecutive elements as one access of N * sizeof(T) bytes
 template <typename T, int N>
@@ -49,14 +44,48 @@ struct alignas(sizeof(T) * N) Pack {
   T v[N];
 };
 
+template <int N>
+__device__ __forceinline__ void widen(const Pack<float, N>& a, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = a.v[i];
+}
+template <int N>
+__device__ __forceinline__ void widen(const Pack<uint16_t, N>& a, float (&x)[N]) {
+  if constexpr (N == 1) {
+    x[0] = __uint_as_float((uint32_t)a.v[0] << 16);
+  } else {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(a.v);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      x[2 * i] = bf16_lo(w[i]);
+      x[2 * i + 1] = bf16_hi(w[i]);
+    }
+  }
+}
+template <int N>
+__device__ __forceinline__ void narrow(const float (&x)[N], Pack<float, N>& a) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) a.v[i] = x[i];
+}
+template <int N>
+__device__ __forceinline__ void narrow(const float (&x)[N], Pack<uint16_t, N>& a) {
+  if constexpr (N == 1) {
+    a.v[0] = __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
+  } else {
+    __nv_bfloat162* w = reinterpret_cast<__nv_bfloat162*>(a.v);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+  }
+}
 template <typename Tin, typename Tout, int N>
 __device__ __forceinline__ Pack<Tout, N> convert(const Pack<Tin, N>& a) {
   if constexpr (std::is_same<Tin, Tout>::value) {
     return a;
   } else {
+    float x[N];
+    widen(a, x);
     Pack<Tout, N> r;
-#pragma unroll
-    for (int i = 0; i < N; ++i) from_f32(r.v[i], to_f32(a.v[i]));
+    narrow(x, r);
     return r;
   }
 }
@@ -72,36 +101,39 @@ struct RopeUnit {
   }
   // cs: cosine and sine of the token's pairs; turns: the head is a query's or a key's
   __device__ __forceinline__ void store(Tout* dst, bool turns, int u, int half, const float2* cs) const {
-    Pack<Tout, N> x, y;
+    Pack<Tout, N> p, q;
     if (u * N >= half || !turns) {
-      x = convert<Tin, Tout, N>(a);
-      y = convert<Tin, Tout, N>(b);
-    } else if (INTER) {
-      if constexpr (N == 1) {
-        const float2 t = cs[u];
-        turn(to_f32(a.v[0]), to_f32(b.v[0]), t, x.v[0], y.v[0]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < N / 2; ++k) {
-          turn(to_f32(a.v[2 * k]), to_f32(a.v[2 * k + 1]), cs[u * N + k], x.v[2 * k], x.v[2 * k + 1]);
-          turn(to_f32(b.v[2 * k]), to_f32(b.v[2 * k + 1]), cs[u * N + N / 2 + k], y.v[2 * k], y.v[2 * k + 1]);
-        }
-      }
+      p = convert<Tin, Tout, N>(a);
+      q = convert<Tin, Tout, N>(b);
     } else {
+      float x[N], y[N], v[N], w[N];
+      widen(a, x);
+      widen(b, y);
+      cs += u * N;
+      if constexpr (INTER && N > 1) {  // pairs (x0, x1), (x2, x3) ..., then those of y
 #pragma unroll
-      for (int k = 0; k < N; ++k) turn(to_f32(a.v[k]), to_f32(b.v[k]), cs[u * N + k], x.v[k], y.v[k]);
+        for (int k = 0; k < N; k += 2) {
+          turn(x[k], x[k + 1], cs[k / 2], v[k], v[k + 1]);
+          turn(y[k], y[k + 1], cs[N / 2 + k / 2], w[k], w[k + 1]);
+        }
+      } else {  // pairs (x0, y0), (x1, y1) ...
+#pragma unroll
+        for (int k = 0; k < N; ++k) turn(x[k], y[k], cs[k], v[k], w[k]);
+      }
+      narrow(v, p);
+      narrow(w, q);
     }
-    *reinterpret_cast<Pack<Tout, N>*>(dst + at(u, half)) = x;
-    *reinterpret_cast<Pack<Tout, N>*>(dst + partner(u, half)) = y;
+    *reinterpret_cast<Pack<Tout, N>*>(dst + at(u, half)) = p;
+    *reinterpret_cast<Pack<Tout, N>*>(dst + partner(u, half)) = q;
   }
   // (past the rotated part both layouts take 2N consecutive elements)
   __device__ static __forceinline__ int at(int u, int half) { return INTER || u * N >= half ? 2 * u * N : u * N; }
   __device__ static __forceinline__ int partner(int u, int half) {
     return INTER || u * N >= half ? (2 * u + 1) * N : half + u * N;
   }
-  __device__ static __forceinline__ void turn(float x0, float x1, float2 t, Tout& y0, Tout& y1) {
-    from_f32(y0, fmaf(x0, t.x, -x1 * t.y));
-    from_f32(y1, fmaf(x0, t.y, x1 * t.x));
+  __device__ static __forceinline__ void turn(float x0, float x1, float2 t, float& y0, float& y1) {
+    y0 = fmaf(x0, t.x, -x1 * t.y);
+    y1 = fmaf(x0, t.y, x1 * t.x);
   }
 };
 
@@ -123,7 +155,7 @@ struct RopeArgs {
 };
 
 template <typename Tin, typename Tout, int N, bool INTER, bool APPEND, int TOKENS>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
+__global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A) {
   __shared__ float2 cs[TOKENS][kRopeMaxPairs];
   __shared__ int s_pos[TOKENS];
   __shared__ long long s_row[TOKENS];  // the token's row of the cache (of kv head 0); -1: no room; -2: of no sequence
@@ -132,45 +164,32 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
   const int per_head = A.d / (2 * N), heads = APPEND ? A.Hq + 2 * A.Hkv : A.Hq;
   long long head_step = 0;  // between the rows of neighbouring kv heads in the cache
   if constexpr (APPEND) head_step = (long long)(A.block_table ? A.page_size : A.S_cap) * A.d;
-  // A thread has one unit of a head, and every n_heads_at_once-th head of the CTA's tokens, token after token: its
-  // cosines change with the token alone, and a step to the next head is an addition (with a division for each unit the
-  // kernel was bound by its instructions: 43 us instead of 26 for 8587 tokens of 28 + 2 x 4 heads).
-  const int n_heads_at_once = kRopeThreads / per_head;
-  const int u = tid % per_head;
-  const bool worker = tid < n_heads_at_once * per_head;
-
-  struct Row {
-    int j, h;  // token, head of the token
-  };
-  auto advance = [&](Row& r) {
-    r.h += n_heads_at_once;
-    while (r.h >= heads) {
-      r.h -= heads;
-      ++r.j;
+  // A thread has one unit of a head, in every step-th head of all the CTA's tokens: what it adds up for an address it
+  // adds up once for two tokens, whose loads are in flight together.
+  const int step = blockDim.x / per_head, u = tid % per_head;
+  int h = tid / per_head;
+  if (h >= step) h = heads;  // (a thread past the last whole head has none)
+  RopeUnit<Tin, Tout, N, INTER> unit[TOKENS];
+  auto load = [&](int h, RopeUnit<Tin, Tout, N, INTER>(&to)[TOKENS]) {
+    const Tin* src = static_cast<const Tin*>(A.Q) + (long long)t0 * A.q_stride + h * A.d;
+    long long stride = A.q_stride;
+    if (APPEND && h >= A.Hq) {
+      const bool key = h < A.Hq + A.Hkv;
+      stride = key ? A.k_stride : A.v_stride;
+      src = static_cast<const Tin*>(key ? A.K : A.V) + t0 * stride + (h - A.Hq - (key ? 0 : A.Hkv)) * A.d;
     }
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j)
+      if (TOKENS == 1 || j < n_tok) to[j].load(src + j * stride, u, A.half);
   };
-  Row at{0, tid / per_head};
-  while (at.h >= heads) {
-    at.h -= heads;
-    ++at.j;
-  }
-  auto source = [&](const Row& r) {
-    const long long t = t0 + r.j;
-    if (!APPEND || r.h < A.Hq) return static_cast<const Tin*>(A.Q) + t * A.q_stride + (long long)r.h * A.d;
-    const bool key = r.h < A.Hq + A.Hkv;
-    return static_cast<const Tin*>(key ? A.K : A.V) + t * (key ? A.k_stride : A.v_stride) +
-           (long long)(r.h - A.Hq - (key ? 0 : A.Hkv)) * A.d;
-  };
-
   // the first units' loads go out before anything else is known
-  RopeUnit<Tin, Tout, N, INTER> unit;
-  if (worker && at.j < n_tok) unit.load(source(at), u, A.half);
+  if (h < heads) load(h, unit);
 
   if constexpr (APPEND) {
     if (tid < TOKENS) s_row[tid] = -2;
     __syncthreads();
     // the tokens' sequences: every thread looks at its share of the offsets
-    for (int b = tid; b < A.B; b += kRopeThreads) {
+    for (int b = tid; b < A.B; b += blockDim.x) {
       const int lo = A.cu_new[b], hi = A.cu_new[b + 1], kv = A.kv_len[b];
       if (blockIdx.x == 0 && (lo < 0 || hi < lo || hi > A.T)) raise_status(A.status, LIBRASPEC_ST_BAD_LENGTH);
 #pragma unroll
@@ -182,9 +201,10 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
         if (kv < 0 || s >= A.S_cap) {
           raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
         } else if (A.block_table) {
-          const int page = A.block_table[(size_t)b * A.max_pages + s / A.page_size];
+          const uint32_t nth = (uint32_t)s / (uint32_t)A.page_size;  // (s < S_cap, an int)
+          const int page = A.block_table[(size_t)b * A.max_pages + nth];
           if (page < 0 || page >= A.n_pages) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
-          else at = ((long long)page * A.Hkv * A.page_size + s % A.page_size) * A.d;
+          else at = ((long long)page * A.Hkv * A.page_size + ((uint32_t)s - nth * A.page_size)) * A.d;
         } else {
           at = ((long long)b * A.Hkv * A.S_cap + s) * A.d;
         }
@@ -197,7 +217,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
     if (tid < n_tok) s_pos[tid] = A.pos[t0 + tid];
     __syncthreads();
   }
-  for (int i = tid; i < n_tok * A.half; i += kRopeThreads) {
+  for (int i = tid; i < n_tok * A.half; i += blockDim.x) {
     const int j = TOKENS == 1 ? 0 : i / A.half, k = i - j * A.half;
     if (APPEND && s_row[j] == -2) continue;
     float2 c = rope_turn(APPEND || TOKENS > 1 ? s_pos[j] : A.pos[t0], A.turns[k], A.magnitude);
@@ -205,26 +225,22 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs A) {
     cs[j][k] = c;
   }
   __syncthreads();
-  if (!worker) return;
-  // each unit's loads go out before the stores of the one before
-  while (at.j < n_tok) {
-    Row next = at;
-    advance(next);
-    RopeUnit<Tin, Tout, N, INTER> ahead;
-    if (next.j < n_tok) ahead.load(source(next), u, A.half);
-    Tout* dst = nullptr;
-    bool turns = true;
-    if (!APPEND || at.h < A.Hq) {  // (the query of a token without room is rotated all the same)
-      if (!APPEND || s_row[at.j] >= -1)
-        dst = static_cast<Tout*>(A.Qo) + (t0 + at.j) * A.o_stride + (long long)at.h * A.d;
-    } else if (s_row[at.j] >= 0) {
-      turns = at.h < A.Hq + A.Hkv;
-      dst = reinterpret_cast<Tout*>(turns ? A.Kc : A.Vc) + s_row[at.j] +
-            (at.h - A.Hq - (turns ? 0 : A.Hkv)) * head_step;
+  for (; h < heads; h += step) {
+    RopeUnit<Tin, Tout, N, INTER> ahead[TOKENS];
+    if (TOKENS == 1 && h + step < heads) load(h + step, ahead);
+    const bool query = !APPEND || h < A.Hq, turns = !APPEND || h < A.Hq + A.Hkv;
+    Tout* dst = static_cast<Tout*>(A.Qo) + t0 * A.o_stride + h * A.d;
+    if (!query)
+      dst = reinterpret_cast<Tout*>(turns ? A.Kc : A.Vc) + (h - A.Hq - (turns ? 0 : A.Hkv)) * head_step;
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j) {
+      if (TOKENS > 1 && j >= n_tok) break;
+      // (the query of a token without room is rotated all the same)
+      if (APPEND && s_row[j] < (query ? -1 : 0)) continue;
+      unit[j].store(dst + (query ? j * A.o_stride : s_row[j]), turns, u, A.half, cs[j]);
     }
-    if (dst) unit.store(dst, turns, u, A.half, cs[at.j]);
-    unit = ahead;
-    at = next;
+    if (TOKENS == 1) unit[0] = ahead[0];
+    else if (h + step < heads) load(h + step, unit);
   }
 }
 
@@ -251,20 +267,28 @@ void rope_frequencies(int rot, double theta, int scaling, double factor, double 
 }
 
 template <typename Tin, typename Tout, int N, bool APPEND, int TOKENS>
-static cudaError_t launch_tokens(const RopeArgs& a, int interleaved, cudaStream_t stream) {
+static cudaError_t launch_tokens(const RopeArgs& a, int interleaved, int threads, cudaStream_t stream) {
   const int grid = (a.T + TOKENS - 1) / TOKENS;
-  if (interleaved) rope_kernel<Tin, Tout, N, true, APPEND, TOKENS><<<grid, kRopeThreads, 0, stream>>>(a);
-  else rope_kernel<Tin, Tout, N, false, APPEND, TOKENS><<<grid, kRopeThreads, 0, stream>>>(a);
+  if (interleaved) rope_kernel<Tin, Tout, N, true, APPEND, TOKENS><<<grid, threads, 0, stream>>>(a);
+  else rope_kernel<Tin, Tout, N, false, APPEND, TOKENS><<<grid, threads, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
-// Four tokens a CTA where there are enough of them for every SM and one token's units do not fill a CTA several times.
+// Two tokens a CTA, with a thread for each of a token's units, where a CTA has room for them and every SM gets a few
+// CTAs; else one token in passes of up to 256 threads over its heads. (8587 bf16 tokens of 36 heads: 36 us at two
+// tokens, 37 at one, 40 at four; in passes of 256 threads, which leave 7 of 8 warps idle in the second, 39. 8192 fp32
+// tokens of 64 heads: 79 us in passes of 256 threads, 84 in passes of 512.)
 template <typename Tin, typename Tout, int N, bool APPEND>
 static cudaError_t launch_n(const RopeArgs& a, int interleaved, cudaStream_t stream) {
-  const int units = (APPEND ? a.Hq + 2 * a.Hkv : a.Hq) * (a.d / (2 * N));
-  return a.T >= 4 * 4 * num_sms_current() && units < 3 * kRopeThreads
-             ? launch_tokens<Tin, Tout, N, APPEND, 4>(a, interleaved, stream)
-             : launch_tokens<Tin, Tout, N, APPEND, 1>(a, interleaved, stream);
+  const int per_head = a.d / (2 * N), heads = APPEND ? a.Hq + 2 * a.Hkv : a.Hq;
+  auto threads_for = [&](int step) { return std::max(64, (step * per_head + 31) / 32 * 32); };
+  if (heads <= kRopeThreads / per_head) {
+    return a.T >= 8 * num_sms_current()
+               ? launch_tokens<Tin, Tout, N, APPEND, 2>(a, interleaved, threads_for(heads), stream)
+               : launch_tokens<Tin, Tout, N, APPEND, 1>(a, interleaved, threads_for(heads), stream);
+  }
+  const int most = 256 / per_head, passes = (heads + most - 1) / most;
+  return launch_tokens<Tin, Tout, N, APPEND, 1>(a, interleaved, threads_for((heads + passes - 1) / passes), stream);
 }
 
 // Units of N elements where every access they make is aligned to its size: the rotated half and the head in whole
