@@ -160,12 +160,80 @@ __device__ __forceinline__ T block_scan(T v, T* warp_sums, T& total) {  // inclu
   return warp > 0 ? v + before : v;
 }
 
-__global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t* __restrict__ cu_new,
-                                                                  const int32_t* __restrict__ kv_len,
-                                                                  const MaskArgs mask, int T, int B, int TB, int S_cap,
-                                                                  int Hkv, int grid, int shared_tiles,
-                                                                  PlanBlock* __restrict__ blocks,
-                                                                  PlanHead* __restrict__ head, int* status) {
+struct PlanArgs {
+  const int32_t* cu_new;
+  const int32_t* kv_len;
+  MaskArgs mask;
+  int T, B, TB;      // TB: tokens of a block
+  int S_cap, Hkv, grid;
+  int shared_tiles;  // key tiles (of all kv heads) beyond which L2 does not hold them
+  int* status;
+};
+
+// New tokens of sequence b, 0 where its offsets or length are out of range (reported if asked to).
+__device__ __forceinline__ int new_tokens(const PlanArgs& a, int b, bool report, int& c0, int& kv) {
+  c0 = a.cu_new[b];
+  kv = a.kv_len[b];
+  const int hi = a.cu_new[b + 1];
+  if (c0 < 0 || hi < c0 || hi > a.T) {
+    if (report) raise_status(a.status, LIBRASPEC_ST_BAD_LENGTH);
+    return 0;
+  }
+  if (kv < 0 || (long long)kv + (hi - c0) > a.S_cap) {
+    if (report) raise_status(a.status, LIBRASPEC_ST_KV_OVERFLOW);
+    return 0;
+  }
+  return hi - c0;
+}
+
+// The most blocks that T tokens of B sequences have: offsets that run backwards could ask for more.
+__device__ __forceinline__ int block_room(const PlanArgs& a) {
+  return (int)min((long long)a.T, (long long)a.T / a.TB + a.B);
+}
+
+// Block of tokens [j0, j0 + TB) of sequence b, whose n tokens start at row c0 and position kv.
+__device__ __forceinline__ PlanBlock make_block(const PlanArgs& a, int b, int c0, int n, int kv, int j0) {
+  const int j1 = min(n, j0 + a.TB), N = kv + n;
+  const int prefix = a.mask.prefix_len ? a.mask.prefix_len[b] : 0;
+  int klo = 0x7fffffff, khi = 0;
+  if (!a.mask.first_key) {  // ranges move forward with the position
+    int l, h;
+    row_range(kv + j0, N, prefix, 0, a.mask.window, klo, h);
+    row_range(kv + j1 - 1, N, prefix, 0, a.mask.window, l, khi);
+  } else {
+    for (int j = j0; j < j1; ++j) {
+      int l, h;
+      row_range(kv + j, N, prefix, a.mask.first_key[c0 + j], a.mask.window, l, h);
+      if (l < h) {
+        klo = min(klo, l);
+        khi = max(khi, h);
+      }
+    }
+    if (klo >= khi) klo = khi = N - 1;  // no row sees anything: one tile, of which nothing is read
+  }
+  PlanBlock p{};
+  p.b = b;
+  p.tok0 = c0 + j0;
+  p.n_tok = j1 - j0;
+  p.pos0 = kv + j0;
+  p.klo = klo;
+  p.khi = khi;
+  p.tile0 = klo / kCKeys;
+  p.n_tiles = max(1, (khi + kCKeys - 1) / kCKeys - p.tile0);
+  return p;
+}
+
+// Blocks of a sequence that start together and walk its keys in step read each K and V tile from HBM once and from L2
+// after that; cut by cost their CTAs are all at different keys, which matters where the keys do not fit L2 (1024 tokens
+// over 131072 keys: 2.96 ms instead of 3.17).
+__device__ __forceinline__ int whole_waves(const PlanArgs& a, int n_blocks, int n_seqs, long long kv_tiles, int t_min,
+                                           int t_max) {
+  const bool together = n_blocks >= 2 * n_seqs && kv_tiles * a.Hkv > a.shared_tiles && t_max - t_min <= t_max / 8;
+  return together ? (int)min((long long)n_blocks * a.Hkv / a.grid, 1ll << 20) : 0;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const PlanArgs a, PlanBlock* __restrict__ blocks,
+                                                                  PlanHead* __restrict__ head) {
   __shared__ int first_block[LIBRASPEC_MAX_B + 1];  // of each sequence
   __shared__ int warp_i[32];
   __shared__ long long warp_l[32];
@@ -174,16 +242,15 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t*
   int carry = 0;
   long long kv_tiles = 0;  // of the sequences that have new tokens
   int n_seqs = 0;
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int nb = 0;
     long long nt = 0;
-    if (b < B) {
-      const int lo = cu_new[b], hi = cu_new[b + 1], kv = kv_len[b];
-      if (lo < 0 || hi < lo || hi > T) raise_status(status, LIBRASPEC_ST_BAD_LENGTH);
-      else if (kv < 0 || (long long)kv + (hi - lo) > S_cap) raise_status(status, LIBRASPEC_ST_KV_OVERFLOW);
-      else nb = (hi - lo + TB - 1) / TB;
-      if (nb) nt = ((long long)kv + hi - lo + kCKeys - 1) / kCKeys;
+    if (b < a.B) {
+      int c0, kv;
+      const int n = new_tokens(a, b, true, c0, kv);
+      nb = (n + a.TB - 1) / a.TB;
+      if (nb) nt = ((long long)kv + n + kCKeys - 1) / kCKeys;
     }
     long long all;
     block_scan(nt, warp_l, all);
@@ -191,58 +258,32 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t*
     n_seqs += __syncthreads_count(nb > 0);
     int total;
     const int inc = block_scan(nb, warp_i, total);
-    if (b < B) first_block[b] = carry + inc - nb;
+    if (b < a.B) first_block[b] = carry + inc - nb;
     carry += total;
   }
-  if (tid == 0) first_block[B] = carry;
+  if (tid == 0) first_block[a.B] = carry;
   __syncthreads();
-  // (offsets that run backwards could ask for more blocks than the table holds)
-  const long long room = min((long long)T, (long long)T / TB + B);
-  const int n_blocks = (int)min((long long)carry, room);
-  if (carry > room && tid == 0) raise_status(status, LIBRASPEC_ST_BAD_LENGTH);
+  const int room = block_room(a), n_blocks = min(carry, room);
+  if (carry > room && tid == 0) raise_status(a.status, LIBRASPEC_ST_BAD_LENGTH);
   long long tiles = 0;
   int pairs = 0, t_min = 0x7fffffff, t_max = 0;
   for (int e0 = 0; e0 < n_blocks; e0 += kPlanThreads) {
     const int e = e0 + tid;
     PlanBlock p{};
     if (e < n_blocks) {
-      int lo = 0, hi = B;  // the sequence: the last b with first_block[b] <= e (which has blocks: e < first_block[b + 1])
+      int lo = 0, hi = a.B;  // the last b with first_block[b] <= e (it has blocks: e < first_block[b + 1])
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (first_block[mid] <= e) lo = mid;
         else hi = mid;
       }
-      const int b = lo, c0 = cu_new[b], n = cu_new[b + 1] - c0, kv = kv_len[b], N = kv + n;
-      const int j0 = (e - first_block[b]) * TB, j1 = min(n, j0 + TB);
-      const int prefix = mask.prefix_len ? mask.prefix_len[b] : 0;
-      int klo = 0x7fffffff, khi = 0;
-      if (!mask.first_key) {  // ranges move forward with the position
-        int l, h;
-        row_range(kv + j0, N, prefix, 0, mask.window, klo, h);
-        row_range(kv + j1 - 1, N, prefix, 0, mask.window, l, khi);
-      } else {
-        for (int j = j0; j < j1; ++j) {
-          int l, h;
-          row_range(kv + j, N, prefix, mask.first_key[c0 + j], mask.window, l, h);
-          if (l < h) {
-            klo = min(klo, l);
-            khi = max(khi, h);
-          }
-        }
-        if (klo >= khi) klo = khi = N - 1;  // no row sees anything: one tile, of which nothing is read
-      }
-      p.b = b;
-      p.tok0 = c0 + j0;
-      p.n_tok = j1 - j0;
-      p.pos0 = kv + j0;
-      p.klo = klo;
-      p.khi = khi;
-      p.tile0 = klo / kCKeys;
-      p.n_tiles = max(1, (khi + kCKeys - 1) / kCKeys - p.tile0);
+      int c0, kv;
+      const int n = new_tokens(a, lo, false, c0, kv);
+      p = make_block(a, lo, c0, n, kv, (e - first_block[lo]) * a.TB);
     }
     long long total;
     const long long inc = block_scan((long long)p.n_tiles, warp_l, total);
-    const int pair = p.n_tok > TB / 2;
+    const int pair = p.n_tok > a.TB / 2;
     int n_pairs;
     const int inc_p = block_scan(pair, warp_i, n_pairs);
     if (e < n_blocks) {
@@ -265,15 +306,78 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const int32_t*
       t_min = min(t_min, (int)(warp_l[w] & 0x7fffffff));
       t_max = max(t_max, (int)(warp_l[w] >> 32));
     }
-    // Blocks of a sequence that start together and walk its keys in step read each K and V tile from HBM once and from
-    // L2 after that; cut by cost their CTAs are all at different keys, which matters where the keys do not fit L2.
-    const long long items = (long long)n_blocks * Hkv;
-    const bool together = n_blocks >= 2 * n_seqs && kv_tiles * Hkv > shared_tiles && t_max - t_min <= t_max / 8;
     head->tiles = tiles;
     head->blocks = n_blocks;
     head->pairs = pairs;
-    head->waves = together ? (int)min(items / grid, (long long)1 << 20) : 0;
+    head->waves = whole_waves(a, n_blocks, n_seqs, kv_tiles, t_min, t_max);
   }
+}
+
+// The same for up to kWarpBlocks blocks by one warp, in its registers: lane l has blocks l and l + 32. Every CTA's
+// producer then plans for itself, and the call is one launch (a decode step of one sequence over 512 keys: 12.7 us with
+// the plan's launch, 11.1 without).
+constexpr int kWarpBlocks = 64;
+constexpr int kWarpSeqs = 512;
+
+__device__ __forceinline__ int warp_scan(int v) {  // inclusive
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, v, off);
+    if (lane >= off) v += x;
+  }
+  return v;
+}
+
+__device__ PlanHead warp_plan(const PlanArgs& a, PlanBlock (&mine)[2]) {
+  const int lane = threadIdx.x & 31, room = block_room(a);
+  mine[0] = mine[1] = PlanBlock{};
+  int carry = 0, n_seqs = 0;
+  long long kv_tiles = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    int c0 = 0, kv = 0, n = 0;
+    if (b0 + lane < a.B) n = new_tokens(a, b0 + lane, blockIdx.x == 0, c0, kv);
+    const int nb = (n + a.TB - 1) / a.TB, inc = warp_scan(nb), total = __shfl_sync(0xffffffffu, inc, 31);
+    n_seqs += __popc(__ballot_sync(0xffffffffu, nb > 0));
+    kv_tiles += nb ? ((long long)kv + n + kCKeys - 1) / kCKeys : 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int e = lane + 32 * k - carry;  // among these sequences' blocks
+      int s = 0;                            // its sequence: the first whose inclusive count is above e
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1)
+        if (__shfl_sync(0xffffffffu, inc, s + off - 1) <= e) s += off;
+      s = min(s, 31);
+      const int sc = __shfl_sync(0xffffffffu, c0, s), sn = __shfl_sync(0xffffffffu, n, s);
+      const int skv = __shfl_sync(0xffffffffu, kv, s), before = __shfl_sync(0xffffffffu, inc - nb, s);
+      if (e >= 0 && e < total && lane + 32 * k < room)
+        mine[k] = make_block(a, b0 + s, sc, sn, skv, (e - before) * a.TB);
+    }
+    carry += total;
+  }
+  if (carry > room && blockIdx.x == 0 && lane == 0) raise_status(a.status, LIBRASPEC_ST_BAD_LENGTH);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) kv_tiles += __shfl_xor_sync(0xffffffffu, kv_tiles, off);
+  PlanHead h{};
+  h.blocks = min(carry, room);
+  int t_min = 0x7fffffff, t_max = 0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    // (at most 64 blocks of 2^24 tiles: an int)
+    const int nt = mine[k].n_tiles, pair = mine[k].n_tok > a.TB / 2, inc = warp_scan(nt), inc_p = warp_scan(pair);
+    mine[k].tiles_before = h.tiles + inc - nt;
+    mine[k].pairs_before = h.pairs + inc_p - pair;
+    h.tiles += __shfl_sync(0xffffffffu, inc, 31);
+    h.pairs += __shfl_sync(0xffffffffu, inc_p, 31);
+    if (nt) {
+      t_min = min(t_min, nt);
+      t_max = max(t_max, nt);
+    }
+  }
+  t_min = __reduce_min_sync(0xffffffffu, t_min);
+  t_max = __reduce_max_sync(0xffffffffu, t_max);
+  h.waves = whole_waves(a, h.blocks, n_seqs, kv_tiles, t_min, t_max);
+  return h;
 }
 
 // ---------------------------------------------------------------------------
@@ -293,7 +397,8 @@ struct ChunkArgs {
   const int32_t* block_table;
   const float* slopes;  // [Hq] or NULL
   MaskArgs mask;
-  const PlanBlock* blocks;
+  PlanArgs plan;
+  const PlanBlock* blocks;  // NULL: each producer plans for itself
   const PlanHead* head;
   float* part_o;
   float* part_ml;
@@ -407,26 +512,60 @@ struct Place {
   long long before;     // tiles before it in the tile sequence
 };
 
-// Warp-wide. Block e's Hkv copies start at Hkv times the weight before it, each with its fixed cost first; x < the total.
-__device__ Place find_place(long long x, const PlanBlock* __restrict__ blocks, int n_blocks, int Hkv, int g,
-                            FixedCost f) {
+// The plan's blocks, by the warp: from the table, or from the lanes' registers.
+struct Blocks {
+  const PlanBlock* __restrict__ table;  // NULL: registers
+  const PlanBlock (&mine)[2];
+  int n;
+  // block e, the same for all lanes
+  __device__ __forceinline__ PlanBlock at(int e) const {
+    if (table) return table[e];
+    const PlanBlock& m = e < 32 ? mine[0] : mine[1];
+    PlanBlock p;
+    p.tiles_before = __shfl_sync(0xffffffffu, m.tiles_before, e);
+    p.pairs_before = __shfl_sync(0xffffffffu, m.pairs_before, e);
+    p.b = __shfl_sync(0xffffffffu, m.b, e);
+    p.tok0 = __shfl_sync(0xffffffffu, m.tok0, e);
+    p.n_tok = __shfl_sync(0xffffffffu, m.n_tok, e);
+    p.pos0 = __shfl_sync(0xffffffffu, m.pos0, e);
+    p.klo = __shfl_sync(0xffffffffu, m.klo, e);
+    p.khi = __shfl_sync(0xffffffffu, m.khi, e);
+    p.tile0 = __shfl_sync(0xffffffffu, m.tile0, e);
+    p.n_tiles = __shfl_sync(0xffffffffu, m.n_tiles, e);
+    p.pad = 0;
+    return p;
+  }
+};
+
+// Block e's Hkv copies start at Hkv times the weight before it, each with its fixed cost first; x < the total.
+__device__ Place find_place(long long x, const Blocks& blocks, int Hkv, int g, FixedCost f) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, n = n_blocks;  // the last block of [lo, lo + n) that starts at or before x
-  while (n > 1) {
-    const int step = (n + 31) / 32, i = lo + lane * step;
-    const bool at = lane * step < n && (long long)Hkv * weight_before(blocks[i], i, f) <= x;
-    const int k = 31 - __clz(__ballot_sync(0xffffffffu, at));  // (lane 0 always holds)
-    n = min(step, n - k * step);
-    lo += k * step;
+  int lo = 0;  // the last block that starts at or before x
+  if (blocks.table) {
+    for (int n = blocks.n; n > 1;) {  // it is in [lo, lo + n)
+      const int step = (n + 31) / 32, i = lo + lane * step;
+      const bool at = lane * step < n && (long long)Hkv * weight_before(blocks.table[i], i, f) <= x;
+      const int k = 31 - __clz(__ballot_sync(0xffffffffu, at));  // (lane 0 always holds)
+      n = min(step, n - k * step);
+      lo += k * step;
+    }
+  } else {
+    for (int k = 0; k < 2; ++k) {
+      const int e = lane + 32 * k;
+      const bool at = e < blocks.n && (long long)Hkv * weight_before(k ? blocks.mine[1] : blocks.mine[0], e, f) <= x;
+      lo += __popc(__ballot_sync(0xffffffffu, at));
+    }
+    --lo;
   }
   Place p;
   p.e = lo;
-  const long long o = x - (long long)Hkv * weight_before(blocks[lo], lo, f);
-  const int nt = blocks[lo].n_tiles, c = fixed_of(blocks[lo], g, f), w = nt + c;
+  const PlanBlock b = blocks.at(lo);
+  const long long o = x - (long long)Hkv * weight_before(b, lo, f);
+  const int c = fixed_of(b, g, f), w = b.n_tiles + c;
   p.kvh = (int)(o / w);
   const int r = (int)(o - (long long)p.kvh * w);
   p.tile = r > c ? r - c : 0;
-  p.before = (long long)Hkv * blocks[lo].tiles_before + (long long)p.kvh * nt + p.tile;
+  p.before = (long long)Hkv * b.tiles_before + (long long)p.kvh * b.n_tiles + p.tile;
   return p;
 }
 
@@ -577,7 +716,9 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
    if (warp == kCProducerWarp) {
     // ======================= producer =======================
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const PlanHead head = *A.head;
+    PlanBlock mine[2];
+    const PlanHead head = A.blocks ? *A.head : warp_plan(A.plan, mine);
+    const Blocks blocks{A.blocks, mine, head.blocks};
     const int c = blockIdx.x;
     // the whole items first, in step; the rest is cut by cost from tile `done` on, weighted position x_done
     const long long all = (long long)A.Hkv * head.tiles;
@@ -588,8 +729,11 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       p.e = id / A.Hkv;
       p.kvh = id - p.e * A.Hkv;
       p.tile = 0;
-      p.before = p.e < head.blocks ? (long long)A.Hkv * A.blocks[p.e].tiles_before + (long long)p.kvh * A.blocks[p.e].n_tiles
-                                   : all;
+      p.before = all;
+      if (p.e < head.blocks) {
+        const PlanBlock b = blocks.at(p.e);
+        p.before = (long long)A.Hkv * b.tiles_before + (long long)p.kvh * b.n_tiles;
+      }
       return p;
     };
     const Place first_cut = place_of_item(n_whole);
@@ -605,7 +749,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
                                                 (long long)fixed.pair * head.pairs);
     long long x_cut = x_all;
     if (first_cut.e < head.blocks) {
-      const PlanBlock& p = A.blocks[first_cut.e];
+      const PlanBlock p = blocks.at(first_cut.e);
       x_cut = (long long)A.Hkv * weight_before(p, first_cut.e, fixed) +
               (long long)first_cut.kvh * (p.n_tiles + fixed_of(p, g, fixed));
     }
@@ -614,8 +758,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     long long left = 0;  // the CTA's tiles of the cut part
     if (c < G) {
       const long long x0 = x_cut + c * W / G, x1 = x_cut + (c + 1) * W / G;
-      at = find_place(x0, A.blocks, head.blocks, A.Hkv, g, fixed);
-      const long long end = x1 < x_all ? find_place(x1, A.blocks, head.blocks, A.Hkv, g, fixed).before : all;
+      at = find_place(x0, blocks, A.Hkv, g, fixed);
+      const long long end = x1 < x_all ? find_place(x1, blocks, A.Hkv, g, fixed).before : all;
       left = end - at.before;
     }
     int whole = head.waves;  // whole items still to do
@@ -626,14 +770,14 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     // a lane's piece of a K or V tile: keys [row, row + piece) of the tile, columns [64 hb, 64 hb + 64)
     const int per_tile = kCKeys / A.piece;
     const int my_row = (lane % per_tile) * A.piece, my_hb = lane / per_tile;
-    const bool mine = my_hb < SM::kBoxes;
+    const bool has_piece = my_hb < SM::kBoxes;
     uint32_t item_ctr = 0, chunk_ctr = 0;
     const uint64_t once = evict_first_policy(), again = evict_normal_policy();
     bool ok = true;
     while ((whole > 0 || left > 0) && ok) {
       const bool cut = whole == 0;
       const Place pl = cut ? at : place_of_item((head.waves - whole) * (int)gridDim.x + c);
-      const PlanBlock p = A.blocks[pl.e];
+      const PlanBlock p = blocks.at(pl.e);
       ChunkItem it{};
       it.b = p.b;
       it.kvh = pl.kvh;
@@ -700,7 +844,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         const int from = t >> 2 == (kt - 1) >> 2 ? pages : pages_before;  // kt - 1: the last K tile
         int page = __shfl_sync(0xffffffffu, from, (t & 3) * 8 + lane % per_tile);
         const int key = (it.tile0 + t) * kCKeys + my_row;
-        const bool load = mine && key < p.khi && key + A.piece > p.klo;
+        const bool load = has_piece && key < p.khi && key + A.piece > p.klo;
         if (A.block_table && load && (page < 0 || page >= A.n_pages)) {
           raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
           page = 0;  // a valid page; the sequence's output is then meaningless
@@ -1209,13 +1353,17 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
       !make_map(&a.Q, Q, D, Hq, T, g, kCRows / g, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
     return cudaErrorInvalidValue;
   const int grid = std::min(num_sms_current(), kCMaxCtas);
-  chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(cu_new, kv_len, a.mask, T, B, block_tokens(g),
-                                                    std::min(S_cap, kCMaxKeys), Hkv, grid,
-                                                    kCSharedBytes / (2 * kCKeys * D * 2),
-                                                    reinterpret_cast<PlanBlock*>(ws + lay.blocks),
-                                                    reinterpret_cast<PlanHead*>(ws + lay.head), a.status);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
+  a.plan = PlanArgs{cu_new, kv_len, a.mask, T, B, block_tokens(g), std::min(S_cap, kCMaxKeys), Hkv, grid,
+                    kCSharedBytes / (2 * kCKeys * D * 2), a.status};
+  // (a lane would go through a block's first keys one by one)
+  if (max_blocks(T, B, g) <= kWarpBlocks && B <= kWarpSeqs && !first_key) {
+    a.blocks = nullptr;
+  } else {
+    chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a.plan, reinterpret_cast<PlanBlock*>(ws + lay.blocks),
+                                                      reinterpret_cast<PlanHead*>(ws + lay.head));
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   using Launch = cudaError_t (*)(const ChunkArgs&, int, cudaStream_t);
   static const Launch launch[2][4] = {
       {launch_attn_t<64, 0>, launch_attn_t<64, kCap>, launch_attn_t<64, kBias>, launch_attn_t<64, kCap | kBias>},
