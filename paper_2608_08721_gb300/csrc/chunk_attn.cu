@@ -493,9 +493,16 @@ __device__ __forceinline__ uint32_t c_pack(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
+// a / b for a >= 0, b > 0, in 32 bits where both fit (a 64-bit division is a long sequence, and a call of one token has
+// several of them between its launch and its first copy)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if ((((unsigned long long)a | (unsigned long long)b) >> 32) == 0) return (long long)((uint32_t)a / (uint32_t)b);
+  return a / b;
+}
+
 // The CTA whose share of the weight W holds position y: the largest c with floor(c W / G) <= y.
 __device__ __forceinline__ int share_of(long long y, long long W, int G) {
-  return (int)(((y + 1) * (long long)G - 1) / W);
+  return (int)quotient((y + 1) * (long long)G - 1, W);
 }
 
 // Weight of the blocks before block e (per kv head), and of block e.
@@ -562,7 +569,7 @@ __device__ Place find_place(long long x, const Blocks& blocks, int Hkv, int g, F
   const PlanBlock b = blocks.at(lo);
   const long long o = x - (long long)Hkv * weight_before(b, lo, f);
   const int c = fixed_of(b, g, f), w = b.n_tiles + c;
-  p.kvh = (int)(o / w);
+  p.kvh = (int)quotient(o, w);
   const int r = (int)(o - (long long)p.kvh * w);
   p.tile = r > c ? r - c : 0;
   p.before = (long long)Hkv * b.tiles_before + (long long)p.kvh * b.n_tiles + p.tile;
@@ -736,30 +743,36 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       }
       return p;
     };
-    const Place first_cut = place_of_item(n_whole);
+    Place first_cut{};
+    if (n_whole) first_cut = place_of_item(n_whole);
     const long long tiles = all - first_cut.before;  // to be cut
     int G = (int)gridDim.x;
     if (tiles < G) G = (int)tiles;
     if (tiles > 0) {  // (a CTA with few tiles would get none if a block's fixed cost were several)
-      const int most = (int)min(1ll << 20, tiles / (4 * (long long)G));
+      const int most = (int)min(1ll << 20, quotient(tiles, 4 * (long long)G));
       fixed.one = min(fixed.one, most);
       fixed.pair = min(fixed.pair, most - fixed.one);
     }
     const long long x_all = (long long)A.Hkv * (head.tiles + (long long)fixed.one * head.blocks +
                                                 (long long)fixed.pair * head.pairs);
-    long long x_cut = x_all;
-    if (first_cut.e < head.blocks) {
+    long long x_cut = 0;
+    if (n_whole && first_cut.e < head.blocks) {
       const PlanBlock p = blocks.at(first_cut.e);
       x_cut = (long long)A.Hkv * weight_before(p, first_cut.e, fixed) +
               (long long)first_cut.kvh * (p.n_tiles + fixed_of(p, g, fixed));
     }
-    const long long W = x_all - x_cut;
+    const long long W = tiles > 0 ? x_all - x_cut : 0;
     Place at{};
     long long left = 0;  // the CTA's tiles of the cut part
     if (c < G) {
-      const long long x0 = x_cut + c * W / G, x1 = x_cut + (c + 1) * W / G;
-      at = find_place(x0, blocks, A.Hkv, g, fixed);
-      const long long end = x1 < x_all ? find_place(x1, blocks, A.Hkv, g, fixed).before : all;
+      // where its share ends, then where it starts (one copy of the code: each line of it is fetched for the first time)
+      long long end = all;
+#pragma unroll 1
+      for (int k = 1; k >= 0; --k) {
+        const long long x = x_cut + quotient((c + k) * W, G);
+        if (x < x_all) at = find_place(x, blocks, A.Hkv, g, fixed);
+        if (k && x < x_all) end = at.before;
+      }
       left = end - at.before;
     }
     int whole = head.waves;  // whole items still to do
@@ -1235,13 +1248,13 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       if (lane == 0 && my_steps > 0) mbar_arrive(bOFree + 8 * st);
       if (it.partial) {
         // counted in once every thread's part is written; the CTA that counts the last merges
-        __threadfence();
+        // (the barrier orders the others' stores before this thread's release, and its acquire before their loads)
         bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
         if (tid == 0) {
-          const uint32_t old = atomicAdd(A.count + it.c0, 1u);
+          uint32_t old;
+          asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(A.count + it.c0) : "memory");
           misc[1] = old == (uint32_t)it.np - 1;
           if (misc[1]) A.count[it.c0] = 0u;
-          __threadfence();
         }
         bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
         if (misc[1]) {
