@@ -1358,7 +1358,7 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   a.piece = 64;
   if (block_table)
     while (page_size % a.piece) a.piece /= 2;
-  a.fixed = FixedCost{2, 2};
+  a.fixed = FixedCost{2, 1};
   a.o_wide = reinterpret_cast<uintptr_t>(O) % 32 == 0;
   const long long rows = block_table ? page_size : S_cap, planes = (long long)(block_table ? n_pages : B) * Hkv;
   if (!make_map(&a.K, Kc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||

@@ -167,8 +167,9 @@ def test_rows_that_see_nothing():
 
 @pytest.mark.parametrize("fill", [float("nan"), float("inf"), -3.0e38])
 @pytest.mark.parametrize("page", [0, 16, 128])
-def test_unwritten_cache_rows_take_no_part(fill, page):
-    check([1, 70, 3], [40, 130, 255], 8, 2, 128, page, fill=fill, extra=200)
+@pytest.mark.parametrize("opts", [dict(), dict(softcap=3.0), dict(slopes=torch.full((8,), 0.3))])
+def test_unwritten_cache_rows_take_no_part(fill, page, opts):
+    check([1, 70, 3], [40, 130, 255], 8, 2, 128, page, fill=fill, extra=200, **opts)
 
 
 def test_window_and_documents_leave_old_pages_unread():
@@ -193,6 +194,11 @@ def test_large_scores_raise_the_reference(q_scale):
     """Peaked rows: the running maximum rises by far more than 2^8 between tiles."""
     check([40, 1], [900, 1500], 8, 2, 64, 0, seed=21, q_scale=q_scale)
     check([150], [300], 4, 2, 128, 64, seed=22, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("softcap,q_scale", [(0.01, 1.0), (1.0, 30.0), (50.0, 8.0), (1000.0, 40.0)])
+def test_caps_far_below_and_above_the_scores(softcap, q_scale):
+    check([70, 1], [200, 600], 8, 2, 64, 0, seed=24, q_scale=q_scale, softcap=softcap)
 
 
 @pytest.mark.parametrize("n,kv", [([1], [40000]), ([2, 1], [9000, 20000]), ([600], [3000])])
@@ -236,13 +242,14 @@ def test_chunks_equal_the_whole_prompt():
             assert_close(O, lse, want[lo:lo + m], A[lo:lo + m], want_lse[lo:lo + m])
 
 
-def test_non_finite_inputs_stay_in_their_rows():
+@pytest.mark.parametrize("softcap", [0.0, 20.0])
+def test_non_finite_inputs_stay_in_their_rows(softcap):
     """A NaN query makes its own rows NaN and no others."""
     n, kv = [5, 130], [700, 0]
     Q, K, V, table, cu, kvl, keys, values = inputs(n, kv, 8, 2, 64, 0, 13)
-    want, A, want_lse = attend64(Q.double(), keys, values, n, kv, 0.125)
+    want, A, want_lse = attend64(Q.double(), keys, values, n, kv, 0.125, softcap=softcap)
     Q[2, 3, 5], Q[40, 0] = float("nan"), float("nan")
-    O, lse, status = run(Q, K, V, table, cu, kvl)
+    O, lse, status = run(Q, K, V, table, cu, kvl, softcap=softcap)
     bad = torch.zeros((135, 8), dtype=torch.bool)
     bad[2, 3] = bad[40, 0] = True
     assert bool(torch.isnan(O.cpu()[bad]).all()) and bool(torch.isnan(lse.cpu()[bad]).all())
