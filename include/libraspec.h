@@ -448,8 +448,8 @@ int libraspec_kv_append_paged(const uint16_t* kv_new, uint16_t* const* Kp, uint1
  * fit the cache LIBRASPEC_ST_KV_OVERFLOW.
  *
  * Rotary positions: frequencies. Pair i < rot_dim / 2 of a head turns by f_i
- * radians per position, f_i = theta^(-2 i / rot_dim), scaled for contexts longer than the model was
- * trained on:
+ * radians per position, f_i = theta^(-2 i / rot_dim), scaled for contexts
+ * longer than the model was trained on:
  *   LIBRASPEC_ROPE_LINEAR    f_i / factor (positions interpolated);
  *   LIBRASPEC_ROPE_NTK       theta factor^(rot_dim / (rot_dim - 2)) in place of theta (rot_dim > 2);
  *   LIBRASPEC_ROPE_BY_PARTS  (1 - k_i) f_i / factor + k_i f_i, where k_i is
@@ -558,10 +558,12 @@ int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const 
  * head_dim in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 128; page_size a multiple
  * of 16 (else LIBRASPEC_EUNSUPPORTED). Scores, sums and O accumulate in
  * binary32; probabilities enter the second product as bf16. Results do not
- * change from run to run. Two launches (a plan from the device's lengths, the
- * attention); workspace: libraspec_chunk_workspace_size(T, B, Hq, Hkv,
- * head_dim) bytes, 256-byte aligned, zero-filled once, of at least the call's
- * T, B and heads; calls sharing it must not overlap. If a wait inside the
+ * change from run to run. One launch, or two (a plan from the device's lengths
+ * before the attention) where T, B allow more than 64 blocks of 2 floor(128 /
+ * g) tokens, with B > 512 or with first_key. workspace:
+ * libraspec_chunk_workspace_size(T, B, Hq, Hkv, head_dim) bytes, 256-byte
+ * aligned, zero-filled once, of at least the call's T, B and heads; calls
+ * sharing it must not overlap. If a wait inside the
  * kernel gives up (LIBRASPEC_ST_TIMEOUT), re-initialise it before its next use.
  */
 typedef struct libraspec_score_opts {

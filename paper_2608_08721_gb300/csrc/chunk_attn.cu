@@ -17,8 +17,9 @@
 // persistent grid (one CTA per SM) by cost: each block weighs its tiles plus C
 // tile-equivalents (its queries' load and its epilogue), and CTA c takes the
 // tiles of the c-th share of the weight, so that CTAs finish together whatever
-// the lengths. A plan kernel lists the blocks and their key tiles from the
-// device-resident lengths; a launch dependent on it does the work.
+// the lengths. The blocks and their key tiles follow from the device-resident
+// lengths: a plan kernel lists them, and a launch dependent on it does the
+// work; up to 64 blocks each CTA's producer lists for itself.
 //
 // Two streams per CTA, each a softmax warpgroup with its own scores and O
 // accumulator in tensor memory, so that one stream's MMAs run beside the
@@ -37,6 +38,15 @@
 // are of the unrounded values, in 32 bits). The reference maximum of a row is
 // raised only when a score exceeds it by more than 8 (a factor of 2^8), so O
 // is rarely rescaled; p <= 2^8 keeps P and O in range.
+//
+// What bounds it, with 128-wide heads: prompts, the chain of a stream's steps
+// (scores, softmax, P V) and the shared memory that S = Q K^T reads, 128 bytes
+// a cycle: 16384 tokens of 8 heads over as many keys run at 1.57 PFLOP/s,
+// where a matrix product reaches 1.92; an item's start and end cost as much as
+// two or three tiles, which is why short prompts stay further off. Decode
+// steps, the cache's bytes: 64 sequences over 512 to 32768 keys run at the
+// copy rate. One sequence over 512 keys: 10.4 us of first instruction fetches
+// and of round trips (plan, K, S, softmax, V, merge), hardly of bytes.
 //
 // Keys that no row of a block sees take no part: K and V pieces that hold none
 // of them are not read (their pages need not exist), and V rows beyond the
@@ -191,35 +201,49 @@ __device__ __forceinline__ int block_room(const PlanArgs& a) {
   return (int)min((long long)a.T, (long long)a.T / a.TB + a.B);
 }
 
-// Block of tokens [j0, j0 + TB) of sequence b, whose n tokens start at row c0 and position kv.
-__device__ __forceinline__ PlanBlock make_block(const PlanArgs& a, int b, int c0, int n, int kv, int j0) {
-  const int j1 = min(n, j0 + a.TB), N = kv + n;
-  const int prefix = a.mask.prefix_len ? a.mask.prefix_len[b] : 0;
+// Keys that some row of tokens [j0, j1) of a sequence sees lie in [klo, khi). Its n tokens start at row c0 and position
+// kv.
+struct KeyRange {
+  int lo, hi;
+};
+// without first keys: ranges move forward with the position
+__device__ __forceinline__ KeyRange key_range(const PlanArgs& a, int b, int n, int kv, int j0) {
+  const int j1 = min(n, j0 + a.TB), N = kv + n, prefix = a.mask.prefix_len ? a.mask.prefix_len[b] : 0;
+  KeyRange k;
+  int l, h;
+  row_range(kv + j0, N, prefix, 0, a.mask.window, k.lo, h);
+  row_range(kv + j1 - 1, N, prefix, 0, a.mask.window, l, k.hi);
+  return k;
+}
+// with them, by a warp (a thread for each block, one key after the other: XXX)
+__device__ __forceinline__ KeyRange key_range_docs(const PlanArgs& a, int b, int c0, int n, int kv, int j0) {
+  const int j1 = min(n, j0 + a.TB), N = kv + n, prefix = a.mask.prefix_len ? a.mask.prefix_len[b] : 0;
   int klo = 0x7fffffff, khi = 0;
-  if (!a.mask.first_key) {  // ranges move forward with the position
+  for (int j = j0 + (threadIdx.x & 31); j < j1; j += 32) {
     int l, h;
-    row_range(kv + j0, N, prefix, 0, a.mask.window, klo, h);
-    row_range(kv + j1 - 1, N, prefix, 0, a.mask.window, l, khi);
-  } else {
-    for (int j = j0; j < j1; ++j) {
-      int l, h;
-      row_range(kv + j, N, prefix, a.mask.first_key[c0 + j], a.mask.window, l, h);
-      if (l < h) {
-        klo = min(klo, l);
-        khi = max(khi, h);
-      }
+    row_range(kv + j, N, prefix, a.mask.first_key[c0 + j], a.mask.window, l, h);
+    if (l < h) {
+      klo = min(klo, l);
+      khi = max(khi, h);
     }
-    if (klo >= khi) klo = khi = N - 1;  // no row sees anything: one tile, of which nothing is read
   }
+  klo = __reduce_min_sync(0xffffffffu, klo);
+  khi = __reduce_max_sync(0xffffffffu, khi);
+  if (klo >= khi) klo = khi = N - 1;  // no row sees anything: one tile, of which nothing is read
+  return KeyRange{klo, khi};
+}
+
+// Block of tokens [j0, j0 + TB) of sequence b.
+__device__ __forceinline__ PlanBlock make_block(const PlanArgs& a, int b, int c0, int n, int kv, int j0, KeyRange k) {
   PlanBlock p{};
   p.b = b;
   p.tok0 = c0 + j0;
-  p.n_tok = j1 - j0;
+  p.n_tok = min(n - j0, a.TB);
   p.pos0 = kv + j0;
-  p.klo = klo;
-  p.khi = khi;
-  p.tile0 = klo / kCKeys;
-  p.n_tiles = max(1, (khi + kCKeys - 1) / kCKeys - p.tile0);
+  p.klo = k.lo;
+  p.khi = k.hi;
+  p.tile0 = k.lo / kCKeys;
+  p.n_tiles = max(1, (k.hi + kCKeys - 1) / kCKeys - p.tile0);
   return p;
 }
 
@@ -237,6 +261,7 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const PlanArgs
   __shared__ int first_block[LIBRASPEC_MAX_B + 1];  // of each sequence
   __shared__ int warp_i[32];
   __shared__ long long warp_l[32];
+  __shared__ KeyRange ranges[kPlanThreads];  // (first keys)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x;
   int carry = 0;
@@ -265,21 +290,33 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const PlanArgs
   __syncthreads();
   const int room = block_room(a), n_blocks = min(carry, room);
   if (carry > room && tid == 0) raise_status(a.status, LIBRASPEC_ST_BAD_LENGTH);
+  auto seq_of = [&](int e) {  // the last b with first_block[b] <= e (it has blocks: e < first_block[b + 1])
+    int lo = 0, hi = a.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first_block[mid] <= e) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  };
   long long tiles = 0;
   int pairs = 0, t_min = 0x7fffffff, t_max = 0;
   for (int e0 = 0; e0 < n_blocks; e0 += kPlanThreads) {
     const int e = e0 + tid;
     PlanBlock p{};
-    if (e < n_blocks) {
-      int lo = 0, hi = a.B;  // the last b with first_block[b] <= e (it has blocks: e < first_block[b + 1])
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (first_block[mid] <= e) lo = mid;
-        else hi = mid;
+    if (a.mask.first_key) {
+      for (int i = tid >> 5; i < kPlanThreads && e0 + i < n_blocks; i += kPlanThreads / 32) {
+        int c0, kv;
+        const int b = seq_of(e0 + i), n = new_tokens(a, b, false, c0, kv);
+        const KeyRange k = key_range_docs(a, b, c0, n, kv, (e0 + i - first_block[b]) * a.TB);
+        if ((tid & 31) == 0) ranges[i] = k;
       }
+      __syncthreads();
+    }
+    if (e < n_blocks) {
       int c0, kv;
-      const int n = new_tokens(a, lo, false, c0, kv);
-      p = make_block(a, lo, c0, n, kv, (e - first_block[lo]) * a.TB);
+      const int b = seq_of(e), n = new_tokens(a, b, false, c0, kv), j0 = (e - first_block[b]) * a.TB;
+      p = make_block(a, b, c0, n, kv, j0, a.mask.first_key ? ranges[tid] : key_range(a, b, n, kv, j0));
     }
     long long total;
     const long long inc = block_scan((long long)p.n_tiles, warp_l, total);
@@ -350,8 +387,10 @@ __device__ PlanHead warp_plan(const PlanArgs& a, PlanBlock (&mine)[2]) {
       s = min(s, 31);
       const int sc = __shfl_sync(0xffffffffu, c0, s), sn = __shfl_sync(0xffffffffu, n, s);
       const int skv = __shfl_sync(0xffffffffu, kv, s), before = __shfl_sync(0xffffffffu, inc - nb, s);
-      if (e >= 0 && e < total && lane + 32 * k < room)
-        mine[k] = make_block(a, b0 + s, sc, sn, skv, (e - before) * a.TB);
+      if (e >= 0 && e < total && lane + 32 * k < room) {
+        const int j0 = (e - before) * a.TB;
+        mine[k] = make_block(a, b0 + s, sc, sn, skv, j0, key_range(a, b0 + s, sn, skv, j0));
+      }
     }
     carry += total;
   }
@@ -383,7 +422,8 @@ __device__ PlanHead warp_plan(const PlanArgs& a, PlanBlock (&mine)[2]) {
 // ---------------------------------------------------------------------------
 // The attention kernel.
 // ---------------------------------------------------------------------------
-// What a block weighs beside its tiles, in tiles: `one` for every block, `pair` more for two row tiles.
+// What a block weighs beside its tiles, in tiles: `one` for every block, `pair` more for two row tiles. (A prompt
+// of 8192 tokens of 32 heads: 419 us at 2 and 2 + 0, 397 at 2 + 1, 399 at 2 + 2, 413 at 2 + 5; decoding is best at 2.)
 struct FixedCost {
   int one, pair;
 };
@@ -405,7 +445,7 @@ struct ChunkArgs {
   uint32_t* count;
   int* status;
   float scale, softcap;
-  int B, Hq, Hkv, max_pages, page_size, n_pages, piece;  // piece: keys of one TMA box
+  int Hq, Hkv, max_pages, page_size, n_pages, piece;  // piece: keys of one TMA box
   FixedCost fixed;
   int o_wide;  // O is aligned to 32 bytes
 };
@@ -611,7 +651,8 @@ __device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem&
           if (p < np) {
             const size_t slot = p == 0 ? 2 * c0 + 1 : 2 * (c0 + p);
             ml[u][q] = __ldcg(reinterpret_cast<const float2*>(A.part_ml) + slot * kCBlockRows + r[u]);
-            const float4* o = reinterpret_cast<const float4*>(A.part_o) + (slot * (D / 4) + 2 * c[u]) * kCBlockRows + r[u];
+            const float4* o =
+                reinterpret_cast<const float4*>(A.part_o) + (slot * (D / 4) + 2 * c[u]) * kCBlockRows + r[u];
             v[u][q][0] = __ldcg(o);
             v[u][q][1] = __ldcg(o + kCBlockRows);
           }
@@ -719,258 +760,259 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
   if (misaligned) {
     if (tid == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
   } else if (warp >= kCSoftmaxWarps) {
-   regs_leave<kCOtherRegs>();
-   if (warp == kCProducerWarp) {
-    // ======================= producer =======================
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    PlanBlock mine[2];
-    const PlanHead head = A.blocks ? *A.head : warp_plan(A.plan, mine);
-    const Blocks blocks{A.blocks, mine, head.blocks};
-    const int c = blockIdx.x;
-    // the whole items first, in step; the rest is cut by cost from tile `done` on, weighted position x_done
-    const long long all = (long long)A.Hkv * head.tiles;
-    const int n_whole = head.waves * (int)gridDim.x;
-    FixedCost fixed = A.fixed;
-    auto place_of_item = [&](int id) {
-      Place p;
-      p.e = id / A.Hkv;
-      p.kvh = id - p.e * A.Hkv;
-      p.tile = 0;
-      p.before = all;
-      if (p.e < head.blocks) {
-        const PlanBlock b = blocks.at(p.e);
-        p.before = (long long)A.Hkv * b.tiles_before + (long long)p.kvh * b.n_tiles;
-      }
-      return p;
-    };
-    Place first_cut{};
-    if (n_whole) first_cut = place_of_item(n_whole);
-    const long long tiles = all - first_cut.before;  // to be cut
-    int G = (int)gridDim.x;
-    if (tiles < G) G = (int)tiles;
-    if (tiles > 0) {  // (a CTA with few tiles would get none if a block's fixed cost were several)
-      const int most = (int)min(1ll << 20, quotient(tiles, 4 * (long long)G));
-      fixed.one = min(fixed.one, most);
-      fixed.pair = min(fixed.pair, most - fixed.one);
-    }
-    const long long x_all = (long long)A.Hkv * (head.tiles + (long long)fixed.one * head.blocks +
-                                                (long long)fixed.pair * head.pairs);
-    long long x_cut = 0;
-    if (n_whole && first_cut.e < head.blocks) {
-      const PlanBlock p = blocks.at(first_cut.e);
-      x_cut = (long long)A.Hkv * weight_before(p, first_cut.e, fixed) +
-              (long long)first_cut.kvh * (p.n_tiles + fixed_of(p, g, fixed));
-    }
-    const long long W = tiles > 0 ? x_all - x_cut : 0;
-    Place at{};
-    long long left = 0;  // the CTA's tiles of the cut part
-    if (c < G) {
-      // where its share ends, then where it starts (one copy of the code: each line of it is fetched for the first time)
-      long long end = all;
-#pragma unroll 1
-      for (int k = 1; k >= 0; --k) {
-        const long long x = x_cut + quotient((c + k) * W, G);
-        if (x < x_all) at = find_place(x, blocks, A.Hkv, g, fixed);
-        if (k && x < x_all) end = at.before;
-      }
-      left = end - at.before;
-    }
-    int whole = head.waves;  // whole items still to do
-    if (whole == 0 && left <= 0 && lane == 0) {
-      info[0].last = 2;
-      mbar_arrive(bIFull);
-    }
-    // a lane's piece of a K or V tile: keys [row, row + piece) of the tile, columns [64 hb, 64 hb + 64)
-    const int per_tile = kCKeys / A.piece;
-    const int my_row = (lane % per_tile) * A.piece, my_hb = lane / per_tile;
-    const bool has_piece = my_hb < SM::kBoxes;
-    uint32_t item_ctr = 0, chunk_ctr = 0;
-    const uint64_t once = evict_first_policy(), again = evict_normal_policy();
-    bool ok = true;
-    while ((whole > 0 || left > 0) && ok) {
-      const bool cut = whole == 0;
-      const Place pl = cut ? at : place_of_item((head.waves - whole) * (int)gridDim.x + c);
-      const PlanBlock p = blocks.at(pl.e);
-      ChunkItem it{};
-      it.b = p.b;
-      it.kvh = pl.kvh;
-      it.tok0 = p.tok0;
-      it.pos0 = p.pos0;
-      it.rows = p.n_tok * g;
-      it.pair = p.n_tok > Rt;
-      it.tile0 = p.tile0 + pl.tile;
-      it.n_tiles = cut ? (int)min((long long)(p.n_tiles - pl.tile), left) : p.n_tiles;
-      it.klo = p.klo;
-      it.khi = p.khi;
-      it.partial = it.n_tiles != p.n_tiles;
-      it.slot = pl.tile == 0 ? 2 * c + 1 : 2 * c;
-      it.c0 = c;
-      it.np = 1;
-      if (it.partial) {
-        const int fc = fixed_of(p, g, fixed);
-        const long long y = (long long)A.Hkv * weight_before(p, pl.e, fixed) + (long long)pl.kvh * (p.n_tiles + fc) + fc -
-                            x_cut;  // of the block's first tile, from the cut part's start
-        it.c0 = share_of(y, W, G);
-        it.np = share_of(y + p.n_tiles - 1, W, G) - it.c0 + 1;
-      }
-      if (cut) left -= it.n_tiles;
-      else --whole;
-      it.last = whole == 0 && left <= 0;
-      const int n = it.n_tiles, lag = it.pair ? 1 : 2;
-      // keys of a sequence that has one block are read once per kv head
-      const int n_new = A.cu_new[p.b + 1] - A.cu_new[p.b];
-      const uint64_t policy = n_new <= 2 * Rt ? once : again;
-      // pages of the item's tiles, four tiles at a time: lane 8 k + i holds that of piece i of the k-th
-      auto load_pages = [&](int group) {
-        if (!A.block_table) return p.b;
-        const int tile = 4 * group + lane / 8, i = lane % 8;
-        const int key = (it.tile0 + tile) * kCKeys + i * A.piece;
-        if (tile >= n || i >= per_tile || key >= p.khi || key + A.piece <= p.klo) return 0;
-        return __ldg(A.block_table + (size_t)p.b * A.max_pages + key / A.page_size);
+    regs_leave<kCOtherRegs>();
+    if (warp == kCProducerWarp) {
+      // ======================= producer =======================
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      PlanBlock mine[2];
+      const PlanHead head = A.blocks ? *A.head : warp_plan(A.plan, mine);
+      const Blocks blocks{A.blocks, mine, head.blocks};
+      const int c = blockIdx.x;
+      // the whole items first, in step; the items from n_whole on are cut by cost
+      const long long all = (long long)A.Hkv * head.tiles;
+      const int n_whole = head.waves * (int)gridDim.x;
+      FixedCost fixed = A.fixed;
+      auto place_of_item = [&](int id) {
+        Place p;
+        p.e = id / A.Hkv;
+        p.kvh = id - p.e * A.Hkv;
+        p.tile = 0;
+        p.before = all;
+        if (p.e < head.blocks) {
+          const PlanBlock b = blocks.at(p.e);
+          p.before = (long long)A.Hkv * b.tiles_before + (long long)p.kvh * b.n_tiles;
+        }
+        return p;
       };
-      int pages_before = 0, pages = load_pages(0), pages_next = load_pages(1);
-      // the item's queries, once the item before has issued its last S
-      ok = warp_wait(bIEmpty + 8 * (item_ctr & 1), ((item_ctr >> 1) & 1) ^ 1) &&
-           warp_wait(bQEmpty, (item_ctr & 1) ^ 1);
-      if (!ok) break;
-      if (lane == 0) {
-        info[item_ctr & 1] = it;
-        mbar_arrive(bIFull + 8 * (item_ctr & 1));
-        mbar_expect_tx(bQFull, (it.pair ? 2 : 1) * R * D * 2);
-        for (int s = 0; s <= it.pair; ++s)
-          for (int hb = 0; hb < SM::kBoxes; ++hb)
-            tma_load_3d(sQ + s * SM::kTile + hb * 16384, &A.Q, bQFull, hb * 64, it.kvh * g, it.tok0 + s * Rt);
+      Place first_cut{};
+      if (n_whole) first_cut = place_of_item(n_whole);
+      const long long tiles = all - first_cut.before;  // to be cut
+      int G = (int)gridDim.x;
+      if (tiles < G) G = (int)tiles;
+      if (tiles > 0) {  // (a CTA with few tiles would get none if a block's fixed cost were several)
+        const int most = (int)min(1ll << 20, quotient(tiles, 4 * (long long)G));
+        fixed.one = min(fixed.one, most);
+        fixed.pair = min(fixed.pair, most - fixed.one);
       }
-      __syncwarp();
-      // chunks in the order in which the MMA warp uses them: K of tile t, then V of tile t - lag + 1
-      for (int kt = 0, vt = 0; vt < n && ok;) {
-        const bool is_k = kt < n && kt < vt + lag;
-        const int t = is_k ? kt++ : vt++;
-        const uint32_t ch = chunk_ctr % SM::kChunks;
-        ok = warp_wait(bEmpty + 8 * ch, ((chunk_ctr / SM::kChunks) & 1) ^ 1);
+      const long long x_all = (long long)A.Hkv * (head.tiles + (long long)fixed.one * head.blocks +
+                                                  (long long)fixed.pair * head.pairs);
+      long long x_cut = 0;
+      if (n_whole && first_cut.e < head.blocks) {
+        const PlanBlock p = blocks.at(first_cut.e);
+        x_cut = (long long)A.Hkv * weight_before(p, first_cut.e, fixed) +
+                (long long)first_cut.kvh * (p.n_tiles + fixed_of(p, g, fixed));
+      }
+      const long long W = tiles > 0 ? x_all - x_cut : 0;
+      Place at{};
+      long long left = 0;  // the CTA's tiles of the cut part
+      if (c < G) {
+        // where its share ends, then where it starts (one copy of the code: each line of it is a first fetch)
+        long long end = all;
+#pragma unroll 1
+        for (int k = 1; k >= 0; --k) {
+          const long long x = x_cut + quotient((c + k) * W, G);
+          if (x < x_all) at = find_place(x, blocks, A.Hkv, g, fixed);
+          if (k && x < x_all) end = at.before;
+        }
+        left = end - at.before;
+      }
+      int whole = head.waves;  // whole items still to do
+      if (whole == 0 && left <= 0 && lane == 0) {
+        info[0].last = 2;
+        mbar_arrive(bIFull);
+      }
+      // a lane's piece of a K or V tile: keys [row, row + piece) of the tile, columns [64 hb, 64 hb + 64)
+      const int per_tile = kCKeys / A.piece;
+      const int my_row = (lane % per_tile) * A.piece, my_hb = lane / per_tile;
+      const bool has_piece = my_hb < SM::kBoxes;
+      uint32_t item_ctr = 0, chunk_ctr = 0;
+      const uint64_t once = evict_first_policy(), again = evict_normal_policy();
+      bool ok = true;
+      while ((whole > 0 || left > 0) && ok) {
+        const bool cut = whole == 0;
+        const Place pl = cut ? at : place_of_item((head.waves - whole) * (int)gridDim.x + c);
+        const PlanBlock p = blocks.at(pl.e);
+        ChunkItem it{};
+        it.b = p.b;
+        it.kvh = pl.kvh;
+        it.tok0 = p.tok0;
+        it.pos0 = p.pos0;
+        it.rows = p.n_tok * g;
+        it.pair = p.n_tok > Rt;
+        it.tile0 = p.tile0 + pl.tile;
+        it.n_tiles = cut ? (int)min((long long)(p.n_tiles - pl.tile), left) : p.n_tiles;
+        it.klo = p.klo;
+        it.khi = p.khi;
+        it.partial = it.n_tiles != p.n_tiles;
+        it.slot = pl.tile == 0 ? 2 * c + 1 : 2 * c;
+        it.c0 = c;
+        it.np = 1;
+        if (it.partial) {
+          const int fc = fixed_of(p, g, fixed);
+          // of the block's first tile, from the cut part's start
+          const long long y = (long long)A.Hkv * weight_before(p, pl.e, fixed) +
+                              (long long)pl.kvh * (p.n_tiles + fc) + fc - x_cut;
+          it.c0 = share_of(y, W, G);
+          it.np = share_of(y + p.n_tiles - 1, W, G) - it.c0 + 1;
+        }
+        if (cut) left -= it.n_tiles;
+        else --whole;
+        it.last = whole == 0 && left <= 0;
+        const int n = it.n_tiles, lag = it.pair ? 1 : 2;
+        // keys of a sequence that has one block are read once per kv head
+        const int n_new = A.cu_new[p.b + 1] - A.cu_new[p.b];
+        const uint64_t policy = n_new <= 2 * Rt ? once : again;
+        // pages of the item's tiles, four tiles at a time: lane 8 k + i holds that of piece i of the k-th
+        auto load_pages = [&](int group) {
+          if (!A.block_table) return p.b;
+          const int tile = 4 * group + lane / 8, i = lane % 8;
+          const int key = (it.tile0 + tile) * kCKeys + i * A.piece;
+          if (tile >= n || i >= per_tile || key >= p.khi || key + A.piece <= p.klo) return 0;
+          return __ldg(A.block_table + (size_t)p.b * A.max_pages + key / A.page_size);
+        };
+        int pages_before = 0, pages = load_pages(0), pages_next = load_pages(1);
+        // the item's queries, once the item before has issued its last S
+        ok = warp_wait(bIEmpty + 8 * (item_ctr & 1), ((item_ctr >> 1) & 1) ^ 1) &&
+             warp_wait(bQEmpty, (item_ctr & 1) ^ 1);
         if (!ok) break;
-        if (is_k && t > 0 && (t & 3) == 0) {
-          pages_before = pages;
-          pages = pages_next;
-          pages_next = load_pages((t >> 2) + 1);
+        if (lane == 0) {
+          info[item_ctr & 1] = it;
+          mbar_arrive(bIFull + 8 * (item_ctr & 1));
+          mbar_expect_tx(bQFull, (it.pair ? 2 : 1) * R * D * 2);
+          for (int s = 0; s <= it.pair; ++s)
+            for (int hb = 0; hb < SM::kBoxes; ++hb)
+              tma_load_3d(sQ + s * SM::kTile + hb * 16384, &A.Q, bQFull, hb * 64, it.kvh * g, it.tok0 + s * Rt);
         }
-        const int from = t >> 2 == (kt - 1) >> 2 ? pages : pages_before;  // kt - 1: the last K tile
-        int page = __shfl_sync(0xffffffffu, from, (t & 3) * 8 + lane % per_tile);
-        const int key = (it.tile0 + t) * kCKeys + my_row;
-        const bool load = has_piece && key < p.khi && key + A.piece > p.klo;
-        if (A.block_table && load && (page < 0 || page >= A.n_pages)) {
-          raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
-          page = 0;  // a valid page; the sequence's output is then meaningless
-        }
-        const uint32_t bar = bFull + 8 * ch;
-        const int pieces = __popc(__ballot_sync(0xffffffffu, load));
-        if (lane == 0) mbar_expect_tx(bar, pieces * A.piece * 128);
         __syncwarp();
-        if (load) {
-          const int z = page * A.Hkv + it.kvh, y = A.block_table ? key % A.page_size : key;
-          tma_load_3d_hint(sRing + ch * SM::kTile + my_hb * 16384 + my_row * 128, is_k ? &A.K : &A.V, bar, my_hb * 64,
-                           y, z, policy);
-        }
-        ++chunk_ctr;
-      }
-      ++item_ctr;
-      if (cut) {  // the next item: the next kv head, or the next block
-        at.tile = 0;
-        if (++at.kvh == A.Hkv) {
-          at.kvh = 0;
-          ++at.e;
-        }
-      }
-    }
-    if (!ok) {
-      if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-      misc[0] = 1;
-    }
-    // before leaving, wait (bounded) for the copies still in flight
-    if (lane == 0) {
-      for (uint32_t k = 0; k < (uint32_t)SM::kChunks && k < chunk_ctr; ++k) {
-        const uint32_t i = chunk_ctr - 1 - k;
-        mbar_wait(bFull + 8 * (i % SM::kChunks), (i / SM::kChunks) & 1);
-      }
-      if (item_ctr > 0) mbar_wait(bQFull, (item_ctr - 1) & 1);
-    }
-    __syncwarp();
-  } else if (warp == kCMmaWarp) {
-    // ======================= MMA issue =======================
-    // The whole warp walks the steps, one elected lane issues.
-    uint32_t item_ctr = 0, chunk_ctr = 0;
-    uint32_t p_ctr = 0;  // bit s: parity of the next P of stream s
-    uint32_t o_ctr = 3;  // bit s: parity of stream s's accumulator being free
-    bool ok = true;
-    auto take = [&]() {  // the next chunk, once it is filled
-      const uint32_t ch = chunk_ctr % SM::kChunks;
-      ok = ok && warp_wait(bFull + 8 * ch, (chunk_ctr / SM::kChunks) & 1);
-      ++chunk_ctr;
-      return ch;
-    };
-    for (int last = 0; !last && ok; ++item_ctr) {
-      ok = warp_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
-      if (!ok) break;
-      const int n_tiles = __shfl_sync(0xffffffffu, info[item_ctr & 1].n_tiles, 0);
-      const bool pair = __shfl_sync(0xffffffffu, info[item_ctr & 1].pair, 0);
-      last = __shfl_sync(0xffffffffu, info[item_ctr & 1].last, 0);
-      if (last == 2) break;
-      if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
-      __syncwarp();
-      // Step n belongs to stream n & 1: tile n / 2 of the stream's own rows (a pair), or tile n of the same rows.
-      // S of a step goes where P of the stream's step before lies, so that one's PV is issued first.
-      const int steps = pair ? 2 * n_tiles : n_tiles;
-      uint32_t kch = 0, vch = 0;
-      for (int n = 0; n < steps + 2 && ok; ++n) {
-        const int s = n & 1;
-        const uint32_t ts = tmem + SM::kColS + s * 128;
-        if (n >= 2) {  // O += P V of step n - 2
-          if (!pair || s == 0) vch = take();
-          if (n < 4) {
-            ok = ok && warp_wait(bOFree + 8 * s, (o_ctr >> s) & 1);
-            o_ctr ^= 1u << s;
+        // chunks in the order in which the MMA warp uses them: K of tile t, then V of tile t - lag + 1
+        for (int kt = 0, vt = 0; vt < n && ok;) {
+          const bool is_k = kt < n && kt < vt + lag;
+          const int t = is_k ? kt++ : vt++;
+          const uint32_t ch = chunk_ctr % SM::kChunks;
+          ok = warp_wait(bEmpty + 8 * ch, ((chunk_ctr / SM::kChunks) & 1) ^ 1);
+          if (!ok) break;
+          if (is_k && t > 0 && (t & 3) == 0) {
+            pages_before = pages;
+            pages = pages_next;
+            pages_next = load_pages((t >> 2) + 1);
           }
-          constexpr uint32_t idesc = mma_idesc(128, D, 1);
-          const uint32_t va = desc_lo(sRing + vch * SM::kTile, 16384);
-          const uint32_t d = tmem + SM::kColO + s * 128;
-          const uint32_t par = (p_ctr >> s) & 1;
-          p_ctr ^= 1u << s;
-          ok = ok && warp_wait(bPFull + 16 * s, par);
-          if (!ok) break;
-          tc_fence_after();
-          mma_ts4_warp<2048>(d, ts, va, idesc, n < 4 ? 0u : 1u);
-          ok = warp_wait(bPFull + 16 * s + 8, par);
-          if (!ok) break;
-          tc_fence_after();
-          mma_ts4_warp<2048>(d, ts + 32, va + 512, idesc, 1u);
-          mma_commit_warp(bPVDone + 8 * s);
-          if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * vch);
+          const int from = t >> 2 == (kt - 1) >> 2 ? pages : pages_before;  // kt - 1: the last K tile
+          int page = __shfl_sync(0xffffffffu, from, (t & 3) * 8 + lane % per_tile);
+          const int key = (it.tile0 + t) * kCKeys + my_row;
+          const bool load = has_piece && key < p.khi && key + A.piece > p.klo;
+          if (A.block_table && load && (page < 0 || page >= A.n_pages)) {
+            raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
+            page = 0;  // a valid page; the sequence's output is then meaningless
+          }
+          const uint32_t bar = bFull + 8 * ch;
+          const int pieces = __popc(__ballot_sync(0xffffffffu, load));
+          if (lane == 0) mbar_expect_tx(bar, pieces * A.piece * 128);
+          __syncwarp();
+          if (load) {
+            const int z = page * A.Hkv + it.kvh, y = A.block_table ? key % A.page_size : key;
+            tma_load_3d_hint(sRing + ch * SM::kTile + my_hb * 16384 + my_row * 128, is_k ? &A.K : &A.V, bar, my_hb * 64,
+                             y, z, policy);
+          }
+          ++chunk_ctr;
         }
-        if (n < steps) {  // S = Q K^T of step n
-          if (!pair || s == 0) kch = take();
-          if (n == 0) ok = ok && warp_wait(bQFull, item_ctr & 1);
-          if (!ok) break;
-          tc_fence_after();
-          constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
-          const uint32_t qa = desc_lo(sQ + (pair ? s : 0) * SM::kTile, 16);
-          const uint32_t ka = desc_lo(sRing + kch * SM::kTile, 16);
-#pragma unroll
-          for (int hb = 0; hb < SM::kBoxes; ++hb)
-            mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
-          mma_commit_warp(bSFull + 8 * s);
-          if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * kch);
-          if (n == steps - 1) mma_commit_warp(bQEmpty);
+        ++item_ctr;
+        if (cut) {  // the next item: the next kv head, or the next block
+          at.tile = 0;
+          if (++at.kvh == A.Hkv) {
+            at.kvh = 0;
+            ++at.e;
+          }
         }
       }
+      if (!ok) {
+        if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+        misc[0] = 1;
+      }
+      // before leaving, wait (bounded) for the copies still in flight
+      if (lane == 0) {
+        for (uint32_t k = 0; k < (uint32_t)SM::kChunks && k < chunk_ctr; ++k) {
+          const uint32_t i = chunk_ctr - 1 - k;
+          mbar_wait(bFull + 8 * (i % SM::kChunks), (i / SM::kChunks) & 1);
+        }
+        if (item_ctr > 0) mbar_wait(bQFull, (item_ctr - 1) & 1);
+      }
+      __syncwarp();
+    } else if (warp == kCMmaWarp) {
+      // ======================= MMA issue =======================
+      // The whole warp walks the steps, one elected lane issues.
+      uint32_t item_ctr = 0, chunk_ctr = 0;
+      uint32_t p_ctr = 0;  // bit s: parity of the next P of stream s
+      uint32_t o_ctr = 3;  // bit s: parity of stream s's accumulator being free
+      bool ok = true;
+      auto take = [&]() {  // the next chunk, once it is filled
+        const uint32_t ch = chunk_ctr % SM::kChunks;
+        ok = ok && warp_wait(bFull + 8 * ch, (chunk_ctr / SM::kChunks) & 1);
+        ++chunk_ctr;
+        return ch;
+      };
+      for (int last = 0; !last && ok; ++item_ctr) {
+        ok = warp_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
+        if (!ok) break;
+        const int n_tiles = __shfl_sync(0xffffffffu, info[item_ctr & 1].n_tiles, 0);
+        const bool pair = __shfl_sync(0xffffffffu, info[item_ctr & 1].pair, 0);
+        last = __shfl_sync(0xffffffffu, info[item_ctr & 1].last, 0);
+        if (last == 2) break;
+        if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
+        __syncwarp();
+        // Step n belongs to stream n & 1: tile n / 2 of the stream's own rows (a pair), or tile n of the same rows.
+        // S of a step goes where P of the stream's step before lies, so that one's PV is issued first.
+        const int steps = pair ? 2 * n_tiles : n_tiles;
+        uint32_t kch = 0, vch = 0;
+        for (int n = 0; n < steps + 2 && ok; ++n) {
+          const int s = n & 1;
+          const uint32_t ts = tmem + SM::kColS + s * 128;
+          if (n >= 2) {  // O += P V of step n - 2
+            if (!pair || s == 0) vch = take();
+            if (n < 4) {
+              ok = ok && warp_wait(bOFree + 8 * s, (o_ctr >> s) & 1);
+              o_ctr ^= 1u << s;
+            }
+            constexpr uint32_t idesc = mma_idesc(128, D, 1);
+            const uint32_t va = desc_lo(sRing + vch * SM::kTile, 16384);
+            const uint32_t d = tmem + SM::kColO + s * 128;
+            const uint32_t par = (p_ctr >> s) & 1;
+            p_ctr ^= 1u << s;
+            ok = ok && warp_wait(bPFull + 16 * s, par);
+            if (!ok) break;
+            tc_fence_after();
+            mma_ts4_warp<2048>(d, ts, va, idesc, n < 4 ? 0u : 1u);
+            ok = warp_wait(bPFull + 16 * s + 8, par);
+            if (!ok) break;
+            tc_fence_after();
+            mma_ts4_warp<2048>(d, ts + 32, va + 512, idesc, 1u);
+            mma_commit_warp(bPVDone + 8 * s);
+            if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * vch);
+          }
+          if (n < steps) {  // S = Q K^T of step n
+            if (!pair || s == 0) kch = take();
+            if (n == 0) ok = ok && warp_wait(bQFull, item_ctr & 1);
+            if (!ok) break;
+            tc_fence_after();
+            constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
+            const uint32_t qa = desc_lo(sQ + (pair ? s : 0) * SM::kTile, 16);
+            const uint32_t ka = desc_lo(sRing + kch * SM::kTile, 16);
+#pragma unroll
+            for (int hb = 0; hb < SM::kBoxes; ++hb)
+              mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
+            mma_commit_warp(bSFull + 8 * s);
+            if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * kch);
+            if (n == steps - 1) mma_commit_warp(bQEmpty);
+          }
+        }
+      }
+      if (!ok) {
+        if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
+        misc[0] = 1;
+      }
+      // every MMA issued has completed before the tensor memory is released
+      mma_commit_warp(bDrain);
+      warp_wait(bDrain, 0);
     }
-    if (!ok) {
-      if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-      misc[0] = 1;
-    }
-    // every MMA issued has completed before the tensor memory is released
-    mma_commit_warp(bDrain);
-    warp_wait(bDrain, 0);
-   }
   } else {
     regs_take<kCSoftmaxRegs>();
     // ======================= softmax warpgroups =======================
@@ -1306,7 +1348,8 @@ static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stre
   using SM = ChunkSmem<D>;
   static bool configured = false;
   if (!configured) {
-    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D, SHAPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes);
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D, SHAPE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         SM::kBytes);
     if (e != cudaSuccess) return e;
     configured = true;
   }
@@ -1348,7 +1391,6 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   a.status = reinterpret_cast<int*>(ws + lay.status);
   a.scale = scale;
   a.softcap = softcap;
-  a.B = B;
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.max_pages = max_pages;

@@ -109,22 +109,40 @@ struct RopeUnit {
       float x[N], y[N], v[N], w[N];
       widen(a, x);
       widen(b, y);
-      cs += u * N;
+      float2 t[N];
+      if constexpr (N == 1) {
+        t[0] = cs[u];
+      } else {
+#pragma unroll
+        for (int k = 0; k < N; k += 2) {
+          const float4 two = *reinterpret_cast<const float4*>(cs + slot(u * N + k, half));
+          t[k] = make_float2(two.x, two.y);
+          t[k + 1] = make_float2(two.z, two.w);
+        }
+      }
       if constexpr (INTER && N > 1) {  // pairs (x0, x1), (x2, x3) ..., then those of y
 #pragma unroll
         for (int k = 0; k < N; k += 2) {
-          turn(x[k], x[k + 1], cs[k / 2], v[k], v[k + 1]);
-          turn(y[k], y[k + 1], cs[N / 2 + k / 2], w[k], w[k + 1]);
+          turn(x[k], x[k + 1], t[k / 2], v[k], v[k + 1]);
+          turn(y[k], y[k + 1], t[N / 2 + k / 2], w[k], w[k + 1]);
         }
       } else {  // pairs (x0, y0), (x1, y1) ...
 #pragma unroll
-        for (int k = 0; k < N; ++k) turn(x[k], y[k], cs[k], v[k], w[k]);
+        for (int k = 0; k < N; ++k) turn(x[k], y[k], t[k], v[k], w[k]);
       }
       narrow(v, p);
       narrow(w, q);
     }
     *reinterpret_cast<Pack<Tout, N>*>(dst + at(u, half)) = p;
     *reinterpret_cast<Pack<Tout, N>*>(dst + partner(u, half)) = q;
+  }
+  // Where pair i's cosine and sine lie: two pairs of a unit side by side, then the same two of its neighbours, so that
+  // neighbouring threads read neighbouring 16 bytes of shared memory (in the pairs' own order they lie 8 N bytes apart:
+  // XXX).
+  __device__ static __forceinline__ int slot(int i, int half) {
+    if (N == 1) return i;
+    const int e = i % N;
+    return ((e / 2) * (half / N) + i / N) * 2 + (e & 1);
   }
   // (past the rotated part both layouts take 2N consecutive elements)
   __device__ static __forceinline__ int at(int u, int half) { return INTER || u * N >= half ? 2 * u * N : u * N; }
@@ -156,7 +174,7 @@ struct RopeArgs {
 
 template <typename Tin, typename Tout, int N, bool INTER, bool APPEND, int TOKENS>
 __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A) {
-  __shared__ float2 cs[TOKENS][kRopeMaxPairs];
+  __shared__ alignas(16) float2 cs[TOKENS][kRopeMaxPairs];
   __shared__ int s_pos[TOKENS];
   __shared__ long long s_row[TOKENS];  // the token's row of the cache (of kv head 0); -1: no room; -2: of no sequence
   const int t0 = blockIdx.x * TOKENS, tid = threadIdx.x;
@@ -222,7 +240,7 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
     if (APPEND && s_row[j] == -2) continue;
     float2 c = rope_turn(APPEND || TOKENS > 1 ? s_pos[j] : A.pos[t0], A.turns[k], A.magnitude);
     if (A.inverse) c.y = -c.y;
-    cs[j][k] = c;
+    cs[j][RopeUnit<Tin, Tout, N, INTER>::slot(k, A.half)] = c;
   }
   __syncthreads();
   for (; h < heads; h += step) {
