@@ -14,7 +14,7 @@
 // memory (once for all heads) while their first loads are on their way, then
 // they share out the tokens' heads in units of 16 bytes. 8192 tokens of 64
 // heads of 128 in fp32 take 79 us, the copy rate; the append of 8587 tokens of
-// 28 + 2 x 4 heads (158 MB) 36 us, 64% of it, 64 decoding tokens 3.2 us.
+// 28 + 2 x 4 heads (158 MB) 32 us, 72% of it, 64 decoding tokens 3.1 us.
 #include <cmath>
 #include <type_traits>
 
@@ -137,8 +137,8 @@ struct RopeUnit {
     *reinterpret_cast<Pack<Tout, N>*>(dst + partner(u, half)) = q;
   }
   // Where pair i's cosine and sine lie: two pairs of a unit side by side, then the same two of its neighbours, so that
-  // neighbouring threads read neighbouring 16 bytes of shared memory (in the pairs' own order they lie 8 N bytes apart:
-  // XXX).
+  // neighbouring threads read neighbouring 16 bytes of shared memory (in the pairs' own order, 8 N bytes apart, they
+  // meet in the same banks: 36 us for 8587 bf16 tokens of 36 heads, 32 so).
   __device__ static __forceinline__ int slot(int i, int half) {
     if (N == 1) return i;
     const int e = i % N;
