@@ -14,7 +14,7 @@
 // memory (once for all heads) while their first loads are on their way, then
 // they share out the tokens' heads in units of 16 bytes. 8192 tokens of 64
 // heads of 128 in fp32 take 79 us, the copy rate; the append of 8587 tokens of
-// 28 + 2 x 4 heads (158 MB) 32 us, 72% of it, 64 decoding tokens 3.1 us.
+// 28 + 2 x 4 heads (158 MB) 30 us, 77% of it, 64 decoding tokens 3.1 us.
 #include <cmath>
 #include <type_traits>
 
@@ -200,8 +200,6 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
     for (int j = 0; j < TOKENS; ++j)
       if (TOKENS == 1 || j < n_tok) to[j].load(src + j * stride, u, A.half);
   };
-  // the first units' loads go out before anything else is known
-  if (h < heads) load(h, unit);
 
   if constexpr (APPEND) {
     if (tid < TOKENS) s_row[tid] = -2;
@@ -235,6 +233,9 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
     if (tid < n_tok) s_pos[tid] = A.pos[t0 + tid];
     __syncthreads();
   }
+  // The first units, in flight while the cosines are formed. (Ahead of the look-ups, which then queue behind them:
+  // 32 us for 8587 bf16 tokens of 36 heads; so, 30.)
+  if (h < heads) load(h, unit);
   for (int i = tid; i < n_tok * A.half; i += blockDim.x) {
     const int j = TOKENS == 1 ? 0 : i / A.half, k = i - j * A.half;
     if (APPEND && s_row[j] == -2) continue;
@@ -293,9 +294,9 @@ static cudaError_t launch_tokens(const RopeArgs& a, int interleaved, int threads
 }
 
 // Two tokens a CTA, with a thread for each of a token's units, where a CTA has room for them and every SM gets a few
-// CTAs; else one token in passes of up to 256 threads over its heads. (8587 bf16 tokens of 36 heads: 36 us at two
-// tokens, 37 at one, 40 at four; in passes of 256 threads, which leave 7 of 8 warps idle in the second, 39. 8192 fp32
-// tokens of 64 heads: 79 us in passes of 256 threads, 84 in passes of 512.)
+// CTAs; else one token in passes of up to 256 threads over its heads. (8587 bf16 tokens of 36 heads: 32 us at two
+// tokens, 34 at one, 41 at four; in passes of 256 threads, which leave 7 of 8 warps idle in the second, slower
+// still. 8192 fp32 tokens of 64 heads: 79 us in passes of 256 threads, 84 in passes of 512.)
 template <typename Tin, typename Tout, int N, bool APPEND>
 static cudaError_t launch_n(const RopeArgs& a, int interleaved, cudaStream_t stream) {
   const int per_head = a.d / (2 * N), heads = APPEND ? a.Hq + 2 * a.Hkv : a.Hq;
