@@ -21,7 +21,7 @@
 // lengths: a plan kernel lists them, and a launch dependent on it does the
 // work; up to 64 blocks each CTA's producer lists for itself.
 //
-// Two streams per CTA, each a softmax warpgroup with its own scores and O
+// Two streams per CTA, each a softmax warpgroup with its own P and O
 // accumulator in tensor memory, so that one stream's MMAs run beside the
 // other's softmax. A block of two row tiles gives each stream one of them, both
 // reading the same K and V tiles in shared memory (loaded once for 256 rows:
@@ -31,22 +31,29 @@
 //
 // Roles in a CTA (384 threads): two softmax warpgroups; a producer warp whose
 // lanes each load their own piece of a K or V tile by TMA (a piece lies within
-// one page) into a ring of chunks; an MMA warp with one issuing thread. Thread
-// i of a warpgroup owns row i of its tile: it reads the tile's 128 scores,
-// masks them only where the tile reaches beyond what its warp's rows all see,
-// and writes P over them as bf16 (16 bits are what the tensor cores take; sums
-// are of the unrounded values, in 32 bits). The reference maximum of a row is
+// one page) into a ring of chunks; an MMA warp, converged, whose elected lane
+// issues. Thread i of a warpgroup owns row i of its tile: it takes the tile's
+// 128 scores into registers, masks them only where the tile reaches beyond
+// what its warp's rows all see, and writes P as bf16 (16 bits are what the
+// tensor cores take; sums are of the unrounded values, in 32 bits). With the
+// scores in registers their place is free for the next S, which runs beside
+// this tile's softmax: at D = 64 the stream's own next, at D = 128, where O
+// and P leave room for the scores of one tile only, the other stream's. (With
+// P over its scores, S waited for the PV before it: 1039 us where it now takes
+// 946, at D = 64 931 where it takes 811.) The reference maximum of a row is
 // raised only when a score exceeds it by more than 8 (a factor of 2^8), so O
 // is rarely rescaled; p <= 2^8 keeps P and O in range.
 //
-// What bounds it, with 128-wide heads: prompts, the chain of a stream's steps
-// (scores, softmax, P V) and the shared memory that S = Q K^T reads, 128 bytes
-// a cycle: 16384 tokens of 8 heads over as many keys run at 1.57 PFLOP/s,
-// where a matrix product reaches 1.92; an item's start and end cost as much as
-// two or three tiles, which is why short prompts stay further off. Decode
-// steps, the cache's bytes: 64 sequences over 512 to 32768 keys run at the
-// copy rate. One sequence over 512 keys: 10.4 us of first instruction fetches
-// and of round trips (plan, K, S, softmax, V, merge), hardly of bytes.
+// What bounds it, with 128-wide heads: prompts, shared memory, from which S =
+// Q K^T alone reads 128 bytes a cycle, and the tensor pipe beside it: 16384
+// tokens of 8 heads over as many keys run at 1.74 PFLOP/s, where a matrix
+// product reaches 1.92; an item's start and end cost as much as three tiles or
+// four, which is why short prompts stay further off. Capped or biased scores,
+// the softmax warps' arithmetic (a capped score takes two exponentials and a
+// reciprocal). Decode steps, the cache's bytes: 64 sequences over 512 to 32768
+// keys run at the copy rate. One sequence over 512 keys: 11 us of first
+// instruction fetches and of round trips (plan, K, S, softmax, V, merge),
+// hardly of bytes.
 //
 // Keys that no row of a block sees take no part: K and V pieces that hold none
 // of them are not read (their pages need not exist), and V rows beyond the
@@ -472,13 +479,17 @@ struct ChunkSmem {
   static constexpr int kQ = 0;                           // two row tiles
   static constexpr int kRing = 2 * kTile;
   static constexpr int kBar = kRing + kChunks * kTile;
-  // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], pfull[2][2], pvdone[2], ofree[2], qfull, qempty, drain
+  // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], got[2][2], pvdone[2], ofree[2], qfull,
+  // qempty, drain
   static constexpr int kNumBars = 2 * kChunks + 14 + 3;
   static constexpr int kInfo = kBar + (8 * kNumBars + 63) / 64 * 64;
   static constexpr int kMisc = kInfo + 2 * 64;           // [0] abort, [1] this CTA merges, [2] tensor-memory address
   static constexpr int kStat = kMisc + 16;               // (m, l) of each stream's rows (streams to be combined)
   static constexpr int kBytes = kStat + kCStreams * kCRows * 8;
-  static constexpr int kColS = 0, kColO = 256;           // per stream 128 columns each
+  // tensor memory: scores, of each stream (D = 64) or of the step at hand (128: no room for two), P and O of each
+  static constexpr int kScores = D == 128 ? 1 : 2;
+  static constexpr int kColS = 0, kColP = kScores * 128, kColO = kColP + kCStreams * 64;
+  static_assert(kColO + kCStreams * D == kCTmemCols, "");
   static_assert(kBytes <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -495,6 +506,9 @@ __device__ __forceinline__ void bar_sync_n(int bar, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory");
 }
 constexpr int kCAllBar = 1;
+
+// A wait that the first ask did not end.
+__device__ __noinline__ bool slow_wait(uint32_t bar, uint32_t parity) { return warp_wait(bar, parity); }
 
 __device__ __forceinline__ void c_fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
   asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
@@ -707,8 +721,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
   const uint32_t bIFull = bEmpty + 8 * SM::kChunks;
   const uint32_t bIEmpty = bIFull + 16;
   const uint32_t bSFull = bIEmpty + 16;   // [stream]
-  const uint32_t bPFull = bSFull + 16;    // [stream][half]
-  const uint32_t bPVDone = bPFull + 32;   // [stream]
+  const uint32_t bGot = bSFull + 16;      // [stream][word & 1]
+  const uint32_t bPVDone = bGot + 32;     // [stream]
   const uint32_t bOFree = bPVDone + 16;   // [stream]
   const uint32_t bQFull = bOFree + 16;
   const uint32_t bQEmpty = bQFull + 8;
@@ -733,8 +747,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       mbar_init(bIFull + 8 * q, 1);
       mbar_init(bIEmpty + 8 * q, 1 + kCSoftmaxWarps);
       mbar_init(bSFull + 8 * q, 1);
-      mbar_init(bPFull + 16 * q, 4);
-      mbar_init(bPFull + 16 * q + 8, 4);
+      mbar_init(bGot + 16 * q, 4);
+      mbar_init(bGot + 16 * q + 8, 4);
       mbar_init(bPVDone + 8 * q, 1);
       mbar_init(bOFree + 8 * q, 4);
     }
@@ -858,7 +872,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         if (cut) left -= it.n_tiles;
         else --whole;
         it.last = whole == 0 && left <= 0;
-        const int n = it.n_tiles, lag = it.pair ? 1 : 2;
+        const int n = it.n_tiles, lag = it.pair ? 2 : 3;
         // keys of a sequence that has one block are read once per kv head
         const int n_new = A.cu_new[p.b + 1] - A.cu_new[p.b];
         const uint64_t policy = n_new <= 2 * Rt ? once : again;
@@ -940,18 +954,51 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     } else if (warp == kCMmaWarp) {
       // ======================= MMA issue =======================
       // The whole warp walks the steps, one elected lane issues.
-      uint32_t item_ctr = 0, chunk_ctr = 0;
-      uint32_t p_ctr = 0;  // bit s: parity of the next P of stream s
-      uint32_t o_ctr = 3;  // bit s: parity of stream s's accumulator being free
+      uint32_t item_ctr = 0;
+      uint32_t ch = 0, ch_par = 0;             // the next chunk and its parity
+      uint32_t g0 = 0, g1 = 0;                 // words heard from the streams
+      uint32_t o0 = 1, o1 = 1;                 // parities: their accumulators are free
       bool ok = true;
+      // (a wait that gives up is noticed at the next tile: what is issued until then reads and writes what is the CTA's)
+      auto need = [&](uint32_t bar, uint32_t parity) {
+        if (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)))
+          ok = __all_sync(0xffffffffu, ok && slow_wait(bar, parity));
+      };
       auto take = [&]() {  // the next chunk, once it is filled
-        const uint32_t ch = chunk_ctr % SM::kChunks;
-        ok = ok && warp_wait(bFull + 8 * ch, (chunk_ctr / SM::kChunks) & 1);
-        ++chunk_ctr;
-        return ch;
+        const uint32_t c = ch;
+        need(bFull + 8 * c, ch_par);
+        if (++ch == SM::kChunks) {
+          ch = 0;
+          ch_par ^= 1;
+        }
+        return c;
+      };
+      auto word = [&](int s, uint32_t& w) {
+        need(bGot + 16 * s + 8 * (w & 1), (w >> 1) & 1);
+        ++w;
+      };
+      const uint32_t k_desc = desc_lo(sRing, 16), v_desc = desc_lo(sRing, 16384), q_desc = desc_lo(sQ, 16);
+      auto issue_s = [&](int s, int qs, uint32_t c) {  // S = Q K^T
+        constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
+        const uint32_t ts = tmem + SM::kColS + (SM::kScores == 2 ? s * 128 : 0);
+        const uint32_t qa = q_desc + qs * (SM::kTile / 16), ka = k_desc + c * (SM::kTile / 16);
+        tc_fence_after();
+#pragma unroll
+        for (int hb = 0; hb < SM::kBoxes; ++hb)
+          mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
+        mma_commit_warp(bSFull + 8 * s);
+      };
+      auto issue_pv = [&](int s, uint32_t c, uint32_t acc) {  // O += P V
+        constexpr uint32_t idesc = mma_idesc(128, D, 1);
+        const uint32_t va = v_desc + c * (SM::kTile / 16);
+        const uint32_t d = tmem + SM::kColO + s * D, tp = tmem + SM::kColP + s * 64;
+        tc_fence_after();
+        mma_ts4_warp<2048>(d, tp, va, idesc, acc);
+        mma_ts4_warp<2048>(d, tp + 32, va + 512, idesc, 1u);
+        mma_commit_warp(bPVDone + 8 * s);
       };
       for (int last = 0; !last && ok; ++item_ctr) {
-        ok = warp_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
+        need(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
         if (!ok) break;
         const int n_tiles = __shfl_sync(0xffffffffu, info[item_ctr & 1].n_tiles, 0);
         const bool pair = __shfl_sync(0xffffffffu, info[item_ctr & 1].pair, 0);
@@ -959,49 +1006,84 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         if (last == 2) break;
         if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
         __syncwarp();
-        // Step n belongs to stream n & 1: tile n / 2 of the stream's own rows (a pair), or tile n of the same rows.
-        // S of a step goes where P of the stream's step before lies, so that one's PV is issued first.
-        const int steps = pair ? 2 * n_tiles : n_tiles;
-        uint32_t kch = 0, vch = 0;
-        for (int n = 0; n < steps + 2 && ok; ++n) {
-          const int s = n & 1;
-          const uint32_t ts = tmem + SM::kColS + s * 128;
-          if (n >= 2) {  // O += P V of step n - 2
-            if (!pair || s == 0) vch = take();
-            if (n < 4) {
-              ok = ok && warp_wait(bOFree + 8 * s, (o_ctr >> s) & 1);
-              o_ctr ^= 1u << s;
-            }
-            constexpr uint32_t idesc = mma_idesc(128, D, 1);
-            const uint32_t va = desc_lo(sRing + vch * SM::kTile, 16384);
-            const uint32_t d = tmem + SM::kColO + s * 128;
-            const uint32_t par = (p_ctr >> s) & 1;
-            p_ctr ^= 1u << s;
-            ok = ok && warp_wait(bPFull + 16 * s, par);
-            if (!ok) break;
-            tc_fence_after();
-            mma_ts4_warp<2048>(d, ts, va, idesc, n < 4 ? 0u : 1u);
-            ok = warp_wait(bPFull + 16 * s + 8, par);
-            if (!ok) break;
-            tc_fence_after();
-            mma_ts4_warp<2048>(d, ts + 32, va + 512, idesc, 1u);
-            mma_commit_warp(bPVDone + 8 * s);
-            if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * vch);
+        need(bQFull, item_ctr & 1);
+        // One word from a stream for each of its tiles, and one more: the tile's scores are in registers, and P of the
+        // tile before is written. Behind it go the next S into the place that it left (D = 64: the stream's own next
+        // tile; D = 128: the other stream's) and that PV. Chunks are asked for before the word. (Words lie on two
+        // barriers in turn: the last two of an item may be there before the first of them is heard, and a warp may be
+        // at the second while another has yet to say the first.)
+        // (A warp by itself takes 5 cycles for an instruction that depends on another, and 150 to 400 for an ask of a
+        // barrier beside MMAs that read shared memory at its full rate: every one of them counts here.)
+        constexpr bool kOwn = SM::kScores == 2;
+        uint32_t kc = take(), vc = 0;
+        if (pair) {
+          issue_s(0, 0, kc);
+          if (kOwn) {
+            issue_s(1, 1, kc);
+            mma_commit_warp(bEmpty + 8 * kc);
+            if (n_tiles == 1) mma_commit_warp(bQEmpty);
           }
-          if (n < steps) {  // S = Q K^T of step n
-            if (!pair || s == 0) kch = take();
-            if (n == 0) ok = ok && warp_wait(bQFull, item_ctr & 1);
-            if (!ok) break;
-            tc_fence_after();
-            constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0);
-            const uint32_t qa = desc_lo(sQ + (pair ? s : 0) * SM::kTile, 16);
-            const uint32_t ka = desc_lo(sRing + kch * SM::kTile, 16);
-#pragma unroll
-            for (int hb = 0; hb < SM::kBoxes; ++hb)
-              mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
-            mma_commit_warp(bSFull + 8 * s);
-            if (!pair || s == 1) mma_commit_warp(bEmpty + 8 * kch);
-            if (n == steps - 1) mma_commit_warp(bQEmpty);
+          for (int t = 0; t <= n_tiles && ok; ++t) {
+            if (t > 0) vc = take();
+            if (t == 1) {
+              need(bOFree, o0);
+              need(bOFree + 8, o1);
+              o0 ^= 1;
+              o1 ^= 1;
+            }
+            if (kOwn && t + 1 < n_tiles) kc = take();
+            word(0, g0);
+            if (kOwn) {
+              if (t + 1 < n_tiles) issue_s(0, 0, kc);
+            } else if (t < n_tiles) {
+              issue_s(1, 1, kc);
+              mma_commit_warp(bEmpty + 8 * kc);
+              if (t == n_tiles - 1) mma_commit_warp(bQEmpty);
+            }
+            if (t > 0) issue_pv(0, vc, t > 1);
+            if (!kOwn && t + 1 < n_tiles) kc = take();
+            word(1, g1);
+            if (t + 1 < n_tiles) {
+              if (kOwn) {
+                issue_s(1, 1, kc);
+                mma_commit_warp(bEmpty + 8 * kc);
+                if (t == n_tiles - 2) mma_commit_warp(bQEmpty);
+              } else {
+                issue_s(0, 0, kc);
+              }
+            }
+            if (t > 0) {
+              issue_pv(1, vc, t > 1);
+              mma_commit_warp(bEmpty + 8 * vc);
+            }
+          }
+        } else {
+          auto next_s = [&](int n) {
+            issue_s(n & 1, 0, kc);
+            mma_commit_warp(bEmpty + 8 * kc);
+            if (n == n_tiles - 1) mma_commit_warp(bQEmpty);
+          };
+          next_s(0);
+          for (int n = 0; n < n_tiles + 2 && ok; ++n) {  // stream n & 1 has tile n
+            const int s = n & 1;
+            if (n >= 2) vc = take();
+            if (n == 2 || n == 3) {
+              need(bOFree + 8 * s, s ? o1 : o0);
+              if (s) o1 ^= 1;
+              else o0 ^= 1;
+            }
+            if (n < n_tiles || n >= 2) {
+              if (s) word(1, g1);
+              else word(0, g0);
+            }
+            if (n >= 2) {
+              issue_pv(s, vc, n >= 4);
+              mma_commit_warp(bEmpty + 8 * vc);
+            }
+            if (n + 1 < n_tiles) {  // (asked for behind the PV, which gives its chunk back while K is on its way)
+              kc = take();
+              next_s(n + 1);
+            }
           }
         }
       }
@@ -1020,11 +1102,17 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     const int st = warp >> 2, wq = warp & 3;
     const int row = wq * 32 + lane;  // tensor-memory lane
     const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-    const uint32_t ts = tmem + lane_off + SM::kColS + st * 128;
+    const uint32_t ts = tmem + lane_off + SM::kColS + (SM::kScores == 2 ? st * 128 : 0);
+    const uint32_t tp = tmem + lane_off + SM::kColP + st * 64;
     const uint32_t to = tmem + lane_off + SM::kColO;
     float2* stat = reinterpret_cast<float2*>(smem + SM::kStat);  // [stream][128]
     const float scale_log2 = A.scale * kLog2e;
+    // The quarter of a tile's keys whose probabilities are the first to be written, with those before them: by then the
+    // PV that reads the tile before's should be done. (At D = 128 it comes behind an S of the other stream: 16384
+    // tokens of 8 heads over as many keys 946 us at 3, 973 at 2, 995 at 1; at D = 64, 811 at 1, 828 at 0, 840 at 3.)
+    constexpr int kFirstP = D == 64 ? 1 : 3;
     uint32_t item_ctr = 0, chunk_base = 0;
+    uint32_t words = 0;             // of this stream in the items before this one
     uint32_t done0 = 0, done1 = 0;  // steps of streams 0 and 1 in the items before this one
     bool ok = true;
     // A wait that fails leaves `ok` false; the item is then finished without further waits, so that every thread
@@ -1067,7 +1155,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           // V rows that no row of the block sees: cleared once they have landed. (Asked after S: a wait on a parity
           // may be one phase ahead of the barrier, not two, and the MMA warp has by now taken every chunk that lay
           // in this place of the ring before.)
-          const uint32_t ci = chunk_base + (pair ? 2 * j + 1 : j + min(j + 2, n_tiles));
+          const uint32_t ci = chunk_base + j + min(j + (pair ? 2 : 3), n_tiles);
           const uint32_t ch = ci % SM::kChunks;
           wait(bFull + 8 * ch, (ci / SM::kChunks) & 1);
           const int key = kt0 + row;
@@ -1083,10 +1171,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         }
         if (!warp_live) {
           __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(bPFull + 16 * st);
-            mbar_arrive(bPFull + 16 * st + 8);
-          }
+          if (lane == 0) mbar_arrive(bGot + 16 * st + 8 * ((words + i) & 1));
           continue;
         }
         tc_fence_after();
@@ -1094,6 +1179,9 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(ts + 32 * q, x[q]);
         tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bGot + 16 * st + 8 * ((words + i) & 1));
         if constexpr (SHAPE & kCap) {  // the scores in units of log 2
           // cap tanh(s / cap) = cap (1 - 2 / (e + 1)), e = exp(2 s / cap)
 #pragma unroll
@@ -1169,19 +1257,19 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll 1
           for (int c0 = 0; c0 < D; c0 += 16) {
             uint32_t o[16];
-            tmem_ld16(to + st * 128 + c0, o);
+            tmem_ld16(to + st * D + c0, o);
             tmem_wait_ld();
 #pragma unroll
             for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-            tmem_st16(to + st * 128 + c0, o);
+            tmem_st16(to + st * D + c0, o);
           }
           tmem_wait_st();
         }
         const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
         float la[2] = {0.f, 0.f}, lb[2] = {0.f, 0.f};
+        uint32_t pk[4][16];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          uint32_t pk[16];
 #pragma unroll
           for (int c = 0; c < 32; c += 4) {
             float y0, y1, y2, y3;
@@ -1193,18 +1281,28 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
             y3 = ex2_approx(y3);
             c_add2(la[0], la[1], y0, y1);
             c_add2(lb[0], lb[1], y2, y3);
-            pk[c >> 1] = c_pack(y0, y1);
-            pk[(c >> 1) + 1] = c_pack(y2, y3);
+            pk[q][c >> 1] = c_pack(y0, y1);
+            pk[q][(c >> 1) + 1] = c_pack(y2, y3);
           }
-          tmem_st16(ts + 16 * q, pk);
-          if (q & 1) {  // 64 keys of P: the first half's MMAs may start
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bPFull + 16 * st + 8 * (q >> 1));
+          if (q == kFirstP) {
+            if (i > 0) {  // the PV before has read P
+              wait(bPVDone + 8 * st, (n - 1) & 1);
+              tc_fence_after();
+            }
+#pragma unroll
+            for (int k = 0; k <= q; ++k) tmem_st16(tp + 16 * k, pk[k]);
+          } else if (q > kFirstP) {
+            tmem_st16(tp + 16 * q, pk[q]);
           }
         }
+        tmem_wait_st();
         l_run += (la[0] + la[1]) + (lb[0] + lb[1]);
+      }
+      if (my_steps > 0) {  // the last P
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bGot + 16 * st + 8 * ((words + my_steps) & 1));
+        words += my_steps + 1;
       }
       // ---- epilogue ----
       float f0 = 1.f, f1 = 0.f;  // factors of the streams' O
@@ -1237,7 +1335,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           f0 *= inv;
           f1 *= inv;
         }
-        const uint32_t oa = to + (pair ? st * 128 : 0);
+        const uint32_t oa = to + (pair ? st * D : 0);
         const int cb = both ? st * (D / 2) : 0, ce = both ? cb + D / 2 : D;
         __nv_bfloat16* orow = A.O + ((size_t)tok * A.Hq + hq) * D;
 #pragma unroll 1
@@ -1246,7 +1344,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           tmem_ld32(oa + c0, o);
           if (both) {
             uint32_t o1[32];
-            tmem_ld32(oa + 128 + c0, o1);
+            tmem_ld32(oa + D + c0, o1);
             tmem_wait_ld();
 #pragma unroll
             for (int c = 0; c < 32; ++c)

@@ -304,6 +304,23 @@ def test_decode_batch_of_uneven_lengths(d, page):
     check([1] * 48, kv, 8, 4, d, page, seed=43, fill=float("nan"))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_short_items_back_to_back(d):
+    """Items of one to three key tiles, single rows and pairs in turn: 200 calls on end, each with the first's result."""
+    r = np.random.default_rng(11)
+    n = np.where(r.random(400) < 0.8, 1, r.integers(2, 60, 400)).tolist()
+    kv = r.integers(0, 300, 400).tolist()
+    Q, K, V, table, cu, kvl, keys, values = inputs(n, kv, 16, 4, d, 32, 47)
+    dev = [x.to(cuda()) for x in (Q, K, V, table, cu, kvl)]
+    ws = lr.ChunkWorkspace(sum(n), 400, 16, 4, d)
+    first, _ = lr.libraspec_chunk_attn_paged(*dev, ws)
+    for _ in range(200):
+        O, lse = lr.libraspec_chunk_attn_paged(*dev, ws, want_lse=True)
+    assert lr.libraspec_get_status(ws) == 0
+    assert torch.equal(O, first)
+    assert_close(O, lse, *attend64(Q.double(), keys, values, n, kv, d ** -0.5))
+
+
 def test_many_sequences():
     """More sequences than the plan's threads; some without new tokens."""
     r = np.random.default_rng(3)
