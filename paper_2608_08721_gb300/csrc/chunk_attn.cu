@@ -430,7 +430,8 @@ __device__ PlanHead warp_plan(const PlanArgs& a, PlanBlock (&mine)[2]) {
 // The attention kernel.
 // ---------------------------------------------------------------------------
 // What a block weighs beside its tiles, in tiles: `one` for every block, `pair` more for two row tiles. (A prompt
-// of 8192 tokens of 32 heads: 419 us at 2 and 2 + 0, 397 at 2 + 1, 399 at 2 + 2, 413 at 2 + 5; decoding is best at 2.)
+// of 8192 tokens of 32 heads: 446 us at 1 and 1 + 1, 375 to 383 at 2 + 1, 374 at 2 + 2, 377 at 2 + 3 and at 3 + 2;
+// decoding is best at 2.)
 struct FixedCost {
   int one, pair;
 };
@@ -959,7 +960,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       uint32_t g0 = 0, g1 = 0;                 // words heard from the streams
       uint32_t o0 = 1, o1 = 1;                 // parities: their accumulators are free
       bool ok = true;
-      // (a wait that gives up is noticed at the next tile: what is issued until then reads and writes what is the CTA's)
+      // (a wait that gives up is noticed at the next tile; what is issued until then stays within the CTA's memory)
       auto need = [&](uint32_t bar, uint32_t parity) {
         if (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)))
           ok = __all_sync(0xffffffffu, ok && slow_wait(bar, parity));
@@ -1498,7 +1499,7 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   a.piece = 64;
   if (block_table)
     while (page_size % a.piece) a.piece /= 2;
-  a.fixed = FixedCost{2, 1};
+  a.fixed = FixedCost{2, 2};
   a.o_wide = reinterpret_cast<uintptr_t>(O) % 32 == 0;
   const long long rows = block_table ? page_size : S_cap, planes = (long long)(block_table ? n_pages : B) * Hkv;
   if (!make_map(&a.K, Kc, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
