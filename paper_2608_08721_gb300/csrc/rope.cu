@@ -207,7 +207,10 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
     // the tokens' sequences: every thread looks at its share of the offsets
     for (int b = tid; b < A.B; b += blockDim.x) {
       const int lo = A.cu_new[b], hi = A.cu_new[b + 1], kv = A.kv_len[b];
-      if (blockIdx.x == 0 && (lo < 0 || hi < lo || hi > A.T)) raise_status(A.status, LIBRASPEC_ST_BAD_LENGTH);
+      if (lo < 0 || hi < lo || hi > A.T) {  // skipped; of the others t - lo lies in [0, T)
+        if (blockIdx.x == 0) raise_status(A.status, LIBRASPEC_ST_BAD_LENGTH);
+        continue;
+      }
 #pragma unroll
       for (int j = 0; j < TOKENS; ++j) {
         const int t = t0 + j;

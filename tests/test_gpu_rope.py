@@ -249,3 +249,36 @@ def test_rope_append_many_sequences_on_another_stream():
     assert_rotated(Kd[seq, :, pos], want, length, True)
     assert torch.equal(Vd[seq, :, pos].cpu(), qkv[:, 2:])
     assert int((Vd != 0).any(-1).sum()) == len(seq) and lr.libraspec_get_status(ws) == 0
+
+
+def _append_case(cu, B, dtype=torch.float32, T=6, S=16):
+    """An append of T tokens into caches of B sequences (their lengths 2, 3, ...) under the offsets `cu`."""
+    Hq, Hkv, d = 2, 2, 64
+    x = torch.randn((T, Hq + 2 * Hkv, d), generator=torch.Generator().manual_seed(12)).to(dtype).to(cuda())
+    Kd, Vd = (torch.zeros((B, Hkv, S, d), dtype=torch.bfloat16, device=cuda()) for _ in range(2))
+    Qo = torch.zeros((T, Hq, d), dtype=torch.bfloat16, device=cuda())
+    kvl = torch.arange(2, 2 + B, dtype=torch.int32, device=cuda())
+    ws = lr.ChunkWorkspace(1, 1, 1, 1, d)
+    lr.libraspec_rope_append(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], Kd, Vd,
+                             torch.tensor(cu, dtype=torch.int32, device=cuda()), kvl, lr.RopeFreqs(d), ws, Qo=Qo)
+    return x.cpu(), Qo, Kd, Vd, lr.libraspec_get_status(ws)
+
+
+@pytest.mark.parametrize("cu,good", [([-1, 2, 6], [1]), ([0, 3, 7], [0]), ([2, 1, 4], [1]),
+                                     ([-(2**31), 2, 6], [1]), ([-(2**31) + 3, 6], []), ([0, 2**31 - 1, 6], [])])
+def test_rope_append_skips_sequences_of_bad_offsets(cu, good):
+    """Offsets below 0, past the rows, or running backwards: the status, and nothing of that sequence written, also
+    where an index counted from such an offset would not fit 32 bits."""
+    x, Qo, Kd, Vd, status = _append_case(cu, len(cu) - 1)
+    assert status == lr.ST_BAD_LENGTH
+    touched = torch.zeros(6, dtype=torch.bool)
+    rows = torch.zeros((len(cu) - 1, 16), dtype=torch.bool)
+    for b in good:
+        n = cu[b + 1] - cu[b]
+        touched[cu[b]:cu[b + 1]] = True
+        rows[b, 2 + b:2 + b + n] = True
+        want, length = rotate64(x[cu[b]:cu[b + 1], 2:4].double(), np.arange(2 + b, 2 + b + n), freqs64(64), False)
+        assert_rotated(Kd[b, :, 2 + b:2 + b + n].transpose(0, 1), want, length, True)
+    assert (Qo != 0).any(-1).any(-1).cpu().tolist() == touched.tolist()
+    for c in (Kd, Vd):
+        assert torch.equal((c != 0).any(-1).all(1).cpu(), rows) and torch.equal((c != 0).any(-1).any(1).cpu(), rows)
