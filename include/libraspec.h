@@ -445,7 +445,9 @@ int libraspec_kv_append_paged(const uint16_t* kv_new, uint16_t* const* Kp, uint1
  * left alone). kv_len [B] i32 counts the sequence's keys before the chunk, so
  * the token's position is kv_len[b] + j. Offsets that decrease or leave [0, T]
  * set LIBRASPEC_ST_BAD_LENGTH (the sequence is skipped), a chunk that does not
- * fit the cache LIBRASPEC_ST_KV_OVERFLOW.
+ * fit the cache LIBRASPEC_ST_KV_OVERFLOW. Beside offsets that decrease, the
+ * ranges of other sequences may overlap: the append gives a row of several to
+ * the first of them, the attention's output for such rows is meaningless.
  *
  * Rotary positions: frequencies. Pair i < rot_dim / 2 of a head turns by f_i
  * radians per position, f_i = theta^(-2 i / rot_dim), scaled for contexts

@@ -26,6 +26,7 @@ int num_sms_current();
 
 constexpr int kRopeThreads = 512;   // of a CTA, at most
 constexpr int kRopeMaxPairs = LIBRASPEC_ROPE_MAX_DIM / 2;
+constexpr unsigned long long kRopeNone = ~0ull;
 
 // cos and sin of a pair at position pos, times the magnitude. The position in two parts that are binary32 numbers each.
 __device__ __forceinline__ float2 rope_turn(int pos, float2 f, float magnitude) {
@@ -176,6 +177,8 @@ template <typename Tin, typename Tout, int N, bool INTER, bool APPEND, int TOKEN
 __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A) {
   __shared__ alignas(16) float2 cs[TOKENS][kRopeMaxPairs];
   __shared__ int s_pos[TOKENS];
+  // (append) a token's sequence, whether that has no room for it, and its key's index there, from bits 33, 32 and 0
+  __shared__ unsigned long long s_owner[TOKENS];
   __shared__ long long s_row[TOKENS];  // the token's row of the cache (of kv head 0); -1: no room; -2: of no sequence
   const int t0 = blockIdx.x * TOKENS, tid = threadIdx.x;
   const int n_tok = min(TOKENS, A.T - t0);
@@ -202,9 +205,10 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
   };
 
   if constexpr (APPEND) {
-    if (tid < TOKENS) s_row[tid] = -2;
+    if (tid < TOKENS) s_owner[tid] = kRopeNone;
     __syncthreads();
-    // the tokens' sequences: every thread looks at its share of the offsets
+    // The tokens' sequences: every thread looks at its share of the offsets. (Ranges overlap only beside offsets that
+    // run backwards: the token is the first sequence's then.)
     for (int b = tid; b < A.B; b += blockDim.x) {
       const int lo = A.cu_new[b], hi = A.cu_new[b + 1], kv = A.kv_len[b];
       if (lo < 0 || hi < lo || hi > A.T) {  // skipped; of the others t - lo lies in [0, T)
@@ -216,19 +220,8 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
         const int t = t0 + j;
         if (j >= n_tok || t < lo || t >= hi) continue;
         const long long s = (long long)kv + (t - lo);
-        long long at = -1;
-        if (kv < 0 || s >= A.S_cap) {
-          raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
-        } else if (A.block_table) {
-          const uint32_t nth = (uint32_t)s / (uint32_t)A.page_size;  // (s < S_cap, an int)
-          const int page = A.block_table[(size_t)b * A.max_pages + nth];
-          if (page < 0 || page >= A.n_pages) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
-          else at = ((long long)page * A.Hkv * A.page_size + ((uint32_t)s - nth * A.page_size)) * A.d;
-        } else {
-          at = ((long long)b * A.Hkv * A.S_cap + s) * A.d;
-        }
-        s_row[j] = at;
-        s_pos[j] = A.pos ? A.pos[t] : (int)s;
+        const bool room = kv >= 0 && s < A.S_cap;
+        atomicMin(&s_owner[j], (unsigned long long)b << 33 | (unsigned long long)!room << 32 | (uint32_t)s);
       }
     }
     __syncthreads();
@@ -236,13 +229,34 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
     if (tid < n_tok) s_pos[tid] = A.pos[t0 + tid];
     __syncthreads();
   }
+  if (APPEND && tid >= (int)blockDim.x - TOKENS) {  // the rows, by the CTA's last threads
+    const int j = blockDim.x - 1 - tid;
+    const unsigned long long owner = s_owner[j];
+    const uint32_t b = (uint32_t)(owner >> 33), s = (uint32_t)owner;
+    long long at = -2;
+    if (owner != kRopeNone) {
+      at = -1;
+      if (owner >> 32 & 1) {
+        raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
+      } else if (A.block_table) {
+        const uint32_t nth = s / (uint32_t)A.page_size;  // (s < S_cap, an int)
+        const int page = A.block_table[(size_t)b * A.max_pages + nth];
+        if (page < 0 || page >= A.n_pages) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
+        else at = ((long long)page * A.Hkv * A.page_size + (s - nth * A.page_size)) * A.d;
+      } else {
+        at = ((long long)b * A.Hkv * A.S_cap + s) * A.d;
+      }
+    }
+    s_row[j] = at;
+  }
   // The first units, in flight while the cosines are formed. (Ahead of the look-ups, which then queue behind them:
   // 32 us for 8587 bf16 tokens of 36 heads; so, 30.)
   if (h < heads) load(h, unit);
   for (int i = tid; i < n_tok * A.half; i += blockDim.x) {
     const int j = TOKENS == 1 ? 0 : i / A.half, k = i - j * A.half;
-    if (APPEND && s_row[j] == -2) continue;
-    float2 c = rope_turn(APPEND || TOKENS > 1 ? s_pos[j] : A.pos[t0], A.turns[k], A.magnitude);
+    if (APPEND && s_owner[j] == kRopeNone) continue;
+    const int pos = APPEND ? (A.pos ? A.pos[t0 + j] : (int)(uint32_t)s_owner[j]) : TOKENS > 1 ? s_pos[j] : A.pos[t0];
+    float2 c = rope_turn(pos, A.turns[k], A.magnitude);
     if (A.inverse) c.y = -c.y;
     cs[j][RopeUnit<Tin, Tout, N, INTER>::slot(k, A.half)] = c;
   }

@@ -282,3 +282,24 @@ def test_rope_append_skips_sequences_of_bad_offsets(cu, good):
     assert (Qo != 0).any(-1).any(-1).cpu().tolist() == touched.tolist()
     for c in (Kd, Vd):
         assert torch.equal((c != 0).any(-1).all(1).cpu(), rows) and torch.equal((c != 0).any(-1).any(1).cpu(), rows)
+
+
+@pytest.mark.parametrize("T,B", [(6, 3), (3000, 3), (6, 1200)])
+def test_rope_append_gives_a_row_of_two_sequences_to_the_first(T, B):
+    """Offsets that decrease, and ranges on either side of it that overlap: each token has one row of the cache, and the
+    position that belongs to it. One token a CTA and two; the second sequence looked up by another thread, and by the
+    same one later."""
+    cu = [0] * (B + 1)
+    later = B - 1
+    cu[1:later] = [4 * T // 6] * (later - 1)
+    cu[later], cu[B] = T // 2, T   # sequence 0: [0, 4 T / 6), the one before the last runs backwards, the last: [T / 2, T)
+    x, Qo, Kd, Vd, status = _append_case(cu, B, T=T, S=T + B + 2)
+    assert status == lr.ST_BAD_LENGTH
+    first = cu[1]
+    for b, lo, hi in ((0, 0, first), (later, first, T)):
+        pos = np.arange(lo, hi) - cu[b] + 2 + b
+        want, length = rotate64(x[lo:hi].double(), pos, freqs64(64), False)
+        assert_rotated(Qo[lo:hi], want[:, :2], length[:, :2], True)
+        assert_rotated(Kd[b, :, pos].transpose(0, 1), want[:, 2:4], length[:, 2:4], True)
+        assert torch.equal(Vd[b, :, pos].transpose(0, 1).cpu(), x[lo:hi, 4:].to(torch.bfloat16))
+    assert int((Vd != 0).any(-1).sum()) == 2 * T
