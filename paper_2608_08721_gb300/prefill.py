@@ -59,14 +59,27 @@ class PagedSequences:
     def layer(self, l: int, qkv: torch.Tensor, step: Step, lse: Optional[torch.Tensor] = None, stream=None, **options):
         """Layer l of the step: qkv [T, Hq + 2 Hkv, d] (f32 or bf16, the projections' output) is rotated and appended,
         and its queries attend to the cache. options: libraspec_chunk_attn's (softcap, slopes, window, first_key,
-        prefix_len, softmax_scale). Returns O [T, Hq, d] bf16."""
+        prefix_len, softmax_scale). Returns O [T, Hq, d] bf16.
+
+        On a stream other than the current one the layer runs behind what the current stream holds, and what the
+        current stream gets next (the advance of the lengths in ``end`` among it) runs behind the layer."""
+        if stream is None:
+            return self._layer(l, qkv, step, lse, options)
+        here = torch.cuda.current_stream()
+        stream.wait_stream(here)
+        with torch.cuda.stream(stream):  # (the rotated queries and O are the stream's own memory)
+            O = self._layer(l, qkv, step, lse, options)
+        here.wait_stream(stream)
+        O.record_stream(here)
+        return O
+
+    def _layer(self, l, qkv, step, lse, options):
         Hq, Hkv, pool = self.Hq, self.Hkv, self.pools[l]
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
         q = binding.libraspec_rope_append_paged(q, k, v, pool["Kp"], pool["Vp"], self.block_table, step.cu_new,
-                                                self.kv_len, self.freqs, self.ws, interleaved=self.interleaved,
-                                                stream=stream)
+                                                self.kv_len, self.freqs, self.ws, interleaved=self.interleaved)
         return binding.libraspec_chunk_attn_paged(q, pool["Kp"], pool["Vp"], self.block_table, step.cu_new, self.kv_len,
-                                                  self.ws, lse=lse, stream=stream, **options)[0]
+                                                  self.ws, lse=lse, **options)[0]
 
     def end(self, step: Step) -> None:
         """Every layer has had the step: its tokens count as the sequences' own."""

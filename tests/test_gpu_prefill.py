@@ -58,3 +58,42 @@ def test_begin_refuses():
     for n in ([1], [-1, 1], [20, 21], [33, 0]):
         with pytest.raises(ValueError):
             seqs.begin(n)
+
+
+def test_layers_on_another_stream_keep_the_order_of_the_steps():
+    """Steps on a side stream that lags behind give what they give on the current one: lengths advance behind the
+    layers that read them, and what a layer drops is not handed out while the stream still works on it."""
+    B, Hq, Hkv, d, layers = 3, 8, 2, 64, 2
+    steps = [[120, 3, 60], [1, 1, 1], [40, 64, 0], [1, 1, 1]]
+    g = torch.Generator(device=cuda()).manual_seed(8)
+    rows = [torch.randn((layers, sum(n), Hq + 2 * Hkv, d), generator=g, device=cuda(), dtype=torch.bfloat16)
+            for n in steps]
+
+    def go(stream):
+        seqs = prefill.PagedSequences(layers, B, 200, Hq, Hkv, d, lr.RopeFreqs(d), 200, page_size=16)
+        for pool in seqs.pools:
+            for p in pool.values():
+                p.zero_()
+        out = []
+        for n, x in zip(steps, rows):
+            step = seqs.begin(n)
+            for l in range(layers):
+                if stream is not None:
+                    with torch.cuda.stream(stream):
+                        torch.cuda._sleep(2_000_000)  # about a millisecond
+                qkv = x[l].clone()  # (from the current stream, and dropped after the layer)
+                O = seqs.layer(l, qkv, step, stream=stream)
+                del qkv
+                scratch = [torch.full((sum(n), Hq, d), 9.0, device=cuda(), dtype=torch.bfloat16) for _ in range(4)]
+                out.append(O.clone())
+                del O, scratch
+            seqs.end(step)
+        torch.cuda.synchronize()
+        seqs.check()
+        return out, seqs
+
+    want, a = go(None)
+    got, b = go(torch.cuda.Stream())
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert a.lengths == b.lengths == b.kv_len.tolist()
+    assert all(torch.equal(p[n], q[n]) for p, q in zip(a.pools, b.pools) for n in p)
