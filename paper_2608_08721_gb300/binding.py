@@ -608,6 +608,15 @@ def _heads_stride(t: torch.Tensor, dtype, name: str, shape=None) -> int:
     return t.stride(0) if T > 1 and t.numel() else H * d
 
 
+def _out(shape, dtype, device, stream) -> torch.Tensor:
+    """An output of a call, made on the stream that it runs on: what the current stream has given back may still be in
+    use there, where nothing orders the call's stream behind it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y=None, stream=None) -> torch.Tensor:
     """X [T, H, d] (f32 or bf16) rotated to the positions pos [T] int32; ``inverse`` rotates back (the gradient of X
     from that of Y). Y may be X (in place)."""
@@ -618,7 +627,7 @@ def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y
     T, H, d = shape
     _req(pos, torch.int32, "pos", (T,))
     if Y is None:
-        Y = torch.empty(shape, dtype=dt, device=X.device)
+        Y = _out(shape, dt, X.device, stream)
         ys = H * d
     else:
         ys = _heads_stride(Y, dt, "Y", shape)
@@ -691,7 +700,7 @@ def _rope_append(Q, K, V, Kc, Vc, block_table, cu_new, kv_len, freqs, ws, pos, i
         if shape[0] != T or shape[2] != d:
             raise ValueError("Q must have shape [%d, Hq, %d], got %s" % (T, d, tuple(shape)))
         if Qo is None:
-            Qo = torch.empty(shape, dtype=torch.bfloat16, device=K.device)
+            Qo = _out(shape, torch.bfloat16, K.device, stream)
         else:
             _req(Qo, torch.bfloat16, "Qo", shape)
     elif Qo is not None:
@@ -767,13 +776,13 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
             _req(prefix_len, torch.int32, "prefix_len", (B,))
         opts = ctypes.byref(_ScoreOpts(float(softcap), int(window), _ptr(slopes), _ptr(first_key), _ptr(prefix_len)))
     if O is None:
-        O = torch.empty_like(Q)
+        O = _out(shape, torch.bfloat16, Q.device, stream)
     else:
         _req(O, torch.bfloat16, "O", shape)
     if lse is not None:
         _req(lse, torch.float32, "lse", (T, Hq))
     elif want_lse:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=Q.device)
+        lse = _out((T, Hq), torch.float32, Q.device, stream)
     tail = (d ** -0.5 if softmax_scale is None else float(softmax_scale), opts, O.data_ptr(), _ptr(lse), ws.ptr,
             ws.nbytes, _stream(stream))
     if block_table is None:

@@ -356,3 +356,31 @@ def test_stream_and_graph():
     assert lr.libraspec_get_status(ws) == 0
     want = attend64(Q.double(), keys, values, n, [77, 5], 0.125, window=64)
     assert_close(O, lse, *want)
+
+
+def test_outputs_belong_to_the_stream_of_the_call():
+    """A call on another stream makes its outputs there: memory that the current stream has given back, and may still be
+    working on, is not written by it."""
+    s, d = torch.cuda.Stream(), 64
+    X = torch.randn((300, 12, d), device=cuda(), dtype=torch.bfloat16)
+    pos = torch.arange(300, dtype=torch.int32, device=cuda())
+    cu, kvl = torch.tensor([0, 300], dtype=torch.int32, device=cuda()), torch.zeros(1, dtype=torch.int32, device=cuda())
+    Kd, Vd = (torch.zeros((1, 2, 300, d), dtype=torch.bfloat16, device=cuda()) for _ in range(2))
+    fr, ws = lr.RopeFreqs(d), lr.ChunkWorkspace(300, 1, 8, 2, d)
+    q, k, v = X[:, :8], X[:, 8:10], X[:, 10:]
+    Q = q.contiguous()
+    torch.cuda.synchronize()
+    calls = [lambda st: [lr.libraspec_rope(Q, pos, fr, stream=st)],
+             lambda st: [lr.libraspec_rope_append(q, k, v, Kd, Vd, cu, kvl, fr, ws, stream=st)],
+             lambda st: list(lr.libraspec_chunk_attn(Q, Kd, Vd, cu, kvl, ws, want_lse=True, stream=st))]
+    for call in calls:
+        here = call(None)
+        torch.cuda.synchronize()
+        want = [(x.data_ptr(), x.clone()) for x in here]
+        del here  # their memory is the first that the current stream hands out again
+        there = call(s)
+        torch.cuda.synchronize()
+        for x in there:
+            assert all(x.data_ptr() != p for p, _ in want)
+        assert all(torch.equal(x, w) for x, (_, w) in zip(there, want))
+        del there
