@@ -559,8 +559,9 @@ int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const 
  * the block's other rows.)
  * head_dim in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 128; page_size a multiple
  * of 16 (else LIBRASPEC_EUNSUPPORTED). Scores, sums and O accumulate in
- * binary32; probabilities enter the second product as bf16. Results do not
- * change from run to run. One launch, or two (a plan from the device's lengths
+ * binary32; probabilities enter the second product as bf16; a capped score is
+ * off by 2^-23 of the cap or of 256, whichever is less, beside its own
+ * rounding. Results do not change from run to run. One launch, or two (a plan from the device's lengths
  * before the attention) where T, B allow more than 64 blocks of 2 floor(128 /
  * g) tokens, with B > 512 or with first_key. workspace:
  * libraspec_chunk_workspace_size(T, B, Hq, Hkv, head_dim) bytes, 256-byte

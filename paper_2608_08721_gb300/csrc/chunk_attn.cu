@@ -441,6 +441,13 @@ struct FixedCost {
   int one, pair;
 };
 
+// Of a cap and the scores' scale, from the host.
+struct CapArgs {
+  float log2;           // the cap in units of log 2
+  float twice_inverse;  // 2 scale / cap in units of log 2 (finite: under the smallest caps a score of zero stays zero)
+  float inverse;        // scale / cap
+};
+
 struct ChunkArgs {
   CUtensorMap K, V, Q;
   __nv_bfloat16* O;
@@ -457,7 +464,8 @@ struct ChunkArgs {
   float* part_ml;
   uint32_t* count;
   int* status;
-  float scale, softcap;
+  float scale;
+  CapArgs cap;
   int Hq, Hkv, max_pages, page_size, n_pages, piece;  // piece: keys of one TMA box
   FixedCost fixed;
   int o_wide;  // O is aligned to 32 bytes
@@ -539,6 +547,19 @@ __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// cap tanh(s / cap) in units of log 2, of a score s = scale x: by the series s (1 - t^2 / 3 + 2 t^4 / 15 - 17 t^6 / 315 +
+// 62 t^8 / 2835), t = s / cap, whose next term is below 2^-26 of s for |t| <= 1 / 4; beyond that with r =
+// 1 / (exp(2 t) + 1).
+constexpr float kSeriesTop = 0.25f;
+__device__ __forceinline__ float cap_series(float x, float scale_log2, float inverse) {
+  const float t = x * inverse, t2 = t * t, s = x * scale_log2;
+  const float p = fmaf(fmaf(fmaf(62.f / 2835.f, t2, -17.f / 315.f), t2, 2.f / 15.f), t2, -1.f / 3.f);
+  return fmaf(s, t2 * p, s);
+}
+__device__ __forceinline__ float wide_cap(float x, float r, float scale_log2, const CapArgs& cap) {
+  return fabsf(x * cap.inverse) <= kSeriesTop ? cap_series(x, scale_log2, cap.inverse)
+                                              : cap.log2 * fmaf(-2.f, r, 1.f);
 }
 // bits [0, n) set, n clamped to [0, 32]
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
@@ -712,9 +733,14 @@ __device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem&
   }
 }
 
-// What scores are beside a scaled product: bit 0 capped, bit 1 biased by distance. (Instantiations: the code of either
-// in the plain kernel's loop costs it instruction fetches.)
-constexpr int kCap = 1, kBias = 2;
+// What scores are beside a scaled product: bit 0 capped, bit 1 biased by distance, bit 2 capped far above the scores.
+// (Instantiations: the code of either in the plain kernel's loop costs it instruction fetches.)
+constexpr int kCap = 1, kBias = 2, kWideCap = 4;
+// Largest cap that kCap alone takes. Its cap (1 - 2 / (e + 1)) is off by up to 2^-23 of the cap (of 256: 3e-5, an eighth
+// of what a sum of products may be off); above it scores below a quarter of the cap take the odd series of the tangent
+// (4000 tokens in windows of 1024 keys: 222 us, 175 under a cap that kCap takes).
+constexpr float kNarrowCap = 256.f;
+constexpr float kFloatMax = 3.402823466e38f;
 
 // The tile that step t of n takes. With a bias by distance from the last one back: the keys nearest to the rows come
 // first and set the reference, which each tile towards the rows would raise (16384 tokens of 8 heads over as many keys:
@@ -1156,7 +1182,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         if (SHAPE & kBias) slope = A.slopes[hq] * kLog2e;
       }
       const float sc = SHAPE ? 1.f : scale_log2;
-      const float cap2 = A.softcap * kLog2e, u2 = 2.f * scale_log2 / A.softcap;
+      const float cap2 = A.cap.log2, u2 = A.cap.twice_inverse;
       float m_run = -INFINITY, l_run = 0.f;
       for (int i = 0; i < my_steps; ++i) {
         const int j = pair ? i : 2 * i + st;  // the item's tile
@@ -1195,22 +1221,45 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         __syncwarp();
         if (lane == 0) mbar_arrive(bGot + 16 * st + 8 * ((words + i) & 1));
         if constexpr (SHAPE & kCap) {  // the scores in units of log 2
-          // cap tanh(s / cap) = cap (1 - 2 / (e + 1)), e = exp(2 s / cap)
+          bool series = false;  // all of the warp's scores are small beside the cap
+          if constexpr (SHAPE & kWideCap) {
+            float top = 0.f;
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-              float a, b;
-              c_fma2(a, b, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), u2, 0.f);
-              a = ex2_approx(a);
-              b = ex2_approx(b);
-              c_add2(a, b, 1.f, 1.f);
-              a = rcp_approx(a);
-              b = rcp_approx(b);
-              c_fma2(a, b, a, b, -2.f * cap2, cap2);
-              x[q][c] = __float_as_uint(a);
-              x[q][c + 1] = __float_as_uint(b);
+              for (int c = 0; c < 32; ++c) top = fmaxf(top, fabsf(__uint_as_float(x[q][c])));
+            series = !__any_sync(0xffffffffu, valid && top * A.cap.inverse > kSeriesTop);
+            if (series) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int c = 0; c < 32; ++c)
+                  x[q][c] = __float_as_uint(cap_series(__uint_as_float(x[q][c]), scale_log2, A.cap.inverse));
             }
+          }
+          // cap tanh(s / cap) = cap (1 - 2 / (e + 1)), e = exp(2 s / cap)
+          if (!series) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int c = 0; c < 32; c += 2) {
+                float a, b;
+                c_fma2(a, b, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), u2, 0.f);
+                a = ex2_approx(a);
+                b = ex2_approx(b);
+                c_add2(a, b, 1.f, 1.f);
+                a = rcp_approx(a);
+                b = rcp_approx(b);
+                if constexpr (SHAPE & kWideCap) {
+                  a = wide_cap(__uint_as_float(x[q][c]), a, scale_log2, A.cap);
+                  b = wide_cap(__uint_as_float(x[q][c + 1]), b, scale_log2, A.cap);
+                } else {
+                  c_fma2(a, b, a, b, -2.f * cap2, cap2);
+                }
+                x[q][c] = __float_as_uint(a);
+                x[q][c + 1] = __float_as_uint(b);
+              }
+          }
         }
         if constexpr (SHAPE & kBias) {
           const float to_log2 = SHAPE & kCap ? 1.f : scale_log2, d0 = (float)(kt0 - pos);
@@ -1500,7 +1549,10 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   a.count = reinterpret_cast<uint32_t*>(ws + lay.count);
   a.status = reinterpret_cast<int*>(ws + lay.status);
   a.scale = scale;
-  a.softcap = softcap;
+  a.cap = CapArgs{};
+  if (softcap > 0.f)
+    a.cap = CapArgs{std::min(softcap * kLog2e, kFloatMax), std::min(2.f * (scale * kLog2e) / softcap, kFloatMax),
+                    scale / softcap};
   a.Hq = Hq;
   a.Hkv = Hkv;
   a.max_pages = max_pages;
@@ -1530,10 +1582,14 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
     if (e != cudaSuccess) return e;
   }
   using Launch = cudaError_t (*)(const ChunkArgs&, int, cudaStream_t);
-  static const Launch launch[2][4] = {
-      {launch_attn_t<64, 0>, launch_attn_t<64, kCap>, launch_attn_t<64, kBias>, launch_attn_t<64, kCap | kBias>},
-      {launch_attn_t<128, 0>, launch_attn_t<128, kCap>, launch_attn_t<128, kBias>, launch_attn_t<128, kCap | kBias>}};
-  return launch[D == 128][(softcap > 0.f ? kCap : 0) | (slopes ? kBias : 0)](a, grid, stream);
+  constexpr int kWide = kCap | kWideCap;
+  static const Launch launch[2][6] = {
+      {launch_attn_t<64, 0>, launch_attn_t<64, kBias>, launch_attn_t<64, kCap>, launch_attn_t<64, kCap | kBias>,
+       launch_attn_t<64, kWide>, launch_attn_t<64, kWide | kBias>},
+      {launch_attn_t<128, 0>, launch_attn_t<128, kBias>, launch_attn_t<128, kCap>, launch_attn_t<128, kCap | kBias>,
+       launch_attn_t<128, kWide>, launch_attn_t<128, kWide | kBias>}};
+  const int cap = softcap > kNarrowCap ? 2 : softcap > 0.f ? 1 : 0;
+  return launch[D == 128][2 * cap + (slopes ? 1 : 0)](a, grid, stream);
 }
 
 }  // namespace libraspec

@@ -384,3 +384,18 @@ def test_outputs_belong_to_the_stream_of_the_call():
             assert all(x.data_ptr() != p for p, _ in want)
         assert all(torch.equal(x, w) for x, (_, w) in zip(there, want))
         del there
+
+
+@pytest.mark.parametrize("softcap", [1e-39, 1e-30, 100.0, 300.0, 1e3, 1e5, 1e7, 1e20, 3e38])
+@pytest.mark.parametrize("q_scale,bias", [(1.0, False), (8.0, True)])
+def test_caps_of_any_size(softcap, q_scale, bias):
+    """The cap's error is relative to the capped score, not to the cap: a cap far above the scores leaves them as they
+    are; scores of zero stay zero under the smallest cap."""
+    n, kv, d = [70, 1], [200, 600], 64
+    Q, K, V, table, cu, kvl, keys, values = inputs(n, kv, 8, 2, d, 0, 25, q_scale=q_scale)
+    Q[3], Q[70, 2] = 0.0, 0.0
+    o = dict(slopes=torch.tensor([2.0 ** -i for i in range(1, 9)])) if bias else {}
+    softcap = float(np.float32(softcap))
+    O, lse, status = run(Q, K, V, table, cu, kvl, softcap=softcap, **o)
+    assert status == 0
+    assert_close(O, lse, *attend64(Q.double(), keys, values, n, kv, d ** -0.5, softcap=softcap, **o), q_scale=q_scale)
