@@ -236,7 +236,7 @@ __device__ __forceinline__ KeyRange key_range_docs(const PlanArgs& a, int b, int
   }
   klo = __reduce_min_sync(0xffffffffu, klo);
   khi = __reduce_max_sync(0xffffffffu, khi);
-  if (klo >= khi) klo = khi = N - 1;  // no row sees anything: one tile, of which nothing is read
+  if (klo >= khi) klo = khi = (N - 1) / kCKeys * kCKeys;  // no row sees anything: one tile, no piece of which is read
   return KeyRange{klo, khi};
 }
 

@@ -399,3 +399,19 @@ def test_caps_of_any_size(softcap, q_scale, bias):
     O, lse, status = run(Q, K, V, table, cu, kvl, softcap=softcap, **o)
     assert status == 0
     assert_close(O, lse, *attend64(Q.double(), keys, values, n, kv, d ** -0.5, softcap=softcap, **o), q_scale=q_scale)
+
+
+@pytest.mark.parametrize("n,kv", [([1, 33], [199, 100]), ([70, 1], [58, 127]), ([300, 5], [0, 128])])
+@pytest.mark.parametrize("page", [0, 16, 48])
+def test_blocks_that_see_nothing_read_nothing(n, kv, page):
+    """A sequence of which no row sees a key: its pages need not exist, and nothing is reported."""
+    Q, K, V, table, cu, kvl, keys, values = inputs(n, kv, 8, 2, 64, page, 19)
+    first = torch.cat([torch.full((n[0],), 2**31 - 1), torch.zeros(n[1], dtype=torch.int64)]).to(torch.int32)
+    if page:
+        K[table[0].long()], V[table[0].long()] = float("nan"), float("nan")
+        table[0] = 10**6
+    else:
+        K[0], V[0] = float("nan"), float("nan")
+    O, lse, status = run(Q, K, V, table, cu, kvl, first_key=first)
+    assert status == 0
+    assert_close(O, lse, *attend64(Q.double(), keys, values, n, kv, 0.125, first_key=first))
