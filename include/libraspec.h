@@ -553,10 +553,10 @@ int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const 
  *   first_key  [T] i32: the first key that a row may see (the start of its
  *              document; any order);
  *   prefix_len [B] i32: keys that every new row sees, later ones included.
- * Keys that no row of a sequence sees need not be initialised; pages that hold
- * none of the others are not read, nor their block-table entries. (A NaN or
- * infinity in a key or value that some row of a block of rows sees may reach
- * the block's other rows.)
+ * Keys that no row of a sequence sees (padding among its new tokens included)
+ * need not be initialised; pages that hold none of the others are not read, nor
+ * their block-table entries. (A NaN or infinity in a key or value that some row
+ * of a block of rows sees may reach the block's other rows.)
  * head_dim in {64, 128}, Hq % Hkv == 0, Hq / Hkv <= 128; page_size a multiple
  * of 16 (else LIBRASPEC_EUNSUPPORTED). Scores, sums and O accumulate in
  * binary32; probabilities enter the second product as bf16; a capped score is

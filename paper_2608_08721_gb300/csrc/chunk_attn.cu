@@ -58,7 +58,8 @@
 // Keys that no row of a block sees take no part: K and V pieces that hold none
 // of them are not read (their pages need not exist), and V rows beyond the
 // block's range are cleared in shared memory before the MMA, so that what an
-// unwritten cache row holds (NaN, say) does not meet the zeros of P.
+// unwritten cache row holds (NaN, say) does not meet the zeros of P; so are the
+// rows within it of tokens that no row sees (padding), which first keys allow.
 //
 // A block cut over CTAs c0..c1 leaves one fp32 partial (O, m, l) per CTA; the
 // CTA that delivers the last of them merges all, in CTA order (results do not
@@ -86,6 +87,7 @@ constexpr int kCTmemCols = 512;
 constexpr float kCRescaleLog2 = 8.f;
 constexpr int kPlanThreads = 1024;
 constexpr int kCSharedBytes = 64 << 20;     // K and V beyond half of L2: see the plan's waves
+constexpr int kNoPage = -2;                 // (of a block table: -1 and below are invalid alike)
 constexpr int kCMaxKeys = 0x7fffffff - 2 * kCKeys;  // of a sequence: its last tile's end is an int
 
 // ---------------------------------------------------------------------------
@@ -99,7 +101,7 @@ struct PlanBlock {       // the rows of one block and the key tiles that they se
   int pos0;                // position of the first token
   int klo, khi;            // keys that some row sees lie in [klo, khi)
   int tile0, n_tiles;      // 128-key tiles
-  int pad;
+  int gaps;                // keys within [klo, khi) may be seen by no row
 };
 static_assert(sizeof(PlanBlock) == 48, "");
 
@@ -111,7 +113,7 @@ struct PlanHead {
 };
 
 struct ChunkWs {
-  size_t status, head, count, blocks, part_o, part_ml, total;
+  size_t status, head, count, blocks, seen, part_o, part_ml, total;
 };
 
 // Tokens of a block and the most blocks that T tokens of B sequences have.
@@ -129,6 +131,7 @@ static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
   w.head = take(sizeof(PlanHead));
   w.count = take(kCMaxCtas * sizeof(uint32_t));
   w.blocks = take((size_t)max_blocks(T, B, Hq / Hkv) * sizeof(PlanBlock));
+  w.seen = take((size_t)max_blocks(T, B, Hq / Hkv) * (kCBlockRows / 8));  // a bit for each token of a block
   // two slots per CTA: its first item, and its last where that goes on in the next CTA
   w.part_o = take(size_t(2 * kCMaxCtas) * kCBlockRows * d * sizeof(float));
   w.part_ml = take(size_t(2 * kCMaxCtas) * kCBlockRows * 2 * sizeof(float));
@@ -137,6 +140,9 @@ static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
 }
 
 size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d) { return chunk_ws(T, B, Hq, Hkv, d).total; }
+
+// bits [0, n) set, n clamped to [0, 32]
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
 // What a row sees.
 struct MaskArgs {
@@ -209,10 +215,14 @@ __device__ __forceinline__ int block_room(const PlanArgs& a) {
 }
 
 // Keys that some row of tokens [j0, j1) of a sequence sees lie in [klo, khi). Its n tokens start at row c0 and position
-// kv.
+// kv. Rows that see their own key leave no gap between them. A row whose document starts behind it does not, and then
+// its key may be one that no row of the block sees. No other key of the range can be: one before the block is seen by
+// the row whose range starts there; one behind it is in the range only through the prefix, with which the rows' ranges
+// end. `gaps`: there are such rows; bits of the tokens whose keys some row sees then lie in a table.
 struct KeyRange {
-  int lo, hi;
+  int lo, hi, gaps;
 };
+constexpr int kSeenWords = kCBlockRows / 32;  // of a block
 // without first keys: ranges move forward with the position
 __device__ __forceinline__ KeyRange key_range(const PlanArgs& a, int b, int n, int kv, int j0) {
   const int j1 = min(n, j0 + a.TB), N = kv + n, prefix = a.mask.prefix_len ? a.mask.prefix_len[b] : 0;
@@ -220,15 +230,19 @@ __device__ __forceinline__ KeyRange key_range(const PlanArgs& a, int b, int n, i
   int l, h;
   row_range(kv + j0, N, prefix, 0, a.mask.window, k.lo, h);
   row_range(kv + j1 - 1, N, prefix, 0, a.mask.window, l, k.hi);
+  k.gaps = 0;
   return k;
 }
 // with them, by a warp (a thread for each block, one key after the other, took 17 us longer for 5721 tokens)
-__device__ __forceinline__ KeyRange key_range_docs(const PlanArgs& a, int b, int c0, int n, int kv, int j0) {
+__device__ __forceinline__ KeyRange key_range_docs(const PlanArgs& a, int b, int c0, int n, int kv, int j0,
+                                                   uint32_t* seen) {
   const int j1 = min(n, j0 + a.TB), N = kv + n, prefix = a.mask.prefix_len ? a.mask.prefix_len[b] : 0;
   int klo = 0x7fffffff, khi = 0;
+  bool gaps = false;
   for (int j = j0 + (threadIdx.x & 31); j < j1; j += 32) {
     int l, h;
     row_range(kv + j, N, prefix, a.mask.first_key[c0 + j], a.mask.window, l, h);
+    gaps |= l > kv + j;
     if (l < h) {
       klo = min(klo, l);
       khi = max(khi, h);
@@ -236,8 +250,26 @@ __device__ __forceinline__ KeyRange key_range_docs(const PlanArgs& a, int b, int
   }
   klo = __reduce_min_sync(0xffffffffu, klo);
   khi = __reduce_max_sync(0xffffffffu, khi);
-  if (klo >= khi) klo = khi = (N - 1) / kCKeys * kCKeys;  // no row sees anything: one tile, no piece of which is read
-  return KeyRange{klo, khi};
+  if (klo >= khi) klo = khi = (N - 1) / kCKeys * kCKeys;  // no row sees a key: one tile, no piece of it read
+  gaps = __any_sync(0xffffffffu, gaps);
+  if (gaps) {
+    uint32_t bits[kSeenWords] = {};
+    for (int j = j0 + (threadIdx.x & 31); j < j1; j += 32) {
+      int l, h;
+      row_range(kv + j, N, prefix, a.mask.first_key[c0 + j], a.mask.window, l, h);
+      l = max(l - (kv + j0), 0);
+      h = min(h - (kv + j0), j1 - j0);
+#pragma unroll
+      for (int w = 0; w < kSeenWords; ++w)
+        if (l < h) bits[w] |= bits_below(h - 32 * w) & ~bits_below(l - 32 * w);
+    }
+#pragma unroll
+    for (int w = 0; w < kSeenWords; ++w) {
+      const uint32_t all = __reduce_or_sync(0xffffffffu, bits[w]);
+      if ((threadIdx.x & 31) == 0) seen[w] = all;
+    }
+  }
+  return KeyRange{klo, khi, gaps};
 }
 
 // Block of tokens [j0, j0 + TB) of sequence b.
@@ -251,6 +283,7 @@ __device__ __forceinline__ PlanBlock make_block(const PlanArgs& a, int b, int c0
   p.khi = k.hi;
   p.tile0 = k.lo / kCKeys;
   p.n_tiles = max(1, (k.hi + kCKeys - 1) / kCKeys - p.tile0);
+  p.gaps = k.gaps;
   return p;
 }
 
@@ -266,7 +299,8 @@ __device__ __forceinline__ int whole_waves(const PlanArgs& a, int n_blocks, int 
 // (Two scans of up to a thousand entries each, all else by shared atomics: with four scans a prompt of 8192 tokens took
 // 374 us, with two 368.)
 __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const PlanArgs a, PlanBlock* __restrict__ blocks,
-                                                                  PlanHead* __restrict__ head) {
+                                                                  PlanHead* __restrict__ head,
+                                                                  uint32_t* __restrict__ seen) {
   __shared__ int first_block[LIBRASPEC_MAX_B + 1];  // of each sequence
   __shared__ long long warp_sums[32];
   __shared__ KeyRange ranges[kPlanThreads];  // (first keys)
@@ -325,7 +359,8 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const PlanArgs
       for (int i = tid >> 5; i < kPlanThreads && e0 + i < n_blocks; i += kPlanThreads / 32) {
         int c0, kv;
         const int b = seq_of(e0 + i), n = new_tokens(a, b, false, c0, kv);
-        const KeyRange k = key_range_docs(a, b, c0, n, kv, (e0 + i - first_block[b]) * a.TB);
+        const KeyRange k = key_range_docs(a, b, c0, n, kv, (e0 + i - first_block[b]) * a.TB,
+                                          seen + (size_t)(e0 + i) * kSeenWords);
         if (lane == 0) ranges[i] = k;
       }
       __syncthreads();
@@ -460,6 +495,7 @@ struct ChunkArgs {
   PlanArgs plan;
   const PlanBlock* blocks;  // NULL: each producer plans for itself
   const PlanHead* head;
+  const uint32_t* seen;     // [blocks][kSeenWords], of blocks with gaps
   float* part_o;
   float* part_ml;
   uint32_t* count;
@@ -494,8 +530,8 @@ struct ChunkSmem {
   static constexpr int kRing = 2 * kTile;
   static constexpr int kBar = kRing + kChunks * kTile;
   // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], got[2][2], pvdone[2], ofree[2], qfull,
-  // qempty, drain
-  static constexpr int kNumBars = 2 * kChunks + 14 + 3;
+  // qempty, drain, gap
+  static constexpr int kNumBars = 2 * kChunks + 14 + 4;
   static constexpr int kInfo = kBar + (8 * kNumBars + 63) / 64 * 64;
   static constexpr int kMisc = kInfo + 2 * 64;           // [0] abort, [1] this CTA merges, [2] tensor-memory address
   static constexpr int kStat = kMisc + 16;               // (m, l) of each stream's rows (streams to be combined)
@@ -548,9 +584,9 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// cap tanh(s / cap) in units of log 2, of a score s = scale x: by the series s (1 - t^2 / 3 + 2 t^4 / 15 - 17 t^6 / 315 +
-// 62 t^8 / 2835), t = s / cap, whose next term is below 2^-26 of s for |t| <= 1 / 4; beyond that with r =
-// 1 / (exp(2 t) + 1).
+// cap tanh(s / cap) in units of log 2, of a score s = scale x: by the series s (1 - t^2 / 3 + 2 t^4 / 15 -
+// 17 t^6 / 315 + 62 t^8 / 2835), t = s / cap, whose next term is below 2^-26 of s for |t| <= 1 / 4; beyond that with
+// r = 1 / (exp(2 t) + 1).
 constexpr float kSeriesTop = 0.25f;
 __device__ __forceinline__ float cap_series(float x, float scale_log2, float inverse) {
   const float t = x * inverse, t2 = t * t, s = x * scale_log2;
@@ -561,8 +597,6 @@ __device__ __forceinline__ float wide_cap(float x, float r, float scale_log2, co
   return fabsf(x * cap.inverse) <= kSeriesTop ? cap_series(x, scale_log2, cap.inverse)
                                               : cap.log2 * fmaf(-2.f, r, 1.f);
 }
-// bits [0, n) set, n clamped to [0, 32]
-__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 // 32 bytes at once
 __device__ __forceinline__ void store32(void* p, const uint32_t (&r)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]),
@@ -620,10 +654,19 @@ struct Blocks {
     p.khi = __shfl_sync(0xffffffffu, m.khi, e);
     p.tile0 = __shfl_sync(0xffffffffu, m.tile0, e);
     p.n_tiles = __shfl_sync(0xffffffffu, m.n_tiles, e);
-    p.pad = 0;
+    p.gaps = 0;  // (without first keys)
     return p;
   }
 };
+
+// Whether a row of a block with gaps sees a key of [key0, key1), which lies in the block's range. seen: as in KeyRange.
+__device__ __forceinline__ bool some_row_sees(const uint32_t* seen, int pos0, int n_tok, int key0, int key1) {
+  const int j0 = key0 - pos0, j1 = key1 - pos0;
+  if (j0 < 0 || j1 > n_tok) return true;
+  for (int w = j0 / 32; w <= (j1 - 1) / 32; ++w)
+    if (seen[w] & bits_below(j1 - 32 * w) & ~bits_below(j0 - 32 * w)) return true;
+  return false;
+}
 
 // Block e's Hkv copies start at Hkv times the weight before it, each with its fixed cost first; x < the total.
 __device__ Place find_place(long long x, const Blocks& blocks, int Hkv, int g, FixedCost f) {
@@ -733,12 +776,13 @@ __device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem&
   }
 }
 
-// What scores are beside a scaled product: bit 0 capped, bit 1 biased by distance, bit 2 capped far above the scores.
-// (Instantiations: the code of either in the plain kernel's loop costs it instruction fetches.)
-constexpr int kCap = 1, kBias = 2, kWideCap = 4;
-// Largest cap that kCap alone takes. Its cap (1 - 2 / (e + 1)) is off by up to 2^-23 of the cap (of 256: 3e-5, an eighth
-// of what a sum of products may be off); above it scores below a quarter of the cap take the odd series of the tangent
-// (4000 tokens in windows of 1024 keys: 222 us, 175 under a cap that kCap takes).
+// What scores are beside a scaled product: bit 0 capped, bit 1 biased by distance, bit 2 capped far above the scores;
+// bit 3: rows have first keys. (Instantiations: the code of each in the plain kernel costs it instruction fetches, also
+// beside its loop.)
+constexpr int kCap = 1, kBias = 2, kWideCap = 4, kDocs = 8;
+// Largest cap that kCap alone takes. Its cap (1 - 2 / (e + 1)) is off by up to 2^-23 of the cap (of 256: 3e-5, an
+// eighth of what a sum of products may be off); above it scores below a quarter of the cap take the odd series of the
+// tangent (4000 tokens in windows of 1024 keys: 222 us, 175 under a cap that kCap takes).
 constexpr float kNarrowCap = 256.f;
 constexpr float kFloatMax = 3.402823466e38f;
 
@@ -765,6 +809,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
   const uint32_t bQFull = bOFree + 16;
   const uint32_t bQEmpty = bQFull + 8;
   const uint32_t bDrain = bQEmpty + 8;
+  const uint32_t bGap = bDrain + 8;       // V tiles of which the producer clears rows
   ChunkItem* info = reinterpret_cast<ChunkItem*>(smem + SM::kInfo);
   volatile int* misc = reinterpret_cast<int*>(smem + SM::kMisc);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -793,6 +838,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     mbar_init(bQFull, 1);
     mbar_init(bQEmpty, 1);
     mbar_init(bDrain, 1);
+    mbar_init(bGap, 1);
     misc[0] = (sQ & 1023) != 0;  // (the swizzled tiles need the alignment that the declaration asks for)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -877,7 +923,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       const int per_tile = kCKeys / A.piece;
       const int my_row = (lane % per_tile) * A.piece, my_hb = lane / per_tile;
       const bool has_piece = my_hb < SM::kBoxes;
-      uint32_t item_ctr = 0, chunk_ctr = 0;
+      uint32_t item_ctr = 0, chunk_ctr = 0, gap_ctr = 0;
       const uint64_t once = evict_first_policy(), again = evict_normal_policy();
       bool ok = true;
       while ((whole > 0 || left > 0) && ok) {
@@ -914,12 +960,20 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
         // keys of a sequence that has one block are read once per kv head
         const int n_new = A.cu_new[p.b + 1] - A.cu_new[p.b];
         const uint64_t policy = n_new <= 2 * Rt ? once : again;
-        // pages of the item's tiles, four tiles at a time: lane 8 k + i holds that of piece i of the k-th
+        const bool gaps = (SHAPE & kDocs) && p.gaps;
+        const uint32_t* seen = A.seen + (size_t)pl.e * kSeenWords;  // (if it has gaps)
+        // pages of the item's tiles, four tiles at a time: lane 8 k + i holds that of piece i of the k-th (kNoPage: no
+        // row of a block with gaps sees the piece)
         auto load_pages = [&](int group) {
-          if (!A.block_table) return p.b;
+          if (!A.block_table && !gaps) return p.b;
           const int tile = 4 * group + lane / 8, i = lane % 8;
           const int key = (it.tile0 + tile_of<SHAPE>(tile, n)) * kCKeys + i * A.piece;
           if (tile >= n || i >= per_tile || key >= p.khi || key + A.piece <= p.klo) return 0;
+          if (gaps) {
+            if (!some_row_sees(seen, p.pos0, p.n_tok, max(key, p.klo), min(key + A.piece, p.khi))) return kNoPage;
+            if (!A.block_table) return p.b;
+            return max(-1, __ldg(A.block_table + (size_t)p.b * A.max_pages + key / A.page_size));
+          }
           return __ldg(A.block_table + (size_t)p.b * A.max_pages + key / A.page_size);
         };
         int pages_before = 0, pages = load_pages(0), pages_next = load_pages(1);
@@ -951,12 +1005,17 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           const int from = t >> 2 == (kt - 1) >> 2 ? pages : pages_before;  // kt - 1: the last K tile
           int page = __shfl_sync(0xffffffffu, from, (t & 3) * 8 + lane % per_tile);
           const int key = (it.tile0 + tile_of<SHAPE>(t, n)) * kCKeys + my_row;
-          const bool load = has_piece && key < p.khi && key + A.piece > p.klo;
+          const bool load = has_piece && key < p.khi && key + A.piece > p.klo && !(gaps && page == kNoPage);
           if (A.block_table && load && (page < 0 || page >= A.n_pages)) {
             raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
             page = 0;  // a valid page; the sequence's output is then meaningless
           }
-          const uint32_t bar = bFull + 8 * ch;
+          // Rows of V within the block's range that no row sees are cleared before the chunk counts as filled. (Here
+          // and not by the softmax warps, who clear those outside the range: with this in their loop, and in kernels
+          // for calls without first keys, a prompt of 64-wide heads took 871 us instead of 812.)
+          const int kt0 = key - my_row;
+          const bool gap = gaps && !is_k && kt0 + kCKeys > p.pos0 && kt0 < p.pos0 + p.n_tok;
+          const uint32_t bar = gap ? bGap : bFull + 8 * ch;
           const int pieces = __popc(__ballot_sync(0xffffffffu, load));
           if (lane == 0) mbar_expect_tx(bar, pieces * A.piece * 128);
           __syncwarp();
@@ -964,6 +1023,19 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
             const int z = page * A.Hkv + it.kvh, y = A.block_table ? key % A.page_size : key;
             tma_load_3d_hint(sRing + ch * SM::kTile + my_hb * 16384 + my_row * 128, is_k ? &A.K : &A.V, bar, my_hb * 64,
                              y, z, policy);
+          }
+          if (gap) {
+            ok = warp_wait(bGap, gap_ctr++ & 1);
+            for (int r = lane; r < kCKeys && ok; r += 32) {
+              const int k = kt0 + r;
+              if (k < p.klo || k >= p.khi || some_row_sees(seen, p.pos0, p.n_tok, k, k + 1)) continue;
+              for (int u = 0; u < SM::kBoxes * 8; ++u)
+                reinterpret_cast<uint4*>(smem + SM::kRing + ch * SM::kTile + u / 8 * 16384 + r * 128)[u % 8] =
+                    make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bFull + 8 * ch);
           }
           ++chunk_ctr;
         }
@@ -1181,7 +1253,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
                   A.mask.first_key ? A.mask.first_key[tok] : 0, A.mask.window, lo, hi);
         if (SHAPE & kBias) slope = A.slopes[hq] * kLog2e;
       }
-      const float sc = SHAPE ? 1.f : scale_log2;
+      const float sc = SHAPE & (kCap | kBias) ? 1.f : scale_log2;
       const float cap2 = A.cap.log2, u2 = A.cap.twice_inverse;
       float m_run = -INFINITY, l_run = 0.f;
       for (int i = 0; i < my_steps; ++i) {
@@ -1525,6 +1597,23 @@ static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stre
   return cudaLaunchKernelEx(&cfg, chunk_attn_kernel<D, SHAPE>, a);
 }
 
+template <int D>
+static cudaError_t launch_shape(int shape, const ChunkArgs& a, int grid, cudaStream_t stream) {
+  switch (shape) {
+#define LAUNCH_SHAPE(S) \
+  case S: return launch_attn_t<D, S>(a, grid, stream); \
+  case S | kDocs: return launch_attn_t<D, S | kDocs>(a, grid, stream)
+    LAUNCH_SHAPE(0);
+    LAUNCH_SHAPE(kBias);
+    LAUNCH_SHAPE(kCap);
+    LAUNCH_SHAPE(kCap | kBias);
+    LAUNCH_SHAPE(kCap | kWideCap);
+    LAUNCH_SHAPE(kCap | kWideCap | kBias);
+#undef LAUNCH_SHAPE
+  }
+  return cudaErrorInvalidValue;
+}
+
 // block_table == nullptr: dense caches [B, Hkv, S_cap, D]. page_size: a multiple of 16.
 cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* block_table,
                               int max_pages, int page_size, int n_pages, const int32_t* cu_new, const int32_t* kv_len,
@@ -1544,6 +1633,7 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
   a.mask = MaskArgs{first_key, prefix_len, window};
   a.blocks = reinterpret_cast<const PlanBlock*>(ws + lay.blocks);
   a.head = reinterpret_cast<const PlanHead*>(ws + lay.head);
+  a.seen = reinterpret_cast<const uint32_t*>(ws + lay.seen);
   a.part_o = reinterpret_cast<float*>(ws + lay.part_o);
   a.part_ml = reinterpret_cast<float*>(ws + lay.part_ml);
   a.count = reinterpret_cast<uint32_t*>(ws + lay.count);
@@ -1577,19 +1667,14 @@ cudaError_t launch_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint1
     a.blocks = nullptr;
   } else {
     chunk_plan_kernel<<<1, kPlanThreads, 0, stream>>>(a.plan, reinterpret_cast<PlanBlock*>(ws + lay.blocks),
-                                                      reinterpret_cast<PlanHead*>(ws + lay.head));
+                                                      reinterpret_cast<PlanHead*>(ws + lay.head),
+                                                      reinterpret_cast<uint32_t*>(ws + lay.seen));
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  using Launch = cudaError_t (*)(const ChunkArgs&, int, cudaStream_t);
-  constexpr int kWide = kCap | kWideCap;
-  static const Launch launch[2][6] = {
-      {launch_attn_t<64, 0>, launch_attn_t<64, kBias>, launch_attn_t<64, kCap>, launch_attn_t<64, kCap | kBias>,
-       launch_attn_t<64, kWide>, launch_attn_t<64, kWide | kBias>},
-      {launch_attn_t<128, 0>, launch_attn_t<128, kBias>, launch_attn_t<128, kCap>, launch_attn_t<128, kCap | kBias>,
-       launch_attn_t<128, kWide>, launch_attn_t<128, kWide | kBias>}};
-  const int cap = softcap > kNarrowCap ? 2 : softcap > 0.f ? 1 : 0;
-  return launch[D == 128][2 * cap + (slopes ? 1 : 0)](a, grid, stream);
+  const int shape = (softcap > kNarrowCap ? kCap | kWideCap : softcap > 0.f ? kCap : 0) | (slopes ? kBias : 0) |
+                    (first_key ? kDocs : 0);
+  return D == 128 ? launch_shape<128>(shape, a, grid, stream) : launch_shape<64>(shape, a, grid, stream);
 }
 
 }  // namespace libraspec

@@ -415,3 +415,44 @@ def test_blocks_that_see_nothing_read_nothing(n, kv, page):
     O, lse, status = run(Q, K, V, table, cu, kvl, first_key=first)
     assert status == 0
     assert_close(O, lse, *attend64(Q.double(), keys, values, n, kv, 0.125, first_key=first))
+
+
+@pytest.mark.parametrize("d,page", [(64, 0), (128, 16), (64, 48)])
+@pytest.mark.parametrize("opts", [dict(), dict(slopes=torch.full((8,), 0.5), softcap=20.0), dict(prefix=True)])
+def test_keys_of_rows_that_see_nothing_need_not_exist(d, page, opts):
+    """Padding within a sequence: rows that see no key, whose own keys no other row sees. Neither what their cache rows
+    hold (not a number), nor the pages that hold nothing else, take part: whole blocks of them, at the end of a block,
+    and between rows of the same block that see keys on both sides."""
+    n, kv, Hq, Hkv = [200, 1, 3], [10, 130, 0], 8, 2
+    Q, K, V, table, cu, kvl, keys, values = inputs(n, kv, Hq, Hkv, d, page, 77, extra=40)
+    first = torch.zeros(204, dtype=torch.int32)
+    first[40:120] = 100000        # positions 50 .. 129: in two or three blocks
+    first[120:190] = 130          # the rows behind them start over
+    first[190:200] = 2**31 - 1    # the sequence's end
+    first[200] = 131              # a decode step that sees nothing
+    first[201:] = 3
+    o = {k: v for k, v in opts.items() if k != "prefix"}
+    if opts.get("prefix"):        # what is seen below 171 is seen as far as there; and a gap behind it
+        o["prefix_len"] = torch.tensor([171, 0, 0], dtype=torch.int32)
+        first[:30], first[30:40] = 100000, 150
+        first[165:176], first[176:190] = 100000, 186
+    want = attend64(Q.double(), keys, values, n, kv, d ** -0.5, first_key=first, **o)
+    at = 0
+    for b in range(3):
+        N = n[b] + kv[b]
+        k, p = torch.arange(N)[None], torch.arange(kv[b], N)[:, None]
+        hi = torch.maximum(p + 1, o["prefix_len"][b] if "prefix_len" in o else torch.tensor(0))
+        seen = ((k >= first[at:at + n[b]][:, None]) & (k < hi)).any(0)
+        assert not bool(seen.all())
+        at += n[b]
+        for s in range(N):
+            if not seen[s]:
+                (K[table[b, s // page], :, s % page] if page else K[b, :, s])[:] = float("nan")
+                (V[table[b, s // page], :, s % page] if page else V[b, :, s])[:] = float("nan")
+        if page:
+            for i in range(table.shape[1]):
+                if not bool(seen[i * page:(i + 1) * page].any()):
+                    table[b, i] = 10**6
+    O, lse, status = run(Q, K, V, table, cu, kvl, first_key=first, **o)
+    assert status == 0
+    assert_close(O, lse, *want)
