@@ -75,6 +75,8 @@ class PagedSequences:
 
     def _layer(self, l, qkv, step, lse, options):
         Hq, Hkv, pool = self.Hq, self.Hkv, self.pools[l]
+        if qkv.shape != (step.T, Hq + 2 * Hkv, self.d):  # (rows of no sequence would come back unwritten)
+            raise ValueError("qkv must be [%d, %d, %d], got %s" % (step.T, Hq + 2 * Hkv, self.d, tuple(qkv.shape)))
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
         q = binding.libraspec_rope_append_paged(q, k, v, pool["Kp"], pool["Vp"], self.block_table, step.cu_new,
                                                 self.kv_len, self.freqs, self.ws, interleaved=self.interleaved)

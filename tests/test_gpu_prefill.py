@@ -97,3 +97,11 @@ def test_layers_on_another_stream_keep_the_order_of_the_steps():
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert a.lengths == b.lengths == b.kv_len.tolist()
     assert all(torch.equal(p[n], q[n]) for p, q in zip(a.pools, b.pools) for n in p)
+
+
+def test_layer_refuses_rows_of_another_step():
+    seqs = prefill.PagedSequences(1, 2, 32, 4, 2, 64, lr.RopeFreqs(64), 40, page_size=16)
+    step = seqs.begin([3, 5])
+    for shape in ((9, 8, 64), (7, 8, 64), (8, 9, 64), (8, 7, 64), (8, 8, 128), (8, 512)):
+        with pytest.raises(ValueError):
+            seqs.layer(0, torch.zeros(shape, device=cuda()), step)
