@@ -608,6 +608,12 @@ def _heads_stride(t: torch.Tensor, dtype, name: str, shape=None) -> int:
     return t.stride(0) if T > 1 and t.numel() else H * d
 
 
+def _check_device(t: torch.Tensor, name: str) -> None:
+    """Frequencies and workspaces may be made on the host; kernels take them on the device."""
+    if not t.is_cuda:
+        raise ValueError("%s must be on a CUDA device" % name)
+
+
 def _out(shape, dtype, device, stream) -> torch.Tensor:
     """An output of a call, made on the stream that it runs on: what the current stream has given back may still be in
     use there, where nothing orders the call's stream behind it."""
@@ -626,6 +632,7 @@ def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y
     shape = X.shape
     T, H, d = shape
     _req(pos, torch.int32, "pos", (T,))
+    _check_device(freqs.turns, "freqs")
     if Y is None:
         Y = _out(shape, dt, X.device, stream)
         ys = H * d
@@ -692,6 +699,8 @@ def _rope_append(Q, K, V, Kc, Vc, block_table, cu_new, kv_len, freqs, ws, pos, i
     S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
     if pos is not None:
         _req(pos, torch.int32, "pos", (T,))
+    _check_device(freqs.turns, "freqs")
+    _check_device(ws.buf, "the workspace")
     Hq = qs = 0
     if Q is not None:
         qs = _heads_stride(Q, dt, "Q")
@@ -766,6 +775,7 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
     B = _check_new(cu_new, kv_len)
     Hkv = Kc.shape[1] if isinstance(Kc, torch.Tensor) and Kc.dim() == 4 else 0
     S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
+    _check_device(ws.buf, "the workspace")
     opts = None
     if softcap or slopes is not None or window or first_key is not None or prefix_len is not None:
         if slopes is not None:

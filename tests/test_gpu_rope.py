@@ -303,3 +303,23 @@ def test_rope_append_gives_a_row_of_two_sequences_to_the_first(T, B):
         assert_rotated(Kd[b, :, pos].transpose(0, 1), want[:, 2:4], length[:, 2:4], True)
         assert torch.equal(Vd[b, :, pos].transpose(0, 1).cpu(), x[lo:hi, 4:].to(torch.bfloat16))
     assert int((Vd != 0).any(-1).sum()) == 2 * T
+
+
+def test_host_memory_is_refused():
+    """Frequencies and workspaces that were made on the host do not reach a kernel."""
+    d = 64
+    X = torch.zeros((4, 4, d), device=cuda(), dtype=torch.bfloat16)
+    pos = torch.zeros(4, dtype=torch.int32, device=cuda())
+    cu, kvl = torch.tensor([0, 4], dtype=torch.int32, device=cuda()), torch.zeros(1, dtype=torch.int32, device=cuda())
+    Kd, Vd = (torch.zeros((1, 1, 8, d), dtype=torch.bfloat16, device=cuda()) for _ in range(2))
+    fr, ws = lr.RopeFreqs(d), lr.ChunkWorkspace(4, 1, 2, 1, d)
+    host_fr, host_ws = lr.RopeFreqs(d, device="cpu"), lr.ChunkWorkspace(4, 1, 2, 1, d, device="cpu")
+    q, k, v = X[:, :2], X[:, 2:3], X[:, 3:]
+    for call in (lambda: lr.libraspec_rope(X, pos, host_fr),
+                 lambda: lr.libraspec_rope_append(q, k, v, Kd, Vd, cu, kvl, host_fr, ws),
+                 lambda: lr.libraspec_rope_append(q, k, v, Kd, Vd, cu, kvl, fr, host_ws),
+                 lambda: lr.libraspec_chunk_attn(q.contiguous(), Kd, Vd, cu, kvl, host_ws)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert int((Kd != 0).sum()) == 0 and lr.libraspec_get_status(ws) == 0
