@@ -460,7 +460,8 @@ int libraspec_kv_append_paged(const uint16_t* kv_new, uint16_t* const* Kp, uint1
  * Writes turns [rot_dim / 2, 2] f32, a HOST array: f_i / (2 pi) as hi + lo, so
  * that kernels know a position's angle to 2^-24 of a turn however long the
  * context. Copy it to the device once per model. rot_dim even, theta > 0 and
- * finite, factor > 0 and finite (with a scaling), low < high and original_len > 0 (by parts).
+ * finite, factor > 0 and finite (with a scaling), low < high,
+ * original_len > 0 (by parts) and no f_i / (2 pi) above 1e29, else LIBRASPEC_EINVAL.
  */
 #define LIBRASPEC_ROPE_PLAIN 0
 #define LIBRASPEC_ROPE_LINEAR 1

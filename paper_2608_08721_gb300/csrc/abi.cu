@@ -29,7 +29,7 @@ cudaError_t launch_lm_head_stats(const uint16_t*, const uint16_t*, const float*,
                                  float*, int32_t*, float*, char*, cudaStream_t);
 cudaError_t launch_kv_append(const uint16_t*, uint16_t* const*, uint16_t* const*, int, const int32_t*,
                              const int32_t*, int, int, int, int, int, int, int, int, int*, cudaStream_t);
-void rope_frequencies(int, double, int, double, double, double, double, float*);
+bool rope_frequencies(int, double, int, double, double, double, double, float*);
 template <typename T>
 cudaError_t launch_rope(const T*, long long, const int32_t*, const float*, float, int, int, int, int, int, int, T*,
                         long long, cudaStream_t);
@@ -450,8 +450,8 @@ int libraspec_rope_frequencies(int rot_dim, double theta, int scaling, double fa
   if (scaling == LIBRASPEC_ROPE_NTK && rot_dim == 2) return LIBRASPEC_EINVAL;
   if (scaling == LIBRASPEC_ROPE_BY_PARTS && (!(low < high) || !pos_finite(original_len) || !(low > -1e300) || !(high < 1e300)))
     return LIBRASPEC_EINVAL;
-  rope_frequencies(rot_dim, theta, scaling, factor, low, high, original_len, turns);
-  return LIBRASPEC_OK;
+  return rope_frequencies(rot_dim, theta, scaling, factor, low, high, original_len, turns) ? LIBRASPEC_OK
+                                                                                           : LIBRASPEC_EINVAL;
 }
 
 extern "C++" {

@@ -283,8 +283,9 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
-// Turns per position of each pair as (hi, lo) floats; scaling as in the header.
-void rope_frequencies(int rot, double theta, int scaling, double factor, double low, double high, double original_len,
+// Turns per position of each pair as (hi, lo) floats; scaling as in the header. False if one of them is beyond what the
+// kernels multiply with a position in binary32.
+bool rope_frequencies(int rot, double theta, int scaling, double factor, double low, double high, double original_len,
                       float* turns) {
   const double two_pi = 6.283185307179586476925;
   if (scaling == LIBRASPEC_ROPE_NTK) theta *= std::pow(factor, rot / (rot - 2.0));
@@ -297,9 +298,11 @@ void rope_frequencies(int rot, double theta, int scaling, double factor, double 
       f = (1.0 - keep) * f / factor + keep * f;
     }
     const double t = f / two_pi;
+    if (!(t <= 1e29)) return false;  // (times 2^31: finite)
     turns[2 * i] = (float)t;
     turns[2 * i + 1] = (float)(t - (double)turns[2 * i]);
   }
+  return true;
 }
 
 template <typename Tin, typename Tout, int N, bool APPEND, int TOKENS>

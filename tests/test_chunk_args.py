@@ -140,3 +140,11 @@ def test_binding_names_what_is_wrong():
         lr.libraspec_rope(x, x, None)
     with pytest.raises(TypeError, match="^K must be"):
         lr.libraspec_rope_append(None, x.half(), x, x, x, x, x, None, None)
+
+
+def test_frequencies_that_no_float_holds_are_refused(lib):
+    out = torch.empty((32, 2))
+    f = lib.libraspec_rope_frequencies
+    assert f(64, 1e-30, 0, 1.0, 1.0, 32.0, 0.0, out.data_ptr()) == lr.OK and bool(torch.isfinite(out).all())
+    assert f(64, 1e-300, 0, 1.0, 1.0, 32.0, 0.0, out.data_ptr()) == lr.EINVAL
+    assert f(64, 10000.0, 1, 1e-300, 1.0, 32.0, 0.0, out.data_ptr()) == lr.EINVAL
