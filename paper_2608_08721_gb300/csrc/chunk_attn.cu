@@ -1577,12 +1577,14 @@ static bool make_map(CUtensorMap* map, const void* base, int D, long long rows, 
 template <int D, int SHAPE>
 static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stream) {
   using SM = ChunkSmem<D>;
-  static bool configured = false;
-  if (!configured) {
-    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D, SHAPE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         SM::kBytes);
+  static int configured = -1;  // the device whose kernel may use as much shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev != configured) {
+    e = cudaFuncSetAttribute(chunk_attn_kernel<D, SHAPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes);
     if (e != cudaSuccess) return e;
-    configured = true;
+    configured = dev;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
