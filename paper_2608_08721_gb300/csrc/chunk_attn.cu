@@ -533,7 +533,7 @@ struct ChunkSmem {
   // qempty, drain, gap
   static constexpr int kNumBars = 2 * kChunks + 14 + 4;
   static constexpr int kInfo = kBar + (8 * kNumBars + 63) / 64 * 64;
-  static constexpr int kMisc = kInfo + 2 * 64;           // [0] abort, [1] this CTA merges, [2] tensor-memory address
+  static constexpr int kMisc = kInfo + 2 * 64;           // [0] misaligned, [1] this CTA merges, [2] tensor memory
   static constexpr int kStat = kMisc + 16;               // (m, l) of each stream's rows (streams to be combined)
   static constexpr int kBytes = kStat + kCStreams * kCRows * 8;
   // tensor memory: scores, of each stream (D = 64) or of the step at hand (128: no room for two), P and O of each
@@ -560,20 +560,8 @@ constexpr int kCAllBar = 1;
 // A wait that the first ask did not end.
 __device__ __noinline__ bool slow_wait(uint32_t bar, uint32_t parity) { return warp_wait(bar, parity); }
 
-__device__ __forceinline__ void c_fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
-  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
-      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
-      : "=f"(d0), "=f"(d1)
-      : "f"(a0), "f"(a1), "f"(b), "f"(c));
-}
-__device__ __forceinline__ void c_add2(float& d0, float& d1, float a0, float a1) {
-  asm("{\n\t.reg .b64 a, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 d, {%0, %1};\n\t"
-      "add.rn.f32x2 d, d, a;\n\tmov.b64 {%0, %1}, d;\n\t}"
-      : "+f"(d0), "+f"(d1)
-      : "f"(a0), "f"(a1));
-}
 // (d0, d1) = (a0, a1) * b + (c0, c1)
-__device__ __forceinline__ void c_fma2v(float& d0, float& d1, float a0, float a1, float b, float c0, float c1) {
+__device__ __forceinline__ void fma2v(float& d0, float& d1, float a0, float a1, float b, float c0, float c1) {
   asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %6};\n\t"
       "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
       : "=f"(d0), "=f"(d1)
@@ -1048,10 +1036,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           }
         }
       }
-      if (!ok) {
-        if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-        misc[0] = 1;
-      }
+      if (!ok && lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
       // before leaving, wait (bounded) for the copies still in flight
       if (lane == 0) {
         for (uint32_t k = 0; k < (uint32_t)SM::kChunks && k < chunk_ctr; ++k) {
@@ -1197,10 +1182,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
           }
         }
       }
-      if (!ok) {
-        if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-        misc[0] = 1;
-      }
+      if (!ok && lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
       // every MMA issued has completed before the tensor memory is released
       mma_commit_warp(bDrain);
       warp_wait(bDrain, 0);
@@ -1316,17 +1298,17 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll
               for (int c = 0; c < 32; c += 2) {
                 float a, b;
-                c_fma2(a, b, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), u2, 0.f);
+                fma2(a, b, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), u2, 0.f);
                 a = ex2_approx(a);
                 b = ex2_approx(b);
-                c_add2(a, b, 1.f, 1.f);
+                add2(a, b, 1.f, 1.f);
                 a = rcp_approx(a);
                 b = rcp_approx(b);
                 if constexpr (SHAPE & kWideCap) {
                   a = wide_cap(__uint_as_float(x[q][c]), a, scale_log2, A.cap);
                   b = wide_cap(__uint_as_float(x[q][c + 1]), b, scale_log2, A.cap);
                 } else {
-                  c_fma2(a, b, a, b, -2.f * cap2, cap2);
+                  fma2(a, b, a, b, -2.f * cap2, cap2);
                 }
                 x[q][c] = __float_as_uint(a);
                 x[q][c + 1] = __float_as_uint(b);
@@ -1349,8 +1331,8 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll
               for (int c = 0; c < 32; c += 2) {
                 float y0, y1;
-                c_fma2v(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), to_log2,
-                        fmaf(slope, (float)(32 * q + c), b0), fmaf(slope, (float)(32 * q + c + 1), b0));
+                fma2v(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), to_log2,
+                      fmaf(slope, (float)(32 * q + c), b0), fmaf(slope, (float)(32 * q + c + 1), b0));
                 x[q][c] = __float_as_uint(y0);
                 x[q][c + 1] = __float_as_uint(y1);
               }
@@ -1406,14 +1388,14 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
 #pragma unroll
           for (int c = 0; c < 32; c += 4) {
             float y0, y1, y2, y3;
-            c_fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), sc, neg_m);
-            c_fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), sc, neg_m);
+            fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), sc, neg_m);
+            fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), sc, neg_m);
             y0 = ex2_approx(y0);
             y1 = ex2_approx(y1);
             y2 = ex2_approx(y2);
             y3 = ex2_approx(y3);
-            c_add2(la[0], la[1], y0, y1);
-            c_add2(lb[0], lb[1], y2, y3);
+            add2(la[0], la[1], y0, y1);
+            add2(lb[0], lb[1], y2, y3);
             pk[q][c >> 1] = c_pack(y0, y1);
             pk[q][(c >> 1) + 1] = c_pack(y2, y3);
           }
@@ -1542,10 +1524,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
       chunk_base += 2 * n_tiles;
       ++item_ctr;
     }
-    if (!ok) {
-      if (lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
-      misc[0] = 1;
-    }
+    if (!ok && lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
   }
   // every role is done with the tensor memory
   __syncwarp();
