@@ -650,7 +650,8 @@ def libraspec_rope(X, pos, freqs: RopeFreqs, interleaved=False, inverse=False, Y
 def libraspec_rope_append(Q, K, V, Kc, Vc, cu_new, kv_len, freqs: RopeFreqs, ws, pos=None, interleaved=False, Qo=None,
                           stream=None):
     """Rotates a ragged chunk's keys into the dense caches Kc, Vc [B, Hkv, S_cap, d] beside its values, and its queries
-    into Qo [T, Hq, d] bf16 (Q None: keys and values alone). Returns Qo."""
+    into Qo [T, Hq, d] bf16 (Q None: keys and values alone). ws: any of the library's workspaces (its status word).
+    Returns Qo."""
     return _rope_append(Q, K, V, Kc, Vc, None, cu_new, kv_len, freqs, ws, pos, interleaved, Qo, stream)
 
 

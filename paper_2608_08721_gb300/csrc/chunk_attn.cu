@@ -40,13 +40,13 @@
 // this tile's softmax: at D = 64 the stream's own next, at D = 128, where O
 // and P leave room for the scores of one tile only, the other stream's. (With
 // P over its scores, S waited for the PV before it: 1039 us where it now takes
-// 946, at D = 64 931 where it takes 811.) The reference maximum of a row is
+// 960, at D = 64 931 where it takes 816.) The reference maximum of a row is
 // raised only when a score exceeds it by more than 8 (a factor of 2^8), so O
 // is rarely rescaled; p <= 2^8 keeps P and O in range.
 //
 // What bounds it, with 128-wide heads: prompts, shared memory, from which S =
 // Q K^T alone reads 128 bytes a cycle, and the tensor pipe beside it: 16384
-// tokens of 8 heads over as many keys run at 1.74 PFLOP/s, where a matrix
+// tokens of 8 heads over as many keys run at 1.72 PFLOP/s, where a matrix
 // product reaches 1.92; an item's start and end cost as much as three tiles or
 // four, which is why short prompts stay further off. Capped or biased scores,
 // the softmax warps' arithmetic (a capped score takes two exponentials and a
@@ -398,8 +398,8 @@ __global__ void __launch_bounds__(kPlanThreads) chunk_plan_kernel(const PlanArgs
 }
 
 // The same for up to kWarpBlocks blocks by one warp, in its registers: lane l has blocks l and l + 32. Every CTA's
-// producer then plans for itself, and the call is one launch (a decode step of one sequence over 512 keys: 12.7 us with
-// the plan's launch, 11.1 without).
+// producer then plans for itself, and the call is one launch (a decode step of one sequence over 512 keys: 12.8 us with
+// the plan's launch, 10.9 without).
 constexpr int kWarpBlocks = 64;
 constexpr int kWarpSeqs = 512;
 
@@ -470,7 +470,7 @@ __device__ PlanHead warp_plan(const PlanArgs& a, PlanBlock (&mine)[2]) {
 // The attention kernel.
 // ---------------------------------------------------------------------------
 // What a block weighs beside its tiles, in tiles: `one` for every block, `pair` more for two row tiles. (A prompt
-// of 8192 tokens of 32 heads: 446 us at 1 and 1 + 1, 375 to 383 at 2 + 1, 374 at 2 + 2, 377 at 2 + 3 and at 3 + 2;
+// of 8192 tokens of 32 heads: 445 us at 1 + 1, 380 at 2 + 1, 372 at 2 + 2, 376 at 2 + 3 and at 3 + 2;
 // decoding is best at 2.)
 struct FixedCost {
   int one, pair;
@@ -776,7 +776,7 @@ constexpr float kFloatMax = 3.402823466e38f;
 
 // The tile that step t of n takes. With a bias by distance from the last one back: the keys nearest to the rows come
 // first and set the reference, which each tile towards the rows would raise (16384 tokens of 8 heads over as many keys:
-// 1425 us from the front, 1141 from the back; at a head dim of 64, 1385 and 1196).
+// 1457 us from the front, 1105 from the back; at a head dim of 64, 1374 and 1165).
 template <int SHAPE>
 __device__ __forceinline__ int tile_of(int t, int n) { return SHAPE & kBias ? n - 1 - t : t; }
 
@@ -1201,7 +1201,7 @@ __global__ void __launch_bounds__(kCThreads, 1) chunk_attn_kernel(const __grid_c
     const float scale_log2 = A.scale * kLog2e;
     // The quarter of a tile's keys whose probabilities are the first to be written, with those before them: by then the
     // PV that reads the tile before's should be done. (At D = 128 it comes behind an S of the other stream: 16384
-    // tokens of 8 heads over as many keys 946 us at 3, 973 at 2, 995 at 1; at D = 64, 811 at 1, 828 at 0, 840 at 3.)
+    // tokens of 8 heads over as many keys 960 us at 3, 969 at 2, 1004 at 1; at D = 64, 816 at 1, 827 at 0, 934 at 3.)
     constexpr int kFirstP = D == 64 ? 1 : 3;
     uint32_t item_ctr = 0, chunk_base = 0;
     uint32_t words = 0;             // of this stream in the items before this one

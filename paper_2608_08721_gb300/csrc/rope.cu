@@ -13,8 +13,8 @@
 // one token or two: its threads form the tokens' cosines and sines in shared
 // memory (once for all heads) while their first loads are on their way, then
 // they share out the tokens' heads in units of 16 bytes. 8192 tokens of 64
-// heads of 128 in fp32 take 79 us, the copy rate; the append of 8587 tokens of
-// 28 + 2 x 4 heads (158 MB) 30 us, 77% of it, 64 decoding tokens 3.1 us.
+// heads of 128 in fp32 take 80 us, 98% of the copy rate; the append of 8587
+// tokens of 28 + 2 x 4 heads (158 MB) 30 us, 78% of it, 64 decoding tokens 3.1.
 #include <cmath>
 #include <type_traits>
 
@@ -138,8 +138,9 @@ struct RopeUnit {
     *reinterpret_cast<Pack<Tout, N>*>(dst + partner(u, half)) = q;
   }
   // Where pair i's cosine and sine lie: two pairs of a unit side by side, then the same two of its neighbours, so that
-  // neighbouring threads read neighbouring 16 bytes of shared memory (in the pairs' own order, 8 N bytes apart, they
-  // meet in the same banks: 36 us for 8587 bf16 tokens of 36 heads, 32 so).
+  // neighbouring threads read neighbouring 16 bytes of shared memory. (In the pairs' own order, 8 N bytes apart, they
+  // meet in the same banks: 34.7 us for 8587 bf16 tokens of 36 heads, 29.8 so. Units of four fp32 elements gain
+  // nothing: 27.1 and 28.1 for 8192 tokens of 48 heads of 64.)
   __device__ static __forceinline__ int slot(int i, int half) {
     if (N == 1) return i;
     const int e = i % N;
@@ -249,8 +250,8 @@ __global__ void __launch_bounds__(kRopeThreads, 3) rope_kernel(const RopeArgs A)
     }
     s_row[j] = at;
   }
-  // The first units, in flight while the cosines are formed. (Ahead of the look-ups, which then queue behind them:
-  // 32 us for 8587 bf16 tokens of 36 heads; so, 30.)
+  // The first units, in flight while the cosines are formed. (Ahead of the page's look-up, which then queues behind
+  // them: 30.3 us for 8587 bf16 tokens of 36 heads; so, 29.8.)
   if (h < heads) load(h, unit);
   for (int i = tid; i < n_tok * A.half; i += blockDim.x) {
     const int j = TOKENS == 1 ? 0 : i / A.half, k = i - j * A.half;
@@ -314,9 +315,9 @@ static cudaError_t launch_tokens(const RopeArgs& a, int interleaved, int threads
 }
 
 // Two tokens a CTA, with a thread for each of a token's units, where a CTA has room for them and every SM gets a few
-// CTAs; else one token in passes of up to 256 threads over its heads. (8587 bf16 tokens of 36 heads: 32 us at two
-// tokens, 34 at one, 41 at four; in passes of 256 threads, which leave 7 of 8 warps idle in the second, slower
-// still. 8192 fp32 tokens of 64 heads: 79 us in passes of 256 threads, 84 in passes of 512.)
+// CTAs; else one token in passes of up to 256 threads over its heads. (8587 bf16 tokens of 36 heads: 29.8 us at two
+// tokens, 37 at one, 39 at four; in passes of 256 threads, which leave 7 of 8 warps idle in the second, slower still.
+// 8192 fp32 tokens of 64 heads: 80 us in passes of 256 threads, 82 in passes of 512.)
 template <typename Tin, typename Tout, int N, bool APPEND>
 static cudaError_t launch_n(const RopeArgs& a, int interleaved, cudaStream_t stream) {
   const int per_head = a.d / (2 * N), heads = APPEND ? a.Hq + 2 * a.Hkv : a.Hq;
