@@ -534,6 +534,98 @@ int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const 
                                      void* stream);
 
 /*
+ * Norm of query and key heads with their rotation, in one pass (models that
+ * norm each head before it turns): for every head x of a token
+ *   y = x w / sqrt(mean(x^2) + eps),   Y = libraspec_rope's rotation of y.
+ * X, Y [T, Hq + Hk, head_dim] f32 (or bf16, computed in binary32 and rounded
+ * once), laid out and strided as for libraspec_rope: heads 0 .. Hq - 1 take
+ * q_weight, the others k_weight (both [head_dim] f32; queries and keys lie side
+ * by side in a projection's output; Hq or Hk may be 0, its weights then NULL).
+ * eps >= 0 and finite; a head of zeros with eps = 0 gives NaN. The norm is of
+ * the whole head, rotated or not. Y may be X with the same stride; else they
+ * must not overlap. Limits as for libraspec_rope. One launch, no workspace.
+ */
+int libraspec_qk_norm_rope(const float* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude,
+                           const float* q_weight, const float* k_weight, float eps, int T, int Hq, int Hk, int head_dim,
+                           int rot_dim, int interleaved, float* Y, int64_t y_stride, void* stream);
+int libraspec_qk_norm_rope_bf16(const uint16_t* X, int64_t x_stride, const int32_t* pos, const float* turns,
+                                float magnitude, const float* q_weight, const float* k_weight, float eps, int T, int Hq,
+                                int Hk, int head_dim, int rot_dim, int interleaved, uint16_t* Y, int64_t y_stride,
+                                void* stream);
+
+/*
+ * The KV cache in 8 bits. Keys and values are e4m3 codes c (a sign, four bits
+ * of exponent, three behind the leading one; passed as uint8_t) with a scale
+ * for every block of `block` tokens of a kv head, a power of two held as its
+ * exponent e in one byte, e + 127: the values are c 2^e, exact in bf16.
+ *   K8, V8  [B, Hkv, S_cap, head_dim] or page pools [n_pages, Hkv, page_size,
+ *           head_dim] (16-byte aligned); Ks, Vs [B, Hkv, S_cap / block] or
+ *           [n_pages, Hkv, page_size / block];
+ *   block   16, 32 or 64 (else LIBRASPEC_EUNSUPPORTED), a divisor of S_cap or
+ *           page_size (else LIBRASPEC_EINVAL).
+ * Scales outside [2^-60, 2^60] are read as the nearer end.
+ *
+ * libraspec_rope_append_q8: libraspec_rope_append into such a cache, with the
+ * norm of libraspec_qk_norm_rope on queries and keys before their rotation if
+ * the weights are given (both or neither). Keys and values are formed in
+ * binary32; with amax the largest finite magnitude among a block's new keys (or
+ * values), the block's exponent is floor(log2 amax) - 7 within [-60, 60]. A
+ * block whose first rows the sequence has already takes the larger of that and
+ * its own, and if it grows those rows' codes are rounded again, to it. Codes
+ * are rounded to the nearest, ties to even; magnitudes above 448 2^e, infinities
+ * among them, become 448 2^e, NaN stays NaN. Rows of a block behind the
+ * sequence's last keep their codes. Sequences write to blocks of their own: two
+ * that share a page must not write to the same block. Where ranges overlap
+ * (beside offsets that decrease), each sequence appends its range as far as the
+ * call's work list reaches (LIBRASPEC_ST_BAD_LENGTH is set), and a query takes
+ * the first's position. One launch.
+ *
+ * libraspec_kv_read_q8: what the cache holds, as bf16: row cu[b] + j of K and V
+ * [T, Hkv, head_dim] (packed, 16-byte aligned) is key start[b] + j of sequence
+ * b, cu [B+1] as cu_new above, start [B] i32. Rows of no sequence are left
+ * alone, and rows that cannot be read: past the capacity
+ * (LIBRASPEC_ST_KV_OVERFLOW), or in a page outside [0, n_pages)
+ * (LIBRASPEC_ST_BAD_PAGE). (With pos = 0, libraspec_rope_append_bf16 puts them into
+ * a 16-bit cache, for the tree calls, say.) One launch.
+ *
+ * head_dim in {64, 128}. The workspace holds the status word only (>= 256 bytes).
+ */
+int libraspec_rope_append_q8(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                             int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                             const float* turns, float magnitude, const float* q_weight, const float* k_weight, float eps,
+                             int T, int B, int Hq, int Hkv, int head_dim, int rot_dim, int interleaved, uint16_t* Qo,
+                             uint8_t* K8, uint8_t* V8, uint8_t* Ks, uint8_t* Vs, int S_cap, int block, void* workspace,
+                             size_t ws_bytes, void* stream);
+int libraspec_rope_append_q8_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                                  const uint16_t* V, int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len,
+                                  const int32_t* pos, const float* turns, float magnitude, const float* q_weight,
+                                  const float* k_weight, float eps, int T, int B, int Hq, int Hkv, int head_dim,
+                                  int rot_dim, int interleaved, uint16_t* Qo, uint8_t* K8, uint8_t* V8, uint8_t* Ks,
+                                  uint8_t* Vs, int S_cap, int block, void* workspace, size_t ws_bytes, void* stream);
+int libraspec_rope_append_q8_paged(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                                   int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                                   const float* turns, float magnitude, const float* q_weight, const float* k_weight,
+                                   float eps, int T, int B, int Hq, int Hkv, int head_dim, int rot_dim, int interleaved,
+                                   uint16_t* Qo, uint8_t* K8, uint8_t* V8, uint8_t* Ks, uint8_t* Vs,
+                                   const int32_t* block_table, int max_pages, int page_size, int n_pages, int block,
+                                   void* workspace, size_t ws_bytes, void* stream);
+int libraspec_rope_append_q8_paged_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                                        const uint16_t* V, int64_t v_stride, const int32_t* cu_new,
+                                        const int32_t* kv_len, const int32_t* pos, const float* turns, float magnitude,
+                                        const float* q_weight, const float* k_weight, float eps, int T, int B, int Hq,
+                                        int Hkv, int head_dim, int rot_dim, int interleaved, uint16_t* Qo, uint8_t* K8,
+                                        uint8_t* V8, uint8_t* Ks, uint8_t* Vs, const int32_t* block_table,
+                                        int max_pages, int page_size, int n_pages, int block, void* workspace,
+                                        size_t ws_bytes, void* stream);
+int libraspec_kv_read_q8(const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks, const uint8_t* Vs, const int32_t* cu,
+                         const int32_t* start, int T, int B, int Hkv, int head_dim, int S_cap, int block, uint16_t* K,
+                         uint16_t* V, void* workspace, size_t ws_bytes, void* stream);
+int libraspec_kv_read_q8_paged(const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks, const uint8_t* Vs,
+                               const int32_t* block_table, int max_pages, int page_size, int n_pages, const int32_t* cu,
+                               const int32_t* start, int T, int B, int Hkv, int head_dim, int block, uint16_t* K,
+                               uint16_t* V, void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Attention of a chunk of new tokens over the cache, one layer: a prompt, a
  * part of one, the single token of a decode step, or all of them in one call.
  * The chunk's keys and values are in the cache already. Query row (b, j) at

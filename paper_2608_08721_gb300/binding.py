@@ -26,6 +26,7 @@ MAX_TREE_NODES = 512
 _P, _I, _U32, _U64, _F, _SZ = (ctypes.c_void_p, ctypes.c_int, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
                                ctypes.c_size_t)
 _I64, _D = ctypes.c_int64, ctypes.c_double
+_Q8_HEAD = [_P, _I64] * 3 + [_P] * 4 + [_F, _P, _P, _F] + [_I] * 7 + [_P] * 5  # of the appends to a cache in 8 bits
 SIGNATURES = {
     "libraspec_version": (ctypes.c_char_p, []),
     "libraspec_status_string": (ctypes.c_char_p, [_I]),
@@ -70,6 +71,14 @@ SIGNATURES = {
                                     [_P, _SZ, _P]),
     "libraspec_rope_append_paged_bf16": (_I, [_P, _I64] * 3 + [_P] * 4 + [_F] + [_I] * 7 + [_P] * 4 + [_I] * 3 +
                                          [_P, _SZ, _P]),
+    "libraspec_qk_norm_rope": (_I, [_P, _I64, _P, _P, _F, _P, _P, _F] + [_I] * 6 + [_P, _I64, _P]),
+    "libraspec_qk_norm_rope_bf16": (_I, [_P, _I64, _P, _P, _F, _P, _P, _F] + [_I] * 6 + [_P, _I64, _P]),
+    "libraspec_rope_append_q8": (_I, _Q8_HEAD + [_I, _I, _P, _SZ, _P]),
+    "libraspec_rope_append_q8_bf16": (_I, _Q8_HEAD + [_I, _I, _P, _SZ, _P]),
+    "libraspec_rope_append_q8_paged": (_I, _Q8_HEAD + [_P, _I, _I, _I, _I, _P, _SZ, _P]),
+    "libraspec_rope_append_q8_paged_bf16": (_I, _Q8_HEAD + [_P, _I, _I, _I, _I, _P, _SZ, _P]),
+    "libraspec_kv_read_q8": (_I, [_P] * 6 + [_I] * 6 + [_P, _P, _P, _SZ, _P]),
+    "libraspec_kv_read_q8_paged": (_I, [_P] * 5 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_P, _P, _P, _SZ, _P]),
     "libraspec_chunk_workspace_size": (_SZ, [_I] * 5),
     "libraspec_chunk_attn": (_I, [_P] * 5 + [_I] * 6 + [_F] + [_P] * 4 + [_SZ, _P]),
     "libraspec_chunk_attn_paged": (_I, [_P] * 4 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_F] + [_P] * 4 + [_SZ, _P]),
@@ -728,6 +737,175 @@ def _rope_append(Q, K, V, Kc, Vc, block_table, cu_new, kv_len, freqs, ws, pos, i
     if rc != OK:
         _check(rc, name)
     return Qo
+
+
+class QkNorm:
+    """Weights of the norm of query and key heads [d] (f32, on the device) and what is added to the mean square."""
+
+    def __init__(self, q_weight: torch.Tensor, k_weight: torch.Tensor, eps: float = 1e-6):
+        _req(q_weight, torch.float32, "q_weight")
+        if q_weight.dim() != 1:
+            raise ValueError("q_weight must be [d], got %s" % (tuple(q_weight.shape),))
+        _req(k_weight, torch.float32, "k_weight", q_weight.shape)
+        self.q_weight, self.k_weight, self.eps, self.d = q_weight, k_weight, float(eps), q_weight.shape[0]
+        self.q_ptr, self.k_ptr = q_weight.data_ptr(), k_weight.data_ptr()
+
+
+def _check_norm(norm, d) -> None:
+    if norm.d != d:
+        raise ValueError("norm: weights of %d elements for heads of %d" % (norm.d, d))
+
+
+def libraspec_qk_norm_rope(X, n_q: int, norm: QkNorm, pos, freqs: RopeFreqs, interleaved=False, Y=None,
+                           stream=None) -> torch.Tensor:
+    """X [T, H, d] (f32 or bf16), queries and keys side by side: each head over its root mean square, times the weights
+    of queries (the first n_q heads) or keys, then rotated to the positions pos [T] int32. Y may be X (in place)."""
+    bf16 = isinstance(X, torch.Tensor) and X.dtype == torch.bfloat16
+    dt = torch.bfloat16 if bf16 else torch.float32
+    xs = _heads_stride(X, dt, "X")
+    shape = X.shape
+    T, H, d = shape
+    if not 0 <= n_q <= H:
+        raise ValueError("n_q must lie in [0, %d], got %s" % (H, n_q))
+    _check_norm(norm, d)
+    _req(pos, torch.int32, "pos", (T,))
+    _check_device(freqs.turns, "freqs")
+    if Y is None:
+        Y = _out(shape, dt, X.device, stream)
+        ys = H * d
+    else:
+        ys = _heads_stride(Y, dt, "Y", shape)
+    lib = load()
+    rc = (lib.libraspec_qk_norm_rope_bf16 if bf16 else lib.libraspec_qk_norm_rope)(
+        X.data_ptr(), xs, pos.data_ptr(), freqs.turns_ptr, freqs.magnitude, norm.q_ptr, norm.k_ptr, norm.eps, T, n_q,
+        H - n_q, d, freqs.rot_dim, 1 if interleaved else 0, Y.data_ptr(), ys, _stream(stream))
+    if rc != OK:
+        _check(rc, "libraspec_qk_norm_rope_bf16" if bf16 else "libraspec_qk_norm_rope")
+    return Y
+
+
+def _check_caches_q8(K8, V8, Ks, Vs, block_table, B):
+    """Codes and exponents of a cache in 8 bits; returns (Hkv, d, capacity, max_pages, page_size, n_pages, block)."""
+    paged = block_table is not None
+    _req(K8, torch.float8_e4m3fn, "K8")
+    shape = K8.shape
+    if len(shape) != 4 or not (paged or shape[0] == B):
+        raise ValueError("K8 must be %s, got %s" % ("[n_pages, Hkv, page_size, d]" if paged else "[%d, Hkv, S_cap, d]" % B,
+                                                    tuple(shape)))
+    _req(V8, torch.float8_e4m3fn, "V8", shape)
+    planes, Hkv, rows, d = shape
+    _req(Ks, torch.uint8, "Ks")
+    n = Ks.shape[2] if Ks.dim() == 3 else 0
+    if n == 0 or Ks.shape[0] != planes or Ks.shape[1] != Hkv or rows % n:
+        raise ValueError("Ks must be [%d, %d, %s / block], got %s" % (planes, Hkv, rows, tuple(Ks.shape)))
+    _req(Vs, torch.uint8, "Vs", Ks.shape)
+    if not paged:
+        return Hkv, d, rows, 0, 0, 0, rows // n
+    _req(block_table, torch.int32, "block_table")
+    t = block_table.shape
+    if len(t) != 2 or t[0] != B:
+        raise ValueError("block_table must be [B, max_pages]")
+    return Hkv, d, 0, t[1], rows, planes, rows // n
+
+
+def libraspec_rope_append_q8(Q, K, V, K8, V8, Ks, Vs, cu_new, kv_len, freqs: RopeFreqs, ws, norm: Optional[QkNorm] = None,
+                             pos=None, interleaved=False, Qo=None, stream=None):
+    """libraspec_rope_append into a cache in 8 bits: codes K8, V8 [B, Hkv, S_cap, d] float8_e4m3fn and exponents Ks, Vs
+    [B, Hkv, S_cap / block] uint8 (e + 127; block 16, 32 or 64). ``norm``: query and key heads are normed first. ws: any
+    of the library's workspaces (its status word). Returns Qo [T, Hq, d] bf16, or None without Q."""
+    return _rope_append_q8(Q, K, V, K8, V8, Ks, Vs, None, cu_new, kv_len, freqs, ws, norm, pos, interleaved, Qo, stream)
+
+
+def libraspec_rope_append_q8_paged(Q, K, V, K8, V8, Ks, Vs, block_table, cu_new, kv_len, freqs: RopeFreqs, ws,
+                                   norm: Optional[QkNorm] = None, pos=None, interleaved=False, Qo=None, stream=None):
+    """libraspec_rope_append_q8 into page pools K8, V8 [n_pages, Hkv, page_size, d] with exponents [n_pages, Hkv,
+    page_size / block], by block_table [B, max_pages]."""
+    return _rope_append_q8(Q, K, V, K8, V8, Ks, Vs, block_table, cu_new, kv_len, freqs, ws, norm, pos, interleaved, Qo,
+                           stream)
+
+
+def _rope_append_q8(Q, K, V, K8, V8, Ks, Vs, block_table, cu_new, kv_len, freqs, ws, norm, pos, interleaved, Qo, stream):
+    bf16 = isinstance(K, torch.Tensor) and K.dtype == torch.bfloat16
+    dt = torch.bfloat16 if bf16 else torch.float32
+    ks = _heads_stride(K, dt, "K")
+    shape = K.shape
+    T, Hkv, d = shape
+    vs = _heads_stride(V, dt, "V", shape)
+    B = _check_new(cu_new, kv_len)
+    h, dc, S_cap, max_pages, page_size, n_pages, block = _check_caches_q8(K8, V8, Ks, Vs, block_table, B)
+    if h != Hkv or dc != d:
+        raise ValueError("the cache has %d heads of %d, K %d of %d" % (h, dc, Hkv, d))
+    if pos is not None:
+        _req(pos, torch.int32, "pos", (T,))
+    _check_device(freqs.turns, "freqs")
+    _check_device(ws.buf, "the workspace")
+    q_w = k_w = None
+    eps = 0.0
+    if norm is not None:
+        _check_norm(norm, d)
+        q_w, k_w, eps = norm.q_ptr, norm.k_ptr, norm.eps
+    Hq = qs = 0
+    if Q is not None:
+        qs = _heads_stride(Q, dt, "Q")
+        shape = Q.shape
+        Hq = shape[1]
+        if shape[0] != T or shape[2] != d:
+            raise ValueError("Q must have shape [%d, Hq, %d], got %s" % (T, d, tuple(shape)))
+        if Qo is None:
+            Qo = _out(shape, torch.bfloat16, K.device, stream)
+        else:
+            _req(Qo, torch.bfloat16, "Qo", shape)
+    elif Qo is not None:
+        raise ValueError("Qo without Q")
+    lib = load()
+    name = "libraspec_rope_append_q8" + ("" if block_table is None else "_paged") + ("_bf16" if bf16 else "")
+    head = (_ptr(Q), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_new.data_ptr(), kv_len.data_ptr(), _ptr(pos),
+            freqs.turns_ptr, freqs.magnitude, q_w, k_w, eps, T, B, Hq, Hkv, d, freqs.rot_dim, 1 if interleaved else 0,
+            _ptr(Qo), K8.data_ptr(), V8.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
+    if block_table is None:
+        rc = getattr(lib, name)(*head, S_cap, block, ws.ptr, ws.nbytes, _stream(stream))
+    else:
+        rc = getattr(lib, name)(*head, block_table.data_ptr(), max_pages, page_size, n_pages, block, ws.ptr, ws.nbytes,
+                                _stream(stream))
+    if rc != OK:
+        _check(rc, name)
+    return Qo
+
+
+def libraspec_kv_read_q8(K8, V8, Ks, Vs, cu, start, T: int, ws, K=None, V=None, stream=None):
+    """Keys start[b] .. start[b] + cu[b + 1] - cu[b] - 1 of every sequence of a dense cache in 8 bits, as packed bf16 rows
+    (K, V) [T, Hkv, d]: row cu[b] + j is key start[b] + j. cu [B + 1], start [B] int32. Rows of no sequence, or that
+    cannot be read, are left alone."""
+    return _kv_read_q8(K8, V8, Ks, Vs, None, cu, start, T, ws, K, V, stream)
+
+
+def libraspec_kv_read_q8_paged(K8, V8, Ks, Vs, block_table, cu, start, T: int, ws, K=None, V=None, stream=None):
+    """libraspec_kv_read_q8 from page pools by block_table [B, max_pages]."""
+    return _kv_read_q8(K8, V8, Ks, Vs, block_table, cu, start, T, ws, K, V, stream)
+
+
+def _kv_read_q8(K8, V8, Ks, Vs, block_table, cu, start, T, ws, K, V, stream):
+    B = _check_new(cu, start)
+    Hkv, d, S_cap, max_pages, page_size, n_pages, block = _check_caches_q8(K8, V8, Ks, Vs, block_table, B)
+    _check_device(ws.buf, "the workspace")
+    T = int(T)
+    if T < 0:
+        raise ValueError("T must not be negative")
+    out = []
+    for t, name in ((K, "K"), (V, "V")):
+        out.append(_out((T, Hkv, d), torch.bfloat16, K8.device, stream) if t is None
+                   else _req(t, torch.bfloat16, name, (T, Hkv, d)))
+    lib = load()
+    tail = (cu.data_ptr(), start.data_ptr(), T, B, Hkv, d)
+    head = (K8.data_ptr(), V8.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
+    end = (block, out[0].data_ptr(), out[1].data_ptr(), ws.ptr, ws.nbytes, _stream(stream))
+    if block_table is None:
+        rc = lib.libraspec_kv_read_q8(*head, *tail, S_cap, *end)
+    else:
+        rc = lib.libraspec_kv_read_q8_paged(*head, block_table.data_ptr(), max_pages, page_size, n_pages, *tail, *end)
+    if rc != OK:
+        _check(rc, "libraspec_kv_read_q8" + ("" if block_table is None else "_paged"))
+    return out[0], out[1]
 
 
 class ChunkWorkspace:

@@ -37,6 +37,17 @@ template <typename T>
 cudaError_t launch_rope_append(const T*, long long, const T*, long long, const T*, long long, const int32_t*,
                                const int32_t*, const int32_t*, const float*, float, const int32_t*, int, int, int, int,
                                int, int, int, int, int, int, uint16_t*, uint16_t*, uint16_t*, int, int*, cudaStream_t);
+template <typename T>
+cudaError_t launch_norm_rope(const T*, long long, const int32_t*, const float*, float, const float*, const float*, float,
+                             int, int, int, int, int, int, T*, long long, cudaStream_t);
+template <typename T>
+cudaError_t launch_rope_append_q8(const T*, long long, const T*, long long, const T*, long long, const int32_t*,
+                                  const int32_t*, const int32_t*, const float*, float, const float*, const float*, float,
+                                  const int32_t*, int, int, int, int, int, int, int, int, int, int, uint16_t*, uint8_t*,
+                                  uint8_t*, uint8_t*, uint8_t*, int, int, int*, cudaStream_t);
+cudaError_t launch_kv_read_q8(const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, const int32_t*, int, int, int,
+                              const int32_t*, const int32_t*, int, int, int, int, int, int, uint16_t*, uint16_t*, int*,
+                              cudaStream_t);
 size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);
 cudaError_t launch_chunk_attn(const uint16_t*, const uint16_t*, const uint16_t*, const int32_t*, int, int, int,
                               const int32_t*, const int32_t*, int, int, int, int, int, int, float, float, const float*,
@@ -555,6 +566,167 @@ int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const 
   return rope_append_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, T, B, Hq, Hkv,
                        head_dim, rot_dim, interleaved, Qo, Kp, Vp, true, block_table, max_pages, page_size, n_pages, 0,
                        workspace, ws_bytes, stream);
+}
+
+extern "C++" {
+template <typename T>
+static int qk_norm_rope_t(const T* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude,
+                          const float* q_weight, const float* k_weight, float eps, int n_tokens, int Hq, int Hk,
+                          int head_dim, int rot_dim, int interleaved, T* Y, int64_t y_stride, void* stream) {
+  if (Hq < 0 || Hk < 0 || Hq > (1 << 20) || Hk > (1 << 20)) return LIBRASPEC_EINVAL;
+  const int H = Hq + Hk;
+  if (!rope_shape_ok(n_tokens, H, head_dim, rot_dim)) return LIBRASPEC_EINVAL;
+  if (!token_stride_ok(x_stride, H, head_dim) || !token_stride_ok(y_stride, H, head_dim)) return LIBRASPEC_EINVAL;
+  if (!(eps >= 0.f && eps <= 1e30f)) return LIBRASPEC_EINVAL;
+  if (n_tokens == 0) return LIBRASPEC_OK;
+  if (!X || !Y || !pos || !turns || !aligned(X, sizeof(T)) || !aligned(Y, sizeof(T)) || !aligned(pos, 4) ||
+      !aligned(turns, 8) || (X == Y && x_stride != y_stride))
+    return LIBRASPEC_EINVAL;
+  if ((Hq && !q_weight) || (Hk && !k_weight) || !aligned(q_weight, 4) || !aligned(k_weight, 4)) return LIBRASPEC_EINVAL;
+  return from_cuda(launch_norm_rope<T>(X, x_stride, pos, turns, magnitude, Hq ? q_weight : k_weight, Hk ? k_weight : q_weight,
+                                       eps, n_tokens, Hq, Hk, head_dim, rot_dim, interleaved, Y, y_stride,
+                                       static_cast<cudaStream_t>(stream)));
+}
+
+// What the 8-bit caches' calls share. Dense: block_table unused; S_cap is set for paged caches.
+static int q8_cache_check(int head_dim, bool paged, int max_pages, int page_size, int n_pages, int block, int& S_cap) {
+  if (head_dim != 64 && head_dim != 128) return LIBRASPEC_EUNSUPPORTED;
+  if (block != 16 && block != 32 && block != 64) return LIBRASPEC_EUNSUPPORTED;
+  if (paged) {
+    if (page_size < 1 || max_pages < 1 || n_pages < 1 || (long)max_pages * page_size > 0x7fffffffL)
+      return LIBRASPEC_EINVAL;
+    S_cap = max_pages * page_size;
+  }
+  if (S_cap < 1 || (paged ? page_size : S_cap) % block != 0) return LIBRASPEC_EINVAL;
+  return LIBRASPEC_OK;
+}
+
+template <typename T>
+static int rope_append_q8_t(const T* Q, int64_t q_stride, const T* K, int64_t k_stride, const T* V, int64_t v_stride,
+                            const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos, const float* turns,
+                            float magnitude, const float* q_weight, const float* k_weight, float eps, int n_tokens, int B,
+                            int Hq, int Hkv, int head_dim, int rot_dim, int interleaved, uint16_t* Qo, uint8_t* K8,
+                            uint8_t* V8, uint8_t* Ks, uint8_t* Vs, bool paged, const int32_t* block_table, int max_pages,
+                            int page_size, int n_pages, int S_cap, int block, void* workspace, size_t ws_bytes,
+                            void* stream) {
+  const int rc = q8_cache_check(head_dim, paged, max_pages, page_size, n_pages, block, S_cap);
+  if (rc != LIBRASPEC_OK) return rc;
+  if (!rope_shape_ok(n_tokens, Hkv, head_dim, rot_dim) || B < 0 || B > LIBRASPEC_MAX_B) return LIBRASPEC_EINVAL;
+  if ((Q != nullptr) != (Qo != nullptr)) return LIBRASPEC_EINVAL;
+  if (Q && (!rope_shape_ok(n_tokens, Hq, head_dim, rot_dim) || !token_stride_ok(q_stride, Hq, head_dim)))
+    return LIBRASPEC_EINVAL;
+  if (!token_stride_ok(k_stride, Hkv, head_dim) || !token_stride_ok(v_stride, Hkv, head_dim)) return LIBRASPEC_EINVAL;
+  if ((q_weight != nullptr) != (k_weight != nullptr) || !aligned(q_weight, 4) || !aligned(k_weight, 4) ||
+      !(eps >= 0.f && eps <= 1e30f))
+    return LIBRASPEC_EINVAL;
+  if (n_tokens == 0 || B == 0) return LIBRASPEC_OK;
+  if (!K || !V || !K8 || !V8 || !Ks || !Vs || !cu_new || !kv_len || !turns || (paged && !block_table))
+    return LIBRASPEC_EINVAL;
+  if ((Q && (!aligned(Q, sizeof(T)) || !aligned(Qo, 16))) || !aligned(K, sizeof(T)) || !aligned(V, sizeof(T)) ||
+      !aligned(K8, 16) || !aligned(V8, 16) || !aligned(cu_new, 4) || !aligned(kv_len, 4) || !aligned(pos, 4) ||
+      !aligned(turns, 8) || !aligned(block_table, 4))
+    return LIBRASPEC_EINVAL;
+  if (!workspace || !aligned(workspace, 256) || ws_bytes < 256) return LIBRASPEC_EINVAL;
+  return from_cuda(launch_rope_append_q8<T>(
+      Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, q_weight, k_weight, eps,
+      paged ? block_table : nullptr, max_pages, page_size, n_pages, n_tokens, B, Hq, Hkv, head_dim, rot_dim, interleaved,
+      Qo, K8, V8, Ks, Vs, S_cap, block, static_cast<int*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+
+static int kv_read_q8(const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks, const uint8_t* Vs, bool paged,
+                      const int32_t* block_table, int max_pages, int page_size, int n_pages, const int32_t* cu,
+                      const int32_t* start, int n_tokens, int B, int Hkv, int head_dim, int S_cap, int block, uint16_t* K,
+                      uint16_t* V, void* workspace, size_t ws_bytes, void* stream) {
+  const int rc = q8_cache_check(head_dim, paged, max_pages, page_size, n_pages, block, S_cap);
+  if (rc != LIBRASPEC_OK) return rc;
+  if (!rope_shape_ok(n_tokens, Hkv, head_dim, head_dim) || B < 0 || B > LIBRASPEC_MAX_B) return LIBRASPEC_EINVAL;
+  if (n_tokens == 0 || B == 0) return LIBRASPEC_OK;
+  if (!K8 || !V8 || !Ks || !Vs || !cu || !start || !K || !V || (paged && !block_table)) return LIBRASPEC_EINVAL;
+  if (!aligned(K8, 16) || !aligned(V8, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(cu, 4) ||
+      !aligned(start, 4) || !aligned(block_table, 4))
+    return LIBRASPEC_EINVAL;
+  if (!workspace || !aligned(workspace, 256) || ws_bytes < 256) return LIBRASPEC_EINVAL;
+  return from_cuda(launch_kv_read_q8(K8, V8, Ks, Vs, paged ? block_table : nullptr, max_pages, page_size, n_pages, cu, start,
+                                     n_tokens, B, Hkv, head_dim, S_cap, block, K, V, static_cast<int*>(workspace),
+                                     static_cast<cudaStream_t>(stream)));
+}
+}  // extern "C++"
+
+int libraspec_qk_norm_rope(const float* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude,
+                           const float* q_weight, const float* k_weight, float eps, int T, int Hq, int Hk, int head_dim,
+                           int rot_dim, int interleaved, float* Y, int64_t y_stride, void* stream) {
+  return qk_norm_rope_t(X, x_stride, pos, turns, magnitude, q_weight, k_weight, eps, T, Hq, Hk, head_dim, rot_dim,
+                        interleaved, Y, y_stride, stream);
+}
+
+int libraspec_qk_norm_rope_bf16(const uint16_t* X, int64_t x_stride, const int32_t* pos, const float* turns,
+                                float magnitude, const float* q_weight, const float* k_weight, float eps, int T, int Hq,
+                                int Hk, int head_dim, int rot_dim, int interleaved, uint16_t* Y, int64_t y_stride,
+                                void* stream) {
+  return qk_norm_rope_t(X, x_stride, pos, turns, magnitude, q_weight, k_weight, eps, T, Hq, Hk, head_dim, rot_dim,
+                        interleaved, Y, y_stride, stream);
+}
+
+int libraspec_rope_append_q8(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                             int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                             const float* turns, float magnitude, const float* q_weight, const float* k_weight, float eps,
+                             int T, int B, int Hq, int Hkv, int head_dim, int rot_dim, int interleaved, uint16_t* Qo,
+                             uint8_t* K8, uint8_t* V8, uint8_t* Ks, uint8_t* Vs, int S_cap, int block, void* workspace,
+                             size_t ws_bytes, void* stream) {
+  return rope_append_q8_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, q_weight, k_weight,
+                          eps, T, B, Hq, Hkv, head_dim, rot_dim, interleaved, Qo, K8, V8, Ks, Vs, false, nullptr, 0, 0, 0,
+                          S_cap, block, workspace, ws_bytes, stream);
+}
+
+int libraspec_rope_append_q8_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                                  const uint16_t* V, int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len,
+                                  const int32_t* pos, const float* turns, float magnitude, const float* q_weight,
+                                  const float* k_weight, float eps, int T, int B, int Hq, int Hkv, int head_dim,
+                                  int rot_dim, int interleaved, uint16_t* Qo, uint8_t* K8, uint8_t* V8, uint8_t* Ks,
+                                  uint8_t* Vs, int S_cap, int block, void* workspace, size_t ws_bytes, void* stream) {
+  return rope_append_q8_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, q_weight, k_weight,
+                          eps, T, B, Hq, Hkv, head_dim, rot_dim, interleaved, Qo, K8, V8, Ks, Vs, false, nullptr, 0, 0, 0,
+                          S_cap, block, workspace, ws_bytes, stream);
+}
+
+int libraspec_rope_append_q8_paged(const float* Q, int64_t q_stride, const float* K, int64_t k_stride, const float* V,
+                                   int64_t v_stride, const int32_t* cu_new, const int32_t* kv_len, const int32_t* pos,
+                                   const float* turns, float magnitude, const float* q_weight, const float* k_weight,
+                                   float eps, int T, int B, int Hq, int Hkv, int head_dim, int rot_dim, int interleaved,
+                                   uint16_t* Qo, uint8_t* K8, uint8_t* V8, uint8_t* Ks, uint8_t* Vs,
+                                   const int32_t* block_table, int max_pages, int page_size, int n_pages, int block,
+                                   void* workspace, size_t ws_bytes, void* stream) {
+  return rope_append_q8_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, q_weight, k_weight,
+                          eps, T, B, Hq, Hkv, head_dim, rot_dim, interleaved, Qo, K8, V8, Ks, Vs, true, block_table,
+                          max_pages, page_size, n_pages, 0, block, workspace, ws_bytes, stream);
+}
+
+int libraspec_rope_append_q8_paged_bf16(const uint16_t* Q, int64_t q_stride, const uint16_t* K, int64_t k_stride,
+                                        const uint16_t* V, int64_t v_stride, const int32_t* cu_new,
+                                        const int32_t* kv_len, const int32_t* pos, const float* turns, float magnitude,
+                                        const float* q_weight, const float* k_weight, float eps, int T, int B, int Hq,
+                                        int Hkv, int head_dim, int rot_dim, int interleaved, uint16_t* Qo, uint8_t* K8,
+                                        uint8_t* V8, uint8_t* Ks, uint8_t* Vs, const int32_t* block_table,
+                                        int max_pages, int page_size, int n_pages, int block, void* workspace,
+                                        size_t ws_bytes, void* stream) {
+  return rope_append_q8_t(Q, q_stride, K, k_stride, V, v_stride, cu_new, kv_len, pos, turns, magnitude, q_weight, k_weight,
+                          eps, T, B, Hq, Hkv, head_dim, rot_dim, interleaved, Qo, K8, V8, Ks, Vs, true, block_table,
+                          max_pages, page_size, n_pages, 0, block, workspace, ws_bytes, stream);
+}
+
+int libraspec_kv_read_q8(const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks, const uint8_t* Vs, const int32_t* cu,
+                         const int32_t* start, int T, int B, int Hkv, int head_dim, int S_cap, int block, uint16_t* K,
+                         uint16_t* V, void* workspace, size_t ws_bytes, void* stream) {
+  return kv_read_q8(K8, V8, Ks, Vs, false, nullptr, 0, 0, 0, cu, start, T, B, Hkv, head_dim, S_cap, block, K, V, workspace,
+                    ws_bytes, stream);
+}
+
+int libraspec_kv_read_q8_paged(const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks, const uint8_t* Vs,
+                               const int32_t* block_table, int max_pages, int page_size, int n_pages, const int32_t* cu,
+                               const int32_t* start, int T, int B, int Hkv, int head_dim, int block, uint16_t* K,
+                               uint16_t* V, void* workspace, size_t ws_bytes, void* stream) {
+  return kv_read_q8(K8, V8, Ks, Vs, true, block_table, max_pages, page_size, n_pages, cu, start, T, B, Hkv, head_dim, 0,
+                    block, K, V, workspace, ws_bytes, stream);
 }
 
 namespace {
