@@ -682,6 +682,52 @@ int libraspec_chunk_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint
                                size_t ws_bytes, void* stream);
 
 /*
+ * Attention of a chunk in a sliding window whose first tokens stay visible
+ * (sinks: a window without them loses the weight that models put on a
+ * sequence's first tokens). libraspec_chunk_attn in all else: query row (b, j)
+ * sees key k iff
+ *   k < N,  and  k <= p or k < prefix_len[b],
+ *   and  k > p - window or k < sinks  (window > 0).
+ * 0 <= sinks <= LIBRASPEC_MAX_SINKS; sinks with first_key (whose documents start
+ * elsewhere) is LIBRASPEC_EINVAL. Keys between the sinks and the window of a
+ * sequence's first new token are not read.
+ */
+#define LIBRASPEC_MAX_SINKS (1 << 20)
+int libraspec_sink_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* cu_new,
+                        const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap,
+                        float softmax_scale, const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse,
+                        void* workspace, size_t ws_bytes, void* stream);
+int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint16_t* Vp, const int32_t* block_table,
+                              int max_pages, int page_size, int n_pages, const int32_t* cu_new, const int32_t* kv_len,
+                              int T, int B, int Hq, int Hkv, int head_dim, float softmax_scale,
+                              const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse, void* workspace,
+                              size_t ws_bytes, void* stream);
+
+/*
+ * The same attention over a cache in 8 bits (libraspec_rope_append_q8: codes
+ * K8, V8, exponents Ks, Vs, `block`; the shapes, their checks and the ends of
+ * the exponents as there), with every option of libraspec_chunk_attn, and sinks:
+ *   s_k = softmax_scale 2^ek Q . K8[k],   O = sum_k softmax(s)_k 2^ev V8[k].
+ * Codes and queries meet as f16, the queries after a power of two of their own
+ * row (all eight bits of what lies above 2^-31 of a row's largest); scores, sums
+ * and O accumulate in binary32; probabilities times their value's scale enter
+ * the second product as f16 (11 bits) down to 2^-24 of 2^-7 of the largest. Codes
+ * and exponents of blocks that no row sees need not be initialised. Reads half
+ * the bytes of a bf16 cache. workspace as for libraspec_chunk_attn.
+ */
+int libraspec_chunk_attn_q8(const uint16_t* Q, const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks,
+                            const uint8_t* Vs, const int32_t* cu_new, const int32_t* kv_len, int T, int B, int Hq,
+                            int Hkv, int head_dim, int S_cap, int block, float softmax_scale,
+                            const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse, void* workspace,
+                            size_t ws_bytes, void* stream);
+int libraspec_chunk_attn_q8_paged(const uint16_t* Q, const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks,
+                                  const uint8_t* Vs, const int32_t* block_table, int max_pages, int page_size,
+                                  int n_pages, const int32_t* cu_new, const int32_t* kv_len, int T, int B, int Hq,
+                                  int Hkv, int head_dim, int block, float softmax_scale,
+                                  const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse,
+                                  void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Failure-detection self-test (no counterpart in the paper: it checks the
  * library's own bounded waits). One CTA waits, with the bounded wait that
  * acceptance's draws use for their sequence's decision, until the device

@@ -82,6 +82,10 @@ SIGNATURES = {
     "libraspec_chunk_workspace_size": (_SZ, [_I] * 5),
     "libraspec_chunk_attn": (_I, [_P] * 5 + [_I] * 6 + [_F] + [_P] * 4 + [_SZ, _P]),
     "libraspec_chunk_attn_paged": (_I, [_P] * 4 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_F] + [_P] * 4 + [_SZ, _P]),
+    "libraspec_sink_attn": (_I, [_P] * 5 + [_I] * 6 + [_F, _P, _I] + [_P] * 3 + [_SZ, _P]),
+    "libraspec_sink_attn_paged": (_I, [_P] * 4 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_F, _P, _I] + [_P] * 3 + [_SZ, _P]),
+    "libraspec_chunk_attn_q8": (_I, [_P] * 7 + [_I] * 7 + [_F, _P, _I] + [_P] * 3 + [_SZ, _P]),
+    "libraspec_chunk_attn_q8_paged": (_I, [_P] * 6 + [_I] * 3 + [_P] * 2 + [_I] * 6 + [_F, _P, _I] + [_P] * 3 + [_SZ, _P]),
     "libraspec_accept": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _U64, _U64, _U32, _P, _P, _P, _SZ, _P]),
     "libraspec_accept_bf16": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _U64, _U64, _U32, _P, _P, _P, _SZ, _P]),
     "libraspec_verify_round": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, _I, _I, _I, _I, _I, _I, _I,
@@ -944,16 +948,59 @@ def libraspec_chunk_attn_paged(Q, Kp, Vp, block_table, cu_new, kv_len, ws: Chunk
                        prefix_len, O, lse, want_lse, stream)
 
 
+def libraspec_sink_attn(Q, Kc, Vc, cu_new, kv_len, ws: ChunkWorkspace, window: int, sinks: int, softmax_scale=None,
+                        softcap: float = 0.0, slopes=None, prefix_len=None, O=None, lse=None, want_lse=False, stream=None):
+    """libraspec_chunk_attn in a window whose first ``sinks`` tokens stay visible to every row. Returns (O, lse or None)."""
+    return _chunk_attn(Q, Kc, Vc, None, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, None, prefix_len, O, lse,
+                       want_lse, stream, "libraspec_sink_attn", sinks)
+
+
+def libraspec_sink_attn_paged(Q, Kp, Vp, block_table, cu_new, kv_len, ws: ChunkWorkspace, window: int, sinks: int,
+                              softmax_scale=None, softcap: float = 0.0, slopes=None, prefix_len=None, O=None, lse=None,
+                              want_lse=False, stream=None):
+    """libraspec_sink_attn over page pools Kp, Vp [n_pages, Hkv, page_size, d] by block_table [B, max_pages]."""
+    return _chunk_attn(Q, Kp, Vp, block_table, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, None, prefix_len,
+                       O, lse, want_lse, stream, "libraspec_sink_attn", sinks)
+
+
+def libraspec_chunk_attn_q8(Q, K8, V8, Ks, Vs, cu_new, kv_len, ws: ChunkWorkspace, softmax_scale=None, softcap: float = 0.0,
+                            slopes=None, window: int = 0, sinks: int = 0, first_key=None, prefix_len=None, O=None, lse=None,
+                            want_lse=False, stream=None):
+    """libraspec_chunk_attn over a cache in 8 bits (as libraspec_rope_append_q8 fills it): codes K8, V8 [B, Hkv, S_cap, d]
+    float8_e4m3fn and exponents Ks, Vs [B, Hkv, S_cap / block] uint8; sinks: first tokens that the window leaves visible
+    (not with first_key). Returns (O, lse or None)."""
+    return _chunk_attn(Q, K8, V8, None, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key, prefix_len, O,
+                       lse, want_lse, stream, "libraspec_chunk_attn_q8", sinks, Ks, Vs)
+
+
+def libraspec_chunk_attn_q8_paged(Q, K8, V8, Ks, Vs, block_table, cu_new, kv_len, ws: ChunkWorkspace, softmax_scale=None,
+                                  softcap: float = 0.0, slopes=None, window: int = 0, sinks: int = 0, first_key=None,
+                                  prefix_len=None, O=None, lse=None, want_lse=False, stream=None):
+    """libraspec_chunk_attn_q8 over page pools K8, V8 [n_pages, Hkv, page_size, d] with exponents [n_pages, Hkv,
+    page_size / block], by block_table [B, max_pages]."""
+    return _chunk_attn(Q, K8, V8, block_table, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key,
+                       prefix_len, O, lse, want_lse, stream, "libraspec_chunk_attn_q8", sinks, Ks, Vs)
+
+
 def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softcap, slopes, window, first_key,
-                prefix_len, O, lse, want_lse, stream):
+                prefix_len, O, lse, want_lse, stream, name="libraspec_chunk_attn", sinks=None, Ks=None, Vs=None):
     _req(Q, torch.bfloat16, "Q")
     shape = Q.shape
     if len(shape) != 3:
         raise ValueError("Q must be [T, Hq, d]")
     T, Hq, d = shape
     B = _check_new(cu_new, kv_len)
-    Hkv = Kc.shape[1] if isinstance(Kc, torch.Tensor) and Kc.dim() == 4 else 0
-    S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
+    block = ()
+    if Ks is None:
+        Hkv = Kc.shape[1] if isinstance(Kc, torch.Tensor) and Kc.dim() == 4 else 0
+        S_cap, max_pages, page_size, n_pages = _check_caches(Kc, Vc, block_table, B, Hkv, d)
+        caches = (Kc.data_ptr(), Vc.data_ptr())
+    else:
+        Hkv, dc, S_cap, max_pages, page_size, n_pages, block = _check_caches_q8(Kc, Vc, Ks, Vs, block_table, B)
+        if dc != d:
+            raise ValueError("the cache has heads of %d, Q of %d" % (dc, d))
+        caches = (Kc.data_ptr(), Vc.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
+        block = (block,)
     _check_device(ws.buf, "the workspace")
     opts = None
     if softcap or slopes is not None or window or first_key is not None or prefix_len is not None:
@@ -972,17 +1019,17 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
         _req(lse, torch.float32, "lse", (T, Hq))
     elif want_lse:
         lse = _out((T, Hq), torch.float32, Q.device, stream)
-    tail = (d ** -0.5 if softmax_scale is None else float(softmax_scale), opts, O.data_ptr(), _ptr(lse), ws.ptr,
-            ws.nbytes, _stream(stream))
+    tail = (d ** -0.5 if softmax_scale is None else float(softmax_scale), opts,
+            *(() if sinks is None else (int(sinks),)), O.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes, _stream(stream))
     if block_table is None:
-        rc = load().libraspec_chunk_attn(Q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(), cu_new.data_ptr(),
-                                         kv_len.data_ptr(), T, B, Hq, Hkv, d, S_cap, *tail)
+        rc = getattr(load(), name)(Q.data_ptr(), *caches, cu_new.data_ptr(), kv_len.data_ptr(), T, B, Hq, Hkv, d, S_cap,
+                                   *block, *tail)
     else:
-        rc = load().libraspec_chunk_attn_paged(Q.data_ptr(), Kc.data_ptr(), Vc.data_ptr(), block_table.data_ptr(),
-                                               max_pages, page_size, n_pages, cu_new.data_ptr(), kv_len.data_ptr(), T, B,
-                                               Hq, Hkv, d, *tail)
+        name += "_paged"
+        rc = getattr(load(), name)(Q.data_ptr(), *caches, block_table.data_ptr(), max_pages, page_size, n_pages,
+                                   cu_new.data_ptr(), kv_len.data_ptr(), T, B, Hq, Hkv, d, *block, *tail)
     if rc != OK:
-        _check(rc, "libraspec_chunk_attn" if block_table is None else "libraspec_chunk_attn_paged")
+        _check(rc, name)
     return O, lse
 
 

@@ -5,6 +5,7 @@
 #include <cstring>
 #include <vector>
 
+#include "chunk_call.h"
 #include "common.cuh"
 
 namespace libraspec {
@@ -48,10 +49,6 @@ cudaError_t launch_rope_append_q8(const T*, long long, const T*, long long, cons
 cudaError_t launch_kv_read_q8(const uint8_t*, const uint8_t*, const uint8_t*, const uint8_t*, const int32_t*, int, int, int,
                               const int32_t*, const int32_t*, int, int, int, int, int, int, uint16_t*, uint16_t*, int*,
                               cudaStream_t);
-size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);
-cudaError_t launch_chunk_attn(const uint16_t*, const uint16_t*, const uint16_t*, const int32_t*, int, int, int,
-                              const int32_t*, const int32_t*, int, int, int, int, int, int, float, float, const float*,
-                              int, const int32_t*, const int32_t*, uint16_t*, float*, char*, cudaStream_t);
 template <typename T>
 cudaError_t launch_accept_tree(const T*, const int32_t*, const int32_t*, const int32_t*, const float*, int, int, int,
                                uint64_t, uint64_t, uint32_t, int32_t*, int32_t*, int32_t*, char*, const WsLayout&,
@@ -736,37 +733,52 @@ bool chunk_shape_ok(int T, int B, int Hq, int Hkv) {
          Hq / Hkv <= kAttnRows && Hq <= (1 << 16);
 }
 
-int chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, bool paged, const int32_t* block_table,
-               int max_pages, int page_size, int n_pages, const int32_t* cu_new, const int32_t* kv_len, int T, int B,
-               int Hq, int Hkv, int head_dim, int S_cap, float softmax_scale, const libraspec_score_opts* opts,
-               uint16_t* O, float* lse, void* workspace, size_t ws_bytes, void* stream) {
-  if (head_dim != 64 && head_dim != 128) return LIBRASPEC_EUNSUPPORTED;
-  if (!chunk_shape_ok(T, B, Hq, Hkv)) return LIBRASPEC_EINVAL;
-  if (paged) {
-    if (page_size < 1 || max_pages < 1 || n_pages < 1 || (long)max_pages * page_size > 0x7fffffffL ||
-        (long)n_pages * Hkv > 0x7fffffffL)
-      return LIBRASPEC_EINVAL;
-    if (page_size % 16 != 0) return LIBRASPEC_EUNSUPPORTED;
-    S_cap = max_pages * page_size;
+// kind: the cache's and what the window leaves visible (0: bf16, 1: bf16 with sinks, 8: in 8 bits, sinks as well).
+int chunk_attn(int kind, ChunkCall c, bool paged, const libraspec_score_opts* opts, size_t ws_bytes) {
+  if (c.D != 64 && c.D != 128) return LIBRASPEC_EUNSUPPORTED;
+  if (!chunk_shape_ok(c.T, c.B, c.Hq, c.Hkv)) return LIBRASPEC_EINVAL;
+  if (kind == 8) {
+    const int rc = q8_cache_check(c.D, paged, c.max_pages, c.page_size, c.n_pages, c.block, c.S_cap);
+    if (rc != LIBRASPEC_OK) return rc;
   }
-  if (S_cap < 1 || (long)B * Hkv > (1L << 30)) return LIBRASPEC_EINVAL;
+  if (paged) {
+    if (c.page_size < 1 || c.max_pages < 1 || c.n_pages < 1 || (long)c.max_pages * c.page_size > 0x7fffffffL ||
+        (long)c.n_pages * c.Hkv > 0x7fffffffL)
+      return LIBRASPEC_EINVAL;
+    if (c.page_size % 16 != 0) return LIBRASPEC_EUNSUPPORTED;
+    c.S_cap = c.max_pages * c.page_size;
+  }
+  if (c.S_cap < 1 || (long)c.B * c.Hkv > (1L << 30)) return LIBRASPEC_EINVAL;
   libraspec_score_opts o{};
   if (opts) o = *opts;
-  if (!(softmax_scale > 0.f) || !isfinite(softmax_scale) || !(o.softcap >= 0.f) || !isfinite(o.softcap) ||
-      o.window < 0)
+  if (!(c.scale > 0.f) || !isfinite(c.scale) || !(o.softcap >= 0.f) || !isfinite(o.softcap) || o.window < 0)
     return LIBRASPEC_EINVAL;
-  if (T == 0 || B == 0) return LIBRASPEC_OK;
-  if (!Q || !Kc || !Vc || !O || !cu_new || !kv_len || (paged && !block_table)) return LIBRASPEC_EINVAL;
-  if (!aligned(Q, 16) || !aligned(Kc, 16) || !aligned(Vc, 16) || !aligned(O, 16) || !aligned(lse, 4) ||
-      !aligned(cu_new, 4) || !aligned(kv_len, 4) || !aligned(block_table, 4) || !aligned(o.slopes, 4) ||
+  if (c.sinks < 0 || c.sinks > kChunkMaxSinks || (c.sinks > 0 && o.first_key)) return LIBRASPEC_EINVAL;
+  if (c.T == 0 || c.B == 0) return LIBRASPEC_OK;
+  if (!c.Q || !c.K || !c.V || !c.O || !c.cu_new || !c.kv_len || (paged && !c.block_table)) return LIBRASPEC_EINVAL;
+  if (kind == 8 && (!c.Ks || !c.Vs)) return LIBRASPEC_EINVAL;
+  if (!aligned(c.Q, 16) || !aligned(c.K, 16) || !aligned(c.V, 16) || !aligned(c.O, 16) || !aligned(c.lse, 4) ||
+      !aligned(c.cu_new, 4) || !aligned(c.kv_len, 4) || !aligned(c.block_table, 4) || !aligned(o.slopes, 4) ||
       !aligned(o.first_key, 4) || !aligned(o.prefix_len, 4))
     return LIBRASPEC_EINVAL;
-  if (!workspace || !aligned(workspace, 256) || ws_bytes < chunk_workspace_bytes(T, B, Hq, Hkv, head_dim))
+  if (!c.ws || !aligned(c.ws, 256) || ws_bytes < chunk_workspace_bytes(c.T, c.B, c.Hq, c.Hkv, c.D))
     return LIBRASPEC_EINVAL;
-  return from_cuda(launch_chunk_attn(Q, Kc, Vc, paged ? block_table : nullptr, max_pages, page_size, n_pages, cu_new,
-                                     kv_len, T, B, Hq, Hkv, head_dim, S_cap, softmax_scale, o.softcap, o.slopes,
-                                     o.window, o.first_key, o.prefix_len, O, lse, static_cast<char*>(workspace),
-                                     static_cast<cudaStream_t>(stream)));
+  if (!paged) c.block_table = nullptr;
+  c.softcap = o.softcap;
+  c.slopes = o.slopes;
+  c.window = o.window;
+  c.first_key = o.first_key;
+  c.prefix_len = o.prefix_len;
+  return from_cuda(kind == 8 ? launch_chunk_attn_q8(c) : c.sinks > 0 ? launch_sink_attn(c) : launch_chunk_attn(c));
+}
+
+ChunkCall chunk_call(const uint16_t* Q, const void* K, const void* V, const uint8_t* Ks, const uint8_t* Vs, int block,
+                     const int32_t* block_table, int max_pages, int page_size, int n_pages, const int32_t* cu_new,
+                     const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap, float softmax_scale,
+                     int sinks, uint16_t* O, float* lse, void* workspace, void* stream) {
+  return ChunkCall{Q, K, V, Ks, Vs, block, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
+                   head_dim, S_cap, softmax_scale, 0.f, nullptr, 0, sinks, nullptr, nullptr, O, lse,
+                   static_cast<char*>(workspace), static_cast<cudaStream_t>(stream)};
 }
 
 }  // namespace
@@ -780,8 +792,10 @@ int libraspec_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* 
                          const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap,
                          float softmax_scale, const libraspec_score_opts* opts, uint16_t* O, float* lse,
                          void* workspace, size_t ws_bytes, void* stream) {
-  return chunk_attn(Q, Kc, Vc, false, nullptr, 0, 0, 0, cu_new, kv_len, T, B, Hq, Hkv, head_dim, S_cap, softmax_scale,
-                    opts, O, lse, workspace, ws_bytes, stream);
+  return chunk_attn(0,
+                    chunk_call(Q, Kc, Vc, nullptr, nullptr, 0, nullptr, 0, 0, 0, cu_new, kv_len, T, B, Hq, Hkv,
+                               head_dim, S_cap, softmax_scale, 0, O, lse, workspace, stream),
+                    false, opts, ws_bytes);
 }
 
 int libraspec_chunk_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint16_t* Vp, const int32_t* block_table,
@@ -789,8 +803,54 @@ int libraspec_chunk_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint
                                const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, float softmax_scale,
                                const libraspec_score_opts* opts, uint16_t* O, float* lse, void* workspace,
                                size_t ws_bytes, void* stream) {
-  return chunk_attn(Q, Kp, Vp, true, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
-                    head_dim, 0, softmax_scale, opts, O, lse, workspace, ws_bytes, stream);
+  return chunk_attn(0,
+                    chunk_call(Q, Kp, Vp, nullptr, nullptr, 0, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
+                               head_dim, 0, softmax_scale, 0, O, lse, workspace, stream),
+                    true, opts, ws_bytes);
+}
+
+int libraspec_sink_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* cu_new,
+                        const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap,
+                        float softmax_scale, const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse,
+                        void* workspace, size_t ws_bytes, void* stream) {
+  return chunk_attn(1,
+                    chunk_call(Q, Kc, Vc, nullptr, nullptr, 0, nullptr, 0, 0, 0, cu_new, kv_len, T, B, Hq, Hkv,
+                               head_dim, S_cap, softmax_scale, sinks, O, lse, workspace, stream),
+                    false, opts, ws_bytes);
+}
+
+int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint16_t* Vp, const int32_t* block_table,
+                              int max_pages, int page_size, int n_pages, const int32_t* cu_new, const int32_t* kv_len,
+                              int T, int B, int Hq, int Hkv, int head_dim, float softmax_scale,
+                              const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse, void* workspace,
+                              size_t ws_bytes, void* stream) {
+  return chunk_attn(1,
+                    chunk_call(Q, Kp, Vp, nullptr, nullptr, 0, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
+                               head_dim, 0, softmax_scale, sinks, O, lse, workspace, stream),
+                    true, opts, ws_bytes);
+}
+
+int libraspec_chunk_attn_q8(const uint16_t* Q, const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks,
+                            const uint8_t* Vs, const int32_t* cu_new, const int32_t* kv_len, int T, int B, int Hq,
+                            int Hkv, int head_dim, int S_cap, int block, float softmax_scale,
+                            const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse, void* workspace,
+                            size_t ws_bytes, void* stream) {
+  return chunk_attn(8,
+                    chunk_call(Q, K8, V8, Ks, Vs, block, nullptr, 0, 0, 0, cu_new, kv_len, T, B, Hq, Hkv,
+                               head_dim, S_cap, softmax_scale, sinks, O, lse, workspace, stream),
+                    false, opts, ws_bytes);
+}
+
+int libraspec_chunk_attn_q8_paged(const uint16_t* Q, const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks,
+                                  const uint8_t* Vs, const int32_t* block_table, int max_pages, int page_size,
+                                  int n_pages, const int32_t* cu_new, const int32_t* kv_len, int T, int B, int Hq,
+                                  int Hkv, int head_dim, int block, float softmax_scale,
+                                  const libraspec_score_opts* opts, int sinks, uint16_t* O, float* lse,
+                                  void* workspace, size_t ws_bytes, void* stream) {
+  return chunk_attn(8,
+                    chunk_call(Q, K8, V8, Ks, Vs, block, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
+                               head_dim, 0, softmax_scale, sinks, O, lse, workspace, stream),
+                    true, opts, ws_bytes);
 }
 
 extern "C++" {

@@ -95,3 +95,58 @@ def test_binding_names_what_is_wrong():
         lr.libraspec_rope_append_q8(None, x.half(), x, x, x, x, x, x, x, None, None)
     with pytest.raises(TypeError, match="^start must be|^kv_len must be"):
         lr.libraspec_kv_read_q8(x, x, x, x, x, x, 4, None)
+
+
+def _opts(cap=0.0, window=0, slopes=None, first=None, prefix=None):
+    return ctypes.byref(lr._ScoreOpts(cap, window, slopes, first, prefix))
+
+
+def test_chunk_attn_q8_refuses(lib):
+    big = 1 << 40
+
+    def dense(Q=FAKE, K8=FAKE, V8=FAKE, Ks=FAKE, Vs=FAKE, cu=FAKE, kv=FAKE, T=4, B=2, Hq=8, Hkv=2, d=64, S=64, block=16,
+              scale=0.125, opts=None, sinks=0, O=FAKE, lse=None, ws=FAKE, wb=big):
+        return lib.libraspec_chunk_attn_q8(Q, K8, V8, Ks, Vs, cu, kv, T, B, Hq, Hkv, d, S, block, scale, opts, sinks, O, lse, ws,
+                                           wb, None)
+
+    for kw in (dict(d=96), dict(block=8), dict(block=48)):
+        assert dense(**kw) == lr.EUNSUPPORTED, kw
+    for kw in (dict(Q=None), dict(K8=None), dict(V8=None), dict(Ks=None), dict(Vs=None), dict(cu=None), dict(kv=None),
+               dict(O=None), dict(T=-1), dict(B=-1), dict(B=4097), dict(Hq=7), dict(Hkv=0), dict(Hq=258, Hkv=2), dict(S=0),
+               dict(S=72), dict(scale=0.0), dict(scale=math.inf), dict(Q=P(0x10008)), dict(K8=P(0x10008)), dict(O=P(0x10008)),
+               dict(ws=None), dict(ws=P(0x10010)), dict(wb=1 << 16), dict(opts=_opts(cap=-1.0)), dict(opts=_opts(window=-1)),
+               dict(sinks=-1), dict(sinks=(1 << 20) + 1, opts=_opts(window=5)), dict(sinks=1, opts=_opts(window=5, first=0x10000)),
+               dict(opts=_opts(first=0x10001))):
+        assert dense(**kw) == lr.EINVAL, kw
+    assert dense(T=0, Q=None) == lr.OK and dense(B=0, Q=None) == lr.OK
+
+    def paged(table=FAKE, mp=4, ps=32, np_=9, block=16):
+        return lib.libraspec_chunk_attn_q8_paged(FAKE, FAKE, FAKE, FAKE, FAKE, table, mp, ps, np_, FAKE, FAKE, 4, 2, 8, 2, 64,
+                                                 block, 0.125, None, 0, FAKE, None, None, 0, None)
+
+    for kw in (dict(), dict(table=None), dict(mp=0), dict(ps=0), dict(ps=48, block=32), dict(ps=24), dict(np_=0),
+               dict(mp=1 << 20, ps=1 << 12)):
+        assert paged(**kw) == lr.EINVAL, kw  # (the first: no workspace)
+
+
+def test_sink_attn_refuses(lib):
+    def dense(K=FAKE, S=64, opts=None, sinks=4, ws=FAKE, wb=1 << 40, d=64):
+        return lib.libraspec_sink_attn(FAKE, K, FAKE, FAKE, FAKE, 4, 2, 8, 2, d, S, 0.125, opts, sinks, FAKE, None, ws, wb, None)
+
+    assert dense(d=96) == lr.EUNSUPPORTED
+    for kw in (dict(K=None), dict(S=0), dict(sinks=-1), dict(sinks=(1 << 20) + 1), dict(opts=_opts(window=5, first=0x10000)),
+               dict(ws=None), dict(wb=1 << 10), dict(opts=_opts(window=-2))):
+        assert dense(**kw) == lr.EINVAL, kw
+    assert lib.libraspec_sink_attn_paged(FAKE, FAKE, FAKE, FAKE, 4, 24, 9, FAKE, FAKE, 4, 2, 8, 2, 64, 0.125, None, 4, FAKE, None,
+                                         FAKE, 1 << 40, None) == lr.EUNSUPPORTED
+
+
+def test_limits_match_the_header():
+    import os
+    import re
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    header = open(os.path.join(root, "include", "libraspec.h")).read()
+    call = open(os.path.join(root, "paper_2608_08721_gb300", "csrc", "chunk_call.h")).read()
+    shift = re.search(r"LIBRASPEC_MAX_SINKS \(1 << (\d+)\)", header).group(1)
+    assert re.search(r"kChunkMaxSinks = 1 << (\d+);", call).group(1) == shift
