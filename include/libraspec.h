@@ -708,9 +708,9 @@ int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint1
  * K8, V8, exponents Ks, Vs, `block`; the shapes, their checks and the ends of
  * the exponents as there), with every option of libraspec_chunk_attn, and sinks:
  *   s_k = softmax_scale 2^ek Q . K8[k],   O = sum_k softmax(s)_k 2^ev V8[k].
- * Codes and queries meet as f16, the queries after a power of two of their own
- * row (all eight bits of what lies above 2^-31 of a row's largest); scores, sums
- * and O accumulate in binary32; probabilities times their value's scale enter
+ * Queries meet the codes as two e4m3 parts (all eight bits of what lies within
+ * 2^-9 of a row's largest element, else off by 2^-17 of that); scores, sums and O
+ * accumulate in binary32; probabilities times their value's scale enter
  * the second product as f16 (11 bits) down to 2^-24 of 2^-7 of the largest. Codes
  * and exponents of blocks that no row sees need not be initialised. Reads half
  * the bytes of a bf16 cache. workspace as for libraspec_chunk_attn.

@@ -553,22 +553,25 @@ __device__ __forceinline__ int item_tile(const ChunkItem& it, int j) {
 // plain kernel costs it instruction fetches, also beside its loop.)
 constexpr int kCap = 1, kBias = 2, kWideCap = 4, kDocs = 8, kQ8 = 16, kSink = 32;
 
-// A cache in 8 bits: raw tiles in a ring of their own, converted to f16 by a warpgroup into the ring that the MMAs read.
+// A cache in 8 bits: tiles of K in a ring that the MMAs read as it is; raw tiles of V in another, converted to f16 by a
+// warpgroup into the ring of chunks.
 template <int D, bool Q8>
 struct ChunkSmem {
   static constexpr int kBoxes = D / 64;
   static constexpr int kTile = kBoxes * 16384;           // 128 rows of Q, K or V: per 64 columns 128 rows of 128 bytes
-  static constexpr int kChunks = Q8 ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);
+  static constexpr int kChunks = Q8 ? (D == 128 ? 2 : 4) : (D == 128 ? 5 : 10);
   static constexpr int kRawTile = 128 * D;
-  static constexpr int kRaws = Q8 ? (D == 128 ? 4 : 8) : 0;
+  static constexpr int kKs = Q8 ? (D == 128 ? 3 : 6) : 0, kRaws = Q8 ? (D == 128 ? 3 : 6) : 0;
   static constexpr int kScaleStages = 4;                 // of each stream
   static constexpr int kQ = 0;                           // two row tiles
   static constexpr int kRing = 2 * kTile;
-  static constexpr int kRaw = kRing + kChunks * kTile;
+  static constexpr int kKRing = kRing + kChunks * kTile;
+  static constexpr int kRaw = kKRing + kKs * kRawTile;
   static constexpr int kBar = kRaw + kRaws * kRawTile;
   // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], got[2][2], pvdone[2], ofree[2], qfull,
-  // qempty, drain, gap; 8 bits: rfull[raws], rempty[raws], qready, qread, cfull[2][stages], cempty[2][stages]
-  static constexpr int kNumBars = 2 * kChunks + 14 + 4 + (Q8 ? 2 * kRaws + 2 + 4 * kScaleStages : 0);
+  // qempty, drain, gap; 8 bits: kfull[ks], kempty[ks], rfull[raws], rempty[raws], qready, qread, cfull[2][stages],
+  // cempty[2][stages]
+  static constexpr int kNumBars = 2 * kChunks + 14 + 4 + (Q8 ? 2 * kKs + 2 * kRaws + 2 + 4 * kScaleStages : 0);
   static constexpr int kInfo = kBar + (8 * kNumBars + 63) / 64 * 64;
   static constexpr int kMisc = kInfo + 2 * 80;           // [0] misaligned, [1] this CTA merges, [2] tensor memory
   static constexpr int kStat = kMisc + 16;               // (m, l) of each stream's rows (streams to be combined)
@@ -587,11 +590,11 @@ struct ChunkSmem {
 constexpr int kCSoftmaxRegs = 208, kCOtherRegs = 88;
 static_assert(kCSoftmaxWarps * 32 * kCSoftmaxRegs + 128 * kCOtherRegs <= kCThreads * 168, "");
 // A cache in 8 bits takes a warpgroup more: 512 threads start with 128 each (65536 in all), of which the softmax keeps
-// 192, the third warpgroup 88 and the converters 40 (256 x 192 + 128 x 88 + 128 x 40 = 65536).
+// 184, the third warpgroup 80 and the converters 64 (256 x 184 + 128 x 80 + 128 x 64 = 65536).
 constexpr int kCThreadsQ8 = kCThreads + 128;
 constexpr int kScaleWarp = kCMmaWarp + 1, kConvertWarp = kCMmaWarp + 3, kConverters = 4;
-constexpr int kQ8SoftmaxRegs = 192, kQ8ConvertRegs = 40;
-static_assert(kCSoftmaxWarps * 32 * kQ8SoftmaxRegs + 128 * kCOtherRegs + 128 * kQ8ConvertRegs <= kCThreadsQ8 * 128, "");
+constexpr int kQ8SoftmaxRegs = 184, kQ8OtherRegs = 80, kQ8ConvertRegs = 64;
+static_assert(kCSoftmaxWarps * 32 * kQ8SoftmaxRegs + 128 * kQ8OtherRegs + 128 * kQ8ConvertRegs <= kCThreadsQ8 * 128, "");
 template <int N>
 __device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -643,6 +646,12 @@ __device__ __forceinline__ uint32_t c_pack(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+// two values as e4m3, to the nearest, ties to even, saturating
+__device__ __forceinline__ uint32_t e4m3_of(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 // two e4m3 codes as f16, exactly
 __device__ __forceinline__ uint32_t f16_of_e4m3(uint16_t c) {
@@ -841,7 +850,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sQ = smem_u32(smem + SM::kQ);
   const uint32_t sRing = smem_u32(smem + SM::kRing);
-  const uint32_t sRaw = smem_u32(smem + SM::kRaw);
+  const uint32_t sK = smem_u32(smem + SM::kKRing), sRaw = smem_u32(smem + SM::kRaw);
   const uint32_t bFull = smem_u32(smem + SM::kBar);
   const uint32_t bEmpty = bFull + 8 * SM::kChunks;
   const uint32_t bIFull = bEmpty + 8 * SM::kChunks;
@@ -854,7 +863,9 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
   const uint32_t bQEmpty = bQFull + 8;
   const uint32_t bDrain = bQEmpty + 8;
   const uint32_t bGap = bDrain + 8;       // V tiles of which the producer clears rows
-  const uint32_t bRFull = bGap + 8;       // 8 bits: raw tiles, Q converted, its scales read, the tiles' scales
+  const uint32_t bKFull = bGap + 8;       // 8 bits: tiles of K, raw ones of V, Q in parts, its scales read, the tiles' scales
+  const uint32_t bKEmpty = bKFull + 8 * SM::kKs;
+  const uint32_t bRFull = bKEmpty + 8 * SM::kKs;
   const uint32_t bREmpty = bRFull + 8 * SM::kRaws;
   const uint32_t bQReady = bREmpty + 8 * SM::kRaws;
   const uint32_t bQRead = bQReady + 8;
@@ -890,6 +901,10 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
     mbar_init(bDrain, 1);
     mbar_init(bGap, 1);
     if constexpr (Q8) {
+      for (int s = 0; s < SM::kKs; ++s) {
+        mbar_init(bKFull + 8 * s, 1);
+        mbar_init(bKEmpty + 8 * s, 1);
+      }
       for (int s = 0; s < SM::kRaws; ++s) {
         mbar_init(bRFull + 8 * s, 1);
         mbar_init(bREmpty + 8 * s, kConverters);
@@ -920,7 +935,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
   if (misaligned) {
     if (tid == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
   } else if (Q8 && warp >= kConvertWarp) {
-    // ======================= converters: raw tiles and Q to f16 =======================
+    // ======================= converters: raw tiles of V to f16, Q to e4m3 parts =======================
     regs_leave<kQ8ConvertRegs>();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int ct = tid - kConvertWarp * 32;
@@ -947,49 +962,106 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       if (last == 2) break;
       __syncwarp();
       if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
-      // Q, a row a thread: times the power of two that brings its largest into [2^14, 2^15), so that f16 holds all eight
-      // bits of what is above 2^-31 of that
+      // Q, a row a thread: times the power of two that brings its largest into [2^7, 2^8), as two e4m3 parts, the nearest
+      // and the rest: together all eight bits of what lies within 2^-9 of the largest, else off by 2^-17 of it at most.
       ok = warp_wait(bQFull, item_ctr & 1) && (item_ctr == 0 || warp_wait(bQRead, (item_ctr - 1) & 1));
       if (!ok) break;
 #pragma unroll 1
       for (int s = 0; s <= it.pair; ++s) {
+        if (ct >= R || s * R + ct >= it.rows) break;
         uint8_t* q = smem + SM::kQ + s * SM::kTile + ct * 128;
+        auto chunk = [&](int box, int k) { return reinterpret_cast<uint4*>(q + box * 16384 + ((k ^ ct) & 7) * 16); };
         uint32_t top = 0;
 #pragma unroll
         for (int k = 0; k < SM::kBoxes * 8; ++k) {
-          const uint4 v = *reinterpret_cast<const uint4*>(q + k / 8 * 16384 + ((k ^ ct) & 7) * 16);
+          const uint4 v = *chunk(k / 8, k % 8);
           const uint32_t a = __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), b = __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu);
           top = __vmaxu2(top, __vmaxu2(a, b));
         }
-        // (rows below 2^-49 are not brought up that far: the factor times a scale stays a normal number)
-        const int e = (int)(max(top & 0xffffu, top >> 16) >> 7), fe = min(268 - e, 190);
-        const float f = power_of_two_biased(fe);
-#pragma unroll
-        for (int k = 0; k < SM::kBoxes * 8; ++k) {
-          uint4* at = reinterpret_cast<uint4*>(q + k / 8 * 16384 + ((k ^ ct) & 7) * 16);
-          const uint4 v = *at;
-          *at = make_uint4(pack_f16(bf16_lo(v.x) * f, bf16_hi(v.x) * f), pack_f16(bf16_lo(v.y) * f, bf16_hi(v.y) * f),
-                           pack_f16(bf16_lo(v.z) * f, bf16_hi(v.z) * f), pack_f16(bf16_lo(v.w) * f, bf16_hi(v.w) * f));
-        }
+        // (rows below 2^-119 are not brought up that far: the factor and its inverse are normal numbers)
+        const int e = (int)(max(top & 0xffffu, top >> 16) >> 7), fe = min(261 - e, 253);
         smem[SM::kQExp + s * kCRows + ct] = (uint8_t)fe;
+        const float f = power_of_two_biased(fe);
+        // sixteen elements, to their first parts and their second
+        auto split = [&](uint4& u, uint4& v) {
+          const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+          uint32_t first[4], rest[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x0 = bf16_lo(w[2 * k]) * f, x1 = bf16_hi(w[2 * k]) * f;
+            const float x2 = bf16_lo(w[2 * k + 1]) * f, x3 = bf16_hi(w[2 * k + 1]) * f;
+            const uint32_t lo = e4m3_of(x0, x1), hi = e4m3_of(x2, x3);
+            const uint32_t hl = f16_of_e4m3((uint16_t)lo), hh = f16_of_e4m3((uint16_t)hi);
+            const float2 yl = __half22float2(*reinterpret_cast<const __half2*>(&hl));
+            const float2 yh = __half22float2(*reinterpret_cast<const __half2*>(&hh));
+            first[k] = lo | hi << 16;
+            rest[k] = e4m3_of(x0 - yl.x, x1 - yl.y) | e4m3_of(x2 - yh.x, x3 - yh.y) << 16;
+          }
+          u = make_uint4(first[0], first[1], first[2], first[3]);
+          v = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+        };
+        uint4 u[8];
+        if constexpr (D == 64) {  // a row: the first parts, then the second
+#pragma unroll
+          for (int k = 0; k < 8; ++k) u[k] = *chunk(0, k);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            split(u[2 * k], u[2 * k + 1]);
+            *chunk(0, k) = u[2 * k];
+            *chunk(0, 4 + k) = u[2 * k + 1];
+          }
+        } else {
+          // The first parts lie where the row's first 64 elements lay, the second where the others did: chunk k of both
+          // is written once chunk k of both has been read, half of the row in registers at a time.
+          auto put = [&](int k, uint4 a, uint4 b) {
+            *chunk(0, k) = a;
+            *chunk(1, k) = b;
+          };
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            u[k] = *chunk(0, k);
+            u[4 + k] = *chunk(1, k);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; k += 2) split(u[k], u[k + 1]);
+          put(0, u[0], u[1]);
+          put(1, u[2], u[3]);
+          u[0] = *chunk(0, 4);
+          u[1] = *chunk(0, 5);
+          u[2] = *chunk(1, 4);
+          u[3] = *chunk(1, 5);
+          put(4, u[4], u[5]);
+          put(5, u[6], u[7]);
+          split(u[0], u[1]);
+          split(u[2], u[3]);
+          put(2, u[0], u[1]);
+          u[4] = *chunk(0, 6);
+          u[5] = *chunk(0, 7);
+          u[6] = *chunk(1, 6);
+          u[7] = *chunk(1, 7);
+          put(6, u[2], u[3]);
+          split(u[4], u[5]);
+          split(u[6], u[7]);
+          put(3, u[4], u[5]);
+          put(7, u[6], u[7]);
+        }
       }
+      __syncwarp();
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(bQReady);
-      const int n = it.n_tiles, lag = it.pair ? 2 : 3, n_tok = it.rows / g;
+      const int n = it.n_tiles, n_tok = it.rows / g;
       const int sinks = SINK ? min(A.mask.sinks, it.khi) : 0;
       const uint32_t* seen = A.seen + (size_t)max(it.gaps, 0) * kSeenWords;
-      for (int kt = 0, vt = 0; vt < n; ++raw_ctr) {  // in the producer's order
-        const bool is_k = kt < n && kt < vt + lag;
-        const int t = is_k ? kt++ : vt++;
+      for (int t = 0; t < n; ++t, ++raw_ctr) {
         const uint32_t rc = raw_ctr % SM::kRaws, ch = raw_ctr % SM::kChunks;
         ok = warp_wait(bRFull + 8 * rc, (raw_ctr / SM::kRaws) & 1) &&
              warp_wait(bEmpty + 8 * ch, ((raw_ctr / SM::kChunks) & 1) ^ 1);
         if (!ok) break;
         const int kt0 = item_tile<SINK>(it, tile_of<SHAPE>(t, n)) * kCKeys;
-        // V rows that no row of the block sees become zeros (what they hold, NaN say, does not meet the zeros of P)
+        // rows that no row of the block sees become zeros (what they hold, NaN say, does not meet the zeros of P)
         const bool gap = (SHAPE & kDocs) && it.gaps >= 0 && kt0 + kCKeys > it.pos0 && kt0 < it.pos0 + n_tok;
-        const bool edge = !is_k && (kt0 < it.klo || kt0 + kCKeys > it.khi || gap);
+        const bool edge = kt0 < it.klo || kt0 + kCKeys > it.khi || gap;
         const uint8_t* raw = smem + SM::kRaw + rc * SM::kRawTile + ct * 16;
         uint8_t* dst = smem + SM::kRing + ch * SM::kTile + (D == 128 ? cj / 4 * 16384 : 0);
 #pragma unroll
@@ -1029,7 +1101,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
     }
     if (!ok && lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
   } else if (warp >= kCSoftmaxWarps) {
-    regs_leave<kCOtherRegs>();
+    regs_leave<Q8 ? kQ8OtherRegs : kCOtherRegs>();
     if (warp == kCProducerWarp) {
       // ======================= producer =======================
       asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -1095,7 +1167,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       const int my_row = (lane % per_tile) * A.piece, my_hb = lane / per_tile;
       const bool has_piece = my_hb < (Q8 ? 1 : SM::kBoxes);  // (in 8 bits a box holds whole rows)
       uint32_t item_ctr = 0, chunk_ctr = 0, gap_ctr = 0;
-      constexpr uint32_t kRing = Q8 ? SM::kRaws : SM::kChunks;
+      uint32_t n_k = 0;
       const uint64_t once = evict_first_policy(), again = evict_normal_policy();
       bool ok = true;
       while ((whole > 0 || left > 0) && ok) {
@@ -1169,8 +1241,11 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         for (int kt = 0, vt = 0; vt < n && ok;) {
           const bool is_k = kt < n && kt < vt + lag;
           const int t = is_k ? kt++ : vt++;
-          const uint32_t ch = chunk_ctr % kRing;
-          ok = warp_wait((Q8 ? bREmpty : bEmpty) + 8 * ch, ((chunk_ctr / kRing) & 1) ^ 1);
+          // (in 8 bits K and V have rings of their own; n_k: the tiles of K loaded so far)
+          const uint32_t nth = !Q8 ? chunk_ctr : is_k ? n_k++ : chunk_ctr - n_k;
+          const uint32_t size = !Q8 ? SM::kChunks : is_k ? SM::kKs : SM::kRaws;
+          const uint32_t ch = nth % size;
+          ok = warp_wait((!Q8 ? bEmpty : is_k ? bKEmpty : bREmpty) + 8 * ch, ((nth / size) & 1) ^ 1);
           if (!ok) break;
           if (is_k && t > 0 && (t & 3) == 0) {
             pages_before = pages;
@@ -1190,13 +1265,13 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           // for calls without first keys, a prompt of 64-wide heads took 871 us instead of 812.)
           const int kt0 = key - my_row;
           const bool gap = !Q8 && gaps && !is_k && kt0 + kCKeys > p.pos0 && kt0 < p.pos0 + p.n_tok;
-          const uint32_t bar = gap ? bGap : (Q8 ? bRFull : bFull) + 8 * ch;
+          const uint32_t bar = gap ? bGap : (!Q8 ? bFull : is_k ? bKFull : bRFull) + 8 * ch;
           const int pieces = __popc(__ballot_sync(0xffffffffu, load));
           if (lane == 0) mbar_expect_tx(bar, pieces * A.piece * (Q8 ? D : 128));
           __syncwarp();
           if (load) {
             const int z = page * A.Hkv + it.kvh, y = A.block_table ? key % A.page_size : key;
-            const uint32_t to = Q8 ? sRaw + ch * SM::kRawTile + my_row * D
+            const uint32_t to = Q8 ? (is_k ? sK : sRaw) + ch * SM::kRawTile + my_row * D
                                    : sRing + ch * SM::kTile + my_hb * 16384 + my_row * 128;
             tma_load_3d_hint(to, is_k ? &A.K : &A.V, bar, my_hb * 64, y, z, policy);
           }
@@ -1227,9 +1302,14 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       if (!ok && lane == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
       // before leaving, wait (bounded) for the copies still in flight
       if (lane == 0) {
-        for (uint32_t k = 0; k < kRing && k < chunk_ctr; ++k) {
-          const uint32_t i = chunk_ctr - 1 - k;
-          mbar_wait((Q8 ? bRFull : bFull) + 8 * (i % kRing), (i / kRing) & 1);
+        auto drain = [&](uint32_t bars, uint32_t size, uint32_t count) {
+          for (uint32_t k = 0; k < size && k < count; ++k) mbar_wait(bars + 8 * ((count - 1 - k) % size), ((count - 1 - k) / size) & 1);
+        };
+        if constexpr (Q8) {
+          drain(bKFull, SM::kKs, n_k);
+          drain(bRFull, SM::kRaws, chunk_ctr - n_k);
+        } else {
+          drain(bFull, SM::kChunks, chunk_ctr);
         }
         if (item_ctr > 0) mbar_wait(bQFull, (item_ctr - 1) & 1);
       }
@@ -1247,15 +1327,23 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         if (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)))
           ok = __all_sync(0xffffffffu, ok && slow_wait(bar, parity));
       };
-      auto take = [&]() {  // the next chunk, once it is filled
-        const uint32_t c = ch;
-        need(bFull + 8 * c, ch_par);
-        if (++ch == SM::kChunks) {
-          ch = 0;
-          ch_par ^= 1;
+      auto next_of = [&](uint32_t bars, uint32_t& at, uint32_t& par, uint32_t size) {
+        const uint32_t c = at;
+        need(bars + 8 * c, par);
+        if (++at == size) {
+          at = 0;
+          par ^= 1;
         }
         return c;
       };
+      uint32_t kch = 0, kch_par = 0;  // (8 bits) the next tile of K
+      // the next chunk of V, or of K, once it is filled
+      auto take = [&]() { return next_of(bFull, ch, ch_par, SM::kChunks); };
+      auto take_k = [&]() {
+        if constexpr (Q8) return next_of(bKFull, kch, kch_par, SM::kKs);
+        else return take();
+      };
+      auto free_k = [&](uint32_t c) { mma_commit_warp((Q8 ? bKEmpty : bEmpty) + 8 * c); };
       auto word = [&](int s, uint32_t& w) {
         need(bGot + 16 * s + 8 * (w & 1), (w >> 1) & 1);
         ++w;
@@ -1264,11 +1352,19 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       auto issue_s = [&](int s, int qs, uint32_t c) {  // S = Q K^T
         constexpr uint32_t idesc = mma_idesc(128, kCKeys, 0) & ~(Q8 ? kBf16Operands : 0u);
         const uint32_t ts = tmem + SM::kColS + (SM::kScores == 2 ? s * 128 : 0);
-        const uint32_t qa = q_desc + qs * (SM::kTile / 16), ka = k_desc + c * (SM::kTile / 16);
         tc_fence_after();
+        const uint32_t qa = q_desc + qs * (SM::kTile / 16);
+        if constexpr (Q8) {  // the parts of Q one after the other
+          const uint32_t ka = desc_lo(sK, 16) + c * (SM::kRawTile / 16);
 #pragma unroll
-        for (int hb = 0; hb < SM::kBoxes; ++hb)
-          mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
+          for (int part = 0; part < SM::kBoxes; ++part)
+            mma_f8_ss4_warp<D == 64>(ts, qa + part * 1024, ka, idesc, part != 0 ? 1u : 0u);
+        } else {
+          const uint32_t ka = k_desc + c * (SM::kTile / 16);
+#pragma unroll
+          for (int hb = 0; hb < SM::kBoxes; ++hb)
+            mma_ss4_warp<32, 32>(ts, qa + hb * 1024, ka + hb * 1024, idesc, hb != 0 ? 1u : 0u);
+        }
         mma_commit_warp(bSFull + 8 * s);
       };
       auto issue_pv = [&](int s, uint32_t c, uint32_t acc) {  // O += P V
@@ -1298,12 +1394,12 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         // (A warp by itself takes 5 cycles for an instruction that depends on another, and 150 to 400 for an ask of a
         // barrier beside MMAs that read shared memory at its full rate: every one of them counts here.)
         constexpr bool kOwn = SM::kScores == 2;
-        uint32_t kc = take(), vc = 0;
+        uint32_t kc = take_k(), vc = 0;
         if (pair) {
           issue_s(0, 0, kc);
           if (kOwn) {
             issue_s(1, 1, kc);
-            mma_commit_warp(bEmpty + 8 * kc);
+            free_k(kc);
             if (n_tiles == 1) mma_commit_warp(bQEmpty);
           }
           for (int t = 0; t <= n_tiles && ok; ++t) {
@@ -1314,22 +1410,22 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
               o0 ^= 1;
               o1 ^= 1;
             }
-            if (kOwn && t + 1 < n_tiles) kc = take();
+            if (kOwn && t + 1 < n_tiles) kc = take_k();
             word(0, g0);
             if (kOwn) {
               if (t + 1 < n_tiles) issue_s(0, 0, kc);
             } else if (t < n_tiles) {
               issue_s(1, 1, kc);
-              mma_commit_warp(bEmpty + 8 * kc);
+              free_k(kc);
               if (t == n_tiles - 1) mma_commit_warp(bQEmpty);
             }
             if (t > 0) issue_pv(0, vc, t > 1);
-            if (!kOwn && t + 1 < n_tiles) kc = take();
+            if (!kOwn && t + 1 < n_tiles) kc = take_k();
             word(1, g1);
             if (t + 1 < n_tiles) {
               if (kOwn) {
                 issue_s(1, 1, kc);
-                mma_commit_warp(bEmpty + 8 * kc);
+                free_k(kc);
                 if (t == n_tiles - 2) mma_commit_warp(bQEmpty);
               } else {
                 issue_s(0, 0, kc);
@@ -1343,7 +1439,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         } else {
           auto next_s = [&](int n) {
             issue_s(n & 1, 0, kc);
-            mma_commit_warp(bEmpty + 8 * kc);
+            free_k(kc);
             if (n == n_tiles - 1) mma_commit_warp(bQEmpty);
           };
           next_s(0);
@@ -1364,7 +1460,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
               mma_commit_warp(bEmpty + 8 * vc);
             }
             if (n + 1 < n_tiles) {  // (asked for behind the PV, which gives its chunk back while K is on its way)
-              kc = take();
+              kc = take_k();
               next_s(n + 1);
             }
           }
@@ -1869,8 +1965,9 @@ static bool make_map(CUtensorMap* map, const void* base, int D, long long rows, 
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Codes of a cache in 8 bits [planes, rows, D] in boxes of whole rows.
-static bool make_map8(CUtensorMap* map, const void* base, int D, long long rows, long long planes, int box_rows) {
+// Codes of a cache in 8 bits [planes, rows, D] in boxes of whole rows; swizzled for the MMA, or as they are.
+static bool make_map8(CUtensorMap* map, const void* base, int D, long long rows, long long planes, int box_rows,
+                      bool swizzled) {
   auto enc = get_encode();
   if (!enc) return false;
   cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)rows, (cuuint64_t)planes};
@@ -1878,8 +1975,9 @@ static bool make_map8(CUtensorMap* map, const void* base, int D, long long rows,
   cuuint32_t box[3] = {(cuuint32_t)D, (cuuint32_t)box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr,
-             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             CU_TENSOR_MAP_INTERLEAVE_NONE,
+             !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE : D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D, int SHAPE>
@@ -1971,11 +2069,11 @@ static cudaError_t launch_chunk(const ChunkCall& c) {
   a.rows = (int)rows;
   a.block_log2 = 0;
   while ((1 << a.block_log2) < c.block) ++a.block_log2;
-  auto cache_map = [&](CUtensorMap* m, const void* base) {
-    return Q8 ? make_map8(m, base, c.D, rows, planes, a.piece)
+  auto cache_map = [&](CUtensorMap* m, const void* base, bool keys) {
+    return Q8 ? make_map8(m, base, c.D, rows, planes, a.piece, keys)
               : make_map(m, base, c.D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
   };
-  if (!cache_map(&a.K, c.K) || !cache_map(&a.V, c.V) ||
+  if (!cache_map(&a.K, c.K, true) || !cache_map(&a.V, c.V, false) ||
       !make_map(&a.Q, c.Q, c.D, c.Hq, c.T, g, kCRows / g, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
     return cudaErrorInvalidValue;
   const int grid = std::min(num_sms_current(), kCMaxCtas);

@@ -1,9 +1,9 @@
 """GPU: attention of a chunk over a cache in 8 bits (libraspec_chunk_attn_q8[_paged]) and in a window with sinks
 (libraspec_sink_attn[_paged]), against the definition in 64 bits.
 
-Tolerances, from the arithmetic. Over 8 bits: codes and queries meet exactly as f16. A score is a binary32 sum of 64 or 128
-exact products, off by up to 2^-17 of the sum of their magnitudes; its exponent takes a few roundings more of 2^-24 of its
-size. A probability (times its value's scale) enters the second product as f16: off by 2^-11 of itself, or by 2^-25 where it
+Tolerances, from the arithmetic. Over 8 bits: a query's elements are off by up to 2^-17 of the largest of their row. A score is
+a binary32 sum of 64 or 128 exact products, off by up to 2^-17 of the sum of their magnitudes; its exponent takes a few
+roundings more of 2^-24 of its size. A probability (times its value's scale) enters the second product as f16: off by 2^-11 of itself, or by 2^-25 where it
 is below 2^-14, against a largest of 2^7 at least; with N keys and 2^e the largest scale that moves O by up to N 2^-23 2^e.
 So with A = sum p |v| / sum p, and delta the scores' error, O is off by (2^-11 + 2 delta) A + N 2^-23 2^e and its own
 rounding, 2^-8 |O|. In 16 bits: 2^-8 for 2^-11, and no last term (test_gpu_chunk_attn.py).
@@ -21,8 +21,8 @@ pytestmark = pytest.mark.gpu
 
 
 def attend64(Q, keys, values, n, kv, scale, softcap=0.0, slopes=None, window=0, sinks=0, first_key=None, prefix_len=None):
-    """Q [T, Hq, d]; keys[b], values[b] [Hkv, N_b, d] float64. Returns O, A [T, Hq, d], lse [T, Hq], and the largest score
-    and sum of magnitudes of a score's products."""
+    """Q [T, Hq, d]; keys[b], values[b] [Hkv, N_b, d] float64. Returns O, A [T, Hq, d], lse [T, Hq], the largest score,
+    and the largest sum of magnitudes of a score's products, with the row's largest added to each of its elements."""
     T, Hq, d = Q.shape
     O, A = torch.zeros((T, Hq, d), dtype=torch.float64), torch.zeros((T, Hq, d), dtype=torch.float64)
     lse = torch.full((T, Hq), -math.inf, dtype=torch.float64)
@@ -44,7 +44,8 @@ def attend64(Q, keys, values, n, kv, scale, softcap=0.0, slopes=None, window=0, 
             V = torch.where(see.any(0)[:, None], values[b][kvh, :N], 0.0)
             s = Q[rows, h] @ K.T * scale
             if N and n[b]:
-                mag = max(mag, float((Q[rows, h].abs() @ K.abs().T * scale).max()))
+                q = Q[rows, h].abs()
+                mag = max(mag, float(((q + q.amax(-1, keepdim=True)) @ K.abs().T * scale).max()))
             if softcap:
                 s = softcap * torch.tanh(s / softcap)
             if slopes is not None:
