@@ -122,7 +122,7 @@ struct PlanHead {
 };
 
 struct ChunkWs {
-  size_t status, head, count, blocks, seen, part_o, part_ml, total;
+  size_t status, head, count, blocks, seen, part_o, part_ml, q_parts, q_exp, total;
 };
 
 // Tokens of a block and the most blocks that T tokens of B sequences have.
@@ -144,6 +144,9 @@ static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
   // two slots per CTA: its first item, and its last where that goes on in the next CTA
   w.part_o = take(size_t(2 * kCMaxCtas) * kCBlockRows * d * sizeof(float));
   w.part_ml = take(size_t(2 * kCMaxCtas) * kCBlockRows * 2 * sizeof(float));
+  // (a cache in 8 bits) the queries as e4m3 parts, and their exponents
+  w.q_parts = take((size_t)T * Hq * d * 2);
+  w.q_exp = take((size_t)T * Hq);
   w.total = off;
   return w;
 }
@@ -518,6 +521,7 @@ struct ChunkArgs {
   // cache in 8 bits: exponents of the scales [planes, Hkv, rows / 2^block_log2] (rows: of a page, or S_cap)
   const uint8_t *Ks, *Vs;
   int block_log2, rows;
+  const uint8_t* q_exp;  // [T, Hq]: exponent + 127 of what the queries were multiplied by
 };
 
 // One item: a run of key tiles of one block for one kv head.
@@ -553,6 +557,15 @@ __device__ __forceinline__ int item_tile(const ChunkItem& it, int j) {
 // plain kernel costs it instruction fetches, also beside its loop.)
 constexpr int kCap = 1, kBias = 2, kWideCap = 4, kDocs = 8, kQ8 = 16, kSink = 32;
 
+// (8 bits) What the softmax takes of a tile's scales: of K for every 16 keys; of V the largest, to whose exponent the
+// tile's values are brought by their conversion.
+struct TileScales {
+  float k[8];
+  float v_log2, v_inverse;
+  float pad[2];
+};
+static_assert(sizeof(TileScales) == 48, "");
+
 // A cache in 8 bits: tiles of K in a ring that the MMAs read as it is; raw tiles of V in another, converted to f16 by a
 // warpgroup into the ring of chunks.
 template <int D, bool Q8>
@@ -561,23 +574,22 @@ struct ChunkSmem {
   static constexpr int kTile = kBoxes * 16384;           // 128 rows of Q, K or V: per 64 columns 128 rows of 128 bytes
   static constexpr int kChunks = Q8 ? (D == 128 ? 2 : 4) : (D == 128 ? 5 : 10);
   static constexpr int kRawTile = 128 * D;
-  static constexpr int kKs = Q8 ? (D == 128 ? 3 : 6) : 0, kRaws = Q8 ? (D == 128 ? 3 : 6) : 0;
-  static constexpr int kScaleStages = 4;                 // of each stream
+  static constexpr int kKs = D == 128 ? 3 : 6, kRaws = D == 128 ? 3 : 6;
+  static constexpr int kScaleStages = 2;                 // of each stream
   static constexpr int kQ = 0;                           // two row tiles
   static constexpr int kRing = 2 * kTile;
   static constexpr int kKRing = kRing + kChunks * kTile;
-  static constexpr int kRaw = kKRing + kKs * kRawTile;
-  static constexpr int kBar = kRaw + kRaws * kRawTile;
+  static constexpr int kRaw = kKRing + (Q8 ? kKs * kRawTile : 0);
+  static constexpr int kBar = kRaw + (Q8 ? kRaws * kRawTile : 0);
   // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], got[2][2], pvdone[2], ofree[2], qfull,
-  // qempty, drain, gap; 8 bits: kfull[ks], kempty[ks], rfull[raws], rempty[raws], qready, qread, cfull[2][stages],
-  // cempty[2][stages]
-  static constexpr int kNumBars = 2 * kChunks + 14 + 4 + (Q8 ? 2 * kKs + 2 * kRaws + 2 + 4 * kScaleStages : 0);
-  static constexpr int kInfo = kBar + (8 * kNumBars + 63) / 64 * 64;
+  // qempty, drain, gap; 8 bits: kfull[ks], kempty[ks], rfull[raws], rempty[raws], cfull[2][stages], cempty[2][stages]
+  static constexpr int kNumBars = 2 * kChunks + 14 + 4 + (Q8 ? 2 * kKs + 2 * kRaws + 4 * kScaleStages : 0);
+  static constexpr int kInfo = kBar + (8 * kNumBars + 15) / 16 * 16;
   static constexpr int kMisc = kInfo + 2 * 80;           // [0] misaligned, [1] this CTA merges, [2] tensor memory
-  static constexpr int kStat = kMisc + 16;               // (m, l) of each stream's rows (streams to be combined)
-  static constexpr int kScales = kStat + kCStreams * kCRows * 8;  // [stream][stage]: 8 exponents of K, 8 of V
-  static constexpr int kQExp = kScales + (Q8 ? kCStreams * kScaleStages * 16 : 0);  // [row tile][row]: Q's scale
-  static constexpr int kBytes = kQExp + (Q8 ? 2 * kCRows : 0);
+  static constexpr int kStat = kMisc + 16;               // (m, l) of streams to be combined: of each, or of one at a time
+  static constexpr int kScales = kStat + (Q8 ? 1 : kCStreams) * kCRows * 8;  // [stream][stage]: struct TileScales
+  static constexpr int kVScales = kScales + (Q8 ? kCStreams * kScaleStages * 48 : 0);  // [raw tile]: 8 f16 factors
+  static constexpr int kBytes = kVScales + (Q8 ? kRaws * 16 : 0);
   // tensor memory: scores, of each stream (D = 64) or of the step at hand (128: no room for two), P and O of each
   static constexpr int kScores = D == 128 ? 1 : 2;
   static constexpr int kColS = 0, kColP = kScores * 128, kColO = kColP + kCStreams * 64;
@@ -590,10 +602,10 @@ struct ChunkSmem {
 constexpr int kCSoftmaxRegs = 208, kCOtherRegs = 88;
 static_assert(kCSoftmaxWarps * 32 * kCSoftmaxRegs + 128 * kCOtherRegs <= kCThreads * 168, "");
 // A cache in 8 bits takes a warpgroup more: 512 threads start with 128 each (65536 in all), of which the softmax keeps
-// 184, the third warpgroup 80 and the converters 64 (256 x 184 + 128 x 80 + 128 x 64 = 65536).
+// 200, the third warpgroup 72 and the converters 40 (256 x 200 + 128 x 72 + 128 x 40 = 65536).
 constexpr int kCThreadsQ8 = kCThreads + 128;
 constexpr int kScaleWarp = kCMmaWarp + 1, kConvertWarp = kCMmaWarp + 3, kConverters = 4;
-constexpr int kQ8SoftmaxRegs = 184, kQ8OtherRegs = 80, kQ8ConvertRegs = 64;
+constexpr int kQ8SoftmaxRegs = 200, kQ8OtherRegs = 72, kQ8ConvertRegs = 40;
 static_assert(kCSoftmaxWarps * 32 * kQ8SoftmaxRegs + 128 * kQ8OtherRegs + 128 * kQ8ConvertRegs <= kCThreadsQ8 * 128, "");
 template <int N>
 __device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -660,6 +672,54 @@ __device__ __forceinline__ uint32_t f16_of_e4m3(uint16_t c) {
   return h;
 }
 __device__ __forceinline__ float power_of_two_biased(uint32_t e) { return __uint_as_float(e << 23); }  // 2^(e - 127)
+
+// (8 bits) The queries as two e4m3 parts: a row (a token's head) times the power of two that brings its largest into
+// [2^7, 2^8) becomes the nearest e4m3 and the rest, together all eight bits of what lies within 2^-9 of the largest, else
+// off by 2^-17 of it at most. Per 64 elements the first parts, then the second, in the bytes that the elements took. A
+// launch of its own: in the attention, where each CTA did it for its items, a prompt of 8192 tokens took 92 us longer.
+constexpr int kSplitThreads = 256;
+template <int D>
+static __global__ void __launch_bounds__(kSplitThreads) split_q_kernel(const uint16_t* __restrict__ Q, long long rows,
+                                                                       uint8_t* __restrict__ parts,
+                                                                       uint8_t* __restrict__ exps) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  constexpr int kLanes = D / 16;  // of a row
+  const long long i = (long long)blockIdx.x * kSplitThreads + threadIdx.x, row = i / kLanes;
+  const int j = (int)(i % kLanes);
+  uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  if (row < rows) {
+    const uint4* src = reinterpret_cast<const uint4*>(Q + row * D) + 2 * j;
+    v[0] = src[0];
+    v[1] = src[1];
+  }
+  const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = __vmaxu2(top, w[k] & 0x7fff7fffu);
+  top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+  for (int off = 1; off < kLanes; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+  // (rows below 2^-119 are not brought up that far: the factor and its inverse are normal numbers)
+  const int fe = min(261 - (int)(top >> 7), 253);
+  const float f = power_of_two_biased(fe);
+  uint32_t first[4], rest[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float x0 = bf16_lo(w[2 * k]) * f, x1 = bf16_hi(w[2 * k]) * f;
+    const float x2 = bf16_lo(w[2 * k + 1]) * f, x3 = bf16_hi(w[2 * k + 1]) * f;
+    const uint32_t lo = e4m3_of(x0, x1), hi = e4m3_of(x2, x3);
+    const uint32_t hl = f16_of_e4m3((uint16_t)lo), hh = f16_of_e4m3((uint16_t)hi);
+    const float2 yl = __half22float2(*reinterpret_cast<const __half2*>(&hl));
+    const float2 yh = __half22float2(*reinterpret_cast<const __half2*>(&hh));
+    first[k] = lo | hi << 16;
+    rest[k] = e4m3_of(x0 - yl.x, x1 - yl.y) | e4m3_of(x2 - yh.x, x3 - yh.y) << 16;
+  }
+  if (row >= rows) return;
+  uint4* dst = reinterpret_cast<uint4*>(parts + row * D * 2 + j / 4 * 128 + j % 4 * 16);
+  dst[0] = make_uint4(first[0], first[1], first[2], first[3]);
+  dst[4] = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+  if (j == 0) exps[row] = (uint8_t)fe;
+}
 
 // a / b for a >= 0, b > 0, in 32 bits where both fit (a 64-bit division is a long sequence, and a call of one token has
 // several of them between its launch and its first copy)
@@ -863,13 +923,11 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
   const uint32_t bQEmpty = bQFull + 8;
   const uint32_t bDrain = bQEmpty + 8;
   const uint32_t bGap = bDrain + 8;       // V tiles of which the producer clears rows
-  const uint32_t bKFull = bGap + 8;       // 8 bits: tiles of K, raw ones of V, Q in parts, its scales read, the tiles' scales
+  const uint32_t bKFull = bGap + 8;       // 8 bits: tiles of K, raw ones of V, the tiles' scales
   const uint32_t bKEmpty = bKFull + 8 * SM::kKs;
   const uint32_t bRFull = bKEmpty + 8 * SM::kKs;
   const uint32_t bREmpty = bRFull + 8 * SM::kRaws;
-  const uint32_t bQReady = bREmpty + 8 * SM::kRaws;
-  const uint32_t bQRead = bQReady + 8;
-  const uint32_t bCFull = bQRead + 8;
+  const uint32_t bCFull = bREmpty + 8 * SM::kRaws;
   const uint32_t bCEmpty = bCFull + 16 * SM::kScaleStages;
   ChunkItem* info = reinterpret_cast<ChunkItem*>(smem + SM::kInfo);
   volatile int* misc = reinterpret_cast<int*>(smem + SM::kMisc);
@@ -906,11 +964,9 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         mbar_init(bKEmpty + 8 * s, 1);
       }
       for (int s = 0; s < SM::kRaws; ++s) {
-        mbar_init(bRFull + 8 * s, 1);
+        mbar_init(bRFull + 8 * s, 2);  // the tile, and its factors
         mbar_init(bREmpty + 8 * s, kConverters);
       }
-      mbar_init(bQReady, kConverters);
-      mbar_init(bQRead, kCSoftmaxWarps);
       for (int s = 0; s < 2 * SM::kScaleStages; ++s) {
         mbar_init(bCFull + 8 * s, 1);
         mbar_init(bCEmpty + 8 * s, 4);
@@ -935,7 +991,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
   if (misaligned) {
     if (tid == 0) raise_status(A.status, LIBRASPEC_ST_TIMEOUT);
   } else if (Q8 && warp >= kConvertWarp) {
-    // ======================= converters: raw tiles of V to f16, Q to e4m3 parts =======================
+    // ======================= converters: raw tiles of V to f16 =======================
     regs_leave<kQ8ConvertRegs>();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int ct = tid - kConvertWarp * 32;
@@ -954,7 +1010,6 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       it.sink = src.sink;
       it.klo = src.klo;
       it.khi = src.khi;
-      it.pair = src.pair;
       it.gaps = src.gaps;
       it.pos0 = src.pos0;
       it.rows = src.rows;
@@ -962,94 +1017,6 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       if (last == 2) break;
       __syncwarp();
       if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
-      // Q, a row a thread: times the power of two that brings its largest into [2^7, 2^8), as two e4m3 parts, the nearest
-      // and the rest: together all eight bits of what lies within 2^-9 of the largest, else off by 2^-17 of it at most.
-      ok = warp_wait(bQFull, item_ctr & 1) && (item_ctr == 0 || warp_wait(bQRead, (item_ctr - 1) & 1));
-      if (!ok) break;
-#pragma unroll 1
-      for (int s = 0; s <= it.pair; ++s) {
-        if (ct >= R || s * R + ct >= it.rows) break;
-        uint8_t* q = smem + SM::kQ + s * SM::kTile + ct * 128;
-        auto chunk = [&](int box, int k) { return reinterpret_cast<uint4*>(q + box * 16384 + ((k ^ ct) & 7) * 16); };
-        uint32_t top = 0;
-#pragma unroll
-        for (int k = 0; k < SM::kBoxes * 8; ++k) {
-          const uint4 v = *chunk(k / 8, k % 8);
-          const uint32_t a = __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), b = __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu);
-          top = __vmaxu2(top, __vmaxu2(a, b));
-        }
-        // (rows below 2^-119 are not brought up that far: the factor and its inverse are normal numbers)
-        const int e = (int)(max(top & 0xffffu, top >> 16) >> 7), fe = min(261 - e, 253);
-        smem[SM::kQExp + s * kCRows + ct] = (uint8_t)fe;
-        const float f = power_of_two_biased(fe);
-        // sixteen elements, to their first parts and their second
-        auto split = [&](uint4& u, uint4& v) {
-          const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-          uint32_t first[4], rest[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float x0 = bf16_lo(w[2 * k]) * f, x1 = bf16_hi(w[2 * k]) * f;
-            const float x2 = bf16_lo(w[2 * k + 1]) * f, x3 = bf16_hi(w[2 * k + 1]) * f;
-            const uint32_t lo = e4m3_of(x0, x1), hi = e4m3_of(x2, x3);
-            const uint32_t hl = f16_of_e4m3((uint16_t)lo), hh = f16_of_e4m3((uint16_t)hi);
-            const float2 yl = __half22float2(*reinterpret_cast<const __half2*>(&hl));
-            const float2 yh = __half22float2(*reinterpret_cast<const __half2*>(&hh));
-            first[k] = lo | hi << 16;
-            rest[k] = e4m3_of(x0 - yl.x, x1 - yl.y) | e4m3_of(x2 - yh.x, x3 - yh.y) << 16;
-          }
-          u = make_uint4(first[0], first[1], first[2], first[3]);
-          v = make_uint4(rest[0], rest[1], rest[2], rest[3]);
-        };
-        uint4 u[8];
-        if constexpr (D == 64) {  // a row: the first parts, then the second
-#pragma unroll
-          for (int k = 0; k < 8; ++k) u[k] = *chunk(0, k);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            split(u[2 * k], u[2 * k + 1]);
-            *chunk(0, k) = u[2 * k];
-            *chunk(0, 4 + k) = u[2 * k + 1];
-          }
-        } else {
-          // The first parts lie where the row's first 64 elements lay, the second where the others did: chunk k of both
-          // is written once chunk k of both has been read, half of the row in registers at a time.
-          auto put = [&](int k, uint4 a, uint4 b) {
-            *chunk(0, k) = a;
-            *chunk(1, k) = b;
-          };
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            u[k] = *chunk(0, k);
-            u[4 + k] = *chunk(1, k);
-          }
-#pragma unroll
-          for (int k = 0; k < 8; k += 2) split(u[k], u[k + 1]);
-          put(0, u[0], u[1]);
-          put(1, u[2], u[3]);
-          u[0] = *chunk(0, 4);
-          u[1] = *chunk(0, 5);
-          u[2] = *chunk(1, 4);
-          u[3] = *chunk(1, 5);
-          put(4, u[4], u[5]);
-          put(5, u[6], u[7]);
-          split(u[0], u[1]);
-          split(u[2], u[3]);
-          put(2, u[0], u[1]);
-          u[4] = *chunk(0, 6);
-          u[5] = *chunk(0, 7);
-          u[6] = *chunk(1, 6);
-          u[7] = *chunk(1, 7);
-          put(6, u[2], u[3]);
-          split(u[4], u[5]);
-          split(u[6], u[7]);
-          put(3, u[4], u[5]);
-          put(7, u[6], u[7]);
-        }
-      }
-      __syncwarp();
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bQReady);
       const int n = it.n_tiles, n_tok = it.rows / g;
       const int sinks = SINK ? min(A.mask.sinks, it.khi) : 0;
       const uint32_t* seen = A.seen + (size_t)max(it.gaps, 0) * kSeenWords;
@@ -1064,7 +1031,8 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const bool edge = kt0 < it.klo || kt0 + kCKeys > it.khi || gap;
         const uint8_t* raw = smem + SM::kRaw + rc * SM::kRawTile + ct * 16;
         uint8_t* dst = smem + SM::kRing + ch * SM::kTile + (D == 128 ? cj / 4 * 16384 : 0);
-#pragma unroll
+        const uint4 factors = *reinterpret_cast<const uint4*>(smem + SM::kVScales + rc * 16);  // of each 16 keys
+#pragma unroll 1
         for (int i0 = 0; i0 < kUnits; i0 += 4) {
           uint4 v[4];
 #pragma unroll
@@ -1081,10 +1049,23 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int row = crow + (i0 + i) * kRowStep;
-            const uint4 lo = make_uint4(f16_of_e4m3((uint16_t)v[i].x), f16_of_e4m3((uint16_t)(v[i].x >> 16)),
-                                        f16_of_e4m3((uint16_t)v[i].y), f16_of_e4m3((uint16_t)(v[i].y >> 16)));
-            const uint4 hi = make_uint4(f16_of_e4m3((uint16_t)v[i].z), f16_of_e4m3((uint16_t)(v[i].z >> 16)),
-                                        f16_of_e4m3((uint16_t)v[i].w), f16_of_e4m3((uint16_t)(v[i].w >> 16)));
+            __half2 f;  // of the row's 16 keys
+            if constexpr (D == 128) {  // the (i0 + i)-th
+              const uint32_t w = i < 2 ? (i0 ? factors.z : factors.x) : (i0 ? factors.w : factors.y);
+              const uint32_t p = __byte_perm(w, 0, i % 2 ? 0x3232 : 0x1010);
+              f = *reinterpret_cast<const __half2*>(&p);
+            } else {
+              const uint32_t w = i == 0 ? factors.x : i == 1 ? factors.y : i == 2 ? factors.z : factors.w;
+              const uint32_t p = __byte_perm(w, 0, crow >= 16 ? 0x3232 : 0x1010);
+              f = *reinterpret_cast<const __half2*>(&p);
+            }
+            auto to_f16 = [&](uint32_t codes) {
+              const uint32_t h = f16_of_e4m3((uint16_t)codes);
+              const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h), f);
+              return *reinterpret_cast<const uint32_t*>(&y);
+            };
+            const uint4 lo = make_uint4(to_f16(v[i].x), to_f16(v[i].x >> 16), to_f16(v[i].y), to_f16(v[i].y >> 16));
+            const uint4 hi = make_uint4(to_f16(v[i].z), to_f16(v[i].z >> 16), to_f16(v[i].w), to_f16(v[i].w >> 16));
             const int c = 2 * cj & 7;
             uint8_t* r = dst + row * 128;
             *reinterpret_cast<uint4*>(r + (((c + order) ^ row) & 7) * 16) = order ? hi : lo;
@@ -1354,11 +1335,11 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const uint32_t ts = tmem + SM::kColS + (SM::kScores == 2 ? s * 128 : 0);
         tc_fence_after();
         const uint32_t qa = q_desc + qs * (SM::kTile / 16);
-        if constexpr (Q8) {  // the parts of Q one after the other
+        if constexpr (Q8) {  // both parts of Q's 64 columns at a time
           const uint32_t ka = desc_lo(sK, 16) + c * (SM::kRawTile / 16);
 #pragma unroll
-          for (int part = 0; part < SM::kBoxes; ++part)
-            mma_f8_ss4_warp<D == 64>(ts, qa + part * 1024, ka, idesc, part != 0 ? 1u : 0u);
+          for (int hb = 0; hb < SM::kBoxes; ++hb)
+            mma_f8_ss4_warp<D == 64>(ts, qa + hb * 1024, ka + hb * 4, idesc, hb != 0 ? 1u : 0u);
         } else {
           const uint32_t ka = k_desc + c * (SM::kTile / 16);
 #pragma unroll
@@ -1385,7 +1366,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         if (last == 2) break;
         if (lane == 0) mbar_arrive(bIEmpty + 8 * (item_ctr & 1));
         __syncwarp();
-        need(Q8 ? bQReady : bQFull, item_ctr & 1);
+        need(bQFull, item_ctr & 1);
         // One word from a stream for each of its tiles, and one more: the tile's scores are in registers, and P of the
         // tile before is written. Behind it go the next S into the place that it left (D = 64: the stream's own next
         // tile; D = 128: the other stream's) and that PV. Chunks are asked for before the word. (Words lie on two
@@ -1475,7 +1456,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       // Lane 8 k + i has those of the i-th 16 keys of the k-th of four tiles; the next four are on their way meanwhile.
       asm volatile("griddepcontrol.wait;" ::: "memory");
       const int i = lane & 7;
-      uint32_t item_ctr = 0, ctr[2] = {0, 0};
+      uint32_t item_ctr = 0, raw_ctr = 0, ctr[2] = {0, 0};
       bool ok = true;
       for (int last = 0; !last && ok; ++item_ctr) {
         ok = warp_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
@@ -1490,7 +1471,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           const int t = t0 + lane / 8;
           if (t >= n) return 0u;
           const int key = item_tile<SINK>(it, tile_of<SHAPE>(t, n)) * kCKeys + 16 * i;
-          if (key >= it.khi || (key + 16 <= it.klo && key >= sinks)) return 127u | 127u << 8;
+          if (key >= it.khi || (key + 16 <= it.klo && key >= sinks)) return 127u;  // (of V: below all others)
           int plane = it.b, row = key;
           if (A.block_table) {
             plane = __ldg(A.block_table + (size_t)it.b * A.max_pages + key / A.page_size);
@@ -1504,15 +1485,34 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         uint32_t now = load(0);
         for (int t0 = 0; t0 < n && ok; t0 += 4) {
           const uint32_t next = load(t0 + 4);
+          // the largest exponent of V of a tile, and its groups' factors 2^(e - largest) as f16
+          const int ev = (int)(now >> 8);
+          int top = ev;
+#pragma unroll
+          for (int off = 4; off > 0; off >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const int down = top - ev;
+          const uint16_t factor = down <= 14 ? (uint16_t)((15 - down) << 10) : down <= 24 ? (uint16_t)(1 << (24 - down)) : 0;
+          if (top == 0) top = 127;  // (no group of the tile is seen)
           for (int k = 0; k < 4 && t0 + k < n && ok; ++k) {
+            const uint32_t rc = raw_ctr % SM::kRaws;
+            ok = warp_wait(bREmpty + 8 * rc, ((raw_ctr / SM::kRaws) & 1) ^ 1);
+            if (!ok) break;
+            if (lane / 8 == k) reinterpret_cast<uint16_t*>(smem + SM::kVScales + rc * 16)[i] = factor;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bRFull + 8 * rc);
+            ++raw_ctr;
             for (int s = 0; s < 2 && ok; ++s) {
               if (!it.pair && s != ((t0 + k) & 1)) continue;
               const uint32_t c = s ? ctr[1]++ : ctr[0]++, stage = s * SM::kScaleStages + c % SM::kScaleStages;
               ok = warp_wait(bCEmpty + 8 * stage, ((c / SM::kScaleStages) & 1) ^ 1);
               if (!ok) break;
               if (lane / 8 == k) {
-                smem[SM::kScales + stage * 16 + i] = (uint8_t)now;
-                smem[SM::kScales + stage * 16 + 8 + i] = (uint8_t)(now >> 8);
+                TileScales* to = reinterpret_cast<TileScales*>(smem + SM::kScales) + stage;
+                to->k[i] = power_of_two_biased(now & 0xffu);
+                if (i == 0) {
+                  to->v_log2 = (float)(top - 127);
+                  to->v_inverse = power_of_two_biased(254u - top);
+                }
               }
               __syncwarp();
               if (lane == 0) mbar_arrive(bCFull + 8 * stage);
@@ -1573,10 +1573,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       }
       float unscale = 1.f;  // of the row's Q
       if constexpr (Q8) {
-        wait(bQReady, item_ctr & 1);
-        unscale = power_of_two_biased(254u - smem[SM::kQExp + (pair ? st : 0) * kCRows + row]);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bQRead);
+        if (valid) unscale = power_of_two_biased(254u - __ldcg(A.q_exp + (size_t)tok * A.Hq + hq));
       }
       const float sc = SHAPE & (kCap | kBias) ? 1.f : scale_log2 * unscale;
       const int sinks = SINK ? min(A.mask.sinks, hi) : 0;  // (the row's)
@@ -1586,11 +1583,17 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const int j = pair ? i : 2 * i + st;  // the item's tile
         const int kt0 = item_tile<SINK>(it, tile_of<SHAPE>(j, n_tiles)) * kCKeys;
         const uint32_t n = (st ? done1 : done0) + i;
-        uint4 tile_scales = make_uint4(0, 0, 0, 0);
+        float k_scale[8] = {};
+        float v_log2 = 0.f, v_inverse = 0.f;
         if constexpr (Q8) {
           const uint32_t stage = st * SM::kScaleStages + n % SM::kScaleStages;
           wait(bCFull + 8 * stage, (n / SM::kScaleStages) & 1);
-          tile_scales = *reinterpret_cast<const uint4*>(smem + SM::kScales + stage * 16);
+          const float4* from = reinterpret_cast<const float4*>(smem + SM::kScales + stage * 48);
+          const float4 a = from[0], b = from[1], c = from[2];
+          k_scale[0] = a.x, k_scale[1] = a.y, k_scale[2] = a.z, k_scale[3] = a.w;
+          k_scale[4] = b.x, k_scale[5] = b.y, k_scale[6] = b.z, k_scale[7] = b.w;
+          v_log2 = c.x;
+          v_inverse = c.y;
           __syncwarp();
           if (lane == 0) mbar_arrive(bCEmpty + 8 * stage);
         }
@@ -1626,17 +1629,10 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bGot + 16 * st + 8 * ((words + i) & 1));
-        // Of 16 keys: 2^(e + 127) of their K scale, and of V's; e of V's.
-        auto k_scale = [&](int gr) {
-          return power_of_two_biased(((gr < 4 ? tile_scales.x : tile_scales.y) >> (8 * (gr & 3))) & 0xffu);
-        };
-        auto v_exp = [&](int gr) { return ((gr < 4 ? tile_scales.z : tile_scales.w) >> (8 * (gr & 3))) & 0xffu; };
-        // (a small whole number as a float: 2^23 + e, less 2^23 + 127)
-        auto v_log2 = [&](int gr) { return __uint_as_float(0x4b000000u | v_exp(gr)) - 8388735.f; };
         if constexpr (Q8 && (SHAPE & (kCap | kBias))) {
 #pragma unroll
           for (int gr = 0; gr < 8; ++gr) {
-            const float f = k_scale(gr) * unscale;
+            const float f = k_scale[gr] * unscale;
 #pragma unroll
             for (int c = 0; c < 16; ++c)
               x[gr / 2][gr % 2 * 16 + c] = __float_as_uint(__uint_as_float(x[gr / 2][gr % 2 * 16 + c]) * f);
@@ -1718,9 +1714,9 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         }
         float cmax;
         // (not zero: a masked score stays minus infinity)
-        auto group_scale = [&](int gr) { return SHAPE & (kCap | kBias) ? 1.f : fmaxf(sc * k_scale(gr), kFloatMin); };
+        auto group_scale = [&](int gr) { return SHAPE & (kCap | kBias) ? 1.f : fmaxf(sc * k_scale[gr], kFloatMin); };
         if constexpr (Q8) {
-          // the largest term of O's sum: P times V's scale
+          // the largest term of O's sum: P times the tile's scale of V
           cmax = -INFINITY;
 #pragma unroll
           for (int gr = 0; gr < 8; ++gr) {
@@ -1729,9 +1725,9 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
 #pragma unroll
             for (int c = 1; c < 15; c += 2) m = fmaxf(fmaxf(m, __uint_as_float(y[c])), __uint_as_float(y[c + 1]));
             m = fmaxf(m, __uint_as_float(y[15]));
-            cmax = fmaxf(cmax, fmaf(m, group_scale(gr), v_log2(gr)));
+            cmax = fmaxf(cmax, m * group_scale(gr));
           }
-          if (!valid) cmax = 0.f;
+          cmax = valid ? cmax + v_log2 : 0.f;
         } else {
           float mx[4];
 #pragma unroll
@@ -1768,7 +1764,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           }
           tmem_wait_st();
         }
-        const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+        const float neg_m = (m_run == -INFINITY ? 0.f : -m_run) + v_log2;
         float la[2] = {0.f, 0.f}, lb[2] = {0.f, 0.f};
         uint32_t pk[4][16];
 #pragma unroll
@@ -1776,24 +1772,21 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           if constexpr (Q8) {
 #pragma unroll
             for (int gr = 2 * q; gr < 2 * q + 2; ++gr) {
-              const float f = group_scale(gr), off = v_log2(gr) + neg_m;
-              float ga[2] = {0.f, 0.f}, gb[2] = {0.f, 0.f};
+              const float f = group_scale(gr);
 #pragma unroll
               for (int c = gr % 2 * 16; c < gr % 2 * 16 + 16; c += 4) {
                 float y0, y1, y2, y3;
-                fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), f, off);
-                fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), f, off);
+                fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), f, neg_m);
+                fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), f, neg_m);
                 y0 = ex2_approx(y0);
                 y1 = ex2_approx(y1);
                 y2 = ex2_approx(y2);
                 y3 = ex2_approx(y3);
-                add2(ga[0], ga[1], y0, y1);
-                add2(gb[0], gb[1], y2, y3);
+                add2(la[0], la[1], y0, y1);
+                add2(lb[0], lb[1], y2, y3);
                 pk[q][c >> 1] = pack_f16(y0, y1);
                 pk[q][(c >> 1) + 1] = pack_f16(y2, y3);
               }
-              // the sum of P itself: without V's scale
-              la[0] = fmaf((ga[0] + ga[1]) + (gb[0] + gb[1]), power_of_two_biased(254u - v_exp(gr)), la[0]);
             }
           } else {
 #pragma unroll
@@ -1823,7 +1816,8 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           }
         }
         tmem_wait_st();
-        l_run += (la[0] + la[1]) + (lb[0] + lb[1]);
+        const float tile_sum = (la[0] + la[1]) + (lb[0] + lb[1]);
+        l_run = Q8 ? fmaf(tile_sum, v_inverse, l_run) : l_run + tile_sum;
       }
       if (my_steps > 0) {  // the last P
         tc_fence_before();
@@ -1835,10 +1829,26 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       float f0 = 1.f, f1 = 0.f;  // factors of the streams' O
       const bool both = !pair && steps1 > 0;  // the streams hold keys of the same rows
       if (both) {
-        if (warp_live) stat[st * kCRows + row] = make_float2(m_run, l_run);
-        bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+        float2 a, b;  // of streams 0 and 1
+        if constexpr (Q8) {  // (through one place for each row, in turns)
+          a = b = make_float2(m_run, l_run);
+          if (warp_live && st == 1) stat[row] = b;
+          bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+          if (warp_live && st == 0) {
+            b = stat[row];
+            stat[row] = a;
+          }
+          bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+          if (warp_live && st == 1) a = stat[row];
+        } else {
+          if (warp_live) stat[st * kCRows + row] = make_float2(m_run, l_run);
+          bar_sync_n(kCAllBar, kCSoftmaxWarps * 32);
+          if (warp_live) {
+            a = stat[row];
+            b = stat[kCRows + row];
+          }
+        }
         if (warp_live) {
-          const float2 a = stat[row], b = stat[kCRows + row];
           const float M = fmaxf(a.x, b.x);
           f0 = M == -INFINITY ? 0.f : ex2_approx(a.x - M);
           f1 = M == -INFINITY ? 0.f : ex2_approx(b.x - M);
@@ -2074,8 +2084,19 @@ static cudaError_t launch_chunk(const ChunkCall& c) {
               : make_map(m, base, c.D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
   };
   if (!cache_map(&a.K, c.K, true) || !cache_map(&a.V, c.V, false) ||
-      !make_map(&a.Q, c.Q, c.D, c.Hq, c.T, g, kCRows / g, CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
+      !make_map(&a.Q, Q8 ? reinterpret_cast<const uint16_t*>(ws + lay.q_parts) : c.Q, c.D, c.Hq, c.T, g, kCRows / g,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
     return cudaErrorInvalidValue;
+  if constexpr (Q8) {
+    uint8_t *parts = reinterpret_cast<uint8_t*>(ws + lay.q_parts), *exps = reinterpret_cast<uint8_t*>(ws + lay.q_exp);
+    a.q_exp = exps;
+    const long long heads = (long long)c.T * c.Hq, grid_q = (heads * (c.D / 16) + kSplitThreads - 1) / kSplitThreads;
+    if (grid_q > 0x7fffffffll) return cudaErrorInvalidValue;
+    if (c.D == 128) split_q_kernel<128><<<(int)grid_q, kSplitThreads, 0, c.stream>>>(c.Q, heads, parts, exps);
+    else split_q_kernel<64><<<(int)grid_q, kSplitThreads, 0, c.stream>>>(c.Q, heads, parts, exps);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   const int grid = std::min(num_sms_current(), kCMaxCtas);
   a.plan = PlanArgs{c.cu_new, c.kv_len, a.mask, c.T, c.B, block_tokens(g), std::min(c.S_cap, kCMaxKeys), c.Hkv, grid,
                     kCSharedBytes / (2 * kCKeys * c.D * (Q8 ? 1 : 2)), a.status};

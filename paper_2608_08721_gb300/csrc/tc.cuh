@@ -231,25 +231,25 @@ __device__ __forceinline__ void mma_ss4_warp(uint32_t d_tmem, uint32_t a_lo, uin
       : "memory");
 }
 
-// Four K steps (32 elements each) of e4m3 operands for a converged warp. A: rows of 128 bytes, 128-byte swizzle. B: the
-// same, or (NARROW) rows of 64 bytes under a 64-byte swizzle (SBO = 512, layout 4), whose two steps are taken twice.
+// Four K steps (32 elements each) of e4m3 operands for a converged warp: A's are those of a row of 128 bytes (128-byte
+// swizzle), B's two, taken twice: of a row of 128 bytes, or (NARROW) of one of 64 under a 64-byte swizzle (SBO = 512,
+// layout 4). A holds two parts of the same elements, one behind the other.
 constexpr uint32_t kDescHi64 = (512u >> 4) | (1u << 14) | (4u << 29);
 template <bool NARROW>
 __device__ __forceinline__ void mma_f8_ss4_warp(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc,
                                                 uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p, e;\n\t.reg .b32 x, y;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "{\n\t.reg .pred p, e;\n\t.reg .b32 x, y;\n\t.reg .b64 a, b, c;\n\tsetp.ne.u32 p, %4, 0;\n\t"
       "elect.sync _|e, 0xffffffff;\n\t"
-      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %6};\n\t"
+      "add.u32 y, %2, 2;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %6};\n\tmov.b64 c, {y, %6};\n\t"
       "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, p;\n\t"
-      "add.u32 x, %1, 2;\n\tadd.u32 y, %2, 2;\n\tmov.b64 a, {x, %5};\n\tmov.b64 b, {y, %6};\n\t"
+      "add.u32 x, %1, 2;\n\tmov.b64 a, {x, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, c, %3, 1;\n\t"
+      "add.u32 x, %1, 4;\n\tmov.b64 a, {x, %5};\n\t"
       "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, 1;\n\t"
-      "add.u32 x, %1, 4;\n\tadd.u32 y, %2, %7;\n\tmov.b64 a, {x, %5};\n\tmov.b64 b, {y, %6};\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, 1;\n\t"
-      "add.u32 x, %1, 6;\n\tadd.u32 y, %2, %8;\n\tmov.b64 a, {x, %5};\n\tmov.b64 b, {y, %6};\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %3, 1;\n\t}" ::"r"(d_tmem),
-      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "n"(kDescHi), "n"(NARROW ? kDescHi64 : kDescHi), "n"(NARROW ? 0 : 4),
-      "n"(NARROW ? 2 : 6)
+      "add.u32 x, %1, 6;\n\tmov.b64 a, {x, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, c, %3, 1;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(acc), "n"(kDescHi), "n"(NARROW ? kDescHi64 : kDescHi)
       : "memory");
 }
 
