@@ -86,6 +86,7 @@ constexpr int kCRows = 128;                 // rows of a tile (tensor-memory lan
 constexpr int kCBlockRows = 2 * kCRows;     // rows of a block, at most
 constexpr int kCKeys = 128;                 // keys of a tile
 constexpr int kCMaxCtas = 192;
+constexpr int kCMaxCounts = 1024;           // merge counters (the few-row kernel has several CTAs per SM)
 constexpr int kCTmemCols = 512;
 constexpr float kCRescaleLog2 = 8.f;
 // A cache in 8 bits has P in f16, whose least step is 2^-24: the reference lies 2^7 below the maximum (P <= 2^15 then,
@@ -132,15 +133,26 @@ inline long long max_blocks(long long T, int B, int g) {
   return a < T ? a : T;
 }
 
+// Rows of a block of the few-row kernel (few_attn_q8.cu): at most 8, or 16. It takes calls whose sequences have 16 rows
+// per kv head on average at most.
+constexpr int kFewRows = 16;
+inline int few_tokens(int g, int rows) { return rows / g; }
+inline bool few_fits(long long T, int B, int g) { return g <= kFewRows && T * g <= (long long)kFewRows * B; }
+inline long long few_blocks(long long T, int B, int tokens) { return std::min(T, T / tokens + B); }
+
 static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
   ChunkWs w{};
+  const int g = Hq / Hkv;
+  long long blocks = max_blocks(T, B, g);
+  // (also of calls with fewer tokens)
+  if (g <= kFewRows) blocks = std::max(blocks, few_blocks(std::min(T, (long long)kFewRows * B / g), B, std::max(1, 8 / g)));
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align256(off + bytes); return o; };
   w.status = take(256);
   w.head = take(sizeof(PlanHead));
-  w.count = take(kCMaxCtas * sizeof(uint32_t));
-  w.blocks = take((size_t)max_blocks(T, B, Hq / Hkv) * sizeof(PlanBlock));
-  w.seen = take((size_t)max_blocks(T, B, Hq / Hkv) * (kCBlockRows / 8));  // a bit for each token of a block
+  w.count = take(kCMaxCounts * sizeof(uint32_t));
+  w.blocks = take((size_t)blocks * sizeof(PlanBlock));
+  w.seen = take((size_t)blocks * (kCBlockRows / 8));  // a bit for each token of a block
   // two slots per CTA: its first item, and its last where that goes on in the next CTA
   w.part_o = take(size_t(2 * kCMaxCtas) * kCBlockRows * d * sizeof(float));
   w.part_ml = take(size_t(2 * kCMaxCtas) * kCBlockRows * 2 * sizeof(float));
@@ -1975,6 +1987,11 @@ static bool make_map(CUtensorMap* map, const void* base, int D, long long rows, 
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+inline CapArgs cap_args(float scale, float softcap) {
+  return CapArgs{std::min(softcap * kLog2e, kFloatMax), std::min(2.f * (scale * kLog2e) / softcap, kFloatMax),
+                 scale / softcap};
+}
+
 // Codes of a cache in 8 bits [planes, rows, D] in boxes of whole rows; swizzled for the MMA, or as they are.
 static bool make_map8(CUtensorMap* map, const void* base, int D, long long rows, long long planes, int box_rows,
                       bool swizzled) {
@@ -2058,10 +2075,7 @@ static cudaError_t launch_chunk(const ChunkCall& c) {
   a.count = reinterpret_cast<uint32_t*>(ws + lay.count);
   a.status = reinterpret_cast<int*>(ws + lay.status);
   a.scale = c.scale;
-  a.cap = CapArgs{};
-  if (c.softcap > 0.f)
-    a.cap = CapArgs{std::min(c.softcap * kLog2e, kFloatMax), std::min(2.f * (c.scale * kLog2e) / c.softcap, kFloatMax),
-                    c.scale / c.softcap};
+  a.cap = c.softcap > 0.f ? cap_args(c.scale, c.softcap) : CapArgs{};
   a.Hq = c.Hq;
   a.Hkv = c.Hkv;
   a.max_pages = c.max_pages;

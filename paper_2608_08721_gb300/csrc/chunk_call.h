@@ -31,5 +31,6 @@ size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);
 cudaError_t launch_chunk_attn(const ChunkCall& c);
 cudaError_t launch_sink_attn(const ChunkCall& c);     // without first keys
 cudaError_t launch_chunk_attn_q8(const ChunkCall& c);
+cudaError_t launch_few_attn_q8(const ChunkCall& c);   // of calls that few_fits
 
 }  // namespace libraspec

@@ -302,3 +302,61 @@ def test_lengths_out_of_range_are_reported():
     x.dev[-1][1, 0] = -1
     O, _, status = x.run()
     assert status == lr.ST_BAD_PAGE and torch.equal(O[:3], want[0][:3])
+
+
+# ------------------------------------------------------------------------------------ few rows: a decode step, a few tokens each
+FEW = [([1, 2, 0, 1], [300, 411, 3, 0]), ([1] * 5, [127, 128, 129, 15, 16]), ([2, 0, 1], [700, 5, 2100]), ([3, 0, 0], [1000, 4, 4])]
+
+
+@pytest.mark.parametrize("n,kv", FEW)
+@pytest.mark.parametrize("Hq,Hkv", [(4, 4), (8, 2), (7, 1), (16, 2), (11, 1), (16, 1)])
+@pytest.mark.parametrize("page,d,block", [(0, 64, 32), (32, 128, 16), (0, 128, 64), (16, 64, 16)])
+def test_few_rows(n, kv, Hq, Hkv, page, d, block):
+    Inputs(n, kv, Hq, Hkv, d, page, block, seed=Hq + d).check()
+
+
+@pytest.mark.parametrize("opts", [dict(window=1), dict(window=5, sinks=1), dict(window=128, sinks=130), dict(window=100000, sinks=7),
+                                  dict(softcap=2.0), dict(softcap=30.0, window=77, sinks=4), dict(softcap=1e4), dict(bias=True),
+                                  dict(bias=True, window=60, sinks=3), dict(softcap=500.0, bias=True, window=90, sinks=40),
+                                  dict(prefix=True), dict(prefix=True, window=40, sinks=2), dict(docs=True),
+                                  dict(docs=True, prefix=True, bias=True, softcap=5.0, window=200)])
+@pytest.mark.parametrize("Hq,page,d,block", [(4, 0, 64, 32), (4, 32, 128, 16), (14, 16, 64, 16), (14, 64, 128, 64)])
+def test_few_rows_and_options(opts, Hq, page, d, block):
+    n, kv = [2, 1, 0, 1, 1], [300, 411, 3, 0, 1500]
+    Inputs(n, kv, Hq, 2, d, page, block, seed=3, q_scale=2.0).check(**options(opts, n, kv, Hq))
+
+
+@pytest.mark.parametrize("exps", [(67, 68), (100, 150), (186, 188)])
+def test_few_rows_and_scales_over_their_whole_range(exps):
+    q = 2.0 ** (127 - 6 - (exps[0] + exps[1]) // 2)
+    x = Inputs([1, 1], [200, 500], 4, 2, 128, 32, 16, seed=2, q_scale=min(max(q, 2.0 ** -66), 2.0 ** 54), exps=exps)
+    if exps[1] - exps[0] > 40:
+        x.Q *= 2.0 ** -20
+    x.check()
+
+
+def test_few_rows_of_long_caches():
+    """Items of several CTAs, more pieces than a warp looks up at once; the same bits from run to run."""
+    x = Inputs([1, 1, 2], [40000, 9000, 17], 4, 1, 64, 64, 16, seed=3)
+    x.check()
+    x = Inputs([1, 1], [30000, 12345], 8, 1, 128, 0, 64, seed=4)
+    x.check()
+    first = x.run()
+    assert all(torch.equal(a, b) for a, b in zip(first[:2], x.run()[:2]))
+
+
+def test_few_rows_of_many_sequences():
+    r = np.random.default_rng(6)
+    B = 700
+    Inputs(r.integers(0, 3, B).tolist(), r.integers(0, 300, B).tolist(), 4, 1, 64, 16, 16, seed=7).check(window=100, sinks=2)
+
+
+def test_few_and_many_rows_share_a_workspace():
+    """Calls of both kernels in turn on one workspace, as steps of a server make them."""
+    big, few = Inputs([300, 40], [500, 90], 8, 2, 128, 64, 16, seed=1), Inputs([1, 1], [4000, 2500], 8, 2, 128, 64, 16, seed=2)
+    ws = lr.ChunkWorkspace(340, 2, 8, 2, 128)
+    want = [x.run() for x in (big, few)]
+    for _ in range(2):
+        for x, w in zip((big, few), want):
+            got = x.run(ws)
+            assert got[2] == 0 and torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])
