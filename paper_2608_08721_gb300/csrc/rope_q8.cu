@@ -18,9 +18,9 @@
 // larger one that the new tokens ask for, and then the codes that it had are
 // rounded to it (to the nearest, ties to even, as the new ones).
 //
-// A CTA takes one block of a (sequence, kv head), keys or values: its threads
-// hold the new rows in registers between the maximum and the codes. Other CTAs
-// of the launch rotate the queries, a token each.
+// A CTA (or, with few new tokens, a warp) takes one block of a (sequence, kv
+// head), keys or values, at a time: its threads hold the new rows in registers
+// between the maximum and the codes.
 #include <cuda_fp16.h>
 
 #include "rope.cuh"
@@ -68,43 +68,46 @@ struct HeadPart {
     }
   }
   // x r w; all lanes of the warp take part, groups of G lanes (a power of two) have a head each
-  __device__ __forceinline__ void norm(const float* w, float eps, int d, int l, int G, int per_head, int half) {
+  __device__ __forceinline__ void norm(const float* w, float eps, float inv_d, int l, int G, int per_head, int half) {
     float ss = 0.f;
 #pragma unroll
     for (int k = 0; k < U; ++k)
 #pragma unroll
       for (int i = 0; i < N; ++i) ss = fmaf(x[k][i], x[k][i], fmaf(y[k][i], y[k][i], ss));
     for (int off = G >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-    const float r = rsqrtf(ss / (float)d + eps);
+    const float r = rsqrtf(fmaf(ss, inv_d, eps));
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int u = l + k * G;
       if (u >= per_head) continue;
-      const float *wa = w + Unit::at(u, half), *wb = w + Unit::partner(u, half);
+      const Pack<float, N> wa = *reinterpret_cast<const Pack<float, N>*>(w + Unit::at(u, half));
+      const Pack<float, N> wb = *reinterpret_cast<const Pack<float, N>*>(w + Unit::partner(u, half));
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        x[k][i] = x[k][i] * r * wa[i];
-        y[k][i] = y[k][i] * r * wb[i];
+        x[k][i] = x[k][i] * r * wa.v[i];
+        y[k][i] = y[k][i] * r * wb.v[i];
       }
     }
   }
-  // The rotation, with the token's cosines and sines `cs` in the order of RopeUnit::slot; turn(i): the pair's.
+  // The rotation; turns(u, t): the cosines and sines of unit u's pairs.
   template <typename F>
-  __device__ __forceinline__ void rotate(int l, int G, int half, F&& turn_of) {
+  __device__ __forceinline__ void rotate(int l, int G, int half, F&& turns) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int u = l + k * G;
       if (u * N >= half) continue;
       float v[N], z[N];
+      float2 c[N];
+      turns(u, c);
       if constexpr (INTER && N > 1) {
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-          Unit::turn(x[k][i], x[k][i + 1], turn_of(u * N + i / 2), v[i], v[i + 1]);
-          Unit::turn(y[k][i], y[k][i + 1], turn_of(u * N + N / 2 + i / 2), z[i], z[i + 1]);
+          Unit::turn(x[k][i], x[k][i + 1], c[i / 2], v[i], v[i + 1]);
+          Unit::turn(y[k][i], y[k][i + 1], c[N / 2 + i / 2], z[i], z[i + 1]);
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) Unit::turn(x[k][i], y[k][i], turn_of(u * N + i), v[i], z[i]);
+        for (int i = 0; i < N; ++i) Unit::turn(x[k][i], y[k][i], c[i], v[i], z[i]);
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -112,6 +115,21 @@ struct HeadPart {
         y[k][i] = z[i];
       }
     }
+  }
+  // ... from the table `cs` of a token, in the order of RopeUnit::slot
+  __device__ __forceinline__ void rotate_by(const float2* cs, int l, int G, int half) {
+    rotate(l, G, half, [&](int u, float2(&c)[N]) {
+      if constexpr (N == 1) {
+        c[0] = cs[u];
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+          const float4 two = *reinterpret_cast<const float4*>(cs + Unit::slot(u * N + i, half));
+          c[i] = make_float2(two.x, two.y);
+          c[i + 1] = make_float2(two.z, two.w);
+        }
+      }
+    });
   }
   template <typename Tout>
   __device__ __forceinline__ void store(Tout* dst, int l, int G, int per_head, int half) const {
@@ -135,22 +153,39 @@ __host__ __device__ constexpr int head_lanes(int units) {
   return g;
 }
 
-// Heads [0, H) of one token: normed (if w_q is given; heads from Hq on take w_k), rotated by cs, written.
+// Heads [0, H) of one token: normed (w: the weights in shared memory, those of heads from Hq on behind the others', or
+// NULL), rotated by the table cs, written. The heads of the next pass are on their way meanwhile.
 template <typename Tin, typename Tout, int N, bool INTER, int U>
-__device__ __forceinline__ void turn_heads(const Tin* src, Tout* dst, int H, int Hq, int d, int half, const NormArgs& nm,
-                                           const float2* cs) {
+__device__ __forceinline__ void turn_heads(const Tin* src, Tout* dst, int H, int Hq, int d, int half, const float* w,
+                                           float eps, const float2* cs) {
   const int per_head = d / (2 * N), G = head_lanes(per_head), l = threadIdx.x % G;
   const int step = blockDim.x / G;
-  for (int h0 = 0; h0 < H; h0 += step) {  // (all lanes of a warp go round together)
-    const int h = h0 + threadIdx.x / G;
-    const bool has = h < H;
-    HeadPart<Tin, N, INTER, U> p;
-    p.load(src + (size_t)(has ? h : 0) * d, l, G, per_head, half);
-    p.widen_all(l, G, per_head);
-    if (nm.q || nm.k) p.norm(has && h >= Hq ? nm.k : nm.q, nm.eps, d, l, G, per_head, half);
-    p.rotate(l, G, half, [&](int i) { return cs[i]; });
-    if (has) p.store(dst + (size_t)h * d, l, G, per_head, half);
+  const float inv_d = 1.f / (float)d;
+  HeadPart<Tin, N, INTER, U> now, next;
+  int h = threadIdx.x / G;
+  if (h < H) now.load(src + (size_t)h * d, l, G, per_head, half);
+  for (int h0 = 0; h0 < H; h0 += step, h += step) {  // (all lanes of a warp go round together)
+    if (h + step < H) next.load(src + (size_t)(h + step) * d, l, G, per_head, half);
+    if (h0 == 0) __syncthreads();  // the tables are written
+    now.widen_all(l, G, per_head);
+    if (w) now.norm(h >= Hq ? w + d : w, eps, inv_d, l, G, per_head, half);
+    now.rotate_by(cs, l, G, half);
+    if (h < H) now.store(dst + (size_t)h * d, l, G, per_head, half);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      now.a[k] = next.a[k];
+      now.b[k] = next.b[k];
+    }
   }
+}
+
+// A token's table of turns, and the weights, into shared memory.
+template <typename Unit>
+__device__ __forceinline__ void fill_tables(float2* cs, float* w, int pos, const float2* turns, float magnitude, int half,
+                                            const NormArgs& nm, int d) {
+  for (int i = threadIdx.x; i < half; i += blockDim.x) cs[Unit::slot(i, half)] = rope_turn(pos, turns[i], magnitude);
+  if (nm.q)
+    for (int i = threadIdx.x; i < 2 * d; i += blockDim.x) w[i] = i < d ? nm.q[i] : nm.k[i - d];
 }
 
 struct NormRopeArgs {
@@ -167,11 +202,11 @@ struct NormRopeArgs {
 template <typename T, int N, bool INTER, int U>
 __global__ void __launch_bounds__(kQThreads) norm_rope_kernel(const NormRopeArgs A) {
   __shared__ alignas(16) float2 cs[kRopeMaxPairs];
-  const int t = blockIdx.x, pos = A.pos[t];
-  for (int i = threadIdx.x; i < A.half; i += blockDim.x) cs[i] = rope_turn(pos, A.turns[i], A.magnitude);
-  __syncthreads();
+  __shared__ alignas(32) float w[2 * LIBRASPEC_ROPE_MAX_DIM];
+  const int t = blockIdx.x;
+  fill_tables<RopeUnit<T, T, N, INTER>>(cs, w, A.pos[t], A.turns, A.magnitude, A.half, A.norm, A.d);
   turn_heads<T, T, N, INTER, U>(static_cast<const T*>(A.X) + t * A.x_stride, static_cast<T*>(A.Y) + t * A.y_stride, A.H,
-                                A.Hq, A.d, A.half, A.norm, cs);
+                                A.Hq, A.d, A.half, w, A.norm.eps, cs);
 }
 
 // ---------------------------------------------------------------------------
@@ -186,7 +221,10 @@ struct AppendQ8Args {
   NormArgs norm;
   int T, B, Hq, Hkv, half;
   int max_pages, page_size, n_pages, S_cap, block;
-  int n_blocks;  // blocks that the launch has CTAs for
+  int n_blocks;    // blocks that the launch has CTAs for
+  int per;         // of each
+  int block_ctas;  // all of them; the queries' follow
+  int heads;       // kv heads that one of them takes one after the other
   uint16_t* Qo;
   uint8_t *K8, *V8, *Ks, *Vs;
   int* status;
@@ -228,7 +266,7 @@ __device__ __forceinline__ Codes<N> encode(const float (&x)[N], float inv) {
   return c;
 }
 
-// New tokens of sequence b (0 where its offsets are out of range), and the blocks that they touch.
+// New tokens of sequence b that have room (0 where its offsets are out of range), and the blocks that they touch.
 __device__ __forceinline__ int new_blocks(const AppendQ8Args& A, int b, bool report, int& lo, int& kv, int& n) {
   lo = A.cu_new[b];
   kv = A.kv_len[b];
@@ -240,7 +278,7 @@ __device__ __forceinline__ int new_blocks(const AppendQ8Args& A, int b, bool rep
   }
   n = hi - lo;
   if (n == 0) return 0;
-  if (kv < 0 || (long long)kv + n > A.S_cap) {  // rows that have no room are skipped
+  if (kv < 0 || (long long)kv + n > A.S_cap) {
     if (report) raise_status(A.status, LIBRASPEC_ST_KV_OVERFLOW);
     n = kv < 0 || kv >= A.S_cap ? 0 : A.S_cap - kv;
     if (n == 0) return 0;
@@ -249,7 +287,7 @@ __device__ __forceinline__ int new_blocks(const AppendQ8Args& A, int b, bool rep
 }
 
 // Block `i` of the chunk, by all threads of the CTA; false: there is none.
-__device__ bool find_block(const AppendQ8Args& A, int i, bool report, BlockOf& out) {
+static __device__ bool find_block(const AppendQ8Args& A, int i, bool report, BlockOf& out) {
   __shared__ long long warp_sum[kQThreads / 32];
   __shared__ BlockOf found;
   __shared__ int is_found;
@@ -257,9 +295,9 @@ __device__ bool find_block(const AppendQ8Args& A, int i, bool report, BlockOf& o
   if (tid == 0) is_found = 0;
   long long before = 0;
   for (int b0 = 0; b0 < A.B; b0 += kQThreads) {
-    int lo = 0, kv = 0, n = 0, nb = 0;
-    if (b0 + tid < A.B) nb = new_blocks(A, b0 + tid, report, lo, kv, n);
-    const long long mine = nb;
+    int lo = 0, kv = 0, n = 0;
+    long long mine = 0;
+    if (b0 + tid < A.B) mine = new_blocks(A, b0 + tid, report, lo, kv, n);
     long long inc = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -295,132 +333,241 @@ __device__ bool find_block(const AppendQ8Args& A, int i, bool report, BlockOf& o
   return is_found != 0;
 }
 
-template <typename Tin, int N, bool INTER, int D>
-__global__ void __launch_bounds__(kQThreads) append_q8_kernel(const AppendQ8Args A) {
+// Where block `o` lies for kv head 0: its first row and its scale, with the steps from head to head.
+struct BlockPlace {
+  size_t row, scale;
+  int row_step, scale_step;
+};
+// (false: its page does not exist)
+__device__ __forceinline__ bool place_block(const AppendQ8Args& A, const BlockOf& o, BlockPlace& p) {
+  const int rows = A.block_table ? A.page_size : A.S_cap;
+  size_t plane = o.b;
+  int key = o.key0;
+  if (A.block_table) {
+    const int page = A.block_table[(size_t)o.b * A.max_pages + key / A.page_size];
+    if (page < 0 || page >= A.n_pages) {
+      if (threadIdx.x == 0) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
+      return false;
+    }
+    plane = page;
+    key %= A.page_size;
+  }
+  p.row_step = rows;
+  p.scale_step = rows / A.block;
+  p.row = plane * A.Hkv * p.row_step + key;
+  p.scale = plane * A.Hkv * p.scale_step + key / A.block;
+  return true;
+}
+
+template <typename Tin, int N, bool INTER, int U>
+__device__ __forceinline__ uint32_t largest_of(const HeadPart<Tin, N, INTER, U>& p, uint32_t amax) {
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t a = __float_as_uint(p.x[k][e]) & 0x7fffffffu, b = __float_as_uint(p.y[k][e]) & 0x7fffffffu;
+      if (a < 0x7f800000u) amax = max(amax, a);  // (of finite values; magnitudes are ordered as their bits)
+      if (b < 0x7f800000u) amax = max(amax, b);
+    }
+  return amax;
+}
+__device__ __forceinline__ int exponent_of(uint32_t amax) { return clamp_exp((int)(amax >> 23) - 127 - 7); }
+
+// 16 codes to another scale, f = 2^(old - new)
+__device__ __forceinline__ void recode(uint4* at, float f) {
+  uint4 c = *at;
+  uint32_t* w = &c.x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 a = of_e4m3x2((uint16_t)w[k]), b = of_e4m3x2((uint16_t)(w[k] >> 16));
+    w[k] = e4m3x2(a.x * f, a.y * f) | e4m3x2(b.x * f, b.y * f) << 16;
+  }
+  *at = c;
+}
+
+template <typename Tin, int N, bool INTER, int U>
+__device__ __forceinline__ void write_codes(const HeadPart<Tin, N, INTER, U>& p, uint8_t* row, float inv, int l, int G,
+                                            int half) {
+  using Unit = RopeUnit<Tin, Tin, N, INTER>;
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    const int u = l + k * G;
+    *reinterpret_cast<Codes<N>*>(row + Unit::at(u, half)) = encode(p.x[k], inv);
+    *reinterpret_cast<Codes<N>*>(row + Unit::partner(u, half)) = encode(p.y[k], inv);
+  }
+}
+
+// CTAs of the launch: first those of the blocks, `per` each, then those of the queries (kTokens tokens each). With FEW, a
+// CTA has 8 of a block's (kv head, K or V), a warp each; else it goes through `heads` kv heads of the block's keys or
+// values one after the other, the rows of the next on their way, all from one table of cosines.
+template <typename Tin, int N, bool INTER, int D, bool FEW>
+__global__ void __launch_bounds__(kQThreads, 4) append_q8_kernel(const AppendQ8Args A) {
+  constexpr int kTokens = FEW ? 1 : 2;
   constexpr int kPer = D / (2 * N), kG = kPer < 32 ? kPer : 32, kU = kPer / kG;
-  constexpr int kRows = kQThreads / kG, kPasses = (kQMaxBlock + kRows - 1) / kRows;
-  const int tid = threadIdx.x, half = A.half;
-  const int n_kv = A.n_blocks * A.Hkv * 2;
-  if ((int)blockIdx.x < n_kv) {
-    const int i = blockIdx.x / (2 * A.Hkv), hk = blockIdx.x % (2 * A.Hkv);
-    const bool key = hk < A.Hkv;
-    const int h = key ? hk : hk - A.Hkv;
-    __shared__ uint32_t s_amax;
-    __shared__ int s_exp[2];  // the block's exponent now and before
-    if (tid == 0) s_amax = 0;
+  using Part = HeadPart<Tin, N, INTER, kU>;
+  using Unit = RopeUnit<Tin, Tin, N, INTER>;
+  __shared__ alignas(32) float w[2 * D];
+  // cosines and sines: of the block's rows, or of the token
+  __shared__ alignas(16) float2 cs[FEW ? 1 : kQMaxBlock][D / 2];
+  const int tid = threadIdx.x, half = A.half, l = tid % kG;
+  if ((int)blockIdx.x < A.block_ctas) {
+    const int per = A.per, i = blockIdx.x / per, sub = blockIdx.x % per;
     BlockOf o;
+    BlockPlace at;
     if (!find_block(A, i, blockIdx.x == 0, o)) return;
-    size_t row0, sc;  // the block's first row, and its scale
-    if (A.block_table) {
-      int page = A.block_table[(size_t)o.b * A.max_pages + o.key0 / A.page_size];
-      if (page < 0 || page >= A.n_pages) {
-        if (tid == 0) raise_status(A.status, LIBRASPEC_ST_BAD_PAGE);
-        return;
+    if (!place_block(A, o, at)) return;
+    if constexpr (FEW) {
+      if (A.norm.k)
+        for (int j = tid; j < D; j += kQThreads) w[j] = A.norm.k[j];
+      __syncthreads();
+      const int hk = sub * (kQThreads / 32) + tid / 32, lane = tid % 32;
+      if (hk >= 2 * A.Hkv) return;
+      const bool key = hk < A.Hkv;
+      const int h = key ? hk : hk - A.Hkv;
+      const Tin* src = static_cast<const Tin*>(key ? A.K : A.V) + h * D;
+      const long long stride = key ? A.k_stride : A.v_stride;
+      uint8_t* codes = (key ? A.K8 : A.V8) + (at.row + (size_t)h * at.row_step) * D;
+      uint8_t* scale = (key ? A.Ks : A.Vs) + at.scale + (size_t)h * at.scale_step;
+      const int before = o.r0 > 0 ? clamp_exp((int)*scale - 127) : kQMinExp;
+      constexpr int kRows = 32 / kG;  // at a time
+      Part part;
+      auto form = [&](int r) {
+        const bool has = r < o.r1;
+        const int t = o.t0 + r - o.r0;
+        if (has) part.load(src + t * stride, l, kG, kPer, half);
+        part.widen_all(l, kG, has ? kPer : 0);
+        if (key) {
+          if (A.norm.k) part.norm(w, A.norm.eps, 1.f / D, l, kG, kPer, half);
+          if (has) {
+            const int pos = A.pos ? A.pos[t] : o.key0 + r;
+            part.rotate(l, kG, half, [&](int u, float2(&c)[N]) {
+#pragma unroll
+              for (int j = 0; j < N; ++j) c[j] = rope_turn(pos, A.turns[u * N + j], A.magnitude);
+            });
+          }
+        }
+      };
+      uint32_t amax = 0;
+      for (int r = o.r0; r < o.r1; r += kRows) {
+        form(r + lane / kG);
+        amax = largest_of(part, amax);
       }
-      const size_t plane = (size_t)page * A.Hkv + h;
-      row0 = plane * A.page_size + o.key0 % A.page_size;
-      sc = plane * (A.page_size / A.block) + o.key0 % A.page_size / A.block;
+      const int e = max(exponent_of(__reduce_max_sync(0xffffffffu, amax)), before);
+      if (o.r0 > 0 && e != before)  // the rows that the block had, to the new scale
+        for (int u = lane; u < o.r0 * (D / 16); u += 32) recode(reinterpret_cast<uint4*>(codes) + u, power_of_two(before - e));
+      const float inv = power_of_two(-e);
+      for (int r = o.r0; r < o.r1; r += kRows) {
+        if (o.r1 - o.r0 > kRows) form(r + lane / kG);  // (a single pass is still in registers)
+        if (r + lane / kG < o.r1) write_codes(part, codes + (r + lane / kG) * D, inv, l, kG, half);
+      }
+      __syncwarp();  // (all lanes have read the scale)
+      if (lane == 0) *scale = (uint8_t)(e + 127);
     } else {
-      const size_t plane = (size_t)o.b * A.Hkv + h;
-      row0 = plane * A.S_cap + o.key0;
-      sc = plane * (A.S_cap / A.block) + o.key0 / A.block;
-    }
-    const Tin* src = static_cast<const Tin*>(key ? A.K : A.V) + h * D;
-    const long long stride = key ? A.k_stride : A.v_stride;
-    uint8_t* codes = (key ? A.K8 : A.V8) + row0 * D;
-    uint8_t* scales = key ? A.Ks : A.Vs;
-    const int l = tid % kG, rr = tid / kG;
-    HeadPart<Tin, N, INTER, kU> part[kPasses];
+      constexpr int kRows = kQThreads / kG, kPasses = (kQMaxBlock + kRows - 1) / kRows;
+      __shared__ uint32_t s_amax[2];
+      const int groups = per / 2;
+      const bool key = sub < groups;
+      const int h0 = (key ? sub : sub - groups) * A.heads, h1 = min(h0 + A.heads, A.Hkv);
+      const long long stride = key ? A.k_stride : A.v_stride;
+      const Tin* src = static_cast<const Tin*>(key ? A.K : A.V) + o.t0 * stride;
+      const int rr = tid / kG;
+      Part part[kPasses];
+      auto load = [&](int h) {
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const int r = rr + p * kRows;
-      if (r >= o.r0 && r < o.r1) part[p].load(src + (o.t0 + r - o.r0) * stride, l, kG, kPer, half);
-    }
-    uint32_t amax = 0;
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const int r = rr + p * kRows;
-      const bool has = r >= o.r0 && r < o.r1;
-      if (has) part[p].widen_all(l, kG, kPer);
+        for (int p = 0; p < kPasses; ++p) {
+          const int r = rr + p * kRows;
+          if (r >= o.r0 && r < o.r1) part[p].load(src + (r - o.r0) * stride + h * D, l, kG, kPer, half);
+        }
+      };
+      load(h0);
+      if (tid < 2) s_amax[tid] = 0;
       if (key) {
-        if (A.norm.k) part[p].norm(A.norm.k, A.norm.eps, D, l, kG, kPer, half);
-        if (has) {
-          const int pos = A.pos ? A.pos[o.t0 + r - o.r0] : o.key0 + r;
-          part[p].rotate(l, kG, half, [&](int j) { return rope_turn(pos, A.turns[j], A.magnitude); });
+        for (int j = tid; j < (o.r1 - o.r0) * half; j += kQThreads) {
+          const int r = o.r0 + j / half, k = j % half;
+          cs[r][Unit::slot(k, half)] = rope_turn(A.pos ? A.pos[o.t0 + r - o.r0] : o.key0 + r, A.turns[k], A.magnitude);
         }
+        if (A.norm.k)
+          for (int j = tid; j < D; j += kQThreads) w[j] = A.norm.k[j];
       }
-      if (!has) continue;
+      __syncthreads();
+      for (int h = h0; h < h1; ++h) {
+        uint8_t* codes = (key ? A.K8 : A.V8) + (at.row + (size_t)h * at.row_step) * D;
+        uint8_t* scale = (key ? A.Ks : A.Vs) + at.scale + (size_t)h * at.scale_step;
+        const int before = o.r0 > 0 ? clamp_exp((int)*scale - 127) : kQMinExp;
+        uint32_t amax = 0;
 #pragma unroll
-      for (int k = 0; k < kU; ++k)
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const uint32_t a = __float_as_uint(part[p].x[k][e]) & 0x7fffffffu, b = __float_as_uint(part[p].y[k][e]) & 0x7fffffffu;
-          if (a < 0x7f800000u) amax = max(amax, a);  // (of finite values; magnitudes are ordered as their bits)
-          if (b < 0x7f800000u) amax = max(amax, b);
+        for (int p = 0; p < kPasses; ++p) {
+          const int r = rr + p * kRows;
+          const bool has = r >= o.r0 && r < o.r1;
+          part[p].widen_all(l, kG, has ? kPer : 0);
+          if (key && A.norm.k) part[p].norm(w, A.norm.eps, 1.f / D, l, kG, kPer, half);
+          if (key && has) part[p].rotate_by(cs[r], l, kG, half);
+          amax = largest_of(part[p], amax);
         }
-    }
-    amax = __reduce_max_sync(0xffffffffu, amax);
-    if (tid % 32 == 0) atomicMax(&s_amax, amax);
-    __syncthreads();
-    if (tid == 0) {
-      int e = clamp_exp((int)(s_amax >> 23) - 127 - 7), before = e;
-      if (o.r0 > 0) {
-        before = clamp_exp((int)scales[sc] - 127);
-        e = max(e, before);
-      }
-      s_exp[0] = e;
-      s_exp[1] = before;
-      scales[sc] = (uint8_t)(e + 127);
-    }
-    __syncthreads();
-    const int e = s_exp[0], before = s_exp[1];
-    if (e != before) {  // the rows that the block had, to the new scale
-      const float f = power_of_two(before - e);
-      for (int u = tid; u < o.r0 * (D / 16); u += kQThreads) {
-        uint4* at = reinterpret_cast<uint4*>(codes) + u;
-        uint4 c = *at;
-        uint32_t* w = &c.x;
+        if (h + 1 < h1) load(h + 1);  // (the raw values have been widened)
+        amax = __reduce_max_sync(0xffffffffu, amax);
+        if (tid % 32 == 0) atomicMax(&s_amax[h & 1], amax);
+        __syncthreads();
+        const int e = max(exponent_of(s_amax[h & 1]), before);
+        if (tid == 0) s_amax[(h + 1) & 1] = 0;  // (read by all before the second barrier of the head before)
+        if (o.r0 > 0 && e != before)
+          for (int u = tid; u < o.r0 * (D / 16); u += kQThreads)
+            recode(reinterpret_cast<uint4*>(codes) + u, power_of_two(before - e));
+        const float inv = power_of_two(-e);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 a = of_e4m3x2((uint16_t)w[k]), b = of_e4m3x2((uint16_t)(w[k] >> 16));
-          w[k] = e4m3x2(a.x * f, a.y * f) | e4m3x2(b.x * f, b.y * f) << 16;
+        for (int p = 0; p < kPasses; ++p) {
+          const int r = rr + p * kRows;
+          if (r >= o.r0 && r < o.r1) write_codes(part[p], codes + r * D, inv, l, kG, half);
         }
-        *at = c;
-      }
-    }
-    const float inv = power_of_two(-e);
-    using Unit = RopeUnit<Tin, Tin, N, INTER>;
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-      const int r = rr + p * kRows;
-      if (r < o.r0 || r >= o.r1) continue;
-#pragma unroll
-      for (int k = 0; k < kU; ++k) {
-        const int u = l + k * kG;
-        *reinterpret_cast<Codes<N>*>(codes + r * D + Unit::at(u, half)) = encode(part[p].x[k], inv);
-        *reinterpret_cast<Codes<N>*>(codes + r * D + Unit::partner(u, half)) = encode(part[p].y[k], inv);
+        __syncthreads();  // all have read the scale, and the largest is cleared
+        if (tid == 0) *scale = (uint8_t)(e + 127);
       }
     }
     return;
   }
-  // queries, a token a CTA
-  __shared__ alignas(16) float2 cs[D / 2];
-  __shared__ unsigned long long s_owner;  // the token's first sequence and its position there
-  const int t = blockIdx.x - n_kv;
-  if (tid == 0) s_owner = kRopeNone;
+  // queries: the first heads are on their way while the tokens' sequences are looked up
+  __shared__ unsigned long long s_owner[kTokens];  // the token's first sequence and its position there
+  const int t0 = (blockIdx.x - A.block_ctas) * kTokens, n_tok = min(kTokens, A.T - t0), step = kQThreads / kG;
+  const Tin* src = static_cast<const Tin*>(A.Q) + t0 * A.q_stride;
+  Part part[kTokens];
+  auto load = [&](int h) {
+#pragma unroll
+    for (int j = 0; j < kTokens; ++j)
+      if (j < n_tok && h < A.Hq) part[j].load(src + j * A.q_stride + (long long)h * D, l, kG, kPer, half);
+  };
+  load(tid / kG);
+  if (tid < kTokens) s_owner[tid] = kRopeNone;
+  if (A.norm.q)
+    for (int j = tid; j < D; j += kQThreads) w[j] = A.norm.q[j];
   __syncthreads();
   for (int b = tid; b < A.B; b += kQThreads) {
     const int lo = A.cu_new[b], hi = A.cu_new[b + 1];
-    if (lo < 0 || hi < lo || hi > A.T || t < lo || t >= hi) continue;
-    atomicMin(&s_owner, (unsigned long long)b << 32 | (uint32_t)((unsigned)A.kv_len[b] + (unsigned)(t - lo)));
+    if (lo < 0 || hi < lo || hi > A.T) continue;
+#pragma unroll
+    for (int j = 0; j < kTokens; ++j)
+      if (j < n_tok && t0 + j >= lo && t0 + j < hi)
+        atomicMin(&s_owner[j], (unsigned long long)b << 32 | (uint32_t)((unsigned)A.kv_len[b] + (unsigned)(t0 + j - lo)));
   }
   __syncthreads();
-  if (s_owner == kRopeNone) return;
-  const int pos = A.pos ? A.pos[t] : (int)(uint32_t)s_owner;
-  for (int i = tid; i < half; i += kQThreads) cs[i] = rope_turn(pos, A.turns[i], A.magnitude);
+  for (int i = tid; i < kTokens * half; i += kQThreads) {
+    const int j = kTokens == 1 ? 0 : i / half, k = i - j * half;
+    if (j >= n_tok || s_owner[j] == kRopeNone) continue;
+    cs[j][Unit::slot(k, half)] = rope_turn(A.pos ? A.pos[t0 + j] : (int)(uint32_t)s_owner[j], A.turns[k], A.magnitude);
+  }
   __syncthreads();
-  turn_heads<Tin, uint16_t, N, INTER, kU>(static_cast<const Tin*>(A.Q) + t * A.q_stride, A.Qo + (size_t)t * A.Hq * D, A.Hq,
-                                          A.Hq, D, half, A.norm, cs);
+  for (int h0 = 0; h0 < A.Hq; h0 += step) {  // (all lanes of a warp go round together)
+    const int h = h0 + tid / kG;
+#pragma unroll
+    for (int j = 0; j < kTokens; ++j) {
+      if (j >= n_tok) continue;
+      part[j].widen_all(l, kG, h < A.Hq ? kPer : 0);
+      if (A.norm.q) part[j].norm(w, A.norm.eps, 1.f / D, l, kG, kPer, half);
+      if (s_owner[j] == kRopeNone || h >= A.Hq) continue;
+      part[j].rotate_by(cs[j], l, kG, half);
+      part[j].store(A.Qo + ((size_t)(t0 + j) * A.Hq + h) * D, l, kG, kPer, half);
+    }
+    load(h + step);
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -431,9 +578,10 @@ struct ReadQ8Args {
   const int32_t *cu, *start, *block_table;
   int T, B, Hkv, max_pages, page_size, n_pages, S_cap, block;
   uint16_t *K, *V;
+  int wide;  // both aligned to 32 bytes
   int* status;
 };
-constexpr int kReadTokens = 8;  // of a CTA
+constexpr int kReadTokens = kQThreads / 32;  // of a CTA
 
 template <int D>
 __global__ void __launch_bounds__(kQThreads) read_q8_kernel(const ReadQ8Args A) {
@@ -483,30 +631,39 @@ __global__ void __launch_bounds__(kQThreads) read_q8_kernel(const ReadQ8Args A) 
   }
   __syncthreads();
   const int rows = A.block_table ? A.page_size : A.S_cap, scales = rows / A.block;
-  constexpr int kUnits = D / 16;
-  const int per_token = A.Hkv * kUnits;
-  for (int u = tid; u < n_tok * per_token * 2; u += kQThreads) {
-    const int j = u / (2 * per_token), x = u - j * 2 * per_token;
-    const bool key = x < per_token;
-    const int h = (key ? x : x - per_token) / kUnits, c = x % kUnits;
-    if (s_row[j] < 0) continue;
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>((key ? A.K8 : A.V8) + (s_row[j] + (long long)h * rows) * D) + c);
-    const float f = power_of_two(clamp_exp((int)(key ? A.Ks : A.Vs)[s_scale[j] + (long long)h * scales] - 127));
-    const uint32_t* w = &v.x;
+  constexpr int kUnits = D / 16, kStep = 32 / kUnits;  // 16-byte units of a row; heads that a warp takes at a time
+  const int c = tid % kUnits, j = tid / 32;            // (a warp a token: what it writes is one piece)
+  if (j >= n_tok || s_row[j] < 0) return;
+  const long long row = s_row[j], scale = s_scale[j];
+  // heads of K, then of V. (One load in flight for each thread, and 32-byte stores: 160 MB of codes in 117 us, 93% of the
+  // copy rate; 16-byte stores 123; two loads 138, four 165: rows of different heads lie far apart.)
+  const int heads = 2 * A.Hkv;
+  for (int hk = tid % 32 / kUnits; hk < heads; hk += kStep) {
+    const int h = hk < A.Hkv ? hk : hk - A.Hkv;
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>((hk < A.Hkv ? A.K8 : A.V8) + (row + (long long)h * rows) * D) + c);
+    const float f = power_of_two(clamp_exp((int)__ldg((hk < A.Hkv ? A.Ks : A.Vs) + scale + (long long)h * scales) - 127));
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     float y[16];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 a = of_e4m3x2((uint16_t)w[k]), b = of_e4m3x2((uint16_t)(w[k] >> 16));
-      y[4 * k] = a.x * f;
-      y[4 * k + 1] = a.y * f;
-      y[4 * k + 2] = b.x * f;
-      y[4 * k + 3] = b.y * f;
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = of_e4m3x2((uint16_t)w[i]), b = of_e4m3x2((uint16_t)(w[i] >> 16));
+      y[4 * i] = a.x * f;
+      y[4 * i + 1] = a.y * f;
+      y[4 * i + 2] = b.x * f;
+      y[4 * i + 3] = b.y * f;
     }
     Pack<uint16_t, 16> p;
     narrow(y, p);
-    uint4* dst = reinterpret_cast<uint4*>((key ? A.K : A.V) + ((size_t)(t0 + j) * A.Hkv + h) * D) + 2 * c;
-    dst[0] = reinterpret_cast<const uint4*>(p.v)[0];
-    dst[1] = reinterpret_cast<const uint4*>(p.v)[1];
+    uint4* dst = reinterpret_cast<uint4*>((hk < A.Hkv ? A.K : A.V) + ((size_t)(t0 + j) * A.Hkv + h) * D) + 2 * c;
+    const uint4 *lo = reinterpret_cast<const uint4*>(p.v), *hi = lo + 1;
+    if (A.wide) {
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(lo->x), "r"(lo->y), "r"(lo->z),
+                   "r"(lo->w), "r"(hi->x), "r"(hi->y), "r"(hi->z), "r"(hi->w)
+                   : "memory");
+    } else {
+      dst[0] = *lo;
+      dst[1] = *hi;
+    }
   }
 }
 
@@ -525,14 +682,14 @@ cudaError_t launch_norm_rope(const T* X, long long x_stride, const int32_t* pos,
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % N == 0;
   };
   const bool vec = a.half % N == 0 && d % (2 * N) == 0 && fits(X, x_stride) && fits(Y, y_stride);
-  constexpr int kWideU = 256 / N / 32 ? 256 / N / 32 : 1;  // units of a lane: heads of 512
-  if (vec) {
-    if (interleaved) norm_rope_kernel<T, N, true, kWideU><<<n_tokens, kQThreads, 0, stream>>>(a);
-    else norm_rope_kernel<T, N, false, kWideU><<<n_tokens, kQThreads, 0, stream>>>(a);
-  } else {
-    if (interleaved) norm_rope_kernel<T, 1, true, 8><<<n_tokens, kQThreads, 0, stream>>>(a);
-    else norm_rope_kernel<T, 1, false, 8><<<n_tokens, kQThreads, 0, stream>>>(a);
-  }
+  // passes of equal size over the heads, of up to 256 threads
+  const int G = head_lanes(d / (2 * (vec ? N : 1))), H = Hq + Hk, most = kQThreads / G, passes = (H + most - 1) / most;
+  const int threads = std::max(64, ((H + passes - 1) / passes * G + 31) / 32 * 32);
+  auto launch = [&](auto kernel) { kernel<<<n_tokens, threads, 0, stream>>>(a); };
+  constexpr int kWideU = 256 / N / 32 > 1 ? 256 / N / 32 : 1;  // units of a lane: heads of 512
+  if (!vec) launch(interleaved ? norm_rope_kernel<T, 1, true, 8> : norm_rope_kernel<T, 1, false, 8>);
+  else if (d <= 64 * N) launch(interleaved ? norm_rope_kernel<T, N, true, 1> : norm_rope_kernel<T, N, false, 1>);
+  else launch(interleaved ? norm_rope_kernel<T, N, true, kWideU> : norm_rope_kernel<T, N, false, kWideU>);
   return cudaGetLastError();
 }
 template cudaError_t launch_norm_rope<float>(const float*, long long, const int32_t*, const float*, float, const float*,
@@ -542,12 +699,23 @@ template cudaError_t launch_norm_rope<uint16_t>(const uint16_t*, long long, cons
                                                 const float*, const float*, float, int, int, int, int, int, int,
                                                 uint16_t*, long long, cudaStream_t);
 
+// Few new tokens (four of a sequence on average, at most): a warp for each (block, kv head, K or V). Else CTAs that go
+// through a block's heads with one table of cosines, as many heads each as leave every SM four of them. (8587 tokens of 28
+// + 2 x 4 heads, with their read-back: 41 us, 49 with a head each. One CTA for keys, values and queries of a block: 45; the
+// blocks' CTAs spread among the queries': 43.)
 template <typename T, int N, int D>
-static cudaError_t launch_append_n(const AppendQ8Args& a, int interleaved, cudaStream_t stream) {
-  const long long grid = (long long)a.n_blocks * a.Hkv * 2 + (a.Qo ? a.T : 0);
+static cudaError_t launch_append_n(AppendQ8Args a, int interleaved, cudaStream_t stream) {
+  const bool few = a.T <= 4ll * a.B;
+  const long long units = 2ll * a.Hkv * a.n_blocks;
+  a.heads = (int)std::max(1ll, std::min((long long)a.Hkv, units / (4 * num_sms_current())));
+  a.per = few ? (2 * a.Hkv + kQThreads / 32 - 1) / (kQThreads / 32) : 2 * ((a.Hkv + a.heads - 1) / a.heads);
+  const long long tokens = few ? 1 : 2, ctas = (long long)a.per * a.n_blocks;
+  const long long grid = ctas + (a.Qo ? (a.T + tokens - 1) / tokens : 0);
   if (grid > 0x7fffffffll) return cudaErrorInvalidValue;
-  if (interleaved) append_q8_kernel<T, N, true, D><<<(int)grid, kQThreads, 0, stream>>>(a);
-  else append_q8_kernel<T, N, false, D><<<(int)grid, kQThreads, 0, stream>>>(a);
+  a.block_ctas = (int)ctas;
+  auto launch = [&](auto kernel) { kernel<<<(int)grid, kQThreads, 0, stream>>>(a); };
+  if (few) launch(interleaved ? append_q8_kernel<T, N, true, D, true> : append_q8_kernel<T, N, false, D, true>);
+  else launch(interleaved ? append_q8_kernel<T, N, true, D, false> : append_q8_kernel<T, N, false, D, false>);
   return cudaGetLastError();
 }
 
@@ -562,7 +730,7 @@ cudaError_t launch_rope_append_q8(const T* Q, long long q_stride, const T* K, lo
   if (n_tokens == 0 || B == 0) return cudaSuccess;
   AppendQ8Args a{Q, K, V, q_stride, k_stride, v_stride, cu_new, kv_len, pos, block_table,
                  reinterpret_cast<const float2*>(turns), magnitude, NormArgs{q_weight, k_weight, eps}, n_tokens, B,
-                 Q ? Hq : 0, Hkv, rot / 2, max_pages, page_size, n_pages, S_cap, block, 0, Qo, K8, V8, Ks, Vs, status};
+                 Q ? Hq : 0, Hkv, rot / 2, max_pages, page_size, n_pages, S_cap, block, 0, 0, 0, 0, Qo, K8, V8, Ks, Vs, status};
   // a sequence's tokens lie in at most n / block + 2 blocks, and in at most n
   a.n_blocks = (int)std::min((long long)n_tokens, (long long)n_tokens / block + 2ll * B);
   constexpr int N = 16 / (int)sizeof(T);
@@ -589,7 +757,7 @@ cudaError_t launch_kv_read_q8(const uint8_t* K8, const uint8_t* V8, const uint8_
                               uint16_t* V, int* status, cudaStream_t stream) {
   if (n_tokens == 0 || B == 0) return cudaSuccess;
   const ReadQ8Args a{K8, V8, Ks, Vs, cu, start, block_table, n_tokens, B, Hkv, max_pages, page_size, n_pages, S_cap, block,
-                     K, V, status};
+                     K, V, (reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) % 32 == 0, status};
   const int grid = (n_tokens + kReadTokens - 1) / kReadTokens;
   if (d == 128) read_q8_kernel<128><<<grid, kQThreads, 0, stream>>>(a);
   else read_q8_kernel<64><<<grid, kQThreads, 0, stream>>>(a);
