@@ -587,20 +587,19 @@ struct ChunkSmem {
   static constexpr int kChunks = Q8 ? (D == 128 ? 2 : 4) : (D == 128 ? 5 : 10);
   static constexpr int kRawTile = 128 * D;
   static constexpr int kKs = D == 128 ? 3 : 6, kRaws = D == 128 ? 3 : 6;
-  static constexpr int kScaleStages = 2;                 // of each stream
   static constexpr int kQ = 0;                           // two row tiles
   static constexpr int kRing = 2 * kTile;
   static constexpr int kKRing = kRing + kChunks * kTile;
   static constexpr int kRaw = kKRing + (Q8 ? kKs * kRawTile : 0);
   static constexpr int kBar = kRaw + (Q8 ? kRaws * kRawTile : 0);
   // full[chunks], empty[chunks], ifull[2], iempty[2], sfull[2], got[2][2], pvdone[2], ofree[2], qfull,
-  // qempty, drain, gap; 8 bits: kfull[ks], kempty[ks], rfull[raws], rempty[raws], cfull[2][stages], cempty[2][stages]
-  static constexpr int kNumBars = 2 * kChunks + 14 + 4 + (Q8 ? 2 * kKs + 2 * kRaws + 4 * kScaleStages : 0);
+  // qempty, drain, gap; 8 bits: kfull[ks], kempty[ks], rfull[raws], rempty[raws], cempty[2]
+  static constexpr int kNumBars = 2 * kChunks + 14 + 4 + (Q8 ? 2 * kKs + 2 * kRaws + 2 : 0);
   static constexpr int kInfo = kBar + (8 * kNumBars + 15) / 16 * 16;
   static constexpr int kMisc = kInfo + 2 * 80;           // [0] misaligned, [1] this CTA merges, [2] tensor memory
   static constexpr int kStat = kMisc + 16;               // (m, l) of streams to be combined: of each, or of one at a time
-  static constexpr int kScales = kStat + (Q8 ? 1 : kCStreams) * kCRows * 8;  // [stream][stage]: struct TileScales
-  static constexpr int kVScales = kScales + (Q8 ? kCStreams * kScaleStages * 48 : 0);  // [raw tile]: 8 f16 factors
+  static constexpr int kScales = kStat + (Q8 ? 1 : kCStreams) * kCRows * 8;  // [stream]: struct TileScales
+  static constexpr int kVScales = kScales + (Q8 ? kCStreams * 48 : 0);  // [raw tile]: 8 f16 factors
   static constexpr int kBytes = kVScales + (Q8 ? kRaws * 16 : 0);
   // tensor memory: scores, of each stream (D = 64) or of the step at hand (128: no room for two), P and O of each
   static constexpr int kScores = D == 128 ? 1 : 2;
@@ -939,8 +938,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
   const uint32_t bKEmpty = bKFull + 8 * SM::kKs;
   const uint32_t bRFull = bKEmpty + 8 * SM::kKs;
   const uint32_t bREmpty = bRFull + 8 * SM::kRaws;
-  const uint32_t bCFull = bREmpty + 8 * SM::kRaws;
-  const uint32_t bCEmpty = bCFull + 16 * SM::kScaleStages;
+  const uint32_t bCEmpty = bREmpty + 8 * SM::kRaws;  // [stream]
   ChunkItem* info = reinterpret_cast<ChunkItem*>(smem + SM::kInfo);
   volatile int* misc = reinterpret_cast<int*>(smem + SM::kMisc);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -960,7 +958,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
     for (int q = 0; q < 2; ++q) {
       mbar_init(bIFull + 8 * q, 1);
       mbar_init(bIEmpty + 8 * q, 1 + kCSoftmaxWarps + (Q8 ? 1 + kConverters : 0));
-      mbar_init(bSFull + 8 * q, 1);
+      mbar_init(bSFull + 8 * q, Q8 ? 2 : 1);  // (8 bits: the tile's scales count as well)
       mbar_init(bGot + 16 * q, 4);
       mbar_init(bGot + 16 * q + 8, 4);
       mbar_init(bPVDone + 8 * q, 1);
@@ -979,10 +977,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         mbar_init(bRFull + 8 * s, 2);  // the tile, and its factors
         mbar_init(bREmpty + 8 * s, kConverters);
       }
-      for (int s = 0; s < 2 * SM::kScaleStages; ++s) {
-        mbar_init(bCFull + 8 * s, 1);
-        mbar_init(bCEmpty + 8 * s, 4);
-      }
+      for (int s = 0; s < 2; ++s) mbar_init(bCEmpty + 8 * s, 4);
     }
     misc[0] = (sQ & 1023) != 0;  // (the swizzled tiles need the alignment that the declaration asks for)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -1008,8 +1003,10 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int ct = tid - kConvertWarp * 32;
     constexpr int kUnits = D / 16, kRowStep = 128 / kUnits;  // 16-byte units of a row; rows between a thread's units
-    const int cj = ct % kUnits, crow = ct / kUnits;
-    const int order = D == 128 && cj >= 4;  // (neighbouring threads then write to 128 different bytes' banks at a time)
+    // (a row's second box lies on the first's banks: its threads take the row beside it, whose swizzle differs)
+    const int cj = ct % kUnits, crow = ct / kUnits ^ (D == 128 ? cj >> 2 : 0);
+    const int to0 = (D == 128 ? cj / 4 * 16384 : 0) + crow * 128 + ((2 * cj ^ crow) & 7) * 16;
+    const int to1 = to0 ^ 16;
     uint32_t item_ctr = 0, raw_ctr = 0;
     bool ok = true;
     for (int last = 0; !last && ok; ++item_ctr) {
@@ -1041,8 +1038,8 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         // rows that no row of the block sees become zeros (what they hold, NaN say, does not meet the zeros of P)
         const bool gap = (SHAPE & kDocs) && it.gaps >= 0 && kt0 + kCKeys > it.pos0 && kt0 < it.pos0 + n_tok;
         const bool edge = kt0 < it.klo || kt0 + kCKeys > it.khi || gap;
-        const uint8_t* raw = smem + SM::kRaw + rc * SM::kRawTile + ct * 16;
-        uint8_t* dst = smem + SM::kRing + ch * SM::kTile + (D == 128 ? cj / 4 * 16384 : 0);
+        const uint8_t* raw = smem + SM::kRaw + rc * SM::kRawTile + crow * D + cj * 16;
+        uint8_t* dst = smem + SM::kRing + ch * SM::kTile;
         const uint4 factors = *reinterpret_cast<const uint4*>(smem + SM::kVScales + rc * 16);  // of each 16 keys
 #pragma unroll 1
         for (int i0 = 0; i0 < kUnits; i0 += 4) {
@@ -1060,7 +1057,6 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int row = crow + (i0 + i) * kRowStep;
             __half2 f;  // of the row's 16 keys
             if constexpr (D == 128) {  // the (i0 + i)-th
               const uint32_t w = i < 2 ? (i0 ? factors.z : factors.x) : (i0 ? factors.w : factors.y);
@@ -1078,10 +1074,9 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
             };
             const uint4 lo = make_uint4(to_f16(v[i].x), to_f16(v[i].x >> 16), to_f16(v[i].y), to_f16(v[i].y >> 16));
             const uint4 hi = make_uint4(to_f16(v[i].z), to_f16(v[i].z >> 16), to_f16(v[i].w), to_f16(v[i].w >> 16));
-            const int c = 2 * cj & 7;
-            uint8_t* r = dst + row * 128;
-            *reinterpret_cast<uint4*>(r + (((c + order) ^ row) & 7) * 16) = order ? hi : lo;
-            *reinterpret_cast<uint4*>(r + (((c + 1 - order) ^ row) & 7) * 16) = order ? lo : hi;
+            uint8_t* r = dst + (i0 + i) * kRowStep * 128;  // (a multiple of eight rows on: the same swizzle)
+            *reinterpret_cast<uint4*>(r + to0) = lo;
+            *reinterpret_cast<uint4*>(r + to1) = hi;
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1515,11 +1510,12 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
             ++raw_ctr;
             for (int s = 0; s < 2 && ok; ++s) {
               if (!it.pair && s != ((t0 + k) & 1)) continue;
-              const uint32_t c = s ? ctr[1]++ : ctr[0]++, stage = s * SM::kScaleStages + c % SM::kScaleStages;
-              ok = warp_wait(bCEmpty + 8 * stage, ((c / SM::kScaleStages) & 1) ^ 1);
+              // once the stream has read those of its tile before (two arrivals could else make one phase of bSFull)
+              const uint32_t c = s ? ctr[1]++ : ctr[0]++;
+              ok = warp_wait(bCEmpty + 8 * s, (c & 1) ^ 1);
               if (!ok) break;
               if (lane / 8 == k) {
-                TileScales* to = reinterpret_cast<TileScales*>(smem + SM::kScales) + stage;
+                TileScales* to = reinterpret_cast<TileScales*>(smem + SM::kScales) + s;
                 to->k[i] = power_of_two_biased(now & 0xffu);
                 if (i == 0) {
                   to->v_log2 = (float)(top - 127);
@@ -1527,7 +1523,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
                 }
               }
               __syncwarp();
-              if (lane == 0) mbar_arrive(bCFull + 8 * stage);
+              if (lane == 0) mbar_arrive(bSFull + 8 * s);
             }
           }
           now = next;
@@ -1595,21 +1591,19 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const int j = pair ? i : 2 * i + st;  // the item's tile
         const int kt0 = item_tile<SINK>(it, tile_of<SHAPE>(j, n_tiles)) * kCKeys;
         const uint32_t n = (st ? done1 : done0) + i;
+        wait(bSFull + 8 * st, n & 1);
         float k_scale[8] = {};
         float v_log2 = 0.f, v_inverse = 0.f;
         if constexpr (Q8) {
-          const uint32_t stage = st * SM::kScaleStages + n % SM::kScaleStages;
-          wait(bCFull + 8 * stage, (n / SM::kScaleStages) & 1);
-          const float4* from = reinterpret_cast<const float4*>(smem + SM::kScales + stage * 48);
+          const float4* from = reinterpret_cast<const float4*>(smem + SM::kScales + st * 48);
           const float4 a = from[0], b = from[1], c = from[2];
           k_scale[0] = a.x, k_scale[1] = a.y, k_scale[2] = a.z, k_scale[3] = a.w;
           k_scale[4] = b.x, k_scale[5] = b.y, k_scale[6] = b.z, k_scale[7] = b.w;
           v_log2 = c.x;
           v_inverse = c.y;
           __syncwarp();
-          if (lane == 0) mbar_arrive(bCEmpty + 8 * stage);
+          if (lane == 0) mbar_arrive(bCEmpty + 8 * st);
         }
-        wait(bSFull + 8 * st, n & 1);
         if (!Q8 && (kt0 < it.klo || kt0 + kCKeys > it.khi)) {
           // V rows that no row of the block sees: cleared once they have landed. (Asked after S: a wait on a parity
           // may be one phase ahead of the barrier, not two, and the MMA warp has by now taken every chunk that lay
