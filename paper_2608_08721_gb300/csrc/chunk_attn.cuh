@@ -86,7 +86,7 @@ constexpr int kCRows = 128;                 // rows of a tile (tensor-memory lan
 constexpr int kCBlockRows = 2 * kCRows;     // rows of a block, at most
 constexpr int kCKeys = 128;                 // keys of a tile
 constexpr int kCMaxCtas = 192;
-constexpr int kCMaxCounts = 1024;           // merge counters (the few-row kernel has several CTAs per SM)
+constexpr int kCMaxCounts = 2048;           // counters: the few-row kernel has nine shares of its work per SM
 constexpr int kCTmemCols = 512;
 constexpr float kCRescaleLog2 = 8.f;
 // A cache in 8 bits has P in f16, whose least step is 2^-24: the reference lies 2^7 below the maximum (P <= 2^15 then,
