@@ -3,10 +3,14 @@
 ``PagedSequences`` owns what a serving loop keeps for a batch of sequences: every layer's page pools, the block
 table, the sequences' lengths and the workspace. A step takes a ragged chunk of new tokens (a prompt, a part of one,
 the one token of a decode step, or all of these side by side) through ``libraspec_rope_append_paged`` and
-``libraspec_chunk_attn_paged``, layer by layer; the verify attention then reads the same pools.
+``libraspec_chunk_attn_paged``, layer by layer; the verify attention then reads the same pools. The cache may be held
+in 8 bits (``libraspec_rope_append_q8_paged``, ``libraspec_chunk_attn_q8_paged``; a verified chain is then one more
+chunk, and ``unpacked`` gives pools for the tree calls), query and key heads may be normed before they are rotated, and
+a window may leave first tokens visible.
 
 ``python -m paper_2608_08721_gb300.prefill`` fills a cache with prompts of uneven length in chunks, decodes a few
-tokens, verifies a drafted block on the result and prints what it compared.
+tokens, verifies a drafted block on the result and prints what it compared; then the same in 8 bits with normed heads
+and a window with sinks.
 """
 from __future__ import annotations
 
@@ -20,7 +24,7 @@ from . import binding
 class Step:
     """One chunk of new tokens: how many each sequence has, and their offsets in the packed rows."""
 
-    def __init__(self, n_new: Sequence[int], device):
+    def __init__(self, n_new: Sequence[int], device, lengths: Sequence[int]):
         self.n_new = [int(n) for n in n_new]
         offsets = [0]
         for n in self.n_new:
@@ -28,12 +32,16 @@ class Step:
         self.T = offsets[-1]
         self.cu_new = torch.tensor(offsets, dtype=torch.int32).to(device)
         self.n_dev = torch.tensor(self.n_new, dtype=torch.int32).to(device)
+        self.pos = torch.cat([torch.arange(a, a + n, dtype=torch.int32) for a, n in zip(lengths, self.n_new)]).to(device)
 
 
 class PagedSequences:
     def __init__(self, n_layers: int, B: int, capacity: int, Hq: int, Hkv: int, head_dim: int,
-                 freqs: binding.RopeFreqs, max_new: int, page_size: int = 64, interleaved: bool = False, device=None):
-        """capacity: keys per sequence; max_new: new tokens of a step, over all sequences, at most."""
+                 freqs: binding.RopeFreqs, max_new: int, page_size: int = 64, interleaved: bool = False, device=None,
+                 block: int = 0, norm: Optional[binding.QkNorm] = None):
+        """capacity: keys per sequence; max_new: new tokens of a step, over all sequences, at most; block: tokens that
+        share a scale in a cache of 8 bits (16, 32 or 64, a divisor of page_size; 0: a cache of bf16); norm: weights of
+        the norm of query and key heads."""
         self.device = torch.device("cuda") if device is None else torch.device(device)
         self.B, self.Hq, self.Hkv, self.d, self.page_size = B, Hq, Hkv, head_dim, page_size
         self.freqs, self.interleaved, self.max_new = freqs, interleaved, max_new
@@ -41,7 +49,19 @@ class PagedSequences:
         self.capacity = per * page_size
         bf = dict(dtype=torch.bfloat16, device=self.device)
         shape = (B * per, Hkv, page_size, head_dim)
-        self.pools = [{"Kp": torch.empty(shape, **bf), "Vp": torch.empty(shape, **bf)} for _ in range(n_layers)]
+        if block and page_size % block:
+            raise ValueError("pages of %d keys do not hold whole blocks of %d" % (page_size, block))
+        self.block, self.norm = block, norm
+        if block:
+            q8, u8 = (dict(dtype=t, device=self.device) for t in (torch.float8_e4m3fn, torch.uint8))
+            exps = (B * per, Hkv, page_size // block)
+            self.pools = [{"K8": torch.empty(shape, **q8), "V8": torch.empty(shape, **q8), "Ks": torch.empty(exps, **u8),
+                           "Vs": torch.empty(exps, **u8)} for _ in range(n_layers)]
+        else:
+            self.pools = [{"Kp": torch.empty(shape, **bf), "Vp": torch.empty(shape, **bf)} for _ in range(n_layers)]
+        # what is rotated already is appended by a rotation by nothing: of one pair, at position 0
+        self.still = binding.RopeFreqs(2, device=self.device)
+        self.no_pos = torch.zeros(max_new, dtype=torch.int32, device=self.device)
         self.block_table = torch.arange(B * per, dtype=torch.int32, device=self.device).view(B, per)
         self.lengths: List[int] = [0] * B
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=self.device)
@@ -54,12 +74,12 @@ class PagedSequences:
         for b, n in enumerate(n_new):
             if self.lengths[b] + n > self.capacity:
                 raise ValueError("sequence %d: %d + %d keys do not fit %d" % (b, self.lengths[b], n, self.capacity))
-        return Step(n_new, self.device)
+        return Step(n_new, self.device, self.lengths)
 
     def layer(self, l: int, qkv: torch.Tensor, step: Step, lse: Optional[torch.Tensor] = None, stream=None, **options):
         """Layer l of the step: qkv [T, Hq + 2 Hkv, d] (f32 or bf16, the projections' output) is rotated and appended,
         and its queries attend to the cache. options: libraspec_chunk_attn's (softcap, slopes, window, first_key,
-        prefix_len, softmax_scale). Returns O [T, Hq, d] bf16.
+        prefix_len, softmax_scale) and sinks (first tokens that the window leaves visible). Returns O [T, Hq, d] bf16.
 
         On a stream other than the current one the layer runs behind what the current stream holds, and what the
         current stream gets next (the advance of the lengths in ``end`` among it) runs behind the layer."""
@@ -78,10 +98,39 @@ class PagedSequences:
         if qkv.shape != (step.T, Hq + 2 * Hkv, self.d):  # (rows of no sequence would come back unwritten)
             raise ValueError("qkv must be [%d, %d, %d], got %s" % (step.T, Hq + 2 * Hkv, self.d, tuple(qkv.shape)))
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        if self.block:
+            cache = (pool["K8"], pool["V8"], pool["Ks"], pool["Vs"], self.block_table, step.cu_new, self.kv_len)
+            q = binding.libraspec_rope_append_q8_paged(q, k, v, *cache, self.freqs, self.ws, norm=self.norm,
+                                                       interleaved=self.interleaved)
+            return binding.libraspec_chunk_attn_q8_paged(q, *cache, self.ws, lse=lse, **options)[0]
+        freqs, pos = self.freqs, None
+        if self.norm is not None:
+            qk = binding.libraspec_qk_norm_rope(qkv[:, :Hq + Hkv], Hq, self.norm, step.pos, freqs,
+                                                interleaved=self.interleaved)
+            q, k, freqs, pos = qk[:, :Hq], qk[:, Hq:], self.still, self.no_pos[:step.T]
         q = binding.libraspec_rope_append_paged(q, k, v, pool["Kp"], pool["Vp"], self.block_table, step.cu_new,
-                                                self.kv_len, self.freqs, self.ws, interleaved=self.interleaved)
-        return binding.libraspec_chunk_attn_paged(q, pool["Kp"], pool["Vp"], self.block_table, step.cu_new, self.kv_len,
-                                                  self.ws, lse=lse, **options)[0]
+                                                self.kv_len, freqs, self.ws, pos=pos, interleaved=self.interleaved)
+        attend = binding.libraspec_chunk_attn_paged
+        if options.get("sinks") and options.get("window"):
+            attend = binding.libraspec_sink_attn_paged
+        else:
+            options = {k: x for k, x in options.items() if k != "sinks"}
+        return attend(q, pool["Kp"], pool["Vp"], self.block_table, step.cu_new, self.kv_len, self.ws, lse=lse, **options)[0]
+
+    def unpacked(self, l: int, extra: int = 0) -> dict:
+        """Layer l of a cache in 8 bits as bf16 pools {"Kp", "Vp"} under the same block table, for the verify calls: each
+        sequence's keys, and ``extra`` more that were appended behind them. (Exact: a scale is a power of two.)"""
+        if not self.block:
+            return self.pools[l]
+        n = [a + extra for a in self.lengths]
+        whole, pool = Step(n, self.device, [0] * self.B), self.pools[l]
+        start = torch.zeros_like(self.kv_len)
+        K, V = binding.libraspec_kv_read_q8_paged(pool["K8"], pool["V8"], pool["Ks"], pool["Vs"], self.block_table,
+                                                  whole.cu_new, start, whole.T, self.ws)
+        out = {k: torch.empty(pool["K8"].shape, dtype=torch.bfloat16, device=self.device) for k in ("Kp", "Vp")}
+        binding.libraspec_rope_append_paged(None, K, V, out["Kp"], out["Vp"], self.block_table, whole.cu_new, start, self.still,
+                                            self.ws, pos=torch.zeros(whole.T, dtype=torch.int32, device=self.device))
+        return out
 
     def end(self, step: Step) -> None:
         """Every layer has had the step: its tokens count as the sequences' own."""
@@ -149,10 +198,65 @@ def run(prompts=(700, 3, 129, 1500), chunk=256, decode=3, K=7, n_layers=2, Hq=32
     return {"chunks": steps, "cache_equal": same, "verify_rel_diff": diff, "decoded": last[0].shape[0]}
 
 
+def run_q8(prompts=(700, 3, 129, 1500), chunk=256, decode=3, K=7, Hq=32, Hkv=8, d=128, block=16, window=512, sinks=4,
+           seed=0) -> dict:
+    """One layer with normed heads, a window and sinks over a cache in 8 bits: prompts in chunks, ``decode`` tokens one at
+    a time, then K + 1 tokens as one chunk, and by the verify attention (no window) over the unpacked cache."""
+    device = torch.device("cuda")
+    g = torch.Generator(device=device).manual_seed(seed)
+    B, total = len(prompts), [p + decode + K + 1 for p in prompts]
+    qkv = [torch.randn((t, Hq + 2 * Hkv, d), generator=g, dtype=torch.bfloat16, device=device) for t in total]
+    freqs = binding.RopeFreqs(d, theta=500000.0, device=device)
+    norm = binding.QkNorm(*(1.0 + 0.2 * torch.randn((2, d), generator=g, device=device)).unbind())
+    max_new = max(B * chunk, sum(total))
+    both = [PagedSequences(1, B, max(total), Hq, Hkv, d, freqs, max_new, block=b, norm=norm, device=device)
+            for b in (block, 0)]
+
+    def feed(n_new, **options):
+        out = []
+        for seqs in both:
+            step = seqs.begin(n_new)
+            rows = torch.cat([x[a:a + n] for x, a, n in zip(qkv, seqs.lengths, n_new)])
+            out.append(seqs.layer(0, rows, step, **options))
+        return step, rows, out
+
+    def rel(a, b):
+        return float((a.float() - b.float()).norm() / b.float().norm())
+
+    def advance(step):
+        for seqs in both:
+            seqs.end(step)
+
+    worst = 0.0
+    while any(a < p for a, p in zip(both[0].lengths, prompts)):
+        step, _, (O8, O16) = feed([min(chunk, p - a) for a, p in zip(both[0].lengths, prompts)], window=window, sinks=sinks)
+        worst = max(worst, rel(O8, O16))
+        advance(step)
+    for _ in range(decode):
+        step, _, (O8, O16) = feed([1] * B, window=window, sinks=sinks)
+        worst = max(worst, rel(O8, O16))
+        advance(step)
+    seqs = both[0]
+    step, rows, (O8, _) = feed([K + 1] * B)
+    Q = binding.libraspec_qk_norm_rope(rows[:, :Hq], Hq, norm, step.pos, freqs).view(B, K + 1, Hq, d)
+    vws = binding.Workspace(B, K, 1, Hq, Hkv, d, seqs.capacity, device=device)
+    L = torch.full((B,), K, dtype=torch.int32, device=device)
+    verify, _ = binding.libraspec_verify_attn_paged_layers([{"Q": Q, **seqs.unpacked(0, K + 1)}], seqs.block_table, seqs.kv_len,
+                                                           L, vws)
+    for s in both:
+        s.check()
+    if binding.libraspec_get_status(vws):
+        raise RuntimeError("device reported a violation (verify)")
+    return {"rel_to_16_bits": worst, "verify_rel_diff": rel(O8.view(B, K + 1, Hq, d), verify[0])}
+
+
 def main() -> None:
     r = run()
     print("prompts in %d chunks; the cache of one whole step: %s; verify attention against the chunk's: %.1e apart" % (
         r["chunks"], "equal" if r["cache_equal"] else "DIFFERENT", r["verify_rel_diff"]))
+    r = run_q8()
+    print("in 8 bits, with normed heads, a window and sinks: %.1e from the 16-bit cache's; verify attention of the unpacked "
+          "cache against the chunk's: %.1e apart" % (r["rel_to_16_bits"], r["verify_rel_diff"]))
 
 
 if __name__ == "__main__":
