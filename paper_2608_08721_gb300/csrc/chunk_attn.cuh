@@ -584,9 +584,9 @@ template <int D, bool Q8>
 struct ChunkSmem {
   static constexpr int kBoxes = D / 64;
   static constexpr int kTile = kBoxes * 16384;           // 128 rows of Q, K or V: per 64 columns 128 rows of 128 bytes
-  static constexpr int kChunks = Q8 ? (D == 128 ? 2 : 4) : (D == 128 ? 5 : 10);
+  static constexpr int kChunks = Q8 ? (D == 128 ? 3 : 4) : (D == 128 ? 5 : 10);
   static constexpr int kRawTile = 128 * D;
-  static constexpr int kKs = D == 128 ? 3 : 6, kRaws = D == 128 ? 3 : 6;
+  static constexpr int kKs = D == 128 ? 2 : 6, kRaws = D == 128 ? 2 : 6;
   static constexpr int kQ = 0;                           // two row tiles
   static constexpr int kRing = 2 * kTile;
   static constexpr int kKRing = kRing + kChunks * kTile;

@@ -38,6 +38,25 @@ struct NormArgs {
   float eps;
 };
 
+// rope_turn with what its sums round off of the angle (up to 2^-24 of a turn) put in by the angle's derivative: the turn is
+// then as exact as sincospi. (Codes are rounded from what it turns: the further off that is, the more of them are those of
+// the neighbouring step.)
+__device__ __forceinline__ float sum_exactly(float a, float b, float& rest) {  // a + b = sum + rest
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  rest = __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t));
+  return s;
+}
+__device__ __forceinline__ float2 fine_turn(int pos, float2 f, float magnitude) {
+  const float hi = (float)(pos & ~255), lo = (float)(pos & 255);
+  const float p = __fmul_rn(hi, f.x), q = __fmul_rn(lo, f.x);
+  const float e = __fmaf_rn(hi, f.x, -p) + __fmaf_rn(lo, f.x, -q) + __fmaf_rn(hi, f.y, lo * f.y);
+  float r0, r1, sn, cs;
+  const float s = sum_exactly(sum_exactly(p - rintf(p), q - rintf(q), r0), e, r1);
+  sincospif(2.f * (s - rintf(s)), &sn, &cs);
+  const float d = 6.283185307179586f * (r0 + r1);
+  return make_float2(fmaf(-d, sn, cs) * magnitude, fmaf(d, cs, sn) * magnitude);
+}
+
 // A lane's U units of a head that G lanes share: unit l + k G is the k-th of lane l. N elements and their partners a unit.
 template <typename Tin, int N, bool INTER, int U>
 struct HeadPart {
@@ -75,7 +94,7 @@ struct HeadPart {
 #pragma unroll
       for (int i = 0; i < N; ++i) ss = fmaf(x[k][i], x[k][i], fmaf(y[k][i], y[k][i], ss));
     for (int off = G >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-    const float r = rsqrtf(fmaf(ss, inv_d, eps));
+    const float r = __frsqrt_rn(fmaf(ss, inv_d, eps));
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int u = l + k * G;
@@ -183,7 +202,7 @@ __device__ __forceinline__ void turn_heads(const Tin* src, Tout* dst, int H, int
 template <typename Unit>
 __device__ __forceinline__ void fill_tables(float2* cs, float* w, int pos, const float2* turns, float magnitude, int half,
                                             const NormArgs& nm, int d) {
-  for (int i = threadIdx.x; i < half; i += blockDim.x) cs[Unit::slot(i, half)] = rope_turn(pos, turns[i], magnitude);
+  for (int i = threadIdx.x; i < half; i += blockDim.x) cs[Unit::slot(i, half)] = fine_turn(pos, turns[i], magnitude);
   if (nm.q)
     for (int i = threadIdx.x; i < 2 * d; i += blockDim.x) w[i] = i < d ? nm.q[i] : nm.k[i - d];
 }
@@ -442,7 +461,7 @@ __global__ void __launch_bounds__(kQThreads, 4) append_q8_kernel(const AppendQ8A
             const int pos = A.pos ? A.pos[t] : o.key0 + r;
             part.rotate(l, kG, half, [&](int u, float2(&c)[N]) {
 #pragma unroll
-              for (int j = 0; j < N; ++j) c[j] = rope_turn(pos, A.turns[u * N + j], A.magnitude);
+              for (int j = 0; j < N; ++j) c[j] = fine_turn(pos, A.turns[u * N + j], A.magnitude);
             });
           }
         }
@@ -484,7 +503,7 @@ __global__ void __launch_bounds__(kQThreads, 4) append_q8_kernel(const AppendQ8A
       if (key) {
         for (int j = tid; j < (o.r1 - o.r0) * half; j += kQThreads) {
           const int r = o.r0 + j / half, k = j % half;
-          cs[r][Unit::slot(k, half)] = rope_turn(A.pos ? A.pos[o.t0 + r - o.r0] : o.key0 + r, A.turns[k], A.magnitude);
+          cs[r][Unit::slot(k, half)] = fine_turn(A.pos ? A.pos[o.t0 + r - o.r0] : o.key0 + r, A.turns[k], A.magnitude);
         }
         if (A.norm.k)
           for (int j = tid; j < D; j += kQThreads) w[j] = A.norm.k[j];
@@ -552,7 +571,7 @@ __global__ void __launch_bounds__(kQThreads, 4) append_q8_kernel(const AppendQ8A
   for (int i = tid; i < kTokens * half; i += kQThreads) {
     const int j = kTokens == 1 ? 0 : i / half, k = i - j * half;
     if (j >= n_tok || s_owner[j] == kRopeNone) continue;
-    cs[j][Unit::slot(k, half)] = rope_turn(A.pos ? A.pos[t0 + j] : (int)(uint32_t)s_owner[j], A.turns[k], A.magnitude);
+    cs[j][Unit::slot(k, half)] = fine_turn(A.pos ? A.pos[t0 + j] : (int)(uint32_t)s_owner[j], A.turns[k], A.magnitude);
   }
   __syncthreads();
   for (int h0 = 0; h0 < A.Hq; h0 += step) {  // (all lanes of a warp go round together)
