@@ -791,19 +791,29 @@ def libraspec_qk_norm_rope(X, n_q: int, norm: QkNorm, pos, freqs: RopeFreqs, int
 def _check_caches_q8(K8, V8, Ks, Vs, block_table, B):
     """Codes and exponents of a cache in 8 bits; returns (Hkv, d, capacity, max_pages, page_size, n_pages, block)."""
     paged = block_table is not None
-    _req(K8, torch.float8_e4m3fn, "K8")
-    shape = K8.shape
-    if len(shape) != 4 or not (paged or shape[0] == B):
-        raise ValueError("K8 must be %s, got %s" % ("[n_pages, Hkv, page_size, d]" if paged else "[%d, Hkv, S_cap, d]" % B,
-                                                    tuple(shape)))
-    _req(V8, torch.float8_e4m3fn, "V8", shape)
-    planes, Hkv, rows, d = shape
-    _req(Ks, torch.uint8, "Ks")
-    n = Ks.shape[2] if Ks.dim() == 3 else 0
-    if n == 0 or Ks.shape[0] != planes or Ks.shape[1] != Hkv or rows % n:
-        raise ValueError("Ks must be [%d, %d, %s / block], got %s" % (planes, Hkv, rows, tuple(Ks.shape)))
-    _req(Vs, torch.uint8, "Vs", Ks.shape)
+    # every condition at once; what fails is named below
+    try:
+        planes, Hkv, rows, d = shape = K8.shape
+        n = Ks.shape[2]
+        fine = (K8.dtype == V8.dtype == torch.float8_e4m3fn and Ks.dtype == Vs.dtype == torch.uint8 and V8.shape == shape
+                and Ks.shape == Vs.shape == (planes, Hkv, n) and n > 0 and rows % n == 0 and K8.is_cuda and V8.is_cuda
+                and Ks.is_cuda and Vs.is_cuda and K8.is_contiguous() and V8.is_contiguous() and Ks.is_contiguous()
+                and Vs.is_contiguous())
+    except (AttributeError, IndexError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        _req(K8, torch.float8_e4m3fn, "K8")
+        shape = K8.shape
+        if len(shape) != 4:
+            raise ValueError("K8 must be %s, got %s" % ("[n_pages, Hkv, page_size, d]" if paged else "[B, Hkv, S_cap, d]",
+                                                        tuple(shape)))
+        _req(V8, torch.float8_e4m3fn, "V8", shape)
+        _req(Ks, torch.uint8, "Ks")
+        _req(Vs, torch.uint8, "Vs", Ks.shape)
+        raise ValueError("Ks must be [%d, %d, %s / block], got %s" % (shape[0], shape[1], shape[2], tuple(Ks.shape)))
     if not paged:
+        if planes != B:
+            raise ValueError("K8 must be [%d, Hkv, S_cap, d], got %s" % (B, tuple(shape)))
         return Hkv, d, rows, 0, 0, 0, rows // n
     _req(block_table, torch.int32, "block_table")
     t = block_table.shape
@@ -895,21 +905,20 @@ def _kv_read_q8(K8, V8, Ks, Vs, block_table, cu, start, T, ws, K, V, stream):
     T = int(T)
     if T < 0:
         raise ValueError("T must not be negative")
-    out = []
-    for t, name in ((K, "K"), (V, "V")):
-        out.append(_out((T, Hkv, d), torch.bfloat16, K8.device, stream) if t is None
-                   else _req(t, torch.bfloat16, name, (T, Hkv, d)))
+    shape = (T, Hkv, d)
+    K = _out(shape, torch.bfloat16, K8.device, stream) if K is None else _req(K, torch.bfloat16, "K", shape)
+    V = _out(shape, torch.bfloat16, K8.device, stream) if V is None else _req(V, torch.bfloat16, "V", shape)
     lib = load()
     tail = (cu.data_ptr(), start.data_ptr(), T, B, Hkv, d)
     head = (K8.data_ptr(), V8.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
-    end = (block, out[0].data_ptr(), out[1].data_ptr(), ws.ptr, ws.nbytes, _stream(stream))
+    end = (block, K.data_ptr(), V.data_ptr(), ws.ptr, ws.nbytes, _stream(stream))
     if block_table is None:
         rc = lib.libraspec_kv_read_q8(*head, *tail, S_cap, *end)
     else:
         rc = lib.libraspec_kv_read_q8_paged(*head, block_table.data_ptr(), max_pages, page_size, n_pages, *tail, *end)
     if rc != OK:
         _check(rc, "libraspec_kv_read_q8" + ("" if block_table is None else "_paged"))
-    return out[0], out[1]
+    return K, V
 
 
 class ChunkWorkspace:

@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libraspec.so")
 SOURCES = ["conf_select.cu", "accept.cu", "attn.cu", "abi.cu", "noalloc.cu", "kv.cu", "lmhead.cu", "rope.cu",
-           "rope_q8.cu", "chunk_attn.cu", "chunk_attn_q8.cu", "chunk_attn_sink.cu",
+           "rope_q8.cu", "chunk_attn.cu", "chunk_attn_64.cu", "chunk_attn_q8.cu", "chunk_attn_q8_64.cu", "chunk_attn_sink.cu",
            "few_attn_q8.cu"]
 HEADERS = ["attn_rules.h", "chunk_attn.cuh", "chunk_call.h", "common.cuh", "rope.cuh", "rowpass.cuh", "tc.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

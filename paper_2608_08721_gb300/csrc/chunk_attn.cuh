@@ -61,6 +61,20 @@
 // unwritten cache row holds (NaN, say) does not meet the zeros of P; so are the
 // rows within it of tokens that no row sees (padding), which first keys allow.
 //
+// A cache in 8 bits (kQ8): codes c of e4m3, values c 2^e with an exponent for every 16 to 64 keys of a kv head. Keys meet
+// the queries as e4m3, as they lie in memory, the queries in two e4m3 parts (split_q_kernel), one behind the other along
+// the contraction, which costs the tensor pipe what one product of 16-bit operands does. The rows' and keys' scales enter
+// the softmax, which multiplies scores by them anyway. Values are converted to f16 by a fourth warpgroup, brought to the
+// largest exponent of their tile (exact for codes down to 2^15 below it; what lies further below is off by 2^-24 of that
+// scale at most), and P is f16, times that scale: O = sum 2^(s - m + e) V8, l = sum 2^(s - m). One more warp brings the
+// exponents, two tiles' look-ups ahead; a tile's count with its scores on one barrier. What bounds it: the softmax warps'
+// steps, beside which the converters issue (a prompt of 8192 tokens, 478 us: 37 of them go when the conversion is left
+// out, 24 are the queries' parts; the same in bf16 takes 395). Measured and not kept: K converted as well (647), the
+// queries' parts in the kernel (615), their scales on a barrier of their own (518).
+//
+// Sinks (kSink): keys below `sinks` stay visible to every row behind them. A block's tiles are then the first ones of the
+// sequence that hold sinks, and those of its window; what lies between is not read.
+//
 // A block cut over CTAs c0..c1 leaves one fp32 partial (O, m, l) per CTA; the
 // CTA that delivers the last of them merges all, in CTA order (results do not
 // depend on timing). No CTA waits for another.
@@ -687,7 +701,8 @@ __device__ __forceinline__ float power_of_two_biased(uint32_t e) { return __uint
 // (8 bits) The queries as two e4m3 parts: a row (a token's head) times the power of two that brings its largest into
 // [2^7, 2^8) becomes the nearest e4m3 and the rest, together all eight bits of what lies within 2^-9 of the largest, else
 // off by 2^-17 of it at most. Per 64 elements the first parts, then the second, in the bytes that the elements took. A
-// launch of its own: in the attention, where each CTA did it for its items, a prompt of 8192 tokens took 92 us longer.
+// launch of its own (24 us for a prompt of 8192 tokens of 32 heads, as long beside the plan as behind it): in the
+// attention, where each CTA did it for its items, the prompt took 92 us longer.
 constexpr int kSplitThreads = 256;
 template <int D>
 static __global__ void __launch_bounds__(kSplitThreads) split_q_kernel(const uint16_t* __restrict__ Q, long long rows,
@@ -2046,11 +2061,12 @@ static cudaError_t launch_shape(int shape, const ChunkArgs& a, int grid, cudaStr
   return cudaErrorInvalidValue;
 }
 
-template <int KIND>
+// (D: c.D. A translation unit for each: they take a minute and more)
+template <int KIND, int D>
 static cudaError_t launch_chunk(const ChunkCall& c) {
   constexpr bool Q8 = KIND == kQ8;
   if (c.T == 0 || c.B == 0) return cudaSuccess;
-  const ChunkWs lay = chunk_ws(c.T, c.B, c.Hq, c.Hkv, c.D);
+  const ChunkWs lay = chunk_ws(c.T, c.B, c.Hq, c.Hkv, D);
   const int g = c.Hq / c.Hkv;
   char* ws = c.ws;
   ChunkArgs a;
@@ -2088,26 +2104,16 @@ static cudaError_t launch_chunk(const ChunkCall& c) {
   a.block_log2 = 0;
   while ((1 << a.block_log2) < c.block) ++a.block_log2;
   auto cache_map = [&](CUtensorMap* m, const void* base, bool keys) {
-    return Q8 ? make_map8(m, base, c.D, rows, planes, a.piece, keys)
-              : make_map(m, base, c.D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+    return Q8 ? make_map8(m, base, D, rows, planes, a.piece, keys)
+              : make_map(m, base, D, rows, planes, a.piece, 1, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
   };
   if (!cache_map(&a.K, c.K, true) || !cache_map(&a.V, c.V, false) ||
-      !make_map(&a.Q, Q8 ? reinterpret_cast<const uint16_t*>(ws + lay.q_parts) : c.Q, c.D, c.Hq, c.T, g, kCRows / g,
+      !make_map(&a.Q, Q8 ? reinterpret_cast<const uint16_t*>(ws + lay.q_parts) : c.Q, D, c.Hq, c.T, g, kCRows / g,
                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B))
     return cudaErrorInvalidValue;
-  if constexpr (Q8) {
-    uint8_t *parts = reinterpret_cast<uint8_t*>(ws + lay.q_parts), *exps = reinterpret_cast<uint8_t*>(ws + lay.q_exp);
-    a.q_exp = exps;
-    const long long heads = (long long)c.T * c.Hq, grid_q = (heads * (c.D / 16) + kSplitThreads - 1) / kSplitThreads;
-    if (grid_q > 0x7fffffffll) return cudaErrorInvalidValue;
-    if (c.D == 128) split_q_kernel<128><<<(int)grid_q, kSplitThreads, 0, c.stream>>>(c.Q, heads, parts, exps);
-    else split_q_kernel<64><<<(int)grid_q, kSplitThreads, 0, c.stream>>>(c.Q, heads, parts, exps);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-  }
   const int grid = std::min(num_sms_current(), kCMaxCtas);
   a.plan = PlanArgs{c.cu_new, c.kv_len, a.mask, c.T, c.B, block_tokens(g), std::min(c.S_cap, kCMaxKeys), c.Hkv, grid,
-                    kCSharedBytes / (2 * kCKeys * c.D * (Q8 ? 1 : 2)), a.status};
+                    kCSharedBytes / (2 * kCKeys * D * (Q8 ? 1 : 2)), a.status};
   // (a lane would go through a block's first keys one by one)
   if (max_blocks(c.T, c.B, g) <= kWarpBlocks && c.B <= kWarpSeqs && !c.first_key) {
     a.blocks = nullptr;
@@ -2118,9 +2124,18 @@ static cudaError_t launch_chunk(const ChunkCall& c) {
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
+  if constexpr (Q8) {
+    uint8_t *parts = reinterpret_cast<uint8_t*>(ws + lay.q_parts), *exps = reinterpret_cast<uint8_t*>(ws + lay.q_exp);
+    a.q_exp = exps;
+    const long long heads = (long long)c.T * c.Hq, grid_q = (heads * (D / 16) + kSplitThreads - 1) / kSplitThreads;
+    if (grid_q > 0x7fffffffll) return cudaErrorInvalidValue;
+    split_q_kernel<D><<<(int)grid_q, kSplitThreads, 0, c.stream>>>(c.Q, heads, parts, exps);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
   const int shape = (c.softcap > kNarrowCap ? kCap | kWideCap : c.softcap > 0.f ? kCap : 0) | (c.slopes ? kBias : 0) |
                     (c.first_key ? kDocs : 0);
-  return c.D == 128 ? launch_shape<128, KIND>(shape, a, grid, c.stream) : launch_shape<64, KIND>(shape, a, grid, c.stream);
+  return launch_shape<D, KIND>(shape, a, grid, c.stream);
 }
 
 }  // namespace libraspec

@@ -3,6 +3,8 @@
 
 namespace libraspec {
 
-cudaError_t launch_sink_attn(const ChunkCall& c) { return launch_chunk<kSink>(c); }
+cudaError_t launch_sink_attn(const ChunkCall& c) {
+  return c.D == 128 ? launch_chunk<kSink, 128>(c) : launch_chunk<kSink, 64>(c);
+}
 
 }  // namespace libraspec

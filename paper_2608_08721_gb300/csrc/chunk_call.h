@@ -31,6 +31,9 @@ size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);
 cudaError_t launch_chunk_attn(const ChunkCall& c);
 cudaError_t launch_sink_attn(const ChunkCall& c);     // without first keys
 cudaError_t launch_chunk_attn_q8(const ChunkCall& c);
-cudaError_t launch_few_attn_q8(const ChunkCall& c);   // of calls that few_fits
+// what these pass on: heads of 64, and calls that few_fits
+cudaError_t launch_chunk_attn_64(const ChunkCall& c);
+cudaError_t launch_chunk_attn_q8_64(const ChunkCall& c);
+cudaError_t launch_few_attn_q8(const ChunkCall& c);
 
 }  // namespace libraspec

@@ -150,3 +150,33 @@ def test_limits_match_the_header():
     call = open(os.path.join(root, "paper_2608_08721_gb300", "csrc", "chunk_call.h")).read()
     shift = re.search(r"LIBRASPEC_MAX_SINKS \(1 << (\d+)\)", header).group(1)
     assert re.search(r"kChunkMaxSinks = 1 << (\d+);", call).group(1) == shift
+
+
+@pytest.mark.gpu
+def test_binding_names_what_is_wrong_with_a_cache():
+    dev = torch.device("cuda", 0)
+    codes, exps = torch.zeros((2, 1, 64, 64), dtype=torch.float8_e4m3fn, device=dev), torch.zeros((2, 1, 4), dtype=torch.uint8, device=dev)
+    table = torch.zeros((2, 1), dtype=torch.int32, device=dev)
+    check = lr._check_caches_q8
+    assert check(codes, codes, exps, exps, None, 2) == (1, 64, 64, 0, 0, 0, 16)
+    assert check(codes, codes, exps, exps, table, 2) == (1, 64, 0, 1, 64, 2, 16)
+    for args, error, match in (((codes.view(torch.uint8), codes, exps, exps, None, 2), TypeError, "^K8 must be"),
+                               ((codes[0], codes, exps, exps, None, 2), ValueError, "^K8 must be"),
+                               ((codes, codes[:1], exps, exps, None, 2), ValueError, "^V8 must have"),
+                               ((codes, codes.transpose(2, 3), exps, exps, None, 2), ValueError, "^V8 must be contiguous"),
+                               ((codes, codes, exps.float(), exps, None, 2), TypeError, "^Ks must be"),
+                               ((codes, codes, exps, exps.cpu(), None, 2), ValueError, "^Vs must be on"),
+                               ((codes, codes, exps[:, :, :0], exps[:, :, :0], None, 2), ValueError, "^Ks must be"),
+                               ((codes, codes, exps[:, :, :3].contiguous(), exps[:, :, :3].contiguous(), None, 2), ValueError, "^Ks must be"),
+                               ((codes, codes, exps, exps, None, 3), ValueError, "^K8 must be"),
+                               ((codes, codes, exps, exps, table[0], 2), ValueError, "^block_table must be"),
+                               ((codes, codes, exps, exps, table.long(), 2), TypeError, "^block_table must be"),
+                               ((None, codes, exps, exps, None, 2), TypeError, "^K8 must be")):
+        with pytest.raises(error, match=match):
+            check(*args)
+    norm = lr.QkNorm(torch.ones(64, device=dev), torch.ones(64, device=dev))
+    x, pos = torch.zeros((3, 2, 128), device=dev), torch.zeros(3, dtype=torch.int32, device=dev)
+    with pytest.raises(ValueError, match="^norm: weights of 64"):
+        lr.libraspec_qk_norm_rope(x, 1, norm, pos, lr.RopeFreqs(128))
+    with pytest.raises(ValueError, match="^n_q must lie"):
+        lr.libraspec_qk_norm_rope(x[..., :64].contiguous(), 3, norm, pos, lr.RopeFreqs(64))
