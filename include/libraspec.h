@@ -708,12 +708,18 @@ int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint1
  * K8, V8, exponents Ks, Vs, `block`; the shapes, their checks and the ends of
  * the exponents as there), with every option of libraspec_chunk_attn, and sinks:
  *   s_k = softmax_scale 2^ek Q . K8[k],   O = sum_k softmax(s)_k 2^ev V8[k].
- * Queries meet the codes as two e4m3 parts (all eight bits of what lies within
- * 2^-9 of a row's largest element, else off by 2^-17 of that); scores, sums and O
- * accumulate in binary32; probabilities times their value's scale enter
- * the second product as f16 (11 bits) down to 2^-24 of 2^-7 of the largest. Codes
- * and exponents of blocks that no row sees need not be initialised. Reads half
- * the bytes of a bf16 cache. workspace as for libraspec_chunk_attn.
+ * Scores, sums and O accumulate in binary32; probabilities (of the largest
+ * value scale of up to 128 keys) enter the second product as f16, 11 bits down to
+ * 2^-24 of 2^-7 of the largest. Codes and exponents of blocks that no row sees
+ * need not be initialised. Reads half the bytes of a bf16 cache. workspace as for
+ * libraspec_chunk_attn (it holds the queries' parts, T Hq (2 head_dim + 1) bytes).
+ *
+ * Two kernels. One reads a key for 8 or 16 rows, with queries as f16, exact down
+ * to 2^-31 of a row's largest element; it takes decode steps (T <= B), and where
+ * sequences have on average 16 rows per kv head at most, those whose rows fit one
+ * of its blocks. The other takes the rest, in whose scores queries are two e4m3
+ * parts: all eight bits of what lies within 2^-9 of a row's largest element, else
+ * off by 2^-17 of that. One to five launches.
  */
 int libraspec_chunk_attn_q8(const uint16_t* Q, const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks,
                             const uint8_t* Vs, const int32_t* cu_new, const int32_t* kv_len, int T, int B, int Hq,

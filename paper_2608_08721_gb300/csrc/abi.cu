@@ -778,7 +778,7 @@ ChunkCall chunk_call(const uint16_t* Q, const void* K, const void* V, const uint
                      int sinks, uint16_t* O, float* lse, void* workspace, void* stream) {
   return ChunkCall{Q, K, V, Ks, Vs, block, block_table, max_pages, page_size, n_pages, cu_new, kv_len, T, B, Hq, Hkv,
                    head_dim, S_cap, softmax_scale, 0.f, nullptr, 0, sinks, nullptr, nullptr, O, lse,
-                   static_cast<char*>(workspace), static_cast<cudaStream_t>(stream)};
+                   static_cast<char*>(workspace), static_cast<cudaStream_t>(stream), 0};
 }
 
 }  // namespace

@@ -100,7 +100,7 @@ constexpr int kCRows = 128;                 // rows of a tile (tensor-memory lan
 constexpr int kCBlockRows = 2 * kCRows;     // rows of a block, at most
 constexpr int kCKeys = 128;                 // keys of a tile
 constexpr int kCMaxCtas = 192;
-constexpr int kCMaxCounts = 2048;           // counters: the few-row kernel has nine shares of its work per SM
+constexpr int kCMaxCounts = 1024;           // counters, one per CTA: the few-row kernel has up to three on an SM
 constexpr int kCTmemCols = 512;
 constexpr float kCRescaleLog2 = 8.f;
 // A cache in 8 bits has P in f16, whose least step is 2^-24: the reference lies 2^7 below the maximum (P <= 2^15 then,
@@ -147,11 +147,12 @@ inline long long max_blocks(long long T, int B, int g) {
   return a < T ? a : T;
 }
 
-// Rows of a block of the few-row kernel (few_attn_q8.cu): at most 8, or 16. It takes calls whose sequences have 16 rows
-// per kv head on average at most.
+// The few-row kernel (few_attn_q8.cu) has blocks of 8 rows, or of 16. It takes part where the sequences have 16 rows per kv
+// head on average at most: T <= B new tokens (a decode step) are all its own; of more it takes the sequences whose tokens
+// fit a block, the other kernel the rest (a chunk of a prompt beside decoding sequences would be read by 16 rows at a time).
 constexpr int kFewRows = 16;
-inline int few_tokens(int g, int rows) { return rows / g; }
 inline bool few_fits(long long T, int B, int g) { return g <= kFewRows && T * g <= (long long)kFewRows * B; }
+inline int few_rows(long long T, int B, int g) { return g <= 8 && T * g <= 8ll * B ? 8 : 16; }
 inline long long few_blocks(long long T, int B, int tokens) { return std::min(T, T / tokens + B); }
 
 static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
@@ -227,6 +228,7 @@ struct PlanArgs {
   int T, B, TB;      // TB: tokens of a block
   int S_cap, Hkv, grid;
   int shared_tiles;  // key tiles (of all kv heads) beyond which L2 does not hold them
+  int least, most;   // sequences with fewer or more new tokens are another kernel's
   int* status;
 };
 
@@ -243,7 +245,7 @@ __device__ __forceinline__ int new_tokens(const PlanArgs& a, int b, bool report,
     if (report) raise_status(a.status, LIBRASPEC_ST_KV_OVERFLOW);
     return 0;
   }
-  return hi - c0;
+  return hi - c0 < a.least || hi - c0 > a.most ? 0 : hi - c0;
 }
 
 // The most blocks that T tokens of B sequences have: offsets that run backwards could ask for more.
@@ -2113,7 +2115,7 @@ static cudaError_t launch_chunk(const ChunkCall& c) {
     return cudaErrorInvalidValue;
   const int grid = std::min(num_sms_current(), kCMaxCtas);
   a.plan = PlanArgs{c.cu_new, c.kv_len, a.mask, c.T, c.B, block_tokens(g), std::min(c.S_cap, kCMaxKeys), c.Hkv, grid,
-                    kCSharedBytes / (2 * kCKeys * D * (Q8 ? 1 : 2)), a.status};
+                    kCSharedBytes / (2 * kCKeys * D * (Q8 ? 1 : 2)), c.least_new, 0x7fffffff, a.status};
   // (a lane would go through a block's first keys one by one)
   if (max_blocks(c.T, c.B, g) <= kWarpBlocks && c.B <= kWarpSeqs && !c.first_key) {
     a.blocks = nullptr;

@@ -4,8 +4,15 @@
 namespace libraspec {
 
 cudaError_t launch_chunk_attn_q8(const ChunkCall& c) {
-  if (few_fits(c.T, c.B, c.Hq / c.Hkv)) return launch_few_attn_q8(c);
-  return c.D == 128 ? launch_chunk<kQ8, 128>(c) : launch_chunk_attn_q8_64(c);
+  const int g = c.Hq / c.Hkv;
+  ChunkCall rest = c;
+  if (few_fits(c.T, c.B, g)) {
+    const cudaError_t e = launch_few_attn_q8(c);
+    if (e != cudaSuccess || c.T <= c.B) return e;
+    rest.least_new = few_rows(c.T, c.B, g) / g + 1;
+    if (rest.least_new > c.T) return e;  // (no sequence has as many)
+  }
+  return c.D == 128 ? launch_chunk<kQ8, 128>(rest) : launch_chunk_attn_q8_64(rest);
 }
 
 }  // namespace libraspec

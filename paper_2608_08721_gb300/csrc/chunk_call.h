@@ -25,6 +25,7 @@ struct ChunkCall {
   float* lse;
   char* ws;
   cudaStream_t stream;
+  int least_new;  // sequences with fewer new tokens are left out
 };
 
 size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);

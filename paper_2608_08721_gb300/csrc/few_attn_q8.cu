@@ -594,9 +594,8 @@ cudaError_t launch_few_attn_q8(const ChunkCall& c) {
   if (c.T == 0 || c.B == 0) return cudaSuccess;
   const ChunkWs lay = chunk_ws(c.T, c.B, c.Hq, c.Hkv, c.D);
   const int g = c.Hq / c.Hkv;
-  // blocks of 8 rows where the sequences' rows fit them on average
-  const bool eight = g <= 8 && (long long)c.T * g <= 8ll * c.B;
-  const int tokens = few_tokens(g, eight ? 8 : 16);
+  const bool eight = few_rows(c.T, c.B, g) == 8;
+  const int tokens = (eight ? 8 : 16) / g;
   char* ws = c.ws;
   FewArgs a{};
   a.Q = c.Q;
@@ -631,7 +630,7 @@ cudaError_t launch_few_attn_q8(const ChunkCall& c) {
   a.fixed = 6;  // (a decoding batch of 64 sequences: 189 us at 2, 186 at 4, 183 at 6)
   const int grid = std::min(num_sms_current(), kCMaxCtas) * (eight ? kFewCtas : kFewCtas16);
   a.plan = PlanArgs{c.cu_new, c.kv_len, a.mask, c.T, c.B, tokens, std::min(c.S_cap, kCMaxKeys), c.Hkv, grid, 0x7fffffff,
-                    a.status};
+                    0, c.T <= c.B ? 0x7fffffff : tokens, a.status};
   if (few_blocks(c.T, c.B, tokens) <= kWarpBlocks && c.B <= kWarpSeqs && !c.first_key) {
     a.blocks = nullptr;
   } else {

@@ -360,3 +360,102 @@ def test_few_and_many_rows_share_a_workspace():
         for x, w in zip((big, few), want):
             got = x.run(ws)
             assert got[2] == 0 and torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])
+
+
+@pytest.mark.parametrize("n,kv", [([1, 40, 1, 2, 1, 0, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1], [700, 900, 5, 300] + [64 * i for i in range(12)]),
+                                  ([3, 5, 4, 4, 4, 2], [100, 1000, 0, 33, 500, 127]), ([17, 0, 0, 0, 0, 1, 1], [300, 4, 5, 6, 7, 8, 2000])])
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 1, 128), (8, 2, 64), (14, 2, 64)])
+@pytest.mark.parametrize("opts", [dict(), dict(window=100, sinks=5), dict(docs=True)])
+def test_chunks_beside_decoding_sequences(n, kv, Hq, Hkv, d, opts):
+    """More new tokens than sequences, on average few enough for the few-row kernel: it takes those that fit its blocks."""
+    Inputs(n, kv, Hq, Hkv, d, 32, 16, seed=5).check(**options(opts, n, kv, Hq))
+
+
+@pytest.mark.parametrize("block,n", [(16, [1, 1]), (16, [40, 7]), (0, [40, 1])])
+def test_rows_behind_the_last_sequence_are_left_alone(block, n):
+    x = Inputs(n, [100, 50], 4, 2, 64, 16, block, seed=2)
+    T, B, Hq, Hkv, d = x.heads
+    want, want_lse, _ = x.run(window=60, sinks=3)
+    x.Q = torch.cat([x.Q, torch.full((5, Hq, d), math.nan, dtype=torch.bfloat16)])
+    x.heads = (T + 5, B, Hq, Hkv, d)
+    O, lse, status = x.run(window=60, sinks=3)
+    # (blocks may be cut elsewhere: the results of other kernels' parts differ in their last bits)
+    assert status == 0 and bool((O[T:] == 7).all()) and bool((lse[T:] == 7).all())
+    assert bool(((O[:T].float() - want.float()).abs() <= 2.0 ** -6 * want.float().abs() + 1e-3).all())
+    assert bool(((lse[:T] - want_lse).abs() <= 1e-3).all())
+
+
+@pytest.mark.parametrize("block,n", [(16, [1, 1, 1]), (16, [200, 1, 30]), (16, [3, 9, 1]), (0, [200, 1, 30])])
+def test_as_a_graph(block, n):
+    """Captured once, replayed on other queries and lengths in the same buffers: what eager calls give."""
+    x = Inputs(n, [900, 700, 64], 8, 2, 64, 64, block, seed=4)
+    T, B, Hq, Hkv, d = x.heads
+    fn = lr.libraspec_chunk_attn_q8_paged if block else lr.libraspec_sink_attn_paged
+    ws, cu, kvl, Q = lr.ChunkWorkspace(T, B, Hq, Hkv, d), x.cu.to(cuda()), x.kvl.to(cuda()), x.Q.to(cuda())
+
+    def call():
+        return fn(Q, *x.dev, cu, kvl, ws, window=500, sinks=4, want_lse=True)
+
+    call()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = call()
+    for lengths in ([900, 700, 64], [3, 640, 0], [899, 1, 63]):
+        kvl.copy_(torch.tensor(lengths, dtype=torch.int32))
+        Q.copy_(torch.randn(Q.shape, device=cuda()))
+        graph.replay()
+        got = [t.clone() for t in out]
+        want = call()
+        assert lr.libraspec_get_status(ws) == 0
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_call_on_another_stream():
+    x = Inputs([50, 1, 1, 2], [900, 700, 64, 5], 8, 2, 128, 64, 16, seed=4)
+    T, B, Hq, Hkv, d = x.heads
+    ws, cu, kvl, Q = lr.ChunkWorkspace(T, B, Hq, Hkv, d), x.cu.to(cuda()), x.kvl.to(cuda()), x.Q.to(cuda())
+    want = lr.libraspec_chunk_attn_q8_paged(Q, *x.dev, cu, kvl, ws)[0].clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = lr.libraspec_chunk_attn_q8_paged(Q, *x.dev, cu, kvl, ws, stream=side)[0]
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_a_cache_whose_offsets_pass_32_bits():
+    """Keys and codes beyond 2^32 bytes: appended, read back and attended to, by both kernels, at the end of 18 million keys
+    (in a window, with sinks)."""
+    Hq, Hkv, d, block, S = 4, 2, 128, 64, 18_000_000 // 64 * 64
+    codes = [torch.empty((1, Hkv, S, d), dtype=torch.float8_e4m3fn, device=cuda()) for _ in "KV"]
+    exps = [torch.zeros((1, Hkv, S // block), dtype=torch.uint8, device=cuda()) for _ in "KV"]
+    assert codes[0].numel() > 2 ** 32
+    g = torch.Generator().manual_seed(1)
+    ws, freqs, window, sinks = lr.ChunkWorkspace(300, 1, Hq, Hkv, d), lr.RopeFreqs(d), 200, 10
+
+    def step(at, n):
+        x = torch.randn((n, Hq + 2 * Hkv, d), generator=g).to(torch.bfloat16).to(cuda())
+        cu, kv = torch.tensor([0, n], dtype=torch.int32, device=cuda()), torch.tensor([at], dtype=torch.int32, device=cuda())
+        pos = torch.zeros(n, dtype=torch.int32, device=cuda())  # (no rotation: the values are the inputs')
+        q = lr.libraspec_rope_append_q8(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], *codes, *exps, cu, kv, freqs, ws, pos=pos)
+        K, V = lr.libraspec_kv_read_q8(*codes, *exps, cu, kv, n, ws)
+        O, _ = lr.libraspec_chunk_attn_q8(q, *codes, *exps, cu, kv, ws, window=window, sinks=sinks)
+        assert lr.libraspec_get_status(ws) == 0
+        assert bool(((K.float() - x[:, Hq:Hq + Hkv].float()).abs() <= 2.0 ** -4 * x[:, Hq:Hq + Hkv].float().abs() + 2.0 ** -13).all())
+        return q.double().cpu(), K.double().cpu(), V.double().cpu(), O.double().cpu()
+
+    _, K0, V0, _ = step(0, 16)
+    end = S - 300
+    _, K1, V1, _ = step(end - 256, 256)
+    for n in (299, 1):
+        q, K2, V2, O = step(end, n)
+        keys, values = torch.cat([K0[:sinks], K1, K2]), torch.cat([V0[:sinks], V1, V2])
+        pos = torch.cat([torch.arange(sinks), torch.arange(end - 256, end + n)])
+        p = torch.arange(end, end + n)[:, None]
+        see = (pos <= p) & ((pos > p - window) | (pos < sinks))
+        for h in range(Hq):
+            s = (q[:, h] @ keys[:, h // 2].T * d ** -0.5).masked_fill(~see, -math.inf)
+            w = s.softmax(-1)
+            v = values[:, h // 2]
+            assert bool(((O[:, h] - w @ v).abs() <= 2.0 ** -7 * (w @ v.abs())).all())

@@ -409,3 +409,51 @@ def test_append_and_read_as_a_graph():
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(cache.dev, eager.dev))
+
+
+@pytest.mark.parametrize("n", [[2, 1], [40, 9]])
+def test_append_leaves_rows_of_no_sequence_alone(n):
+    d, Hq, Hkv = 64, 3, 1
+    T = sum(n) + 5
+    x = torch.randn((T, Hq + 2 * Hkv, d), generator=torch.Generator().manual_seed(4)).to(cuda())
+    cache = Cache(2, Hkv, d, 64, 16, 16, 9)
+    cu, kv = torch.tensor([0, n[0], sum(n)], dtype=torch.int32, device=cuda()), torch.tensor([3, 16], dtype=torch.int32, device=cuda())
+    Qo = torch.full((T, Hq, d), 7.0, dtype=torch.bfloat16, device=cuda())
+    ws = lr.ChunkWorkspace(1, 1, 1, 1, 64)
+    lr.libraspec_rope_append_q8_paged(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], *cache.dev, *cache.dev_table, cu, kv,
+                                      lr.RopeFreqs(d), ws, Qo=Qo)
+    assert lr.libraspec_get_status(ws) == 0
+    assert bool((Qo[sum(n):] == 7).all()) and not bool((Qo[:sum(n)] == 7).all(-1).any())
+
+
+@pytest.mark.parametrize("B", [3, 40])
+def test_append_of_ranges_that_overlap(B):
+    """Beside offsets that decrease the ranges of others may overlap: reported; a sequence before them holds what it should."""
+    d, Hkv, T = 64, 1, 60
+    x = torch.randn((T, 3, d), generator=torch.Generator().manual_seed(4))
+    cache = Cache(B, Hkv, d, 80, 16, 16, 9)
+    before = [t.cpu().clone() for t in cache.dev]
+    cu = [0, 20] + [0, T] * B
+    cu, kv = torch.tensor(cu[:B + 1], dtype=torch.int32), torch.zeros(B, dtype=torch.int32)
+    _, status = append(cache, x.to(cuda()), 1, cu, kv, lr.RopeFreqs(d))
+    assert status == lr.ST_BAD_LENGTH
+    got, _ = cache.rows(cache.dev[1].cpu(), cache.dev[3].cpu(), 0, 0, 20)
+    v = x[:20, 2:].double()
+    assert bool(((got - v).abs() <= 2.0 ** -4 * v.abs() + 2.0 ** -10).all())
+
+
+def test_empty_calls():
+    d = 64
+    cache = Cache(2, 1, d, 32, 16, 16, 9)
+    before = [t.cpu().clone() for t in cache.dev]
+    x = torch.zeros((0, 3, d), device=cuda())
+    cu, kv = torch.zeros(3, dtype=torch.int32), torch.tensor([3, 0], dtype=torch.int32)
+    out, status = append(cache, x, 1, cu, kv, lr.RopeFreqs(d))
+    assert out.shape == (0, 1, d) and status == 0
+    ws = lr.ChunkWorkspace(1, 1, 1, 1, 64)
+    K, V = lr.libraspec_kv_read_q8_paged(*cache.dev, *cache.dev_table, cu.to(cuda()), kv.to(cuda()), 0, ws)
+    assert K.shape == V.shape == (0, 1, d)
+    one = torch.ones(d, device=cuda())
+    y = lr.libraspec_qk_norm_rope(x, 1, lr.QkNorm(one, one), torch.zeros(0, dtype=torch.int32, device=cuda()), lr.RopeFreqs(d))
+    assert y.shape == x.shape
+    assert all(torch.equal(a.cpu().view(torch.uint8), b.view(torch.uint8)) for a, b in zip(cache.dev, before))
