@@ -716,10 +716,10 @@ int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint1
  *
  * Two kernels. One reads a key for 8 or 16 rows, with queries as f16, exact down
  * to 2^-31 of a row's largest element; it takes decode steps (T <= B), and where
- * sequences have on average 16 rows per kv head at most, those whose rows fit one
- * of its blocks. The other takes the rest, in whose scores queries are two e4m3
- * parts: all eight bits of what lies within 2^-9 of a row's largest element, else
- * off by 2^-17 of that. One to five launches.
+ * sequences have on average 16 rows per kv head at most, all of 1024 rows per kv
+ * head, or those whose rows fit one of its blocks. The other takes the rest, in
+ * whose scores queries are two e4m3 parts: all eight bits of what lies within 2^-9
+ * of a row's largest element, else off by 2^-17 of that. One to five launches.
  */
 int libraspec_chunk_attn_q8(const uint16_t* Q, const uint8_t* K8, const uint8_t* V8, const uint8_t* Ks,
                             const uint8_t* Vs, const int32_t* cu_new, const int32_t* kv_len, int T, int B, int Hq,

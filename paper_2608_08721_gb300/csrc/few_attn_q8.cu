@@ -29,6 +29,10 @@ namespace libraspec {
 constexpr int kFewWarps = 4, kFewThreads = 32 * kFewWarps;
 constexpr int kFewStages = 3;            // of a warp's ring
 constexpr int kFewCtas = 3, kFewCtas16 = 2;  // per SM, of 8 rows and of 16
+constexpr int kGroup = 8;                // parts merged at a time
+constexpr int kTopCounts = kCMaxCtas * kFewCtas;  // counters of a block's groups, behind those of the groups' parts
+static_assert(2 * kTopCounts <= kCMaxCounts && 2 * kFewCtas * 8 <= kCBlockRows && 2 * kFewCtas16 * 16 <= kCBlockRows,
+              "counters and parts fit the workspace");
 
 struct FewArgs {
   const uint16_t* Q;
@@ -511,54 +515,77 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? kFewCtas : kFewCtas16) 
         if (A.lse && d == 0) A.lse[out] = (M + __log2f(L)) * kLn2;
       }
     }
-    if (done.partial) {  // the CTA that delivers the last part merges all, in CTA order
-      __syncthreads();
-      if (tid == 0) {
-        uint32_t old;
-        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(A.count + done.c0) : "memory");
-        s_last = old == (uint32_t)done.np - 1;
-        if (s_last) A.count[done.c0] = 0u;
-      }
-      __syncthreads();
-      if (s_last) {
-        for (int u = tid; u < rows * (D / 2); u += kFewThreads) {
-          const int row = u / (D / 2), d = 2 * (u % (D / 2));
-          auto part = [&](int p) { return (size_t)(p == 0 ? 2 * done.c0 + 1 : 2 * (done.c0 + p)) * kRows + row; };
+    // The CTA that delivers the last part of kGroup merges them, and the one that merges the last group merges the groups,
+    // each in CTA order: a block's parts then take two rounds of loads and not np / 8 (one sequence over 8000 keys and 32
+    // heads, 57 parts of a head: 14.6 us, with eight parts of the row at a
+    // time in one round after the other 22.4; of four tokens 24 and 41).
+    if (done.partial) {
+      auto arrive = [&](int at, int of) {
+        __syncthreads();
+        if (tid == 0) {
+          uint32_t old;
+          asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(A.count + at) : "memory");
+          s_last = old == (uint32_t)of - 1;
+          if (s_last) A.count[at] = 0u;
+        }
+        __syncthreads();
+        return s_last != 0;
+      };
+      const int slots = 2 * gridDim.x;  // (those of the groups lie behind the parts')
+      auto slot_of = [&](int p) { return p == 0 ? 2 * done.c0 + 1 : 2 * (done.c0 + p); };
+      auto merge = [&](int from, int to, int step, int first_slot, int into) {  // into < 0: the results
+        for (int u = tid; u < rows * (D / 4); u += kFewThreads) {
+          const int row = u / (D / 4), d = 4 * (u % (D / 4));
           float M = -INFINITY, L = 0.f;
-          float2 acc = make_float2(0.f, 0.f);
-          constexpr int kParts = 8;  // loads in flight
-          for (int p0 = 0; p0 < done.np; p0 += kParts) {
-            float2 ml[kParts], x[kParts];
-            float to = M;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+          for (int p0 = from; p0 < to; p0 += kGroup * step) {
+            float2 ml[kGroup];
+            float4 x[kGroup];
+            float top = M;
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) {
+            for (int k = 0; k < kGroup; ++k) {
               ml[k] = make_float2(-INFINITY, 0.f);
-              x[k] = make_float2(0.f, 0.f);
-              if (p0 + k < done.np) {
-                ml[k] = __ldcg(reinterpret_cast<const float2*>(A.part_ml) + part(p0 + k));
-                x[k] = __ldcg(reinterpret_cast<const float2*>(A.part_o + part(p0 + k) * D + d));
+              x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (p0 + k * step < to) {
+                const size_t at = (size_t)(first_slot + slot_of(p0 + k * step)) * kRows + row;
+                ml[k] = __ldcg(reinterpret_cast<const float2*>(A.part_ml) + at);
+                x[k] = __ldcg(reinterpret_cast<const float4*>(A.part_o + at * D + d));
               }
             }
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) to = fmaxf(to, ml[k].x);
-            const float old = to == -INFINITY ? 1.f : ex2_approx(M - to);
-            M = to;
+            for (int k = 0; k < kGroup; ++k) top = fmaxf(top, ml[k].x);
+            const float old = top == -INFINITY ? 1.f : ex2_approx(M - top);
+            M = top;
             L *= old;
-            acc.x *= old;
-            acc.y *= old;
+            acc.x *= old, acc.y *= old, acc.z *= old, acc.w *= old;
 #pragma unroll
-            for (int k = 0; k < kParts; ++k) {
-              const float f = to == -INFINITY ? 1.f : ex2_approx(ml[k].x - to);
+            for (int k = 0; k < kGroup; ++k) {
+              const float f = top == -INFINITY ? 1.f : ex2_approx(ml[k].x - top);
               L += f * ml[k].y;
-              acc.x += f * x[k].x;
-              acc.y += f * x[k].y;
+              acc.x += f * x[k].x, acc.y += f * x[k].y, acc.z += f * x[k].z, acc.w += f * x[k].w;
             }
           }
-          const size_t out = (size_t)(done.tok0 + row / g) * A.Hq + done.kvh * g + row % g;
-          const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
-          *reinterpret_cast<uint32_t*>(A.O + out * D + d) = c_pack(acc.x * inv, acc.y * inv);
-          if (A.lse && d == 0) A.lse[out] = (M + __log2f(L)) * kLn2;
+          if (into >= 0) {
+            const size_t at = (size_t)into * kRows + row;
+            *reinterpret_cast<float4*>(A.part_o + at * D + d) = acc;
+            if (d == 0) *reinterpret_cast<float2*>(A.part_ml + at * 2) = make_float2(M, L);
+          } else {
+            const size_t out = (size_t)(done.tok0 + row / g) * A.Hq + done.kvh * g + row % g;
+            const float inv = L > 0.f ? 1.f / L : L == 0.f ? 0.f : L;
+            *reinterpret_cast<uint2*>(A.O + out * D + d) =
+                make_uint2(c_pack(acc.x * inv, acc.y * inv), c_pack(acc.z * inv, acc.w * inv));
+            if (A.lse && d == 0) A.lse[out] = (M + __log2f(L)) * kLn2;
+          }
         }
+      };
+      // (no other block's parts begin in a CTA before its last, so a counter at a group's first CTA is its own)
+      const int first = ((int)blockIdx.x - done.c0) / kGroup * kGroup, n = min(kGroup, done.np - first);
+      if (done.np <= kGroup) {
+        if (arrive(done.c0, done.np)) merge(0, done.np, 1, 0, -1);
+      } else if (n == 1 || arrive(done.c0 + first, n)) {
+        merge(first, first + n, 1, 0, slots + slot_of(first));
+        if (arrive(kTopCounts + done.c0, (done.np + kGroup - 1) / kGroup)) merge(0, done.np, kGroup, slots, -1);
       }
     }
     __syncthreads();
@@ -630,7 +657,7 @@ cudaError_t launch_few_attn_q8(const ChunkCall& c) {
   a.fixed = 6;  // (a decoding batch of 64 sequences: 189 us at 2, 186 at 4, 183 at 6)
   const int grid = std::min(num_sms_current(), kCMaxCtas) * (eight ? kFewCtas : kFewCtas16);
   a.plan = PlanArgs{c.cu_new, c.kv_len, a.mask, c.T, c.B, tokens, std::min(c.S_cap, kCMaxKeys), c.Hkv, grid, 0x7fffffff,
-                    0, c.T <= c.B ? 0x7fffffff : tokens, a.status};
+                    0, few_alone(c.T, c.B, g) ? 0x7fffffff : tokens, a.status};
   if (few_blocks(c.T, c.B, tokens) <= kWarpBlocks && c.B <= kWarpSeqs && !c.first_key) {
     a.blocks = nullptr;
   } else {

@@ -363,11 +363,14 @@ def test_few_and_many_rows_share_a_workspace():
 
 
 @pytest.mark.parametrize("n,kv", [([1, 40, 1, 2, 1, 0, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1], [700, 900, 5, 300] + [64 * i for i in range(12)]),
-                                  ([3, 5, 4, 4, 4, 2], [100, 1000, 0, 33, 500, 127]), ([17, 0, 0, 0, 0, 1, 1], [300, 4, 5, 6, 7, 8, 2000])])
+                                  ([3, 5, 4, 4, 4, 2], [100, 1000, 0, 33, 500, 127]), ([17, 0, 0, 0, 0, 1, 1], [300, 4, 5, 6, 7, 8, 2000]),
+                                  ([1] * 60 + [150] + [1, 0, 3] * 30, [7 * i for i in range(151)]),
+                                  ([0] * 99 + [300] + [0] * 40, [3] * 99 + [80] + [0] * 40)])
 @pytest.mark.parametrize("Hq,Hkv,d", [(4, 1, 128), (8, 2, 64), (14, 2, 64)])
 @pytest.mark.parametrize("opts", [dict(), dict(window=100, sinks=5), dict(docs=True)])
 def test_chunks_beside_decoding_sequences(n, kv, Hq, Hkv, d, opts):
-    """More new tokens than sequences, on average few enough for the few-row kernel: it takes those that fit its blocks."""
+    """More new tokens than sequences, on average few enough for the few-row kernel: it takes all, or (of the last, with 4
+    or 7 heads for each of the cache's) those that fit its blocks."""
     Inputs(n, kv, Hq, Hkv, d, 32, 16, seed=5).check(**options(opts, n, kv, Hq))
 
 
@@ -385,10 +388,12 @@ def test_rows_behind_the_last_sequence_are_left_alone(block, n):
     assert bool(((lse[:T] - want_lse).abs() <= 1e-3).all())
 
 
-@pytest.mark.parametrize("block,n", [(16, [1, 1, 1]), (16, [200, 1, 30]), (16, [3, 9, 1]), (0, [200, 1, 30])])
+@pytest.mark.parametrize("block,n", [(16, [1, 1, 1]), (16, [200, 1, 30]), (16, [3, 9, 1]), (0, [200, 1, 30]),
+                                     (16, [1, 150, 1] + [1] * 77)])
 def test_as_a_graph(block, n):
     """Captured once, replayed on other queries and lengths in the same buffers: what eager calls give."""
-    x = Inputs(n, [900, 700, 64], 8, 2, 64, 64, block, seed=4)
+    B = len(n)
+    x = Inputs(n, [900, 700, 64] + [9] * (B - 3), 8, 2, 64, 64, block, seed=4)
     T, B, Hq, Hkv, d = x.heads
     fn = lr.libraspec_chunk_attn_q8_paged if block else lr.libraspec_sink_attn_paged
     ws, cu, kvl, Q = lr.ChunkWorkspace(T, B, Hq, Hkv, d), x.cu.to(cuda()), x.kvl.to(cuda()), x.Q.to(cuda())
@@ -403,7 +408,7 @@ def test_as_a_graph(block, n):
     with torch.cuda.graph(graph, stream=side):
         out = call()
     for lengths in ([900, 700, 64], [3, 640, 0], [899, 1, 63]):
-        kvl.copy_(torch.tensor(lengths, dtype=torch.int32))
+        kvl[:3].copy_(torch.tensor(lengths, dtype=torch.int32))
         Q.copy_(torch.randn(Q.shape, device=cuda()))
         graph.replay()
         got = [t.clone() for t in out]
