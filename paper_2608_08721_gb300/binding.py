@@ -627,6 +627,14 @@ def _check_device(t: torch.Tensor, name: str) -> None:
         raise ValueError("%s must be on a CUDA device" % name)
 
 
+def _on_current(x: torch.Tensor, y: torch.Tensor) -> None:
+    """Refuses a call on tensors of another device than the current one, where it would launch. (Two of them: to ask each
+    of ten takes 1.5 us.)"""
+    dev = torch.cuda.current_device()
+    if x.get_device() != dev or y.get_device() != dev:
+        raise ValueError("all tensors must be on the current device (%d), got %s and %s" % (dev, x.device, y.device))
+
+
 def _out(shape, dtype, device, stream) -> torch.Tensor:
     """An output of a call, made on the stream that it runs on: what the current stream has given back may still be in
     use there, where nothing orders the call's stream behind it."""
@@ -774,6 +782,7 @@ def libraspec_qk_norm_rope(X, n_q: int, norm: QkNorm, pos, freqs: RopeFreqs, int
     _check_norm(norm, d)
     _req(pos, torch.int32, "pos", (T,))
     _check_device(freqs.turns, "freqs")
+    _on_current(X, freqs.turns)
     if Y is None:
         Y = _out(shape, dt, X.device, stream)
         ys = H * d
@@ -858,6 +867,7 @@ def _rope_append_q8(Q, K, V, K8, V8, Ks, Vs, block_table, cu_new, kv_len, freqs,
     if norm is not None:
         _check_norm(norm, d)
         q_w, k_w, eps = norm.q_ptr, norm.k_ptr, norm.eps
+    _on_current(K, K8)
     Hq = qs = 0
     if Q is not None:
         qs = _heads_stride(Q, dt, "Q")
@@ -905,6 +915,7 @@ def _kv_read_q8(K8, V8, Ks, Vs, block_table, cu, start, T, ws, K, V, stream):
     T = int(T)
     if T < 0:
         raise ValueError("T must not be negative")
+    _on_current(K8, ws.buf)
     shape = (T, Hkv, d)
     K = _out(shape, torch.bfloat16, K8.device, stream) if K is None else _req(K, torch.bfloat16, "K", shape)
     V = _out(shape, torch.bfloat16, K8.device, stream) if V is None else _req(V, torch.bfloat16, "V", shape)
@@ -1011,6 +1022,8 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
         caches = (Kc.data_ptr(), Vc.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
         block = (block,)
     _check_device(ws.buf, "the workspace")
+    if sinks is not None:
+        _on_current(Q, Kc)
     opts = None
     if softcap or slopes is not None or window or first_key is not None or prefix_len is not None:
         if slopes is not None:

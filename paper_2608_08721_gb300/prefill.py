@@ -22,9 +22,10 @@ from . import binding
 
 
 class Step:
-    """One chunk of new tokens: how many each sequence has, and their offsets in the packed rows."""
+    """One chunk of new tokens: how many each sequence has, their offsets in the packed rows and, with the sequences'
+    lengths, the tokens' positions."""
 
-    def __init__(self, n_new: Sequence[int], device, lengths: Sequence[int]):
+    def __init__(self, n_new: Sequence[int], device, lengths: Optional[Sequence[int]] = None):
         self.n_new = [int(n) for n in n_new]
         offsets = [0]
         for n in self.n_new:
@@ -32,7 +33,8 @@ class Step:
         self.T = offsets[-1]
         self.cu_new = torch.tensor(offsets, dtype=torch.int32).to(device)
         self.n_dev = torch.tensor(self.n_new, dtype=torch.int32).to(device)
-        self.pos = torch.cat([torch.arange(a, a + n, dtype=torch.int32) for a, n in zip(lengths, self.n_new)]).to(device)
+        if lengths is not None:
+            self.pos = torch.cat([torch.arange(a, a + n, dtype=torch.int32) for a, n in zip(lengths, self.n_new)]).to(device)
 
 
 class PagedSequences:
@@ -74,7 +76,7 @@ class PagedSequences:
         for b, n in enumerate(n_new):
             if self.lengths[b] + n > self.capacity:
                 raise ValueError("sequence %d: %d + %d keys do not fit %d" % (b, self.lengths[b], n, self.capacity))
-        return Step(n_new, self.device, self.lengths)
+        return Step(n_new, self.device, None if self.norm is None else self.lengths)
 
     def layer(self, l: int, qkv: torch.Tensor, step: Step, lse: Optional[torch.Tensor] = None, stream=None, **options):
         """Layer l of the step: qkv [T, Hq + 2 Hkv, d] (f32 or bf16, the projections' output) is rotated and appended,
@@ -123,7 +125,7 @@ class PagedSequences:
         if not self.block:
             return self.pools[l]
         n = [a + extra for a in self.lengths]
-        whole, pool = Step(n, self.device, [0] * self.B), self.pools[l]
+        whole, pool = Step(n, self.device), self.pools[l]
         start = torch.zeros_like(self.kv_len)
         K, V = binding.libraspec_kv_read_q8_paged(pool["K8"], pool["V8"], pool["Ks"], pool["Vs"], self.block_table,
                                                   whole.cu_new, start, whole.T, self.ws)

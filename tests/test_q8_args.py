@@ -180,3 +180,33 @@ def test_binding_names_what_is_wrong_with_a_cache():
         lr.libraspec_qk_norm_rope(x, 1, norm, pos, lr.RopeFreqs(128))
     with pytest.raises(ValueError, match="^n_q must lie"):
         lr.libraspec_qk_norm_rope(x[..., :64].contiguous(), 3, norm, pos, lr.RopeFreqs(64))
+
+
+@pytest.mark.gpu
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """A call launches on the current device; with tensors of another it is refused, before anything is enqueued."""
+    from helpers import cuda
+
+    d, Hq, Hkv, B, S, T = 64, 4, 2, 1, 64, 2
+    z = dict(device=cuda())
+    X, pos = torch.zeros((T, Hq + 2 * Hkv, d), **z), torch.zeros(T, dtype=torch.int32, **z)
+    K8, V8 = [torch.zeros((B, Hkv, S, d), dtype=torch.uint8, **z).view(torch.float8_e4m3fn) for _ in "KV"]
+    Ks, Vs = [torch.zeros((B, Hkv, S // 16), dtype=torch.uint8, **z) for _ in "KV"]
+    Kc, Vc = [torch.zeros((B, Hkv, S, d), dtype=torch.bfloat16, **z) for _ in "KV"]
+    cu, kv = torch.tensor([0, T], dtype=torch.int32, **z), torch.zeros(B, dtype=torch.int32, **z)
+    one, Q = torch.ones(d, **z), torch.zeros((T, Hq, d), dtype=torch.bfloat16, **z)
+    norm, freqs, ws = lr.QkNorm(one, one), lr.RopeFreqs(d), lr.ChunkWorkspace(T, B, Hq, Hkv, d)
+    calls = [lambda: lr.libraspec_qk_norm_rope(X, Hq, norm, pos, freqs),
+             lambda: lr.libraspec_rope_append_q8(X[:, :Hq], X[:, Hq:Hq + Hkv], X[:, Hq + Hkv:], K8, V8, Ks, Vs, cu, kv, freqs,
+                                                 ws, norm=norm),
+             lambda: lr.libraspec_kv_read_q8(K8, V8, Ks, Vs, cu, kv, T, ws),
+             lambda: lr.libraspec_chunk_attn_q8(Q, K8, V8, Ks, Vs, cu, kv, ws),
+             lambda: lr.libraspec_sink_attn(Q, Kc, Vc, cu, kv, ws, window=8, sinks=1)]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    assert lr.libraspec_get_status(ws) == 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: cuda().index + 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
