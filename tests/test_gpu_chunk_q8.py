@@ -464,3 +464,30 @@ def test_a_cache_whose_offsets_pass_32_bits():
             w = s.softmax(-1)
             v = values[:, h // 2]
             assert bool(((O[:, h] - w @ v).abs() <= 2.0 ** -7 * (w @ v.abs())).all())
+
+
+@pytest.mark.parametrize("n,kv", [([1], [70000]), ([2], [9000]), ([4, 1], [3000, 40000]), ([1, 1, 1], [1030, 0, 20000])])
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 1, 128), (16, 1, 64), (3, 1, 128)])
+@pytest.mark.parametrize("opts", [dict(), dict(window=30000, sinks=200)])
+def test_rows_in_many_parts(n, kv, Hq, Hkv, d, opts):
+    """Few rows over long caches: up to every CTA has a part of a row's keys; parts are merged in groups."""
+    Inputs(n, kv, Hq, Hkv, d, 0, 64, seed=6).check(**options(opts, n, kv, Hq))
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    both = [Inputs(n, kv, 8, 2, 128, 64, 16, seed=i) for i, (n, kv) in enumerate([([1, 1, 1], [3000, 5, 900]),
+                                                                                  ([200, 1], [700, 2000])])]
+    args, want = [], []
+    for x in both:
+        T, B, Hq, Hkv, d = x.heads
+        args.append((x.Q.to(cuda()), *x.dev, x.cu.to(cuda()), x.kvl.to(cuda()), lr.ChunkWorkspace(T, B, Hq, Hkv, d)))
+        want.append(lr.libraspec_chunk_attn_q8_paged(*args[-1], want_lse=True))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in both]
+    got = [[lr.libraspec_chunk_attn_q8_paged(*a, want_lse=True, stream=s) for a, s in zip(args, streams)] for _ in range(20)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for (O, lse), (O1, lse1) in zip(pair, want):
+            assert torch.equal(O, O1) and torch.equal(lse, lse1)
+    assert all(lr.libraspec_get_status(a[-1]) == 0 for a in args)
