@@ -581,6 +581,7 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? kFewCtas : kFewCtas16) 
       };
       // (no other block's parts begin in a CTA before its last, so a counter at a group's first CTA is its own)
       const int first = ((int)blockIdx.x - done.c0) / kGroup * kGroup, n = min(kGroup, done.np - first);
+      if (n == 1) __syncthreads();  // (a group of this CTA's part alone: it is written by all threads)
       if (done.np <= kGroup) {
         if (arrive(done.c0, done.np)) merge(0, done.np, 1, 0, -1);
       } else if (n == 1 || arrive(done.c0 + first, n)) {
