@@ -709,7 +709,8 @@ __device__ __forceinline__ float power_of_two_biased(uint32_t e) { return __uint
 // [2^7, 2^8) becomes the nearest e4m3 and the rest, together all eight bits of what lies within 2^-9 of the largest, else
 // off by 2^-17 of it at most. Per 64 elements the first parts, then the second, in the bytes that the elements took. A
 // launch of its own (24 us for a prompt of 8192 tokens of 32 heads, as long beside the plan as behind it): in the
-// attention, where each CTA did it for its items, the prompt took 92 us longer.
+// attention, where each CTA did it for its items, the prompt took 92 us longer, and 104 in place by the converters (what a
+// warp reads of shared memory beside the MMAs takes 150 to 400 cycles, a shuffle too).
 constexpr int kSplitThreads = 256;
 template <int D>
 static __global__ void __launch_bounds__(kSplitThreads) split_q_kernel(const uint16_t* __restrict__ Q, long long rows,
