@@ -64,13 +64,14 @@
 // A cache in 8 bits (kQ8): codes c of e4m3, values c 2^e with an exponent for every 16 to 64 keys of a kv head. Keys meet
 // the queries as e4m3, as they lie in memory, the queries in two e4m3 parts (split_q_kernel), one behind the other along
 // the contraction, which costs the tensor pipe what one product of 16-bit operands does. The rows' and keys' scales enter
-// the softmax, which multiplies scores by them anyway. Values are converted to f16 by a fourth warpgroup, brought to the
-// largest exponent of their tile (exact for codes down to 2^15 below it; what lies further below is off by 2^-24 of that
-// scale at most), and P is f16, times that scale: O = sum 2^(s - m + e) V8, l = sum 2^(s - m). One more warp brings the
-// exponents, two tiles' look-ups ahead; a tile's count with its scores on one barrier. What bounds it: the softmax warps'
-// steps, beside which the converters issue (a prompt of 8192 tokens, 478 us: 37 of them go when the conversion is left
-// out, 24 are the queries' parts; the same in bf16 takes 395). Measured and not kept: K converted as well (647), the
-// queries' parts in the kernel (615), their scales on a barrier of their own (518).
+// the softmax, which multiplies scores by them anyway. Values are converted to f16 by a fourth warpgroup, code by code
+// (exactly), and P is f16, times its value's scale: P' = 2^(s - m + e), O = sum P' V8, l = sum P' 2^-e. The exponent e of
+// each 16 keys enters behind the mask, so neither the reference m nor P' of a row depends on a key that it does not see.
+// (With a tile's values brought to its largest exponent instead, a hidden key's scale took the bits of what the row sees;
+// it was no faster either: a prompt of 8192 tokens 483 us, 458 so.) One more warp brings the exponents, two tiles'
+// look-ups ahead; a tile's count with its scores on one barrier. What bounds it: the softmax warps' steps, beside which
+// the converters issue (24 of the 458 us are the queries' parts; the same in bf16 takes 385). Measured and not kept, when
+// the prompt took 518: K converted as well (647), the queries' parts in the kernel (615).
 //
 // Sinks (kSink): keys below `sinks` stay visible to every row behind them. A block's tiles are then the first ones of the
 // sequence that hold sinks, and those of its window; what lies between is not read.
@@ -590,12 +591,10 @@ __device__ __forceinline__ int item_tile(const ChunkItem& it, int j) {
 // plain kernel costs it instruction fetches, also beside its loop.)
 constexpr int kCap = 1, kBias = 2, kWideCap = 4, kDocs = 8, kQ8 = 16, kSink = 32;
 
-// (8 bits) What the softmax takes of a tile's scales: of K for every 16 keys; of V the largest, to whose exponent the
-// tile's values are brought by their conversion.
+// (8 bits) What the softmax takes of a tile's scales, for every 16 keys: K's scale, and the exponent of V's.
 struct TileScales {
   float k[8];
-  float v_log2, v_inverse;
-  float pad[2];
+  __half v_log2[8];
 };
 static_assert(sizeof(TileScales) == 48, "");
 
@@ -620,8 +619,7 @@ struct ChunkSmem {
   static constexpr int kMisc = kInfo + 2 * 80;           // [0] misaligned, [1] this CTA merges, [2] tensor memory
   static constexpr int kStat = kMisc + 16;               // (m, l) of streams to be combined: of each, or of one at a time
   static constexpr int kScales = kStat + (Q8 ? 1 : kCStreams) * kCRows * 8;  // [stream]: struct TileScales
-  static constexpr int kVScales = kScales + (Q8 ? kCStreams * 48 : 0);  // [raw tile]: 8 f16 factors
-  static constexpr int kBytes = kVScales + (Q8 ? kRaws * 16 : 0);
+  static constexpr int kBytes = kScales + (Q8 ? kCStreams * 48 : 0);
   // tensor memory: scores, of each stream (D = 64) or of the step at hand (128: no room for two), P and O of each
   static constexpr int kScores = D == 128 ? 1 : 2;
   static constexpr int kColS = 0, kColP = kScores * 128, kColO = kColP + kCStreams * 64;
@@ -997,7 +995,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         mbar_init(bKEmpty + 8 * s, 1);
       }
       for (int s = 0; s < SM::kRaws; ++s) {
-        mbar_init(bRFull + 8 * s, 2);  // the tile, and its factors
+        mbar_init(bRFull + 8 * s, 1);
         mbar_init(bREmpty + 8 * s, kConverters);
       }
       for (int s = 0; s < 2; ++s) mbar_init(bCEmpty + 8 * s, 4);
@@ -1063,7 +1061,6 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const bool edge = kt0 < it.klo || kt0 + kCKeys > it.khi || gap;
         const uint8_t* raw = smem + SM::kRaw + rc * SM::kRawTile + crow * D + cj * 16;
         uint8_t* dst = smem + SM::kRing + ch * SM::kTile;
-        const uint4 factors = *reinterpret_cast<const uint4*>(smem + SM::kVScales + rc * 16);  // of each 16 keys
 #pragma unroll 1
         for (int i0 = 0; i0 < kUnits; i0 += 4) {
           uint4 v[4];
@@ -1080,21 +1077,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            __half2 f;  // of the row's 16 keys
-            if constexpr (D == 128) {  // the (i0 + i)-th
-              const uint32_t w = i < 2 ? (i0 ? factors.z : factors.x) : (i0 ? factors.w : factors.y);
-              const uint32_t p = __byte_perm(w, 0, i % 2 ? 0x3232 : 0x1010);
-              f = *reinterpret_cast<const __half2*>(&p);
-            } else {
-              const uint32_t w = i == 0 ? factors.x : i == 1 ? factors.y : i == 2 ? factors.z : factors.w;
-              const uint32_t p = __byte_perm(w, 0, crow >= 16 ? 0x3232 : 0x1010);
-              f = *reinterpret_cast<const __half2*>(&p);
-            }
-            auto to_f16 = [&](uint32_t codes) {
-              const uint32_t h = f16_of_e4m3((uint16_t)codes);
-              const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h), f);
-              return *reinterpret_cast<const uint32_t*>(&y);
-            };
+            auto to_f16 = [&](uint32_t codes) { return f16_of_e4m3((uint16_t)codes); };
             const uint4 lo = make_uint4(to_f16(v[i].x), to_f16(v[i].x >> 16), to_f16(v[i].y), to_f16(v[i].y >> 16));
             const uint4 hi = make_uint4(to_f16(v[i].z), to_f16(v[i].z >> 16), to_f16(v[i].w), to_f16(v[i].w >> 16));
             uint8_t* r = dst + (i0 + i) * kRowStep * 128;  // (a multiple of eight rows on: the same swizzle)
@@ -1486,7 +1469,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       // Lane 8 k + i has those of the i-th 16 keys of the k-th of four tiles; the next four are on their way meanwhile.
       asm volatile("griddepcontrol.wait;" ::: "memory");
       const int i = lane & 7;
-      uint32_t item_ctr = 0, raw_ctr = 0, ctr[2] = {0, 0};
+      uint32_t item_ctr = 0, ctr[2] = {0, 0};
       bool ok = true;
       for (int last = 0; !last && ok; ++item_ctr) {
         ok = warp_wait(bIFull + 8 * (item_ctr & 1), (item_ctr >> 1) & 1);
@@ -1499,9 +1482,11 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const int n = it.n_tiles, sinks = SINK ? min(A.mask.sinks, it.khi) : 0, per = A.rows >> A.block_log2;
         auto load = [&](int t0) {  // exponents of K (low byte) and V
           const int t = t0 + lane / 8;
-          if (t >= n) return 0u;
+          const uint32_t none = 127u | 127u << 8;
+          if (t >= n) return none;
           const int key = item_tile<SINK>(it, tile_of<SHAPE>(t, n)) * kCKeys + 16 * i;
-          if (key >= it.khi || (key + 16 <= it.klo && key >= sinks)) return 127u;  // (of V: below all others)
+          if (key >= it.khi || (key + 16 <= it.klo && key >= sinks)) return none;
+          // (within, first keys may hide the 16 from all rows: whatever lies there then, any scale will do)
           int plane = it.b, row = key;
           if (A.block_table) {
             plane = __ldg(A.block_table + (size_t)it.b * A.max_pages + key / A.page_size);
@@ -1515,22 +1500,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         uint32_t now = load(0);
         for (int t0 = 0; t0 < n && ok; t0 += 4) {
           const uint32_t next = load(t0 + 4);
-          // the largest exponent of V of a tile, and its groups' factors 2^(e - largest) as f16
-          const int ev = (int)(now >> 8);
-          int top = ev;
-#pragma unroll
-          for (int off = 4; off > 0; off >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-          const int down = top - ev;
-          const uint16_t factor = down <= 14 ? (uint16_t)((15 - down) << 10) : down <= 24 ? (uint16_t)(1 << (24 - down)) : 0;
-          if (top == 0) top = 127;  // (no group of the tile is seen)
           for (int k = 0; k < 4 && t0 + k < n && ok; ++k) {
-            const uint32_t rc = raw_ctr % SM::kRaws;
-            ok = warp_wait(bREmpty + 8 * rc, ((raw_ctr / SM::kRaws) & 1) ^ 1);
-            if (!ok) break;
-            if (lane / 8 == k) reinterpret_cast<uint16_t*>(smem + SM::kVScales + rc * 16)[i] = factor;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bRFull + 8 * rc);
-            ++raw_ctr;
             for (int s = 0; s < 2 && ok; ++s) {
               if (!it.pair && s != ((t0 + k) & 1)) continue;
               // once the stream has read those of its tile before (two arrivals could else make one phase of bSFull)
@@ -1540,10 +1510,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
               if (lane / 8 == k) {
                 TileScales* to = reinterpret_cast<TileScales*>(smem + SM::kScales) + s;
                 to->k[i] = power_of_two_biased(now & 0xffu);
-                if (i == 0) {
-                  to->v_log2 = (float)(top - 127);
-                  to->v_inverse = power_of_two_biased(254u - top);
-                }
+                to->v_log2[i] = __int2half_rn((int)(now >> 8) - 127);
               }
               __syncwarp();
               if (lane == 0) mbar_arrive(bSFull + 8 * s);
@@ -1616,14 +1583,14 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const uint32_t n = (st ? done1 : done0) + i;
         wait(bSFull + 8 * st, n & 1);
         float k_scale[8] = {};
-        float v_log2 = 0.f, v_inverse = 0.f;
+        uint32_t v_exps[4] = {};
         if constexpr (Q8) {
           const float4* from = reinterpret_cast<const float4*>(smem + SM::kScales + st * 48);
           const float4 a = from[0], b = from[1], c = from[2];
           k_scale[0] = a.x, k_scale[1] = a.y, k_scale[2] = a.z, k_scale[3] = a.w;
           k_scale[4] = b.x, k_scale[5] = b.y, k_scale[6] = b.z, k_scale[7] = b.w;
-          v_log2 = c.x;
-          v_inverse = c.y;
+          v_exps[0] = __float_as_uint(c.x), v_exps[1] = __float_as_uint(c.y);
+          v_exps[2] = __float_as_uint(c.z), v_exps[3] = __float_as_uint(c.w);
           __syncwarp();
           if (lane == 0) mbar_arrive(bCEmpty + 8 * st);
         }
@@ -1744,8 +1711,13 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         float cmax;
         // (not zero: a masked score stays minus infinity)
         auto group_scale = [&](int gr) { return SHAPE & (kCap | kBias) ? 1.f : fmaxf(sc * k_scale[gr], kFloatMin); };
+        auto v_log2 = [&](int gr) {
+          const __half2 two = *reinterpret_cast<const __half2*>(&v_exps[gr / 2]);
+          return gr % 2 ? __high2float(two) : __low2float(two);
+        };
         if constexpr (Q8) {
-          // the largest term of O's sum: P times the tile's scale of V
+          // the largest term of O's sum: P times its value's scale. (Behind the mask: what a row does not see has no
+          // part in its reference.)
           cmax = -INFINITY;
 #pragma unroll
           for (int gr = 0; gr < 8; ++gr) {
@@ -1754,9 +1726,9 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
 #pragma unroll
             for (int c = 1; c < 15; c += 2) m = fmaxf(fmaxf(m, __uint_as_float(y[c])), __uint_as_float(y[c + 1]));
             m = fmaxf(m, __uint_as_float(y[15]));
-            cmax = fmaxf(cmax, m * group_scale(gr));
+            cmax = fmaxf(cmax, fmaf(m, group_scale(gr), v_log2(gr)));
           }
-          cmax = valid ? cmax + v_log2 : 0.f;
+          cmax = valid ? cmax : 0.f;
         } else {
           float mx[4];
 #pragma unroll
@@ -1793,7 +1765,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           }
           tmem_wait_st();
         }
-        const float neg_m = (m_run == -INFINITY ? 0.f : -m_run) + v_log2;
+        const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
         float la[2] = {0.f, 0.f}, lb[2] = {0.f, 0.f};
         uint32_t pk[4][16];
 #pragma unroll
@@ -1801,21 +1773,30 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           if constexpr (Q8) {
 #pragma unroll
             for (int gr = 2 * q; gr < 2 * q + 2; ++gr) {
-              const float f = group_scale(gr);
+              const float f = group_scale(gr), v = v_log2(gr), to = neg_m + v;
+              // 2^-v: 1.5 2^23 - v has -v in its lowest bits
+              const float inv = __uint_as_float((__float_as_uint(12582912.f - v) << 23) + 0x3f800000u);
+              float ga[2], gb[2];  // sums of P times V's scale
 #pragma unroll
               for (int c = gr % 2 * 16; c < gr % 2 * 16 + 16; c += 4) {
                 float y0, y1, y2, y3;
-                fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), f, neg_m);
-                fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), f, neg_m);
+                fma2(y0, y1, __uint_as_float(x[q][c]), __uint_as_float(x[q][c + 1]), f, to);
+                fma2(y2, y3, __uint_as_float(x[q][c + 2]), __uint_as_float(x[q][c + 3]), f, to);
                 y0 = ex2_approx(y0);
                 y1 = ex2_approx(y1);
                 y2 = ex2_approx(y2);
                 y3 = ex2_approx(y3);
-                add2(la[0], la[1], y0, y1);
-                add2(lb[0], lb[1], y2, y3);
+                if (c % 16 == 0) {
+                  ga[0] = y0, ga[1] = y1, gb[0] = y2, gb[1] = y3;
+                } else {
+                  add2(ga[0], ga[1], y0, y1);
+                  add2(gb[0], gb[1], y2, y3);
+                }
                 pk[q][c >> 1] = pack_f16(y0, y1);
                 pk[q][(c >> 1) + 1] = pack_f16(y2, y3);
               }
+              add2(ga[0], ga[1], gb[0], gb[1]);
+              fma2v(la[0], la[1], ga[0], ga[1], inv, la[0], la[1]);
             }
           } else {
 #pragma unroll
@@ -1845,8 +1826,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
           }
         }
         tmem_wait_st();
-        const float tile_sum = (la[0] + la[1]) + (lb[0] + lb[1]);
-        l_run = Q8 ? fmaf(tile_sum, v_inverse, l_run) : l_run + tile_sum;
+        l_run += (la[0] + la[1]) + (lb[0] + lb[1]);
       }
       if (my_steps > 0) {  // the last P
         tc_fence_before();
