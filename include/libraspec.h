@@ -709,10 +709,11 @@ int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint1
  * the exponents as there), with every option of libraspec_chunk_attn, and sinks:
  *   s_k = softmax_scale 2^ek Q . K8[k],   O = sum_k softmax(s)_k 2^ev V8[k].
  * Scores, sums and O accumulate in binary32; probabilities, times their value's
- * scale, enter the second product as f16, 11 bits down to 2^-21 of the largest
- * that the row sees and 2^-32 of it at least, the values as they are. Codes and
- * exponents of blocks that no row sees need not be initialised, and do not change
- * what others' rows get. Reads half the bytes of a bf16 cache. workspace as for
+ * scale, enter the second product as f16 (11 bits down to 2^-21 of the largest that
+ * the row sees, off by 2^-32 of it below that), the values as they are. Codes and
+ * exponents of blocks that no row sees need not be initialised; those of blocks
+ * that a row does not see do not change its result. Reads half the bytes of a bf16
+ * cache. workspace as for
  * libraspec_chunk_attn (it holds the queries' parts, T Hq (2 head_dim + 1) bytes).
  *
  * Two kernels. One reads a key for 8 or 16 rows, with queries as f16, exact down
