@@ -892,15 +892,15 @@ __device__ __forceinline__ void merge_parts(const ChunkArgs& A, const ChunkItem&
         float Mn = M[u];
 #pragma unroll
         for (int q = 0; q < P; ++q) Mn = fmaxf(Mn, ml[u][q].x);
-        if (Mn == -INFINITY) continue;  // nothing seen so far
-        const float f = ex2_approx(M[u] - Mn);  // 0 while M is -inf
+        const bool none = Mn == -INFINITY;  // nothing seen so far, or NaN alone
+        const float f = none ? 1.f : ex2_approx(M[u] - Mn);  // 0 while M is -inf
         M[u] = Mn;
         L[u] *= f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[u][e] *= f;
 #pragma unroll
         for (int q = 0; q < P; ++q) {
-          const float w = ex2_approx(ml[u][q].x - Mn);
+          const float w = none ? 1.f : ex2_approx(ml[u][q].x - Mn);
           L[u] += w * ml[u][q].y;
           const float x[8] = {v[u][q][0].x, v[u][q][0].y, v[u][q][0].z, v[u][q][0].w,
                               v[u][q][1].x, v[u][q][1].y, v[u][q][1].z, v[u][q][1].w};
