@@ -709,7 +709,10 @@ __device__ __forceinline__ float power_of_two_biased(uint32_t e) { return __uint
 // launch of its own (24 us for a prompt of 8192 tokens of 32 heads, as long beside the plan as behind it): in the
 // attention, where each CTA did it for its items, the prompt took 92 us longer, and 104 in place by the converters (what a
 // warp reads of shared memory beside the MMAs takes 150 to 400 cycles, a shuffle too).
-constexpr int kSplitThreads = 256;
+// e4m3 has no infinity: of a row that holds some, they become 1 with their sign, finite elements 0 beside them, NaN stays,
+// and the row's factor is infinite (kInfiniteRow in the place of its exponent). Scores are then infinite or NaN as the
+// formula's are.
+constexpr int kSplitThreads = 256, kInfiniteRow = 255;
 template <int D>
 static __global__ void __launch_bounds__(kSplitThreads) split_q_kernel(const uint16_t* __restrict__ Q, long long rows,
                                                                        uint8_t* __restrict__ parts,
@@ -732,13 +735,15 @@ static __global__ void __launch_bounds__(kSplitThreads) split_q_kernel(const uin
 #pragma unroll
   for (int off = 1; off < kLanes; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
   // (rows below 2^-119 are not brought up that far: the factor and its inverse are normal numbers)
-  const int fe = min(261 - (int)(top >> 7), 253);
-  const float f = power_of_two_biased(fe);
+  const bool infinite = top >= 0x7f80u;
+  const int fe = infinite ? kInfiniteRow : min(261 - (int)(top >> 7), 253);
+  const float f = infinite ? 1.f : power_of_two_biased(fe);
+  auto part_of = [&](float x) { return !infinite ? x * f : fabsf(x) == INFINITY ? copysignf(1.f, x) : x == x ? 0.f : x; };
   uint32_t first[4], rest[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float x0 = bf16_lo(w[2 * k]) * f, x1 = bf16_hi(w[2 * k]) * f;
-    const float x2 = bf16_lo(w[2 * k + 1]) * f, x3 = bf16_hi(w[2 * k + 1]) * f;
+    const float x0 = part_of(bf16_lo(w[2 * k])), x1 = part_of(bf16_hi(w[2 * k]));
+    const float x2 = part_of(bf16_lo(w[2 * k + 1])), x3 = part_of(bf16_hi(w[2 * k + 1]));
     const uint32_t lo = e4m3_of(x0, x1), hi = e4m3_of(x2, x3);
     const uint32_t hl = f16_of_e4m3((uint16_t)lo), hh = f16_of_e4m3((uint16_t)hi);
     const float2 yl = __half22float2(*reinterpret_cast<const __half2*>(&hl));
@@ -1571,7 +1576,10 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
       }
       float unscale = 1.f;  // of the row's Q
       if constexpr (Q8) {
-        if (valid) unscale = power_of_two_biased(254u - __ldcg(A.q_exp + (size_t)tok * A.Hq + hq));
+        if (valid) {
+          const uint32_t e = __ldcg(A.q_exp + (size_t)tok * A.Hq + hq);
+          unscale = e == kInfiniteRow ? INFINITY : power_of_two_biased(254u - e);
+        }
       }
       const float sc = SHAPE & (kCap | kBias) ? 1.f : scale_log2 * unscale;
       const int sinks = SINK ? min(A.mask.sinks, hi) : 0;  // (the row's)
