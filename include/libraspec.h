@@ -717,9 +717,9 @@ int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint1
  * libraspec_chunk_attn (it holds the queries' parts, T Hq (2 head_dim + 1) bytes).
  *
  * Two kernels. One reads a key for 8 or 16 rows, with queries as f16, exact down
- * to 2^-31 of a row's largest element; it takes decode steps (T <= B), and where
- * sequences have on average 16 rows per kv head at most, all of 1024 rows per kv
- * head, or those whose rows fit one of its blocks. The other takes the rest, in
+ * to 2^-31 of a row's largest element; where sequences have on average 16 rows per
+ * kv head at most (a decode step) it takes all of up to 1024 rows per kv head, and
+ * of more those whose rows fit one of its blocks. The other takes the rest, in
  * whose scores queries are two e4m3 parts: all eight bits of what lies within 2^-9
  * of a row's largest element, else off by 2^-17 of that. One to five launches.
  */

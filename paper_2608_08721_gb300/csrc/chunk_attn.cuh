@@ -149,14 +149,16 @@ inline long long max_blocks(long long T, int B, int g) {
 }
 
 // The few-row kernel (few_attn_q8.cu) has blocks of 8 rows, or of 16. It takes part where the sequences have 16 rows per kv
-// head on average at most. T <= B new tokens (a decode step) and up to 1024 rows are all its own; of more it takes the
-// sequences whose tokens fit a block and the other kernel the rest, whose keys would be read for 16 rows at a time: 255
-// tokens decoded over 2000 keys each beside a chunk of 512 over 8000 (g = 4) take 312 us so and 640 by itself, 127 beside
-// 300 over 2000 keys 172 and 210. The launches for the rest cost 5 to 20 us, though, also where there is none: with fewer
-// rows that is more than it gives (63 beside 100 over 500 keys 73 and 52, four tokens each of 8 sequences 25 and 19; but 63
-// over 500 keys beside 100 over 16000 110 and 189).
+// head on average at most. Up to 1024 rows are all its own; of more it takes the sequences whose tokens fit a block and the
+// other kernel the rest, whose keys would be read for 16 rows at a time: 255 tokens decoded over 2000 keys each beside a
+// chunk of 512 over 8000 (g = 4) take 312 us so and 640 by itself, 127 beside 300 over 2000 keys 172 and 210; a chunk of
+// 4096 over 2000 keys among 4095 sequences without new tokens 97 and 556. The launches for the rest cost 5 to 16 us, though,
+// also where there is none, in a decode step of many sequences (one token each of 300 over 512 keys, g = 4: 89 us, 81
+// without them; of 1024 over 1024 keys 377 and 365); with fewer rows that is more than it gives (63 beside 100 over 500 keys
+// 73 and 52, four tokens each of 8 sequences 25 and 19; but 63 over 500 keys beside 100 over 16000 110 and 189). The host
+// knows T and B, not how the tokens are spread: T <= B alone does not make a decode step.
 constexpr int kFewRows = 16, kFewAlone = 1024;
-inline bool few_alone(long long T, int B, int g) { return T <= B || T * g <= kFewAlone; }
+inline bool few_alone(long long T, int g) { return T * g <= kFewAlone; }
 inline bool few_fits(long long T, int B, int g) { return g <= kFewRows && T * g <= (long long)kFewRows * B; }
 inline int few_rows(long long T, int B, int g) { return g <= 8 && T * g <= 8ll * B ? 8 : 16; }
 inline long long few_blocks(long long T, int B, int tokens) { return std::min(T, T / tokens + B); }

@@ -658,7 +658,7 @@ cudaError_t launch_few_attn_q8(const ChunkCall& c) {
   a.fixed = 6;  // (a decoding batch of 64 sequences: 189 us at 2, 186 at 4, 183 at 6)
   const int grid = std::min(num_sms_current(), kCMaxCtas) * (eight ? kFewCtas : kFewCtas16);
   a.plan = PlanArgs{c.cu_new, c.kv_len, a.mask, c.T, c.B, tokens, std::min(c.S_cap, kCMaxKeys), c.Hkv, grid, 0x7fffffff,
-                    0, few_alone(c.T, c.B, g) ? 0x7fffffff : tokens, a.status};
+                    0, few_alone(c.T, g) ? 0x7fffffff : tokens, a.status};
   if (few_blocks(c.T, c.B, tokens) <= kWarpBlocks && c.B <= kWarpSeqs && !c.first_key) {
     a.blocks = nullptr;
   } else {
