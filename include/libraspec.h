@@ -657,9 +657,11 @@ int libraspec_kv_read_q8_paged(const uint8_t* K8, const uint8_t* V8, const uint8
  * rounding. Results do not change from run to run. One launch, or two (a plan from the device's lengths
  * before the attention) where T, B allow more than 64 blocks of 2 floor(128 /
  * g) tokens, with B > 512 or with first_key. workspace:
- * libraspec_chunk_workspace_size(T, B, Hq, Hkv, head_dim) bytes, 256-byte
+ * libraspec_chunk_workspace_size_bf16(T, B, Hq, Hkv, head_dim) bytes, 256-byte
  * aligned, zero-filled once, of at least the call's T, B and heads; calls
- * sharing it must not overlap. If a wait inside the
+ * sharing it must not overlap. (libraspec_chunk_workspace_size: for the calls over
+ * a cache in 8 bits as well, which keep T Hq (2 head_dim + 1) bytes of the queries
+ * there.) If a wait inside the
  * kernel gives up (LIBRASPEC_ST_TIMEOUT), re-initialise it before its next use.
  */
 typedef struct libraspec_score_opts {
@@ -671,6 +673,7 @@ typedef struct libraspec_score_opts {
 } libraspec_score_opts;
 
 size_t libraspec_chunk_workspace_size(int T, int B, int Hq, int Hkv, int head_dim);
+size_t libraspec_chunk_workspace_size_bf16(int T, int B, int Hq, int Hkv, int head_dim);
 int libraspec_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* cu_new,
                          const int32_t* kv_len, int T, int B, int Hq, int Hkv, int head_dim, int S_cap,
                          float softmax_scale, const libraspec_score_opts* opts, uint16_t* O, float* lse,
@@ -713,8 +716,8 @@ int libraspec_sink_attn_paged(const uint16_t* Q, const uint16_t* Kp, const uint1
  * the row sees, off by 2^-32 of it below that), the values as they are. Codes and
  * exponents of blocks that no row sees need not be initialised; those of blocks
  * that a row does not see do not change its result. Reads half the bytes of a bf16
- * cache. workspace as for
- * libraspec_chunk_attn (it holds the queries' parts, T Hq (2 head_dim + 1) bytes).
+ * cache. workspace: libraspec_chunk_workspace_size bytes, in all else as for
+ * libraspec_chunk_attn.
  *
  * Two kernels. One reads a key for 8 or 16 rows, with queries as f16, exact down
  * to 2^-31 of a row's largest element; where sequences have on average 16 rows per

@@ -80,6 +80,7 @@ SIGNATURES = {
     "libraspec_kv_read_q8": (_I, [_P] * 6 + [_I] * 6 + [_P, _P, _P, _SZ, _P]),
     "libraspec_kv_read_q8_paged": (_I, [_P] * 5 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_P, _P, _P, _SZ, _P]),
     "libraspec_chunk_workspace_size": (_SZ, [_I] * 5),
+    "libraspec_chunk_workspace_size_bf16": (_SZ, [_I] * 5),
     "libraspec_chunk_attn": (_I, [_P] * 5 + [_I] * 6 + [_F] + [_P] * 4 + [_SZ, _P]),
     "libraspec_chunk_attn_paged": (_I, [_P] * 4 + [_I] * 3 + [_P] * 2 + [_I] * 5 + [_F] + [_P] * 4 + [_SZ, _P]),
     "libraspec_sink_attn": (_I, [_P] * 5 + [_I] * 6 + [_F, _P, _I] + [_P] * 3 + [_SZ, _P]),
@@ -933,10 +934,13 @@ def _kv_read_q8(K8, V8, Ks, Vs, block_table, cu, start, T, ws, K, V, stream):
 
 
 class ChunkWorkspace:
-    """Device scratch of the chunk calls, for up to T new tokens of B sequences."""
+    """Device scratch of the chunk calls, for up to T new tokens of B sequences; q8=False: of those over a bf16 cache alone
+    (T Hq (2 d + 1) bytes less)."""
 
-    def __init__(self, T, B, Hq, Hkv, head_dim, device=None):
-        self.nbytes = int(load().libraspec_chunk_workspace_size(T, B, Hq, Hkv, head_dim))
+    def __init__(self, T, B, Hq, Hkv, head_dim, device=None, q8=True):
+        lib = load()
+        size = lib.libraspec_chunk_workspace_size if q8 else lib.libraspec_chunk_workspace_size_bf16
+        self.nbytes = int(size(T, B, Hq, Hkv, head_dim))
         if self.nbytes == 0:
             raise ValueError("invalid chunk workspace shapes")
         dev = torch.device("cuda") if device is None else torch.device(device)

@@ -761,7 +761,7 @@ int chunk_attn(int kind, ChunkCall c, bool paged, const libraspec_score_opts* op
       !aligned(c.cu_new, 4) || !aligned(c.kv_len, 4) || !aligned(c.block_table, 4) || !aligned(o.slopes, 4) ||
       !aligned(o.first_key, 4) || !aligned(o.prefix_len, 4))
     return LIBRASPEC_EINVAL;
-  if (!c.ws || !aligned(c.ws, 256) || ws_bytes < chunk_workspace_bytes(c.T, c.B, c.Hq, c.Hkv, c.D))
+  if (!c.ws || !aligned(c.ws, 256) || ws_bytes < chunk_workspace_bytes(c.T, c.B, c.Hq, c.Hkv, c.D, kind == 8))
     return LIBRASPEC_EINVAL;
   if (!paged) c.block_table = nullptr;
   c.softcap = o.softcap;
@@ -785,7 +785,12 @@ ChunkCall chunk_call(const uint16_t* Q, const void* K, const void* V, const uint
 
 size_t libraspec_chunk_workspace_size(int T, int B, int Hq, int Hkv, int head_dim) {
   if (!chunk_shape_ok(T, B, Hq, Hkv) || (head_dim != 64 && head_dim != 128)) return 0;
-  return chunk_workspace_bytes(T, B, Hq, Hkv, head_dim);
+  return chunk_workspace_bytes(T, B, Hq, Hkv, head_dim, true);
+}
+
+size_t libraspec_chunk_workspace_size_bf16(int T, int B, int Hq, int Hkv, int head_dim) {
+  if (!chunk_shape_ok(T, B, Hq, Hkv) || (head_dim != 64 && head_dim != 128)) return 0;
+  return chunk_workspace_bytes(T, B, Hq, Hkv, head_dim, false);
 }
 
 int libraspec_chunk_attn(const uint16_t* Q, const uint16_t* Kc, const uint16_t* Vc, const int32_t* cu_new,

@@ -179,7 +179,7 @@ static ChunkWs chunk_ws(long long T, int B, int Hq, int Hkv, int d) {
   // two slots per CTA: its first item, and its last where that goes on in the next CTA
   w.part_o = take(size_t(2 * kCMaxCtas) * kCBlockRows * d * sizeof(float));
   w.part_ml = take(size_t(2 * kCMaxCtas) * kCBlockRows * 2 * sizeof(float));
-  // (a cache in 8 bits) the queries as e4m3 parts, and their exponents
+  // (a cache in 8 bits alone: the other calls' workspaces end here) the queries as e4m3 parts, and their exponents
   w.q_parts = take((size_t)T * Hq * d * 2);
   w.q_exp = take((size_t)T * Hq);
   w.total = off;

@@ -28,7 +28,7 @@ struct ChunkCall {
   int least_new;  // sequences with fewer new tokens are left out
 };
 
-size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d);
+size_t chunk_workspace_bytes(long long T, int B, int Hq, int Hkv, int d, bool q8);
 cudaError_t launch_chunk_attn(const ChunkCall& c);
 cudaError_t launch_sink_attn(const ChunkCall& c);     // without first keys
 cudaError_t launch_chunk_attn_q8(const ChunkCall& c);

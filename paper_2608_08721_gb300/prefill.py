@@ -67,7 +67,7 @@ class PagedSequences:
         self.block_table = torch.arange(B * per, dtype=torch.int32, device=self.device).view(B, per)
         self.lengths: List[int] = [0] * B
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=self.device)
-        self.ws = binding.ChunkWorkspace(max_new, B, Hq, Hkv, head_dim, device=self.device)
+        self.ws = binding.ChunkWorkspace(max_new, B, Hq, Hkv, head_dim, device=self.device, q8=bool(block))
 
     def begin(self, n_new: Sequence[int]) -> Step:
         """A step of n_new[b] tokens for each sequence (0: none)."""
