@@ -628,12 +628,25 @@ def _check_device(t: torch.Tensor, name: str) -> None:
         raise ValueError("%s must be on a CUDA device" % name)
 
 
-def _on_current(x: torch.Tensor, y: torch.Tensor) -> None:
-    """Refuses a call on tensors of another device than the current one, where it would launch. (Two of them: to ask each
-    of ten takes 1.5 us.)"""
+_several = None
+
+
+def _several_devices() -> bool:
+    global _several
+    if _several is None:
+        _several = torch.cuda.device_count() > 1
+    return _several
+
+
+def _on_current(x: torch.Tensor, y: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """Refuses a call with a tensor (of those given) of another device than the current one, where it would launch. Where
+    there is but one device, two are asked: that the others are on a device at all has been checked. (To ask each of
+    fourteen takes 2 to 3 us of a call's 20.)"""
     dev = torch.cuda.current_device()
-    if x.get_device() != dev or y.get_device() != dev:
-        raise ValueError("all tensors must be on the current device (%d), got %s and %s" % (dev, x.device, y.device))
+    if x.get_device() != dev or y.get_device() != dev or (
+            _several_devices() and any(t is not None and t.get_device() != dev for t in others)):
+        raise ValueError("all tensors must be on the current device (%d), got %s" % (
+            dev, ", ".join(sorted({str(t.device) for t in (x, y) + others if t is not None}))))
 
 
 def _out(shape, dtype, device, stream) -> torch.Tensor:
@@ -783,12 +796,12 @@ def libraspec_qk_norm_rope(X, n_q: int, norm: QkNorm, pos, freqs: RopeFreqs, int
     _check_norm(norm, d)
     _req(pos, torch.int32, "pos", (T,))
     _check_device(freqs.turns, "freqs")
-    _on_current(X, freqs.turns)
     if Y is None:
         Y = _out(shape, dt, X.device, stream)
         ys = H * d
     else:
         ys = _heads_stride(Y, dt, "Y", shape)
+    _on_current(X, freqs.turns, pos, norm.q_weight, norm.k_weight, Y)
     lib = load()
     rc = (lib.libraspec_qk_norm_rope_bf16 if bf16 else lib.libraspec_qk_norm_rope)(
         X.data_ptr(), xs, pos.data_ptr(), freqs.turns_ptr, freqs.magnitude, norm.q_ptr, norm.k_ptr, norm.eps, T, n_q,
@@ -868,7 +881,6 @@ def _rope_append_q8(Q, K, V, K8, V8, Ks, Vs, block_table, cu_new, kv_len, freqs,
     if norm is not None:
         _check_norm(norm, d)
         q_w, k_w, eps = norm.q_ptr, norm.k_ptr, norm.eps
-    _on_current(K, K8)
     Hq = qs = 0
     if Q is not None:
         qs = _heads_stride(Q, dt, "Q")
@@ -882,6 +894,8 @@ def _rope_append_q8(Q, K, V, K8, V8, Ks, Vs, block_table, cu_new, kv_len, freqs,
             _req(Qo, torch.bfloat16, "Qo", shape)
     elif Qo is not None:
         raise ValueError("Qo without Q")
+    _on_current(K, K8, Q, V, V8, Ks, Vs, block_table, cu_new, kv_len, pos, freqs.turns, ws.buf, Qo,
+                *(() if norm is None else (norm.q_weight, norm.k_weight)))
     lib = load()
     name = "libraspec_rope_append_q8" + ("" if block_table is None else "_paged") + ("_bf16" if bf16 else "")
     head = (_ptr(Q), qs, K.data_ptr(), ks, V.data_ptr(), vs, cu_new.data_ptr(), kv_len.data_ptr(), _ptr(pos),
@@ -916,10 +930,10 @@ def _kv_read_q8(K8, V8, Ks, Vs, block_table, cu, start, T, ws, K, V, stream):
     T = int(T)
     if T < 0:
         raise ValueError("T must not be negative")
-    _on_current(K8, ws.buf)
     shape = (T, Hkv, d)
     K = _out(shape, torch.bfloat16, K8.device, stream) if K is None else _req(K, torch.bfloat16, "K", shape)
     V = _out(shape, torch.bfloat16, K8.device, stream) if V is None else _req(V, torch.bfloat16, "V", shape)
+    _on_current(K8, ws.buf, V8, Ks, Vs, block_table, cu, start, K, V)
     lib = load()
     tail = (cu.data_ptr(), start.data_ptr(), T, B, Hkv, d)
     head = (K8.data_ptr(), V8.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
@@ -1026,8 +1040,6 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
         caches = (Kc.data_ptr(), Vc.data_ptr(), Ks.data_ptr(), Vs.data_ptr())
         block = (block,)
     _check_device(ws.buf, "the workspace")
-    if sinks is not None:
-        _on_current(Q, Kc)
     opts = None
     if softcap or slopes is not None or window or first_key is not None or prefix_len is not None:
         if slopes is not None:
@@ -1045,6 +1057,8 @@ def _chunk_attn(Q, Kc, Vc, block_table, cu_new, kv_len, ws, softmax_scale, softc
         _req(lse, torch.float32, "lse", (T, Hq))
     elif want_lse:
         lse = _out((T, Hq), torch.float32, Q.device, stream)
+    if sinks is not None:
+        _on_current(Q, Kc, Vc, Ks, Vs, block_table, cu_new, kv_len, ws.buf, slopes, first_key, prefix_len, O, lse)
     tail = (d ** -0.5 if softmax_scale is None else float(softmax_scale), opts,
             *(() if sinks is None else (int(sinks),)), O.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes, _stream(stream))
     if block_table is None:
