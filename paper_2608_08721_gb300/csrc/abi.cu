@@ -63,16 +63,15 @@ cudaError_t launch_accept_plan(const T*, const T*, const float*, const float*, c
                                int, int, int32_t*, int32_t*, char*, const WsLayout&, cudaStream_t);
 
 int num_sms_current() {
-  static int cached_dev = -1, cached_sms = 0;
+  static std::atomic<uint64_t> cached{~0ull};  // device and its SMs, in one word: calls may come from several threads
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-  if (dev != cached_dev) {
-    int sms = 0;
-    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) sms = 148;
-    cached_sms = sms;
-    cached_dev = dev;
-  }
-  return cached_sms;
+  const uint64_t c = cached.load(std::memory_order_relaxed);
+  if (c >> 32 == (uint64_t)dev) return (int)(uint32_t)c;
+  int sms = 0;
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) sms = 148;
+  cached.store((uint64_t)dev << 32 | (uint32_t)sms, std::memory_order_relaxed);
+  return sms;
 }
 
 }  // namespace libraspec

@@ -1002,10 +1002,10 @@ template cudaError_t launch_accept_tree<uint16_t>(const uint16_t*, const int32_t
 // batch: 51.5 us back to back against 54.3 with four waves, 53.0 with three).
 template <bool VEC, typename T>
 int accept_grid() {
-  static int cached[64];
+  static std::atomic<int> cached[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  int g = cached[dev];
+  int g = cached[dev].load(std::memory_order_relaxed);
   if (g == 0) {
     int per_sm = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, accept_rows_kernel<VEC, T, true>, kRowThreads, 0) !=
@@ -1013,7 +1013,7 @@ int accept_grid() {
         per_sm < 1)
       per_sm = 1;
     g = std::min(2 * per_sm * num_sms_current(), kAccMaxGrid);
-    cached[dev] = g;
+    cached[dev].store(g, std::memory_order_relaxed);
   }
   return g;
 }

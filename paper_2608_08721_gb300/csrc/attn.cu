@@ -1565,13 +1565,9 @@ static cudaError_t launch_layers_t(const uint16_t* const* Q, const uint16_t* con
                                    cudaStream_t stream) {
   using SM = AttnSmem<D>;
   constexpr int kSmem = PAGED ? SM::kAllocPaged : SM::kAlloc;
-  static bool configured = false;
-  if (!configured) {
-    cudaError_t e = cudaFuncSetAttribute(verify_attn_kernel<D, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         kSmem);
-    if (e != cudaSuccess) return e;
-    configured = true;
-  }
+  static std::atomic<uint64_t> devices{0};
+  const cudaError_t allowed = allow_shared(verify_attn_kernel<D, PAGED>, kSmem, devices);
+  if (allowed != cudaSuccess) return allowed;
   int grid = num_sms_current();  // one CTA per SM (it holds all 512 tensor-memory columns)
   if (grid > kAttnMaxCtas) grid = kAttnMaxCtas;
   auto kern = verify_attn_kernel<D, PAGED>;

@@ -2017,15 +2017,9 @@ static bool make_map8(CUtensorMap* map, const void* base, int D, long long rows,
 template <int D, int SHAPE>
 static cudaError_t launch_attn_t(const ChunkArgs& a, int grid, cudaStream_t stream) {
   using SM = ChunkSmem<D, (SHAPE & kQ8) != 0>;
-  static int configured = -1;  // the device whose kernel may use as much shared memory
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  static std::atomic<uint64_t> devices{0};
+  const cudaError_t e = allow_shared(chunk_attn_kernel<D, SHAPE>, SM::kBytes, devices);
   if (e != cudaSuccess) return e;
-  if (dev != configured) {
-    e = cudaFuncSetAttribute(chunk_attn_kernel<D, SHAPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SM::kBytes);
-    if (e != cudaSuccess) return e;
-    configured = dev;
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads);

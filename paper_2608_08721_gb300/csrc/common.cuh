@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "attn_rules.h"
 #include "libraspec.h"
@@ -14,6 +15,20 @@ namespace libraspec {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
+
+// Lets `kernel` use that many bytes of dynamic shared memory on the current device, once for each device (a bit of
+// `devices`; calls may come from several threads).
+template <typename F>
+cudaError_t allow_shared(F* kernel, int bytes, std::atomic<uint64_t>& devices) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
+  return e;
+}
 
 // ---------------------------------------------------------------------------
 // Workspace layout. Every region is 256-byte aligned; counters are reset to

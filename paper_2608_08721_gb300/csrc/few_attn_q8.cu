@@ -596,15 +596,9 @@ __global__ void __launch_bounds__(kFewThreads, NT == 1 ? kFewCtas : kFewCtas16) 
 template <int D, int NT, bool OPTS>
 static cudaError_t launch_few_t(const FewArgs& a, int grid, cudaStream_t stream) {
   constexpr int kBytes = kFewWarps * (kFewStages * 32 * D + 8 * NT * D * 4);
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  static std::atomic<uint64_t> devices{0};
+  const cudaError_t e = allow_shared(few_q8_kernel<D, NT, OPTS>, kBytes, devices);
   if (e != cudaSuccess) return e;
-  static int configured = -1;  // the device whose kernel may use as much shared memory
-  if (dev != configured) {
-    e = cudaFuncSetAttribute(few_q8_kernel<D, NT, OPTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (e != cudaSuccess) return e;
-    configured = dev;
-  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kFewThreads);

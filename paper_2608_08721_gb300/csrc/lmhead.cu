@@ -569,13 +569,9 @@ cudaError_t launch_lm_head_stats(const uint16_t* H, const uint16_t* W, const flo
       !make_2d_map(&mapHs, H, Dm, M, std::max(cut.big / 2 - 16, 16)) ||
       !make_2d_map(&mapW, W, Dm, V, kLmHalf) || !make_2d_map(&mapWt, W, Dm, V, cut.tail))
     return cudaErrorInvalidValue;
-  static bool configured = false;
-  if (!configured) {
-    cudaError_t e = cudaFuncSetAttribute(lm_head_stats_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         kLmSmemMax);
-    if (e != cudaSuccess) return e;
-    configured = true;
-  }
+  static std::atomic<uint64_t> devices{0};
+  const cudaError_t allowed = allow_shared(lm_head_stats_kernel, kLmSmemMax, devices);
+  if (allowed != cudaSuccess) return allowed;
   auto* part = reinterpret_cast<LmPartial*>(ws + 256);
   auto* status = reinterpret_cast<int*>(ws);
   lm_head_stats_kernel<<<2 * pairs, kLmThreads, kLmFixed + stages * stage_bytes, stream>>>(

@@ -388,7 +388,8 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 
 // The driver's cuTensorMapEncodeTiled, resolved once.
 static inline PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> found{nullptr};
+  PFN_cuTensorMapEncodeTiled_v12000 fn = found.load(std::memory_order_acquire);
   if (!fn) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -396,6 +397,7 @@ static inline PFN_cuTensorMapEncodeTiled_v12000 get_encode() {
             cudaSuccess &&
         q == cudaDriverEntryPointSuccess)
       fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    found.store(fn, std::memory_order_release);
   }
   return fn;
 }
