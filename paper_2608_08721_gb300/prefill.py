@@ -81,7 +81,8 @@ class PagedSequences:
     def layer(self, l: int, qkv: torch.Tensor, step: Step, lse: Optional[torch.Tensor] = None, stream=None, **options):
         """Layer l of the step: qkv [T, Hq + 2 Hkv, d] (f32 or bf16, the projections' output) is rotated and appended,
         and its queries attend to the cache. options: libraspec_chunk_attn's (softcap, slopes, window, first_key,
-        prefix_len, softmax_scale) and sinks (first tokens that the window leaves visible). Returns O [T, Hq, d] bf16.
+        prefix_len, softmax_scale; None: not given) and sinks (first tokens that the window leaves visible; not with
+        first_key). Returns O [T, Hq, d] bf16.
 
         On a stream other than the current one the layer runs behind what the current stream holds, and what the
         current stream gets next (the advance of the lengths in ``end`` among it) runs behind the layer."""
@@ -100,11 +101,15 @@ class PagedSequences:
         if qkv.shape != (step.T, Hq + 2 * Hkv, self.d):  # (rows of no sequence would come back unwritten)
             raise ValueError("qkv must be [%d, %d, %d], got %s" % (step.T, Hq + 2 * Hkv, self.d, tuple(qkv.shape)))
         q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+        options = {key: x for key, x in options.items() if x is not None}
+        sinks = options.pop("sinks", 0)
+        if sinks and "first_key" in options:
+            raise ValueError("sinks and first_key exclude each other")
         if self.block:
             cache = (pool["K8"], pool["V8"], pool["Ks"], pool["Vs"], self.block_table, step.cu_new, self.kv_len)
             q = binding.libraspec_rope_append_q8_paged(q, k, v, *cache, self.freqs, self.ws, norm=self.norm,
                                                        interleaved=self.interleaved)
-            return binding.libraspec_chunk_attn_q8_paged(q, *cache, self.ws, lse=lse, **options)[0]
+            return binding.libraspec_chunk_attn_q8_paged(q, *cache, self.ws, lse=lse, sinks=sinks, **options)[0]
         freqs, pos = self.freqs, None
         if self.norm is not None:
             qk = binding.libraspec_qk_norm_rope(qkv[:, :Hq + Hkv], Hq, self.norm, step.pos, freqs,
@@ -113,10 +118,9 @@ class PagedSequences:
         q = binding.libraspec_rope_append_paged(q, k, v, pool["Kp"], pool["Vp"], self.block_table, step.cu_new,
                                                 self.kv_len, freqs, self.ws, pos=pos, interleaved=self.interleaved)
         attend = binding.libraspec_chunk_attn_paged
-        if options.get("sinks") and options.get("window"):
+        if sinks:
             attend = binding.libraspec_sink_attn_paged
-        else:
-            options = {k: x for k, x in options.items() if k != "sinks"}
+            options = {"window": 0, **options, "sinks": sinks}
         return attend(q, pool["Kp"], pool["Vp"], self.block_table, step.cu_new, self.kv_len, self.ws, lse=lse, **options)[0]
 
     def unpacked(self, l: int, extra: int = 0) -> dict:
