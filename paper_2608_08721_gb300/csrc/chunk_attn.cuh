@@ -68,9 +68,9 @@
 // (exactly), and P is f16, times its value's scale: P' = 2^(s - m + e), O = sum P' V8, l = sum P' 2^-e. The exponent e of
 // each 16 keys enters behind the mask, so neither the reference m nor P' of a row depends on a key that it does not see.
 // (With a tile's values brought to its largest exponent instead, a hidden key's scale took the bits of what the row sees;
-// it was no faster either: a prompt of 8192 tokens 483 us, 458 so.) One more warp brings the exponents, two tiles'
+// it was no faster either: a prompt of 8192 tokens 484 us, 466 so.) One more warp brings the exponents, two tiles'
 // look-ups ahead; a tile's count with its scores on one barrier. What bounds it: the softmax warps' steps, beside which
-// the converters issue (24 of the 458 us are the queries' parts; the same in bf16 takes 385). Measured and not kept, when
+// the converters issue (24 of the 466 us are the queries' parts; the same in bf16 takes 385). Measured and not kept, when
 // the prompt took 518: K converted as well (647), the queries' parts in the kernel (615).
 //
 // Sinks (kSink): keys below `sinks` stay visible to every row behind them. A block's tiles are then the first ones of the
@@ -634,10 +634,12 @@ struct ChunkSmem {
 constexpr int kCSoftmaxRegs = 208, kCOtherRegs = 88;
 static_assert(kCSoftmaxWarps * 32 * kCSoftmaxRegs + 128 * kCOtherRegs <= kCThreads * 168, "");
 // A cache in 8 bits takes a warpgroup more: 512 threads start with 128 each (65536 in all), of which the softmax keeps
-// 200, the third warpgroup 72 and the converters 40 (256 x 200 + 128 x 72 + 128 x 40 = 65536).
+// 200, the third warpgroup 80 and the converters 32 (256 x 200 + 128 x 80 + 128 x 32 = 65536), which suffices for two
+// units of a tile at a time. (With 72 and 40, and four units, the producer spills: a prompt of 8192 tokens 461 us, 466 so,
+// but 38 sequences of 41 to 82 tokens over up to 336 keys 48.4 and 44.1, chunks with sinks 67.5 and 65.5.)
 constexpr int kCThreadsQ8 = kCThreads + 128;
 constexpr int kScaleWarp = kCMmaWarp + 1, kConvertWarp = kCMmaWarp + 3, kConverters = 4;
-constexpr int kQ8SoftmaxRegs = 200, kQ8OtherRegs = 72, kQ8ConvertRegs = 40;
+constexpr int kQ8SoftmaxRegs = 200, kQ8OtherRegs = 80, kQ8ConvertRegs = 32;
 static_assert(kCSoftmaxWarps * 32 * kQ8SoftmaxRegs + 128 * kQ8OtherRegs + 128 * kQ8ConvertRegs <= kCThreadsQ8 * 128, "");
 template <int N>
 __device__ __forceinline__ void regs_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -1069,13 +1071,13 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
         const uint8_t* raw = smem + SM::kRaw + rc * SM::kRawTile + crow * D + cj * 16;
         uint8_t* dst = smem + SM::kRing + ch * SM::kTile;
 #pragma unroll 1
-        for (int i0 = 0; i0 < kUnits; i0 += 4) {
-          uint4 v[4];
+        for (int i0 = 0; i0 < kUnits; i0 += 2) {
+          uint4 v[2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4*>(raw + (i0 + i) * 2048);
+          for (int i = 0; i < 2; ++i) v[i] = *reinterpret_cast<const uint4*>(raw + (i0 + i) * 2048);
           if (edge) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 2; ++i) {
               const int key = kt0 + crow + (i0 + i) * kRowStep;
               bool some = key < it.khi && (key >= it.klo || key < sinks);
               if (some && gap) some = some_row_sees(seen, it.pos0, n_tok, key, key + 1);
@@ -1083,7 +1085,7 @@ __global__ void __launch_bounds__(SHAPE & kQ8 ? kCThreadsQ8 : kCThreads, 1)
             }
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2; ++i) {
             auto to_f16 = [&](uint32_t codes) { return f16_of_e4m3((uint16_t)codes); };
             const uint4 lo = make_uint4(to_f16(v[i].x), to_f16(v[i].x >> 16), to_f16(v[i].y), to_f16(v[i].y >> 16));
             const uint4 hi = make_uint4(to_f16(v[i].z), to_f16(v[i].z >> 16), to_f16(v[i].w), to_f16(v[i].w >> 16));
