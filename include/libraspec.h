@@ -541,8 +541,9 @@ int libraspec_rope_append_paged_bf16(const uint16_t* Q, int64_t q_stride, const 
  * once), laid out and strided as for libraspec_rope: heads 0 .. Hq - 1 take
  * q_weight, the others k_weight (both [head_dim] f32; queries and keys lie side
  * by side in a projection's output; Hq or Hk may be 0, its weights then NULL).
- * eps >= 0 and finite; a head of zeros with eps = 0 gives NaN. The norm is of
- * the whole head, rotated or not. Y may be X with the same stride; else they
+ * eps >= 0 and finite; a head of zeros with eps = 0 gives NaN. Squares are summed
+ * in binary32: a finite head whose sum passes 2^128 gives 0. The norm is of the
+ * whole head, rotated or not. Y may be X with the same stride; else they
  * must not overlap. Limits as for libraspec_rope. One launch, no workspace.
  */
 int libraspec_qk_norm_rope(const float* X, int64_t x_stride, const int32_t* pos, const float* turns, float magnitude,

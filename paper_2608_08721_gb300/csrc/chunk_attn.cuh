@@ -70,8 +70,8 @@
 // (With a tile's values brought to its largest exponent instead, a hidden key's scale took the bits of what the row sees;
 // it was no faster either: a prompt of 8192 tokens 484 us, 466 so.) One more warp brings the exponents, two tiles'
 // look-ups ahead; a tile's count with its scores on one barrier. What bounds it: the softmax warps' steps, beside which
-// the converters issue (24 of the 466 us are the queries' parts; the same in bf16 takes 385). Measured and not kept, when
-// the prompt took 518: K converted as well (647), the queries' parts in the kernel (615).
+// the converters issue (25 of the 466 us go when the conversion is left out, 25 are the queries' parts; bf16 takes 385).
+// Measured and not kept, when the prompt took 518: K converted as well (647), the queries' parts in the kernel (615).
 //
 // Sinks (kSink): keys below `sinks` stay visible to every row behind them. A block's tiles are then the first ones of the
 // sequence that hold sinks, and those of its window; what lies between is not read.
@@ -710,7 +710,7 @@ __device__ __forceinline__ float power_of_two_biased(uint32_t e) { return __uint
 // (8 bits) The queries as two e4m3 parts: a row (a token's head) times the power of two that brings its largest into
 // [2^7, 2^8) becomes the nearest e4m3 and the rest, together all eight bits of what lies within 2^-9 of the largest, else
 // off by 2^-17 of it at most. Per 64 elements the first parts, then the second, in the bytes that the elements took. A
-// launch of its own (24 us for a prompt of 8192 tokens of 32 heads, as long beside the plan as behind it): in the
+// launch of its own (25 us for a prompt of 8192 tokens of 32 heads, as long beside the plan as behind it): in the
 // attention, where each CTA did it for its items, the prompt took 92 us longer, and 104 in place by the converters (what a
 // warp reads of shared memory beside the MMAs takes 150 to 400 cycles, a shuffle too).
 // e4m3 has no infinity: of a row that holds some, they become 1 with their sign, finite elements 0 beside them, NaN stays,
